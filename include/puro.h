@@ -246,6 +246,103 @@ puro_status puro_rmsnorm_quantize_fp8(const uint16_t* x, const uint16_t* gamma, 
                                       float* scaleT, float* rstd, void* ws, size_t ws_bytes,
                                       hipStream_t stream);
 
+/* ------------------------- query / key norm with position rotation ---
+ * Between the QKV projection and attention, the paper's model (the Qwen3-1.7B
+ * architecture, Section 2) normalises every query and key head and turns it by
+ * its position. For a head x of head_dim values, in binary32:
+ *     n = x * gamma / sqrt(mean(x^2) + eps)       (gamma NULL: n = x)
+ *     the pairs (a, b) of n's first R = rope->dim values become
+ *     (a c - b s, b c + a s), (c, s) = the table's entry of the position and
+ *     the pair; the values from R on stay (rope NULL or R = 0: all of them)
+ * and one rounding to BF16. Pair i < R / 2 is (i, i + R / 2), or
+ * (2 i, 2 i + 1) when interleaved.
+ *
+ * Heads in memory (puro_heads): head h of token s of sequence b starts
+ * b * batch_stride + s * row_stride + h * head_stride elements after `data`,
+ * its head_dim values are contiguous: views of the projection's output, packed
+ * [T, H, D] tensors and heads-first [B, H, S, D] ones alike. Strides are
+ * multiples of 8 and not negative, data 16-byte aligned; an output's heads may
+ * not overlap each other. An output may be the corresponding input itself
+ * (the same data and strides; backward: the incoming gradient), and must not
+ * overlap any input otherwise.
+ *
+ * The rotation (puro_rope): table [len][dim / 2][2] binary32 (cos, sin) pairs,
+ * 16-byte aligned, as puro_rope_table writes them or scaled in any way;
+ * dim a multiple of 16 up to head_dim; positions [batch * seq] int32, or NULL:
+ * token s of every sequence is at position s (then seq <= len). A position
+ * outside [0, len) turns its token's first R values to NaN and reads nothing
+ * outside the table.
+ *
+ * head_dim: a multiple of 8 from 8 to 256. heads_q and heads_k (heads_k also
+ * counts the value heads of the backward): at most 65535; batch * seq < 2^31.
+ * batch * seq = 0 is a valid empty call. gamma_q, gamma_k: BF16 [head_dim],
+ * 16-byte aligned. eps finite and >= 0 (with eps = 0 a head of zeros gives
+ * NaN, as the formula does); heads whose sum of squares overflows binary32
+ * are outside the statement. */
+typedef struct {
+    uint16_t* data;
+    int64_t batch_stride, row_stride, head_stride;
+} puro_heads;
+typedef struct {
+    const float* table;
+    int64_t len;
+    int dim;
+    int interleaved;
+    const int32_t* positions;
+} puro_rope;
+
+/* The table of angles p * theta^(-2 i / dim), position p in [0, len), pair
+ * i < dim / 2: computed in double precision, rounded to binary32. dim a
+ * multiple of 16 (0: nothing is written) up to 256, len < 2^31, theta > 0 and finite. */
+puro_status puro_rope_table(float* table, int64_t len, int dim, double theta, hipStream_t stream);
+
+puro_status puro_qk_norm_rope_fwd(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim,
+                                  const puro_heads* q, const puro_heads* k, const uint16_t* gamma_q,
+                                  const uint16_t* gamma_k, float eps, const puro_rope* rope,
+                                  const puro_heads* q_out, const puro_heads* k_out, hipStream_t stream);
+
+/* Backward: from the gradients dq, dk of the outputs and the forward's inputs
+ * q, k (read only where that kind of heads has a gamma; may be NULL otherwise)
+ * the gradients of the inputs, rounded once to BF16, into dq_in and dk_in; with
+ * dn the gradient turned back, r = 1 / sqrt(mean(x^2) + eps), h = x r,
+ * g = dn gamma:  dx = r (g - h mean(g h)).  dgamma_q, dgamma_k (FP32
+ * [head_dim], overwritten, either NULL: not wanted) = the sums over tokens and
+ * heads of dn h, in binary32 in a fixed order. dv, dv_in (both or neither):
+ * the value heads' gradients, copied, so that one call assembles the gradient
+ * of the projection's output. The statistics are recomputed from the heads,
+ * which the call reads anyway: nothing is kept from the forward but its
+ * inputs. ws: the matching *_workspace_size bytes (for dgamma; 16-byte aligned). */
+size_t puro_qk_norm_rope_bwd_workspace_size(int64_t batch, int64_t seq, int head_dim);
+puro_status puro_qk_norm_rope_bwd(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim,
+                                  const puro_heads* dq, const puro_heads* dk, const puro_heads* dv,
+                                  const puro_heads* q, const puro_heads* k, const uint16_t* gamma_q,
+                                  const uint16_t* gamma_k, float eps, const puro_rope* rope,
+                                  const puro_heads* dq_in, const puro_heads* dk_in, const puro_heads* dv_in,
+                                  float* dgamma_q, float* dgamma_k, void* ws, size_t ws_bytes,
+                                  hipStream_t stream);
+
+/* The same backward with its result quantised: the matrix dqkv [batch * seq,
+ * (heads_q + 2 heads_k) * head_dim] = [dq | dk | dv] of the projection's output
+ * gradient (rounded to BF16), quantised exactly as puro_quantize_fp8 would
+ * quantise a BF16 tensor holding it, without writing it: q8 for the QKV
+ * projection's Dgrad, the transposed copy for its Wgrad. Modes TENSOR,
+ * ROW_1x128 and COL_128x1 with puro_quantize_fp8's outputs, layouts and
+ * requirements (rows = batch * seq, cols = the heads' width); BLOCK_128x128 is
+ * PURO_ERR_UNSUPPORTED, and so is a head_dim other than 64 and 128 (a 128-column
+ * tile then holds no whole heads: use the call above and puro_quantize_fp8).
+ * dv is required when heads_k > 0. ws: its *_workspace_size bytes, 16-byte
+ * aligned (needed in TENSOR mode and for dgamma). */
+size_t puro_qk_norm_rope_bwd_quantize_workspace_size(int64_t batch, int64_t seq, int heads_q, int heads_k,
+                                                     int head_dim);
+puro_status puro_qk_norm_rope_bwd_quantize_fp8(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim,
+                                               const puro_heads* dq, const puro_heads* dk, const puro_heads* dv,
+                                               const puro_heads* q, const puro_heads* k, const uint16_t* gamma_q,
+                                               const uint16_t* gamma_k, float eps, const puro_rope* rope,
+                                               puro_fp8_format fmt, puro_scale_mode mode, puro_scale_rounding rnd,
+                                               uint8_t* q8, float* scale, uint8_t* qT, float* scaleT,
+                                               float* dgamma_q, float* dgamma_k, void* ws, size_t ws_bytes,
+                                               hipStream_t stream);
+
 /* ---------------------------------------------------------------- GEMM ---
  * D[m, n] = sum_k A[m, k] * B[n, k] with FP32 accumulation (Section 3.2:
  * the Fprop, Dgrad and Wgrad GEMMs of a linear layer run on FP8 operands).

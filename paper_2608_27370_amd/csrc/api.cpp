@@ -99,13 +99,15 @@ namespace {
 // 2 cols]; or the RMSNorm y = BF16(x * rstd * gamma) of x [rows, cols], whose
 // per-row rstd is written too.
 struct Source {
-    enum Kind { kBf16, kSwiglu, kRmsnorm, kSwigluBwd } kind = kBf16;
+    enum Kind { kBf16, kSwiglu, kRmsnorm, kSwigluBwd, kQkBwd } kind = kBf16;
     const uint16_t* gamma = nullptr;
     float* rstd = nullptr;
     float eps = 0.0f;
     // the SwiGLU backward's saved gate/up output (x is then dH)
     const uint16_t* gu = nullptr;
     int64_t ld_gu = 0;
+    // the query / key norm's backward (x is then any of its gradients, checked already)
+    const QkArgs* qk = nullptr;
 };
 
 puro_status quantize_impl(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, puro_fp8_format fmt,
@@ -127,7 +129,8 @@ puro_status quantize_impl(const uint16_t* x, int64_t rows, int64_t cols, int64_t
         if (st != PURO_OK) return st;
         if (src.ld_gu >= ((int64_t)1 << 23)) return PURO_ERR_SHAPE;
     }
-    if ((swiglu || rms || bwd) && (amax_in || mode == PURO_SCALE_BLOCK_128x128)) return PURO_ERR_UNSUPPORTED;
+    const bool qk = src.kind == Source::kQkBwd;
+    if ((swiglu || rms || bwd || qk) && (amax_in || mode == PURO_SCALE_BLOCK_128x128)) return PURO_ERR_UNSUPPORTED;
     if (rms) {
         // a row needs its columns (the mean of an empty row is undefined)
         if (rows > 0 && cols == 0) return PURO_ERR_SHAPE;
@@ -203,6 +206,18 @@ puro_status quantize_impl(const uint16_t* x, int64_t rows, int64_t cols, int64_t
             return PURO_OK;
         }
         launch_swiglu_bwd_quantize(fmt, qmode, a, ws, stream);
+        return launched();
+    }
+    if (qk) {
+        const bool sums = src.qk->dgq || src.qk->dgk;
+        if (qmode == kQTensor || sums) {
+            if (!ws) return PURO_ERR_NULL;
+            if (!aligned16(ws)) return PURO_ERR_ALIGN;
+            if (ws_bytes < qk_bwd_quantize_ws_bytes(rows, src.qk->hq, src.qk->hk, src.qk->D)) return PURO_ERR_WORKSPACE;
+        } else if (empty) {
+            return PURO_OK;
+        }
+        launch_qk_norm_rope_bwd_quantize(fmt, qmode, a, *src.qk, ws, stream);
         return launched();
     }
     if (qmode == kQTensor && !amax_in) {
@@ -296,6 +311,202 @@ puro_status puro_rmsnorm_quantize_fp8(const uint16_t* x, const uint16_t* gamma, 
     src.eps = eps;
     return quantize_impl(x, rows, cols, ld, fmt, mode, rnd, nullptr, q, scale, qT, scaleT, ws, ws_bytes, stream,
                          src);
+}
+
+}  // extern "C"
+
+// ------------------------------- query / key norm with position rotation
+namespace {
+
+constexpr int kMaxHeadDim = 256;
+
+bool finite_nonneg(float v) { return v >= 0.0f && v <= 3.4028235e38f; }
+
+// Sizes of a query / key call; tokens = batch * seq.
+puro_status check_qk_sizes(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim, int64_t* tokens) {
+    if (batch < 0 || seq < 0 || heads_q < 0 || heads_k < 0) return PURO_ERR_SHAPE;
+    if (heads_q > 65535 || heads_k > 65535) return PURO_ERR_SHAPE;
+    if (batch > INT32_MAX || seq > INT32_MAX || batch * seq > INT32_MAX) return PURO_ERR_SHAPE;
+    if (head_dim < 8 || head_dim > kMaxHeadDim) return PURO_ERR_SHAPE;
+    if ((head_dim % 8) != 0) return PURO_ERR_ALIGN;
+    *tokens = batch * seq;
+    return PURO_OK;
+}
+
+// Heads that the call touches: their place, and for outputs that no two of
+// them overlap. Strides of dimensions of size one are not looked at.
+puro_status check_heads(const puro_heads* h, int64_t batch, int64_t seq, int heads, int head_dim, bool output,
+                        HeadsArg* arg) {
+    *arg = HeadsArg{};
+    if (batch == 0 || seq == 0 || heads == 0) return PURO_OK;
+    if (!h || !h->data) return PURO_ERR_NULL;
+    struct Dim { int64_t n, stride; } d[3] = {{batch, h->batch_stride}, {seq, h->row_stride}, {heads, h->head_stride}};
+    __int128 span = 0;
+    for (Dim& x : d) {
+        if (x.n == 1) x.stride = 0;
+        if (x.stride < 0) return PURO_ERR_SHAPE;
+        if ((x.stride % 8) != 0) return PURO_ERR_ALIGN;
+        span += (__int128)(x.n - 1) * x.stride;
+    }
+    if (span > ((__int128)1 << 46)) return PURO_ERR_SHAPE;
+    if (!aligned16(h->data)) return PURO_ERR_ALIGN;
+    *arg = HeadsArg{h->data, d[0].stride, d[1].stride, d[2].stride};
+    if (output) {
+        // by rising stride, each dimension steps past everything below it
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2 - i; ++j)
+                if (d[j].stride > d[j + 1].stride) { const Dim t = d[j]; d[j] = d[j + 1]; d[j + 1] = t; }
+        int64_t extent = head_dim;
+        for (const Dim& x : d) {
+            if (x.n == 1) continue;
+            if (x.stride < extent) return PURO_ERR_SHAPE;
+            extent += (x.n - 1) * x.stride;
+        }
+    }
+    return PURO_OK;
+}
+
+puro_status check_rope(const puro_rope* r, int64_t seq, int64_t tokens, int head_dim, RopeArgs* arg) {
+    *arg = RopeArgs{};
+    if (!r || r->dim == 0) return PURO_OK;
+    if (r->dim < 0 || r->dim > head_dim || r->len < 0 || r->len > INT32_MAX) return PURO_ERR_SHAPE;
+    if ((r->dim % 16) != 0) return PURO_ERR_ALIGN;
+    if (r->interleaved != 0 && r->interleaved != 1) return PURO_ERR_UNSUPPORTED;
+    if (tokens > 0) {
+        if (!r->positions && seq > r->len) return PURO_ERR_SHAPE;
+        if (r->len == 0) return PURO_ERR_SHAPE;       // (no entry to stand in for one outside)
+        if (!r->table) return PURO_ERR_NULL;
+        if (!aligned16(r->table) || ((uintptr_t)r->positions & 3) != 0) return PURO_ERR_ALIGN;
+    }
+    *arg = RopeArgs{reinterpret_cast<const float2*>(r->table), r->positions, (int)r->len, r->dim, r->interleaved};
+    return PURO_OK;
+}
+
+// What the three calls have in common: sizes, rotation, weights and the heads
+// before the norm (needed by the backward only where there is a weight).
+puro_status check_qk(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim, const puro_heads* q,
+                     const puro_heads* k, const uint16_t* gamma_q, const uint16_t* gamma_k, float eps,
+                     const puro_rope* rope, bool backward, QkArgs* a) {
+    puro_status st = check_qk_sizes(batch, seq, heads_q, heads_k, head_dim, &a->tokens);
+    if (st != PURO_OK) return st;
+    if (!finite_nonneg(eps)) return PURO_ERR_UNSUPPORTED;
+    if ((gamma_q && !aligned16(gamma_q)) || (gamma_k && !aligned16(gamma_k))) return PURO_ERR_ALIGN;
+    st = check_rope(rope, seq, a->tokens, head_dim, &a->rope);
+    if (st != PURO_OK) return st;
+    if (!backward || gamma_q) st = check_heads(q, batch, seq, heads_q, head_dim, false, &a->q);
+    if (st != PURO_OK) return st;
+    if (!backward || gamma_k) st = check_heads(k, batch, seq, heads_k, head_dim, false, &a->k);
+    if (st != PURO_OK) return st;
+    a->gq = gamma_q; a->gk = gamma_k;
+    a->eps = eps;
+    a->seq = (int)seq; a->hq = heads_q; a->hk = heads_k; a->D = head_dim;
+    return PURO_OK;
+}
+
+// dgamma of heads that have no gamma is not defined.
+puro_status check_dgamma(const QkArgs& a) {
+    if ((a.dgq && !a.gq) || (a.dgk && !a.gk)) return PURO_ERR_NULL;
+    if (((uintptr_t)a.dgq & 3) != 0 || ((uintptr_t)a.dgk & 3) != 0) return PURO_ERR_ALIGN;
+    return PURO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+puro_status puro_rope_table(float* table, int64_t len, int dim, double theta, hipStream_t stream) {
+    if (len < 0 || len > INT32_MAX || dim < 0 || dim > kMaxHeadDim) return PURO_ERR_SHAPE;
+    if ((dim % 16) != 0) return PURO_ERR_ALIGN;
+    if (!(theta > 0.0) || !(theta <= 1.7976931348623157e308)) return PURO_ERR_UNSUPPORTED;
+    if (len == 0 || dim == 0) return PURO_OK;
+    if (!table) return PURO_ERR_NULL;
+    if (!aligned16(table)) return PURO_ERR_ALIGN;
+    launch_rope_table(reinterpret_cast<float2*>(table), len, dim, theta, stream);
+    return launched();
+}
+
+puro_status puro_qk_norm_rope_fwd(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim,
+                                  const puro_heads* q, const puro_heads* k, const uint16_t* gamma_q,
+                                  const uint16_t* gamma_k, float eps, const puro_rope* rope,
+                                  const puro_heads* q_out, const puro_heads* k_out, hipStream_t stream) {
+    QkArgs a{};
+    puro_status st = check_qk(batch, seq, heads_q, heads_k, head_dim, q, k, gamma_q, gamma_k, eps, rope, false, &a);
+    if (st != PURO_OK) return st;
+    if ((st = check_heads(q_out, batch, seq, heads_q, head_dim, true, &a.oq)) != PURO_OK) return st;
+    if ((st = check_heads(k_out, batch, seq, heads_k, head_dim, true, &a.ok)) != PURO_OK) return st;
+    if (a.tokens == 0 || heads_q + heads_k == 0) return PURO_OK;
+    launch_qk_norm_rope_fwd(a, stream);
+    return launched();
+}
+
+size_t puro_qk_norm_rope_bwd_workspace_size(int64_t batch, int64_t seq, int head_dim) {
+    int64_t tokens;
+    if (check_qk_sizes(batch, seq, 0, 0, head_dim, &tokens) != PURO_OK) return 0;
+    return qk_bwd_ws_bytes(tokens, head_dim);
+}
+
+puro_status puro_qk_norm_rope_bwd(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim,
+                                  const puro_heads* dq, const puro_heads* dk, const puro_heads* dv,
+                                  const puro_heads* q, const puro_heads* k, const uint16_t* gamma_q,
+                                  const uint16_t* gamma_k, float eps, const puro_rope* rope,
+                                  const puro_heads* dq_in, const puro_heads* dk_in, const puro_heads* dv_in,
+                                  float* dgamma_q, float* dgamma_k, void* ws, size_t ws_bytes,
+                                  hipStream_t stream) {
+    QkArgs a{};
+    puro_status st = check_qk(batch, seq, heads_q, heads_k, head_dim, q, k, gamma_q, gamma_k, eps, rope, true, &a);
+    if (st != PURO_OK) return st;
+    if ((st = check_heads(dq, batch, seq, heads_q, head_dim, false, &a.dq)) != PURO_OK) return st;
+    if ((st = check_heads(dk, batch, seq, heads_k, head_dim, false, &a.dk)) != PURO_OK) return st;
+    if ((st = check_heads(dq_in, batch, seq, heads_q, head_dim, true, &a.oq)) != PURO_OK) return st;
+    if ((st = check_heads(dk_in, batch, seq, heads_k, head_dim, true, &a.ok)) != PURO_OK) return st;
+    if (dv || dv_in) {
+        if (!dv || !dv_in) return PURO_ERR_NULL;
+        if ((st = check_heads(dv, batch, seq, heads_k, head_dim, false, &a.dv)) != PURO_OK) return st;
+        if ((st = check_heads(dv_in, batch, seq, heads_k, head_dim, true, &a.ov)) != PURO_OK) return st;
+    }
+    a.dgq = dgamma_q; a.dgk = dgamma_k;
+    if ((st = check_dgamma(a)) != PURO_OK) return st;
+    const bool sums = dgamma_q || dgamma_k;
+    if (sums) {
+        if (!ws) return PURO_ERR_NULL;
+        if (!aligned16(ws)) return PURO_ERR_ALIGN;
+        if (ws_bytes < qk_bwd_ws_bytes(a.tokens, head_dim)) return PURO_ERR_WORKSPACE;
+    }
+    if (!sums && (a.tokens == 0 || heads_q + heads_k == 0)) return PURO_OK;
+    launch_qk_norm_rope_bwd(a, ws, stream);
+    return launched();
+}
+
+size_t puro_qk_norm_rope_bwd_quantize_workspace_size(int64_t batch, int64_t seq, int heads_q, int heads_k,
+                                                     int head_dim) {
+    int64_t tokens;
+    if (check_qk_sizes(batch, seq, heads_q, heads_k, head_dim, &tokens) != PURO_OK) return 0;
+    return qk_bwd_quantize_ws_bytes(tokens, heads_q, heads_k, head_dim);
+}
+
+puro_status puro_qk_norm_rope_bwd_quantize_fp8(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim,
+                                               const puro_heads* dq, const puro_heads* dk, const puro_heads* dv,
+                                               const puro_heads* q, const puro_heads* k, const uint16_t* gamma_q,
+                                               const uint16_t* gamma_k, float eps, const puro_rope* rope,
+                                               puro_fp8_format fmt, puro_scale_mode mode, puro_scale_rounding rnd,
+                                               uint8_t* q8, float* scale, uint8_t* qT, float* scaleT,
+                                               float* dgamma_q, float* dgamma_k, void* ws, size_t ws_bytes,
+                                               hipStream_t stream) {
+    QkArgs a{};
+    puro_status st = check_qk(batch, seq, heads_q, heads_k, head_dim, q, k, gamma_q, gamma_k, eps, rope, true, &a);
+    if (st != PURO_OK) return st;
+    if (head_dim != 64 && head_dim != 128) return PURO_ERR_UNSUPPORTED;
+    if ((st = check_heads(dq, batch, seq, heads_q, head_dim, false, &a.dq)) != PURO_OK) return st;
+    if ((st = check_heads(dk, batch, seq, heads_k, head_dim, false, &a.dk)) != PURO_OK) return st;
+    if ((st = check_heads(dv, batch, seq, heads_k, head_dim, false, &a.dv)) != PURO_OK) return st;
+    a.dgq = dgamma_q; a.dgk = dgamma_k;
+    if ((st = check_dgamma(a)) != PURO_OK) return st;
+    Source src;
+    src.kind = Source::kQkBwd;
+    src.qk = &a;
+    const int64_t cols = ((int64_t)heads_q + 2 * heads_k) * head_dim;
+    return quantize_impl(a.dq.p ? a.dq.p : a.dk.p, a.tokens, cols, cols, fmt, mode, rnd, nullptr, q8, scale, qT, scaleT, ws,
+                         ws_bytes, stream, src);
 }
 
 // ------------------------------------------------------------------- GEMM

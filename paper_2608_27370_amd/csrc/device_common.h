@@ -26,6 +26,22 @@ template <> struct Fp8Traits<kE5M2> {
 __device__ __forceinline__ float bf16lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// Division of x < 2^31 by a positive d fixed on the host: the high word of x
+// times m = ceil(2^(32 + s) / d), shifted by s, with 2^s < d <= 2^(s + 1); m d
+// exceeds 2^(32 + s) by less than d <= 2^(s + 1), which x < 2^31 keeps from
+// reaching the quotient.
+struct Divisor {
+    uint32_t d, m, s;
+    static Divisor of(uint32_t d) {
+        Divisor r{d, 0u, 0u};
+        if (d < 2) return r;
+        while ((2u << r.s) < d) ++r.s;
+        r.m = (uint32_t)(((1ull << (32 + r.s)) + d - 1) / d);
+        return r;
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t x) const { return d == 1 ? x : __umulhi(x, m) >> s; }
+};
+
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 

@@ -93,6 +93,50 @@ void launch_rmsnorm_quantize(int fmt, int mode, QuantArgs a, float eps, void* ws
 size_t swiglu_bwd_ws_bytes(int64_t rows, int64_t cols);
 void launch_swiglu_bwd_quantize(int fmt, int mode, QuantArgs a, void* ws, hipStream_t stream);
 
+// ---- query / key norm with rotation (qk_norm_rope.hip) --------------------------
+
+// Heads in memory: head h of token t = b seq + s starts at
+// p + b * bs + s * rs + h * hs (elements), its D values are contiguous.
+struct HeadsArg {
+    const uint16_t* p;
+    int64_t bs, rs, hs;
+};
+// The rotation: table [len][dim / 2] of (cos, sin), the position of each token
+// (NULL: its place s in its sequence); dim = 0: none.
+struct RopeArgs {
+    const float2* table;
+    const int32_t* pos;
+    int len, dim, interleaved;
+};
+struct QkArgs {
+    HeadsArg q, k;             // the heads before norm and rotation
+    HeadsArg dq, dk, dv;       // backward: the gradients coming in (dv.p NULL: no value heads)
+    HeadsArg oq, ok, ov;       // outputs: rotated heads, or (backward) the gradients of q, k, v
+    const uint16_t *gq, *gk;   // norm weights [D]; NULL: those heads are not normalised
+    float eps;
+    RopeArgs rope;
+    int64_t tokens;
+    int seq, hq, hk, D;
+    float* part;               // backward: partial sums of dgamma
+    float *dgq, *dgk;          // [D] each, or NULL
+};
+
+// Table of the angles p theta^(-2 i / dim) of positions p in [0, len), in
+// double precision, rounded to binary32.
+void launch_rope_table(float2* table, int64_t len, int dim, double theta, hipStream_t stream);
+void launch_qk_norm_rope_fwd(const QkArgs& a, hipStream_t stream);
+// ws holds qk_bwd_ws_bytes (the partial sums of dgamma).
+size_t qk_bwd_ws_bytes(int64_t tokens, int D);
+void launch_qk_norm_rope_bwd(QkArgs a, void* ws, hipStream_t stream);
+// out[d] = sum over i < n of part[i * ldp + d], in a fixed order, for both
+// kinds of heads (out NULL: not wanted)
+void launch_dgamma_sum(const float* part_q, int64_t nq, float* dgq, const float* part_k, int64_t nk, float* dgk,
+                       int64_t ldp, int D, hipStream_t stream);
+// The backward quantised: q, qT and their scales of the matrix [tokens,
+// (hq + 2 hk) D] of all heads' gradients, as `a` asks (quant.hip); D 64 or 128.
+size_t qk_bwd_quantize_ws_bytes(int64_t tokens, int hq, int hk, int D);
+void launch_qk_norm_rope_bwd_quantize(int fmt, int mode, QuantArgs a, QkArgs k, void* ws, hipStream_t stream);
+
 // ---- GEMM (gemm.hip) ----------------------------------------------------------
 
 // kSNone: an operand without scales (BF16 operands).

@@ -1,0 +1,264 @@
+// RMSNorm of the query and key heads and their position rotation, forward and
+// backward (gfx950). The mathematics and the lane layout: qk_norm_rope.h.
+//
+// Both passes read every value once and write it once; about ten operations a
+// byte leave them bound by memory. A wave takes one token and walks its heads
+// (64 / L at a time, L lanes a head), so that the position's cosines and sines
+// are loaded once per token instead of once per head: as binary32 they are
+// four times the size of a head's own BF16 values.
+
+#include <algorithm>
+
+#include "qk_norm_rope.h"
+
+namespace puro {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+// Heads that a lane has in flight: their loads are issued together.
+constexpr int kUnroll = 4;
+
+// Table of cosines and sines: the angle in double precision (at position 10^6
+// a binary32 angle is off by 0.03), reduced and evaluated there.
+__global__ __launch_bounds__(kThreads) void rope_table_kernel(float2* __restrict__ table, int64_t len, int dim,
+                                                              double theta) {
+    const int half = dim / 2;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= len * half) return;
+    const int64_t p = i / half;
+    const int e = (int)(i - p * half);
+    double s, c;
+    sincos((double)p * pow(theta, -2.0 * e / dim), &s, &c);
+    table[i] = make_float2((float)c, (float)s);
+}
+
+// Heads of one kind: block row y takes the query heads (0), the key heads (1)
+// or (backward) the value heads (2), so that a wave holds one kind's pointers
+// and strides in scalar registers, which are too few for all of them.
+
+// Forward: wave w takes steps [part * per, part * per + per) of 64 / L heads
+// of token w / parts. Few tokens are split over more waves.
+template <int L>
+__global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Divisor per_seq, int per) {
+    constexpr int GPW = 64 / L;
+    const bool key = blockIdx.y != 0;
+    const HeadsArg in = key ? a.k : a.q, out = key ? a.ok : a.oq;
+    const uint16_t* const gamma = key ? a.gk : a.gq;
+    const int heads = key ? a.hk : a.hq;
+    const int steps = (heads + GPW - 1) / GPW, parts = (steps + per - 1) / per;
+    if (parts == 0) return;
+    const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * kWaves + (int)(threadIdx.x >> 6));
+    const int t = w / parts, part = w - t * parts;
+    if (t >= a.tokens) return;
+    const int lane = threadIdx.x & 63, grp = lane / L;
+    const LaneRole role = lane_role<L>(a.D, a.rope.dim, a.rope.interleaved, lane);
+    const Token tok = token_of(t, per_seq);
+    const bool turned = a.rope.dim > 0, half = a.rope.dim == L * 8;
+    const uint16_t* const x = head_at(in, tok) + role.col;
+    uint16_t* const y = const_cast<uint16_t*>(head_at(out, tok)) + role.col;
+    Turn turn{};
+    if (turned) turn = load_turn(a.rope, role, a.rope.pos ? a.rope.pos[t] : tok.s, false);
+    uint4 gw{};
+    if (gamma) gw = *reinterpret_cast<const uint4*>(gamma + role.col);
+    const float inv_d = 1.0f / (float)a.D;
+    const int i1 = min(steps, part * per + per);
+    for (int i = part * per; i < i1; i += kUnroll) {
+        uint4 raw[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)     // (lanes past the last head read it again and store nothing)
+            raw[u] = *reinterpret_cast<const uint4*>(x + min((i + u) * GPW + grp, heads - 1) * in.hs);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (i + u >= i1) break;
+            const int h = (i + u) * GPW + grp;
+            float v[8], g[8];
+            unpack8(raw[u], v);
+            if (!role.holds) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+            }
+            if (gamma) {
+                const float r = head_rstd<L>(v, inv_d, a.eps);
+                unpack8(gw, g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = v[e] * r * g[e];
+            }
+            if (turned) turn8<L>(v, turn, role, a.rope.interleaved, half);
+            if (role.holds && h < heads) *reinterpret_cast<uint4*>(y + h * out.hs) = pack8(v);
+        }
+    }
+}
+
+// Backward: wave w takes tokens w, w + waves, ..; every lane keeps the sums of
+// dgamma of its eight columns in binary32, the block adds them up in a fixed
+// order and writes part[kind][block][D].
+template <int L>
+__global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Divisor per_seq) {
+    constexpr int GPW = 64 / L;
+    __shared__ float red[kWaves][L * 8];
+    const int kind = blockIdx.y;
+    const HeadsArg grad = kind == 0 ? a.dq : (kind == 1 ? a.dk : a.dv);
+    const HeadsArg out = kind == 0 ? a.oq : (kind == 1 ? a.ok : a.ov);
+    const uint16_t* const gamma = kind == 0 ? a.gq : (kind == 1 ? a.gk : nullptr);
+    // (heads that are not normalised are not read: the gradient stands in)
+    const HeadsArg in = !gamma ? grad : (kind == 0 ? a.q : a.k);
+    const int heads = kind == 0 ? a.hq : a.hk;
+    const int wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, grp = lane / L;
+    const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * kWaves + wave);
+    const int waves = (int)gridDim.x * kWaves;
+    const LaneRole role = lane_role<L>(a.D, a.rope.dim, a.rope.interleaved, lane);
+    const bool turned = kind < 2 && a.rope.dim > 0, half = a.rope.dim == L * 8;
+    float g[8], sum[8];
+    uint4 gw{};
+    if (gamma) gw = *reinterpret_cast<const uint4*>(gamma + role.col);
+    unpack8(gw, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+    const float inv_d = 1.0f / (float)a.D;
+    for (int64_t t64 = w; heads > 0 && t64 < a.tokens; t64 += waves) {
+        const int t = (int)t64;
+        const Token tok = token_of(t, per_seq);
+        const uint16_t* const d = head_at(grad, tok) + role.col;
+        const uint16_t* const x = head_at(in, tok) + role.col;
+        uint16_t* const y = const_cast<uint16_t*>(head_at(out, tok)) + role.col;
+        Turn turn{};
+        if (turned) turn = load_turn(a.rope, role, a.rope.pos ? a.rope.pos[t] : tok.s, true);
+        for (int i = 0; i * GPW < heads; i += kUnroll) {
+            uint4 rd[kUnroll], rx[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int h = min((i + u) * GPW + grp, heads - 1);
+                rd[u] = *reinterpret_cast<const uint4*>(d + h * grad.hs);
+                if (gamma) rx[u] = *reinterpret_cast<const uint4*>(x + h * in.hs);
+                else rx[u] = rd[u];
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                if ((i + u) * GPW >= heads) break;
+                const int h = (i + u) * GPW + grp;
+                const bool live = role.holds && h < heads;
+                float v[8], n[8], wg[8];
+                unpack8(rd[u], v);
+                unpack8(rx[u], n);
+                if (!role.holds) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = n[e] = 0.0f;
+                }
+                if (turned) turn8<L>(v, turn, role, a.rope.interleaved, half);
+                if (gamma) {
+                    norm_bwd8<L>(v, n, g, inv_d, a.eps, wg);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += live ? wg[e] : 0.0f;
+                }
+                // (an untouched head as its bits are: a signalling NaN is not made quiet)
+                if (live) *reinterpret_cast<uint4*>(y + h * out.hs) = turned || gamma ? pack8(v) : rd[u];
+            }
+        }
+    }
+    if (!a.part || kind == 2) return;
+    // the groups of a wave, then the block's waves
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float s = sum[e];
+#pragma unroll
+        for (int o = L; o < 64; o *= 2) s += __shfl_xor(s, o, 64);
+        if (grp == 0) red[wave][lane * 8 + e] = s;
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.D; c += kThreads)
+        a.part[((int64_t)kind * gridDim.x + blockIdx.x) * a.D + c] = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
+}
+
+// dgamma of 8 columns per block: 32 threads a column take every 32nd partial
+// sum, then add up in a tree.
+__global__ __launch_bounds__(kThreads) void dgamma_sum_kernel(const float* __restrict__ pq, int64_t nq,
+                                                              float* __restrict__ dgq, const float* __restrict__ pk,
+                                                              int64_t nk, float* __restrict__ dgk, int64_t ldp, int D) {
+    __shared__ float red[32][9];
+    const float* const p = blockIdx.y ? pk : pq;
+    float* const out = blockIdx.y ? dgk : dgq;
+    const int64_t n = blockIdx.y ? nk : nq;
+    const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
+    const int col = (int)blockIdx.x * 8 + c;
+    if (!out) return;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t i = r; i < n; i += 128) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + 32 * u < n) s[u] += p[(i + 32 * u) * ldp + col];
+    }
+    red[r][c] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    for (int o = 16; o >= 1; o >>= 1) {
+        if (r < o) red[r][c] += red[r + o][c];
+        __syncthreads();
+    }
+    if (r == 0) out[col] = red[0][c];
+}
+
+// Blocks of the backward per kind of heads: enough to fill the chip, each wave
+// with a token or more.
+int64_t bwd_blocks(int64_t tokens) {
+    return std::max<int64_t>(1, std::min<int64_t>((tokens + kWaves - 1) / kWaves, 512));
+}
+
+// f(std::integral_constant<int, L>) with the lanes of a head of D values.
+template <class F>
+void by_lanes(int D, F&& f) {
+    if (D <= 8) f(std::integral_constant<int, 1>{});
+    else if (D <= 16) f(std::integral_constant<int, 2>{});
+    else if (D <= 32) f(std::integral_constant<int, 4>{});
+    else if (D <= 64) f(std::integral_constant<int, 8>{});
+    else if (D <= 128) f(std::integral_constant<int, 16>{});
+    else f(std::integral_constant<int, 32>{});
+}
+
+}  // namespace
+
+void launch_rope_table(float2* table, int64_t len, int dim, double theta, hipStream_t stream) {
+    const int64_t n = len * (dim / 2);
+    if (n == 0) return;
+    rope_table_kernel<<<(unsigned)((n + kThreads - 1) / kThreads), kThreads, 0, stream>>>(table, len, dim, theta);
+}
+
+void launch_qk_norm_rope_fwd(const QkArgs& a, hipStream_t stream) {
+    const int heads = std::max(a.hq, a.hk);
+    if (a.tokens == 0 || heads == 0) return;
+    by_lanes(a.D, [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value, GPW = 64 / L;
+        const int steps = (heads + GPW - 1) / GPW;
+        const int per = a.tokens * steps <= 4096 ? 1 : steps;
+        const int64_t waves = a.tokens * ((steps + per - 1) / per);
+        qk_norm_rope_fwd_kernel<L><<<dim3((unsigned)((waves + kWaves - 1) / kWaves), a.hk > 0 ? 2 : 1), kThreads, 0, stream>>>(
+            a, Divisor::of((uint32_t)a.seq), per);
+    });
+}
+
+void launch_dgamma_sum(const float* part_q, int64_t nq, float* dgq, const float* part_k, int64_t nk, float* dgk,
+                       int64_t ldp, int D, hipStream_t stream) {
+    dgamma_sum_kernel<<<dim3((unsigned)(D / 8), 2), kThreads, 0, stream>>>(part_q, nq, dgq, part_k, nk, dgk, ldp, D);
+}
+
+size_t qk_bwd_ws_bytes(int64_t tokens, int D) {
+    return (size_t)bwd_blocks(tokens) * 2 * D * sizeof(float);
+}
+
+void launch_qk_norm_rope_bwd(QkArgs a, void* ws, hipStream_t stream) {
+    const bool sums = a.dgq || a.dgk;
+    const int64_t blocks = bwd_blocks(a.tokens);
+    a.part = sums ? reinterpret_cast<float*>(ws) : nullptr;
+    if (a.tokens > 0)
+        by_lanes(a.D, [&](auto lanes) {
+            qk_norm_rope_bwd_kernel<decltype(lanes)::value>
+                <<<dim3((unsigned)blocks, a.dv.p ? 3 : 2), kThreads, 0, stream>>>(a, Divisor::of((uint32_t)a.seq));
+        });
+    if (sums) {
+        const int64_t n = a.tokens > 0 ? blocks : 0;
+        launch_dgamma_sum(a.part, n, a.dgq, a.part + blocks * a.D, n, a.dgk, a.D, a.D, stream);
+    }
+}
+
+}  // namespace puro

@@ -39,6 +39,16 @@ class Operand(ctypes.Structure):
     _fields_ = [("data", _p), ("ld", _i64), ("fmt", _i), ("mode", _i), ("scale", _p)]
 
 
+class Heads(ctypes.Structure):
+    """puro_heads: where the heads of a [batch, seq, heads, head_dim] tensor are."""
+    _fields_ = [("data", _p), ("batch_stride", _i64), ("row_stride", _i64), ("head_stride", _i64)]
+
+
+class RopeArgs(ctypes.Structure):
+    """puro_rope."""
+    _fields_ = [("table", _p), ("len", _i64), ("dim", _i), ("interleaved", _i), ("positions", _p)]
+
+
 class Recipe(ctypes.Structure):
     """puro_linear_recipe."""
     _fields_ = [("x_fmt", _i), ("w_fmt", _i), ("dy_fmt", _i), ("blockwise", _i), ("rnd", _i)]
@@ -48,6 +58,8 @@ class Saved(ctypes.Structure):
     """puro_linear_saved."""
     _fields_ = [("xq_t", _p), ("x_scale", _p), ("wq_t", _p), ("w_scale", _p)]
 
+
+_HEADS, _ROPE = ctypes.POINTER(Heads), ctypes.POINTER(RopeArgs)
 
 _SIGS = {
     "puro_status_string": (ctypes.c_char_p, [_i]),
@@ -63,6 +75,15 @@ _SIGS = {
     "puro_rmsnorm_quantize_workspace_size": (_sz, [_i64, _i64]),
     "puro_rmsnorm_quantize_fp8": (_i, [_p, _p, _i64, _i64, _i64, ctypes.c_float, _i, _i, _i, _p, _p, _p, _p, _p,
                                        _p, _sz, _p]),
+    "puro_rope_table": (_i, [_p, _i64, _i, ctypes.c_double, _p]),
+    "puro_qk_norm_rope_fwd": (_i, [_i64, _i64, _i, _i, _i, _HEADS, _HEADS, _p, _p, ctypes.c_float, _ROPE, _HEADS,
+                                   _HEADS, _p]),
+    "puro_qk_norm_rope_bwd_workspace_size": (_sz, [_i64, _i64, _i]),
+    "puro_qk_norm_rope_bwd": (_i, [_i64, _i64, _i, _i, _i] + [_HEADS] * 5 + [_p, _p, ctypes.c_float, _ROPE]
+                              + [_HEADS] * 3 + [_p, _p, _p, _sz, _p]),
+    "puro_qk_norm_rope_bwd_quantize_workspace_size": (_sz, [_i64, _i64, _i, _i, _i]),
+    "puro_qk_norm_rope_bwd_quantize_fp8": (_i, [_i64, _i64, _i, _i, _i] + [_HEADS] * 5 + [_p, _p, ctypes.c_float, _ROPE]
+                                           + [_i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _sz, _p]),
     "puro_fp8_gemm_workspace_size": (_sz, [_i64, _i64, _i64, _i]),
     "puro_fp8_gemm_plan": (_i, [_i64, _i64, _i64, _i, _i, ctypes.POINTER(_i), ctypes.POINTER(_i),
                                 ctypes.POINTER(_i), ctypes.POINTER(_i), ctypes.POINTER(_i)]),
@@ -282,6 +303,205 @@ def swiglu_quantize_fp8(gu, cols, fmt, mode=SCALE_TENSOR, rnd=SCALE_FP32, want_q
         _ptr(gu), rows, cols, _ld(gu), fmt, mode, rnd, _ptr(q), _ptr(scale), _ptr(qT), _ptr(scaleT),
         _ptr(w), nb, _stream()))
     return dict(q=q, scale=scale, qT=qT, scaleT=scaleT)
+
+
+# ------------------------------- query / key norm with position rotation
+# (these calls take few microseconds on the GPU, so their checks are few operations each)
+def _check_tensor(t, what, dtypes, device):
+    """A tensor whose memory a kernel may take: its type, and its device the current one (whose stream runs it)."""
+    if t.dtype not in dtypes:
+        raise TypeError("%s: %s expected, got %s" % (what, " or ".join(str(d) for d in dtypes), t.dtype))
+    if t.get_device() != device:
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (what, t.device, device))
+
+
+_BF16_BITS = (torch.bfloat16, torch.int16, torch.uint16)
+_FP32, _INT32 = (torch.float32,), (torch.int32,)
+_current = torch.cuda.current_device
+
+
+@dataclass
+class Rope:
+    """The position rotation: table [length, dim / 2, 2] FP32 of (cos, sin) per position and pair (``rope_table``
+    makes one; a scaled or interpolated one does as well), pairs (i, i + dim / 2) or, interleaved, (2 i, 2 i + 1)."""
+    table: torch.Tensor
+    interleaved: bool = False
+
+    @property
+    def dim(self):
+        return 2 * self.table.shape[1]
+
+
+def rope_table(length, dim, theta=1e6, interleaved=False, device=None):
+    """The rotation by angles p theta^(-2 i / dim) at positions p < length (angles in double precision)."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    table = torch.empty(length, dim // 2, 2, dtype=torch.float32, device=device)
+    _check_tensor(table, "table", _FP32, _current())
+    _check("puro_rope_table", lib().puro_rope_table(_ptr(table), length, dim, float(theta), _stream()))
+    return Rope(table, interleaved)
+
+
+def _rope_args(rope, positions, tokens, device):
+    if rope is None:
+        return None
+    t = rope.table
+    n, half, two = t.shape
+    if two != 2 or not t.is_contiguous():
+        raise ValueError("the rotation's table is a contiguous [length, dim / 2, 2] tensor")
+    _check_tensor(t, "table", _FP32, device)
+    if positions is not None:
+        _check_tensor(positions, "positions", _INT32, device)
+        if positions.numel() != tokens or not positions.is_contiguous():
+            raise ValueError("positions: one for each of the %d tokens, contiguous" % tokens)
+        positions = positions.data_ptr()
+    return RopeArgs(t.data_ptr(), n, 2 * half, 1 if rope.interleaved else 0, positions)
+
+
+def _heads(t, what, shape, device):
+    """Heads [S, H, D] or [B, S, H, D] of any strides (D contiguous)."""
+    if t.shape != shape:
+        raise ValueError("%s: shape %s expected, got %s" % (what, tuple(shape), tuple(t.shape)))
+    if t.dtype not in _BF16_BITS or t.get_device() != device:
+        _check_tensor(t, what, _BF16_BITS, device)
+    st = t.stride()
+    if st[-1] != 1 and t.numel() > 0 and shape[-1] > 1:
+        raise ValueError("%s: the values of a head are contiguous" % what)
+    return Heads(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
+
+
+def _qk_sizes(q, k):
+    """(batch, seq, heads_q, heads_k, head_dim) of q [.., S, Hq, D] and k [.., S, Hk, D]."""
+    a, b = q.shape, k.shape
+    if len(a) == 3 and len(b) == 3:
+        a, b = (1, *a), (1, *b)
+    if len(a) != 4 or len(b) != 4:
+        raise ValueError("heads are [S, H, D] or [B, S, H, D], both kinds alike")
+    if a[0] != b[0] or a[1] != b[1] or a[3] != b[3]:
+        raise ValueError("q %s and k %s differ in more than their heads" % (tuple(q.shape), tuple(k.shape)))
+    return a[0], a[1], a[2], b[2], a[3]
+
+
+def _gamma(g, what, d, device):
+    if g is None:
+        return None
+    _check_tensor(g, what, _BF16_BITS, device)
+    if g.numel() != d or not g.is_contiguous():
+        raise ValueError("%s: %d contiguous values" % (what, d))
+    return g.data_ptr()
+
+
+def qk_norm_rope_fwd(q, k, gamma_q=None, gamma_k=None, rope=None, positions=None, eps=1e-6, q_out=None, k_out=None):
+    """RMSNorm (weights gamma [D], None: no norm) of every query and key head and the rotation by its token's
+    position (None: no rotation; positions None: a token's place in its sequence). q [.., S, Hq, D], k [.., S, Hk, D]
+    BF16 of any strides, for instance views of the QKV projection's output; returns (q_out, k_out), new contiguous
+    tensors or those given (which may be q and k themselves)."""
+    batch, seq, hq, hk, d = _qk_sizes(q, k)
+    dev = _current()
+    a, b = _heads(q, "q", q.shape, dev), _heads(k, "k", k.shape, dev)
+    q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
+    k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
+    _check("puro_qk_norm_rope_fwd", lib().puro_qk_norm_rope_fwd(
+        batch, seq, hq, hk, d, a, b, _gamma(gamma_q, "gamma_q", d, dev), _gamma(gamma_k, "gamma_k", d, dev), eps,
+        _rope_args(rope, positions, batch * seq, dev), _heads(q_out, "q_out", q.shape, dev),
+        _heads(k_out, "k_out", k.shape, dev), _stream()))
+    return q_out, k_out
+
+
+def _dgamma(gamma, want, d, device):
+    return torch.empty(d, dtype=torch.float32, device=device) if want and gamma is not None else None
+
+
+def _qk_grads(dq, dk, dv, q, k, gamma_q, gamma_k, rope, positions, eps, sizes, dev):
+    """The leading arguments of both backward calls."""
+    d = sizes[4]
+    return (*sizes, _heads(dq, "dq", dq.shape, dev), _heads(dk, "dk", dk.shape, dev),
+            _heads(dv, "dv", dk.shape, dev) if dv is not None else None, _heads(q, "q", dq.shape, dev),
+            _heads(k, "k", dk.shape, dev), _gamma(gamma_q, "gamma_q", d, dev), _gamma(gamma_k, "gamma_k", d, dev), eps,
+            _rope_args(rope, positions, sizes[0] * sizes[1], dev))
+
+
+def qk_norm_rope_bwd(dq, dk, dv, q, k, gamma_q=None, gamma_k=None, rope=None, positions=None, eps=1e-6, out=None,
+                     want_dgamma=True, ws=None):
+    """The gradient dqkv [tokens, (Hq + 2 Hk) D] (BF16) of the QKV projection's output, from the gradients of the
+    rotated heads and of the value heads ([.., S, H, D], any strides; dv None: [tokens, (Hq + Hk) D] without them),
+    and dgamma_q, dgamma_k [D] (FP32; None where there is no weight). q and k are the forward's inputs."""
+    batch, seq, hq, hk, d = sizes = _qk_sizes(dq, dk)
+    dev = _current()
+    args = _qk_grads(dq, dk, dv, q, k, gamma_q, gamma_k, rope, positions, eps, sizes, dev)
+    tokens, width = batch * seq, (hq + (2 if dv is not None else 1) * hk) * d
+    if out is None:
+        out = torch.empty(tokens, width, dtype=dq.dtype, device=dq.device)
+    elif tuple(out.shape) != (tokens, width):
+        raise ValueError("out: shape %s expected, got %s" % ((tokens, width), tuple(out.shape)))
+    _check_tensor(out, "out", _BF16_BITS, dev)
+    ld, at = _ld(out), out.data_ptr()
+    dgq, dgk = _dgamma(gamma_q, want_dgamma, d, dq.device), _dgamma(gamma_k, want_dgamma, d, dq.device)
+    nb = 0
+    if dgq is not None or dgk is not None:
+        ws, nb = _ws(_size("puro_qk_norm_rope_bwd_workspace_size", batch, seq, d), ws, dq.device)
+    _check("puro_qk_norm_rope_bwd", lib().puro_qk_norm_rope_bwd(
+        *args, Heads(at, ld * seq, ld, d), Heads(at + 2 * hq * d, ld * seq, ld, d),
+        Heads(at + 2 * (hq + hk) * d, ld * seq, ld, d) if dv is not None else None, _ptr(dgq), _ptr(dgk),
+        _ptr(ws) if nb else None, nb, _stream()))
+    return out, dgq, dgk
+
+
+def qk_norm_rope_bwd_quantize_fp8(dq, dk, dv, q, k, gamma_q=None, gamma_k=None, rope=None, positions=None, eps=1e-6,
+                                  fmt=E4M3, mode=SCALE_TENSOR, rnd=SCALE_FP32, want_q=True, want_qT=False,
+                                  want_dgamma=True, out=None, ws=None):
+    """qk_norm_rope_bwd with its dqkv quantised (for the QKV projection's Dgrad and Wgrad) instead of written;
+    returns dict(q, scale, qT, scaleT, dgamma_q, dgamma_k). Heads of 64 or 128 values."""
+    batch, seq, hq, hk, d = sizes = _qk_sizes(dq, dk)
+    args = _qk_grads(dq, dk, dv, q, k, gamma_q, gamma_k, rope, positions, eps, sizes, _current())
+    q8, scale, qT, scaleT = _quant_outputs(batch * seq, (hq + 2 * hk) * d, mode, want_q, want_qT, out, dq.device)
+    dgq, dgk = _dgamma(gamma_q, want_dgamma, d, dq.device), _dgamma(gamma_k, want_dgamma, d, dq.device)
+    ws, nb = _ws(_size("puro_qk_norm_rope_bwd_quantize_workspace_size", *sizes), ws, dq.device)
+    _check("puro_qk_norm_rope_bwd_quantize_fp8", lib().puro_qk_norm_rope_bwd_quantize_fp8(
+        *args, fmt, mode, rnd, _ptr(q8), _ptr(scale), _ptr(qT), _ptr(scaleT), _ptr(dgq), _ptr(dgk), _ptr(ws), nb,
+        _stream()))
+    return dict(q=q8, scale=scale, qT=qT, scaleT=scaleT, dgamma_q=dgq, dgamma_k=dgk)
+
+
+def _grad_heads(t):
+    """A gradient as the backward takes it: BF16, 16-byte vectors within a head."""
+    t = t.to(torch.bfloat16)
+    fits = t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and all(s >= 0 and s % 8 == 0 for s in t.stride()[:-1])
+    return t if fits else t.contiguous()
+
+
+class _QkNormRopeFn(torch.autograd.Function):
+    """(q, k, v) heads of a QKV projection's output through puro_qk_norm_rope_fwd; the backward assembles the
+    gradient of that output in one call from the saved output itself (nothing else is kept)."""
+
+    @staticmethod
+    def forward(ctx, qkv, gamma_q, gamma_k, heads_q, heads_k, rope, positions, eps):
+        if qkv.dtype != torch.bfloat16:
+            raise TypeError("the query / key norm takes BF16 heads")
+        heads = qkv.unflatten(-1, (heads_q + 2 * heads_k, -1))
+        q, k, v = heads.split((heads_q, heads_k, heads_k), dim=-2)
+        ctx.save_for_backward(qkv, gamma_q, gamma_k, positions, rope.table if rope is not None else None)
+        ctx.args = heads_q, heads_k, rope is not None and rope.interleaved, eps
+        q, k = qk_norm_rope_fwd(q, k, gamma_q, gamma_k, rope, positions, eps)
+        return q, k, v
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq, dk, dv):
+        qkv, gamma_q, gamma_k, positions, table = ctx.saved_tensors
+        heads_q, heads_k, interleaved, eps = ctx.args
+        rope = Rope(table, interleaved) if table is not None else None
+        q, k, _ = qkv.unflatten(-1, (heads_q + 2 * heads_k, -1)).split((heads_q, heads_k, heads_k), dim=-2)
+        dqkv, dgq, dgk = qk_norm_rope_bwd(_grad_heads(dq), _grad_heads(dk), _grad_heads(dv), q, k, gamma_q, gamma_k,
+                                          rope, positions, eps, want_dgamma=any(ctx.needs_input_grad[1:3]))
+        return (dqkv.view(qkv.shape), dgq.to(gamma_q.dtype) if dgq is not None else None,
+                dgk.to(gamma_k.dtype) if dgk is not None else None, None, None, None, None, None)
+
+
+def qk_norm_rope(qkv, heads_q, heads_k, gamma_q=None, gamma_k=None, rope=None, positions=None, eps=1e-6):
+    """The query / key norm with rotation as an autograd operation on a QKV projection's output [.., S, (Hq + 2 Hk) D]
+    (BF16, one or no leading batch dimension): returns q [.., S, Hq, D], k and v [.., S, Hk, D] for attention (v is a
+    view of qkv)."""
+    return _QkNormRopeFn.apply(qkv, gamma_q, gamma_k, heads_q, heads_k, rope, positions, eps)
 
 
 # ------------------------------------------------------------------- GEMM

@@ -306,8 +306,8 @@ def _own_rope(s):
         return P.qk_norm_rope_bwd(s["dq"], s["dk"], s["dv"], q, k, **args)
     mode, rnd = (P.SCALE_ROW_1x128, P.SCALE_POW2) if c["blockwise"] else (P.SCALE_TENSOR, P.SCALE_FP32)
     r = P.qk_norm_rope_bwd_quantize_fp8(s["dq"], s["dk"], s["dv"], q, k, fmt=P.E4M3, mode=mode, rnd=rnd, want_qT=True, **args)
-    scaleT = r["scaleT"] if c["blockwise"] else r["scale"]
-    return _values(r["q"], r["scale"]), _values(r["qT"], scaleT), r["dgamma_q"], r["dgamma_k"]
+    scale, scaleT = (r["scale"], r["scaleT"]) if c["blockwise"] else (r["scale"][0], r["scale"][0])
+    return _values(r["q"], scale), _values(r["qT"], scaleT), r["dgamma_q"], r["dgamma_k"]
 
 
 def _own_distill(s):

@@ -495,6 +495,52 @@ puro_status puro_lm_head_ce_bwd(const uint16_t* X, const uint16_t* W, const int3
                                 int64_t M, int64_t V, int64_t K, puro_lm_head_recipe recipe, float grad_scale,
                                 uint16_t* dX, float* dW, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ----------------------------- LM head with a teacher's top logits ---
+ * The LM head with distillation as its loss: the divergence of the student's
+ * distribution over the vocabulary from a teacher's, known by its topk largest
+ * entries per token. For hidden states X [M, K] and the output embedding
+ * W [V, K] (BF16, dense rows), a temperature tau and, per row, topk token ids
+ * [M, topk] (int32) with the teacher's values [M, topk] (FP32):
+ *   z = X W^T, a = z / tau, lse[m] = log sum_v exp(a[m, v])
+ *   q = softmax over the row's entries of value / tau   (PURO_DISTILL_LOGITS)
+ *   q = value, a probability as stored, not negative      (PURO_DISTILL_PROBS)
+ *   loss[m] = sum_j q_j (log q_j - a[m, id_j] + lse[m]),  0 log 0 = 0
+ *   z_top[m, j] = z[m, id_j]
+ *   backward, of grad_scale sum_m dloss[m] loss[m] (dloss NULL: ones):
+ *     dz_v = (dloss grad_scale / tau) (Q exp(a_v - lse) - sum_{j: id_j = v} q_j),
+ *     Q = sum_j q_j;  dX = dz W (BF16), dW = dz^T X (FP32 or BF16)
+ * An entry whose id lies outside [0, V) (-1, say: fewer than topk are known)
+ * does not count and has z_top 0; a row without entries (a padding token) has
+ * loss 0 and gradient 0, and so has one whose teacher logits are all -infinity. An id
+ * given twice counts twice: both q are added, which also mixes a hard target
+ * into PURO_DISTILL_PROBS. A NaN among the entries that count, or a teacher
+ * logit of +infinity, makes the row's loss and gradient NaN.
+ * No teacher beyond the entries is assumed (PROBS need not add up to 1).
+ *
+ * The logits are never stored (as puro_lm_head_ce_*): the forward keeps lse and
+ * z_top for the backward, which recomputes the logits in chunks of 8192 vocabulary
+ * columns. BF16 operands with binary32 accumulation, statistics and sums in
+ * binary32; dz is rounded once to BF16, the operand type of its GEMMs. dX and
+ * dW: either may be NULL to skip it. dw_type PURO_OUT_FP32, or PURO_OUT_BF16,
+ * the type a gradient has when ranks exchange it (Appendix C); accumulate_dW
+ * != 0 adds to an FP32 dW (with BF16: PURO_ERR_UNSUPPORTED).
+ *
+ * Any M >= 0 (0: dW is cleared), V >= 1, K a positive multiple of 8, each at
+ * most 2^21; topk from 1 to 1024; tau and 1 / tau positive and normal; X, W, dX, dW
+ * and ws 16-byte aligned. Nothing is allocated or synchronised. */
+typedef enum { PURO_DISTILL_LOGITS = 0, PURO_DISTILL_PROBS = 1 } puro_distill_target;
+size_t puro_lm_head_distill_workspace_size(int64_t M, int64_t V, int64_t K, int64_t topk, int backward);
+puro_status puro_lm_head_distill_fwd(const uint16_t* X, const uint16_t* W, const int32_t* ids, const float* teacher,
+                                     int64_t M, int64_t V, int64_t K, int64_t topk, puro_distill_target target,
+                                     float temperature, float* lse, float* loss, float* z_top, void* ws,
+                                     size_t ws_bytes, hipStream_t stream);
+puro_status puro_lm_head_distill_bwd(const uint16_t* X, const uint16_t* W, const int32_t* ids, const float* teacher,
+                                     const float* lse, const float* z_top, int64_t M, int64_t V, int64_t K,
+                                     int64_t topk, puro_distill_target target, float temperature,
+                                     const float* dloss, float grad_scale, uint16_t* dX, void* dW,
+                                     puro_out_dtype dw_type, int accumulate_dW, void* ws, size_t ws_bytes,
+                                     hipStream_t stream);
+
 /* ---------------------------------------------------------------- MuonH ---
  * Section 3.3 (Hyperball Optimization), equation hyperball-update: a wrapped
  * matrix keeps its initial Frobenius radius R; with the Muon update u and the

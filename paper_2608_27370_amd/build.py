@@ -22,6 +22,7 @@ LIB = os.path.join(HERE, "libpuro.so")
 GEMM_VARIANTS = [(fa, fb, g) for fa in (0, 1) for fb in (0, 1) for g in (0, 1)] + [(2, 2, 0)]   # + BF16
 SOURCES = [("quant.hip", "quant", []), ("qk_quant.hip", "qk_quant", []),
            ("qk_norm_rope.hip", "qk_norm_rope", []), ("gemm.hip", "gemm", []), ("lm_head.hip", "lm_head", []),
+           ("lm_distill.hip", "lm_distill", []),
            ("transpose.hip", "transpose", []), ("muonh.hip", "muonh", []), ("api.cpp", "api", [])] + [
     ("gemm_kernel.hip", "gemm_kernel_%d%d%d" % v, ["-DPURO_FA=%d" % v[0], "-DPURO_FB=%d" % v[1], "-DPURO_GROUPED=%d" % v[2]])
     for v in GEMM_VARIANTS]

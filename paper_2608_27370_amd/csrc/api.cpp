@@ -893,6 +893,88 @@ puro_status puro_lm_head_ce_bwd(const uint16_t* X, const uint16_t* W, const int3
 
 }  // extern "C"
 
+// ------------------------------------- LM head with a teacher's top logits
+namespace {
+
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+puro_status check_distill_sizes(int64_t M, int64_t V, int64_t K, int64_t topk) {
+    // BF16 operand pitches (2 M, 2 V, 2 K bytes, padded to 128 values) within 2^22
+    const int64_t lim = (int64_t)1 << 21;
+    if (M < 0 || V <= 0 || K <= 0 || M > lim || V > lim || K > lim) return PURO_ERR_SHAPE;
+    if (topk < 1 || topk > 1024) return PURO_ERR_SHAPE;
+    if ((K % 8) != 0) return PURO_ERR_ALIGN;
+    return PURO_OK;
+}
+
+puro_status check_distill(const uint16_t* X, const uint16_t* W, const int32_t* ids, const float* teacher, int64_t M,
+                          int64_t V, int64_t K, int64_t topk, puro_distill_target target, float tau, DistillArgs* a) {
+    const puro_status st = check_distill_sizes(M, V, K, topk);
+    if (st != PURO_OK) return st;
+    if (target != PURO_DISTILL_LOGITS && target != PURO_DISTILL_PROBS) return PURO_ERR_UNSUPPORTED;
+    const float least = 1.17549435e-38f, most = 1.0f / least;
+    if (!(tau >= least) || !(tau <= most)) return PURO_ERR_UNSUPPORTED;
+    if (M > 0) {
+        if (!X || !W || !ids || !teacher) return PURO_ERR_NULL;
+        if (!aligned16(X) || !aligned16(W) || !aligned4(ids) || !aligned4(teacher)) return PURO_ERR_ALIGN;
+    }
+    *a = DistillArgs{X, W, ids, teacher, M, V, K, topk, target == PURO_DISTILL_PROBS, tau};
+    return PURO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t puro_lm_head_distill_workspace_size(int64_t M, int64_t V, int64_t K, int64_t topk, int backward) {
+    if (check_distill_sizes(M, V, K, topk) != PURO_OK || M == 0) return 0;
+    return lm_distill_ws_bytes(M, V, K, topk, backward != 0);
+}
+
+puro_status puro_lm_head_distill_fwd(const uint16_t* X, const uint16_t* W, const int32_t* ids, const float* teacher,
+                                     int64_t M, int64_t V, int64_t K, int64_t topk, puro_distill_target target,
+                                     float temperature, float* lse, float* loss, float* z_top, void* ws,
+                                     size_t ws_bytes, hipStream_t stream) {
+    DistillArgs a;
+    const puro_status st = check_distill(X, W, ids, teacher, M, V, K, topk, target, temperature, &a);
+    if (st != PURO_OK) return st;
+    if (M == 0) return PURO_OK;
+    if (!lse || !loss || !z_top || !ws) return PURO_ERR_NULL;
+    if (!aligned4(lse) || !aligned4(loss) || !aligned4(z_top) || !aligned16(ws)) return PURO_ERR_ALIGN;
+    if (ws_bytes < lm_distill_ws_bytes(M, V, K, topk, false)) return PURO_ERR_WORKSPACE;
+    launch_lm_distill_fwd(a, lse, loss, z_top, ws, stream);
+    return launched();
+}
+
+puro_status puro_lm_head_distill_bwd(const uint16_t* X, const uint16_t* W, const int32_t* ids, const float* teacher,
+                                     const float* lse, const float* z_top, int64_t M, int64_t V, int64_t K,
+                                     int64_t topk, puro_distill_target target, float temperature,
+                                     const float* dloss, float grad_scale, uint16_t* dX, void* dW,
+                                     puro_out_dtype dw_type, int accumulate_dW, void* ws, size_t ws_bytes,
+                                     hipStream_t stream) {
+    DistillArgs a;
+    const puro_status st = check_distill(X, W, ids, teacher, M, V, K, topk, target, temperature, &a);
+    if (st != PURO_OK) return st;
+    if (!(grad_scale >= -3.4028235e38f) || !(grad_scale <= 3.4028235e38f)) return PURO_ERR_UNSUPPORTED;
+    if (dw_type != PURO_OUT_BF16 && dw_type != PURO_OUT_FP32) return PURO_ERR_UNSUPPORTED;
+    if (dW && accumulate_dW && dw_type != PURO_OUT_FP32) return PURO_ERR_UNSUPPORTED;
+    if ((dX && !aligned16(dX)) || (dW && !aligned16(dW))) return PURO_ERR_ALIGN;
+    if (M == 0) {
+        // sums of nothing
+        if (!dW || accumulate_dW) return PURO_OK;
+        launch_zero(dW, V * K * (dw_type == PURO_OUT_FP32 ? 4 : 2), stream);
+        return launched();
+    }
+    if (!lse || !z_top || !ws) return PURO_ERR_NULL;
+    if (!aligned4(lse) || !aligned4(z_top) || !aligned4(dloss) || !aligned16(ws)) return PURO_ERR_ALIGN;
+    if (ws_bytes < lm_distill_ws_bytes(M, V, K, topk, true)) return PURO_ERR_WORKSPACE;
+    if (!dX && !dW) return PURO_OK;
+    launch_lm_distill_bwd(a, lse, z_top, dloss, grad_scale, dX, dW, dw_type == PURO_OUT_BF16, accumulate_dW != 0, ws, stream);
+    return launched();
+}
+
+}  // extern "C"
+
 // ------------------------------------------------------------------- MuonH
 namespace {
 

@@ -237,7 +237,9 @@ void run_plan(const GemmProblem& g, const Plan& pl, void* ws, hipStream_t stream
     prm.bsa = g.bsa * eb; prm.bsb = g.bsb * eb; prm.bsd = g.bsd * ob; prm.bsr = g.bsr;
     prm.targets = g.targets; prm.col0 = g.col0;
     prm.stats = g.stats; prm.stats_ld = g.stats_ld; prm.zt = g.zt;
-    prm.lse = g.lse; prm.grad_scale = g.grad_scale;
+    prm.lse = g.lse; prm.grad_scale = g.grad_scale; prm.row_scale = g.row_scale;
+    prm.rows_a = (int)(g.rows_a ? g.rows_a : g.M);
+    prm.rows_b = (int)(g.rows_b ? g.rows_b : g.N);
     prm.q8 = g.q8; prm.q8_scale = g.q8_scale; prm.q8t = g.q8t; prm.q8t_scale = g.q8t_scale;
     const bool grouped = grouped_scales(g);
     const int out = pl.splits > 1 ? 2 : g.out;

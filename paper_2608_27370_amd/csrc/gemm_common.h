@@ -50,8 +50,10 @@ struct Params {
     float2* stats;             // [M][stats_ld]: (max, sum exp(z - max)) per 128-column block
     int64_t stats_ld;
     float* zt;                 // [M]: the target's logit
-    const float* lse;          // [M]
+    const float* lse;          // [rows_a]
     float grad_scale;
+    const float* row_scale;    // kOutSoftmaxGrad: a factor per row in place of grad_scale, or NULL
+    int rows_a, rows_b;        // rows that A and B have (M and N, or fewer)
     uint8_t* q8;               // kOutSoftmaxGradQ: dz's FP8 copies (the GemmProblem fields)
     float* q8_scale;
     uint8_t* q8t;

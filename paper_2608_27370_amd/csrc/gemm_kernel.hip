@@ -386,7 +386,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     const int s0 = ks * p.ksteps_per_split;
     const int s1 = min((ks + 1) * p.ksteps_per_split, p.ksteps);
 
-    const int valid_m = min(BM, p.M - m0), valid_n = min(BN, p.N - n0);
+    const int valid_m = min(BM, p.rows_a - m0), valid_n = min(BN, p.rows_b - n0);
     const v4i ra = make_rsrc(p.A + (int64_t)m0 * p.lda, (uint32_t)(valid_m * p.lda));
     const v4i rb = make_rsrc(p.B + (int64_t)n0 * p.ldb, (uint32_t)(valid_n * p.ldb));
 
@@ -796,8 +796,10 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int64_t m = (int64_t)mrow0 + i * 32 + (lane & 31);
-            tcol[i] = m < p.M ? p.targets[m] - p.col0 - ncol0 - 4 * hl : INT_MIN;
+            tcol[i] = p.targets && m < p.M ? p.targets[m] - p.col0 - ncol0 - 4 * hl : INT_MIN;
         }
+        // columns of the lane past the last one (a ragged last block) count as minus infinity
+        const int past = p.N - ncol0 - 4 * hl;
         constexpr float kLog2e = 1.44269504088896340736f;
         static_for<FM>([&](auto i_c) __attribute__((always_inline)) {
             constexpr int i = decltype(i_c)::value;
@@ -807,6 +809,13 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             if (alpha != 1.0f) {
 #pragma unroll
                 for (int e = 0; e < FN * 16; ++e) v[e] *= alpha;
+            }
+            if (ncol0 + WTN > p.N) {
+#pragma unroll
+                for (int e = 0; e < FN * 16; ++e) {
+                    const int c = e / 16 * 32 + 8 * (e % 16 / 4) + e % 4;
+                    v[e] = c < past ? v[e] : -__builtin_inff();
+                }
             }
             float mq[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
@@ -918,19 +927,22 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             constexpr float kL2eLo = 1.925962989e-8f;                // log2(e) - kL2eHi
             constexpr float kLn2 = 0.693147180559945309f;
             constexpr float kL2eLoLn2 = kL2eLo * kLn2;
-            float row_p[kDz ? FM : 1], row_k[kDz ? FM : 1];
+            float row_p[kDz ? FM : 1], row_k[kDz ? FM : 1], row_g[kDz ? FM : 1];
             int row_tgt[kDz ? FM : 1];
             if constexpr (kDz) {
 #pragma unroll
                 for (int i = 0; i < FM; ++i) {
                     const int64_t m = (int64_t)mrow0 + i * 32 + (lane & 31);
-                    row_tgt[i] = p.targets[m] - p.col0 - ncol0 - 4 * (lane >> 5);
-                    const float l = p.lse[m];
+                    // (rows that A does not have: z = 0, and a gradient of 0 (e^0))
+                    const bool has = m < p.rows_a;
+                    row_tgt[i] = p.targets ? p.targets[m] - p.col0 - ncol0 - 4 * (lane >> 5) : INT_MIN;
+                    const float l = has ? p.lse[m] : 0.0f;
+                    row_g[i] = p.row_scale ? (has ? p.row_scale[m] : 0.0f) : p.grad_scale;
                     row_p[i] = l * kL2eHi;
                     row_k[i] = 1.0f - (fmaf(l, kL2eHi, -row_p[i]) + l * kL2eLo) * kLn2;
                 }
             }
-            (void)row_p; (void)row_k; (void)row_tgt;
+            (void)row_p; (void)row_k; (void)row_tgt; (void)row_g;
             // The bias / residual epilogue in the same one pass: the wave's
             // residual block arrives in its LDS region by DMA, each 16-byte
             // chunk already where the staged output chunk will sit (the lane
@@ -996,7 +1008,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                         // the four sums are columns j*32 + 8g + {0..3} past the
                         // lane's first: tr is the target's position among them
                         const int tr = row_tgt[i] - (j * 32 + 8 * g);
-                        const float P = row_p[i], K = row_k[i], gs = p.grad_scale;
+                        const float P = row_p[i], K = row_k[i], gs = row_g[i];
                         auto dz = [&](float z, int c) __attribute__((always_inline)) {
                             // 2^(z log2 e - lse log2 e) = 2^t (1 + c)
                             const float e = __builtin_amdgcn_exp2f(fmaf(z, kL2eHi, -P)) * fmaf(z, kL2eLoLn2, K);

@@ -204,6 +204,13 @@ struct GemmProblem {
     float* zt;
     const float* lse;
     float grad_scale;
+    // kOutSoftmaxGrad: a factor per row [rows_a] in place of grad_scale; the
+    // rows that A and B have (0: M and N), fewer than the output, whose M and
+    // N are multiples of 128: dz of rows past them is zero, that of columns
+    // past them is left to be cleared. targets NULL: no one-hot term (nor, in
+    // kOutLseStats, a target's logit)
+    const float* row_scale = nullptr;
+    int64_t rows_a = 0, rows_b = 0;
     // kOutSoftmaxGradQ: dz's row-grouped codes [M, N] (ld N) with scales
     // [N / 128][M], and its transposed column-grouped codes [N, M] (ld M)
     // with scales [M / 128][N] (scale arrays k-block-major)
@@ -229,9 +236,11 @@ int gemm_tile(const GemmProblem& p);
 // dst [C, R] (pitch ldd) = src [R, C] (pitch lds), for `batch` problems whose
 // source and destination start bs_src and bs_dst elements after the previous
 // one's. R, C, the pitches and the strides are multiples of 8, the pointers
-// 16-byte aligned (every caller's shapes are multiples of 128).
+// 16-byte aligned (most callers' shapes are multiples of 128). With Rp > 0 (a
+// multiple of 8, Rp >= R) dst is [C, Rp], zeros from column R on, and R may be
+// any number.
 void transpose_bf16(const uint16_t* src, int64_t R, int64_t C, int64_t lds, uint16_t* dst, int64_t ldd,
-                    hipStream_t stream, int batch = 1, int64_t bs_src = 0, int64_t bs_dst = 0);
+                    hipStream_t stream, int batch = 1, int64_t bs_src = 0, int64_t bs_dst = 0, int64_t Rp = 0);
 // The lower triangle of tiles of a symmetric A [R, R] (pitch ld, R a
 // multiple of 64 and of tg) from the upper one: element (i, j) = (j, i)
 // wherever i / tg > j / tg; `batch` matrices bs elements apart.
@@ -256,6 +265,26 @@ void launch_lm_head_fwd(const uint16_t* X, const uint16_t* W, const int32_t* tar
 void launch_lm_head_bwd(const uint16_t* X, const uint16_t* W, const int32_t* targets, const float* lse, int64_t M,
                         int64_t V, int64_t K, int fp8, float grad_scale, uint16_t* dX, float* dW, void* ws,
                         hipStream_t stream);
+
+// ---- LM head with a teacher's top logits (lm_distill.hip) -----------------------
+
+struct DistillArgs {
+    const uint16_t *X, *W;     // [M, K], [V, K] BF16, dense rows
+    const int32_t* ids;        // [M, k]: entries outside [0, V) do not count
+    const float* teacher;      // [M, k]: logits, or (probs) weights
+    int64_t M, V, K, k;
+    int probs;
+    float tau;
+};
+size_t lm_distill_ws_bytes(int64_t M, int64_t V, int64_t K, int64_t k, bool bwd);
+// lse [M], loss [M] and the student's logits z_top [M, k] at the entries.
+void launch_lm_distill_fwd(const DistillArgs& a, float* lse, float* loss, float* z_top, void* ws, hipStream_t stream);
+// dX (BF16) and dW (BF16 or FP32, added to when accumulate_dw) of
+// grad_scale sum_m dloss_m loss_m (dloss NULL: ones); either NULL: not wanted.
+void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* z_top, const float* dloss, float grad_scale,
+                           uint16_t* dX, void* dW, bool dw_bf16, int accumulate_dw, void* ws, hipStream_t stream);
+// Zeros over `bytes` (a multiple of 16) from a 16-byte aligned address.
+void launch_zero(void* dst, int64_t bytes, hipStream_t stream);
 
 // ---- MuonH (muonh.hip) ---------------------------------------------------------
 

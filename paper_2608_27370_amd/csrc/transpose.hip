@@ -14,12 +14,12 @@ constexpr int kT = 64;   // tile edge
 // dst [C, R] (pitch ldd) = src [R, C] (pitch lds) of problem blockIdx.z, in
 // 64 x 64 tiles; R, C and both pitches are multiples of 8 (a 16-byte chunk
 // never straddles an edge). Each thread moves two 16-byte chunks in and two
-// out. The tile sits in LDS as 64 rows of 33 words (one padding word): a
+// out; columns of dst from R up to Rp become zeros. The tile sits in LDS as 64 rows of 33 words (one padding word): a
 // wave's column reads (8 source rows x 8 columns, the lanes' chunks) then
 // fall on 32 distinct banks, two lanes sharing each word.
 __global__ __launch_bounds__(256) void transpose_bf16_kernel(const uint16_t* __restrict__ src, int64_t R, int64_t C,
                                                              int64_t lds, uint16_t* __restrict__ dst, int64_t ldd,
-                                                             int64_t bs_src, int64_t bs_dst) {
+                                                             int64_t bs_src, int64_t bs_dst, int64_t Rp) {
     constexpr int kW = kT / 2 + 1;       // words per LDS row
     __shared__ uint32_t t[kT * kW];
     src += blockIdx.z * bs_src;
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) void transpose_bf16_kernel(const uint16_t* __r
             const uint32_t word = t[(ch * 8 + i) * kW + (cc >> 1)];
             e[i] = (cc & 1) ? (word >> 16) : (word & 0xFFFFu);
         }
-        if (c < C && r < R)
+        if (c < C && r < Rp)
             *reinterpret_cast<uint4*>(dst + c * ldd + r) =
                 make_uint4(e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16), e[6] | (e[7] << 16));
     }
@@ -93,10 +93,11 @@ __global__ __launch_bounds__(256) void mirror_lower_bf16_kernel(uint16_t* __rest
 }  // namespace
 
 void transpose_bf16(const uint16_t* src, int64_t R, int64_t C, int64_t lds, uint16_t* dst, int64_t ldd,
-                    hipStream_t stream, int batch, int64_t bs_src, int64_t bs_dst) {
+                    hipStream_t stream, int batch, int64_t bs_src, int64_t bs_dst, int64_t Rp) {
     if (R <= 0 || C <= 0 || batch <= 0) return;
-    const dim3 grid((unsigned)((C + kT - 1) / kT), (unsigned)((R + kT - 1) / kT), (unsigned)batch);
-    transpose_bf16_kernel<<<grid, 256, 0, stream>>>(src, R, C, lds, dst, ldd, bs_src, bs_dst);
+    if (Rp == 0) Rp = R;
+    const dim3 grid((unsigned)((C + kT - 1) / kT), (unsigned)((Rp + kT - 1) / kT), (unsigned)batch);
+    transpose_bf16_kernel<<<grid, 256, 0, stream>>>(src, R, C, lds, dst, ldd, bs_src, bs_dst, Rp);
 }
 
 void mirror_lower_bf16(uint16_t* A, int64_t R, int64_t ld, int tg, hipStream_t stream, int batch, int64_t bs) {

@@ -101,6 +101,10 @@ _SIGS = {
     "puro_lm_head_ce_workspace_size": (_sz, [_i64, _i64, _i64, _i, _i]),
     "puro_lm_head_ce_fwd": (_i, [_p, _p, _p, _i64, _i64, _i64, _i, _p, _p, _p, _sz, _p]),
     "puro_lm_head_ce_bwd": (_i, [_p, _p, _p, _p, _i64, _i64, _i64, _i, ctypes.c_float, _p, _p, _p, _sz, _p]),
+    "puro_lm_head_distill_workspace_size": (_sz, [_i64, _i64, _i64, _i64, _i]),
+    "puro_lm_head_distill_fwd": (_i, [_p, _p, _p, _p, _i64, _i64, _i64, _i64, _i, ctypes.c_float, _p, _p, _p, _p, _sz, _p]),
+    "puro_lm_head_distill_bwd": (_i, [_p, _p, _p, _p, _p, _p, _i64, _i64, _i64, _i64, _i, ctypes.c_float, _p,
+                                      ctypes.c_float, _p, _p, _i, _i, _p, _sz, _p]),
     "puro_muonh_workspace_size": (_sz, [_i64, _i64, _i64]),
     "puro_muonh_step": (_i, [_i64, _i64, _i64, _p, _p, _p, _p, _p, ctypes.c_float, _i, ctypes.c_float, _i, _p,
                              _p, _sz, _p]),
@@ -741,6 +745,100 @@ def lm_head_ce_bwd(X, W, targets, lse, recipe=LM_HEAD_BF16, grad_scale=1.0, dX=N
         _ptr(X), _ptr(W), _ptr(targets), _ptr(lse), M, V, K, recipe, float(grad_scale), _ptr(dX), _ptr(dW),
         _ptr(w), nb, _stream()))
     return dX, dW
+
+
+# ------------------------------------- LM head with a teacher's top logits
+DISTILL_LOGITS, DISTILL_PROBS = 0, 1
+
+
+def lm_head_distill_workspace_size(M, V, K, topk, backward):
+    return _size("puro_lm_head_distill_workspace_size", M, V, K, topk, int(bool(backward)))
+
+
+def _dense(t, what, dtypes, shape, device):
+    _check_tensor(t, what, dtypes, device)
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s: a contiguous %s tensor expected, got %s" % (what, shape, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _distill_args(X, W, ids, teacher, dev):
+    """Sizes and the pointers of the inputs that both passes take."""
+    if X.dim() != 2 or W.dim() != 2 or ids.dim() != 2:
+        raise ValueError("X [M, K], W [V, K], ids and teacher [M, topk]")
+    (M, K), V, k = X.shape, W.shape[0], ids.shape[1]
+    return M, V, K, k, (_dense(X, "X", _BF16_BITS, (M, K), dev), _dense(W, "W", _BF16_BITS, (V, K), dev),
+                        _dense(ids, "ids", _INT32, (M, k), dev), _dense(teacher, "teacher", _FP32, (M, k), dev))
+
+
+def lm_head_distill_fwd(X, W, ids, teacher, temperature=1.0, target=DISTILL_LOGITS, lse=None, loss=None, z_top=None,
+                        ws=None):
+    """The divergence of softmax(X W^T / temperature) from a teacher known by its topk entries per row: ids [M, topk]
+    int32 (-1: none) and teacher [M, topk] FP32 logits (their softmax is taken) or probabilities (DISTILL_PROBS).
+    Returns (lse, loss, z_top): [M], [M] and the student's logits [M, topk]; the logits X W^T are never stored."""
+    dev = _current()
+    M, V, K, k, inputs = _distill_args(X, W, ids, teacher, dev)
+    new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=X.device)      # noqa: E731
+    lse, loss, z_top = new(M) if lse is None else lse, new(M) if loss is None else loss, new(M, k) if z_top is None else z_top
+    w, nb = _ws(lm_head_distill_workspace_size(M, V, K, k, False), ws, X.device)
+    _check("puro_lm_head_distill_fwd", lib().puro_lm_head_distill_fwd(
+        *inputs, M, V, K, k, target, temperature, _dense(lse, "lse", _FP32, (M,), dev), _dense(loss, "loss", _FP32, (M,), dev),
+        _dense(z_top, "z_top", _FP32, (M, k), dev), _ptr(w), nb, _stream()))
+    return lse, loss, z_top
+
+
+def lm_head_distill_bwd(X, W, ids, teacher, lse, z_top, temperature=1.0, target=DISTILL_LOGITS, dloss=None,
+                        grad_scale=1.0, want_dx=True, want_dw=True, dX=None, dW=None, accumulate_dw=False, ws=None):
+    """dX [M, K] (BF16) and dW [V, K] (FP32; a BF16 tensor given as dW is filled in BF16) of grad_scale times the sum
+    of dloss [M] (None: ones) times the losses, from what the forward kept."""
+    dev = _current()
+    M, V, K, k, inputs = _distill_args(X, W, ids, teacher, dev)
+    if want_dx and dX is None:
+        dX = torch.empty(M, K, dtype=torch.bfloat16, device=X.device)
+    if want_dw and dW is None:
+        dW = (torch.zeros if accumulate_dw else torch.empty)(V, K, dtype=torch.float32, device=X.device)
+    px = _dense(dX, "dX", _BF16_BITS, (M, K), dev) if want_dx else None
+    pw = _dense(dW, "dW", (torch.float32, torch.bfloat16), (V, K), dev) if want_dw else None
+    out = OUT_BF16 if want_dw and dW.dtype == torch.bfloat16 else OUT_FP32
+    w, nb = _ws(lm_head_distill_workspace_size(M, V, K, k, True), ws, X.device)
+    _check("puro_lm_head_distill_bwd", lib().puro_lm_head_distill_bwd(
+        *inputs, _dense(lse, "lse", _FP32, (M,), dev), _dense(z_top, "z_top", _FP32, (M, k), dev), M, V, K, k, target,
+        temperature, _dense(dloss, "dloss", _FP32, (M,), dev) if dloss is not None else None, grad_scale, px, pw, out,
+        int(bool(accumulate_dw)), _ptr(w), nb, _stream()))
+    return (dX if want_dx else None), (dW if want_dw else None)
+
+
+class _DistillFn(torch.autograd.Function):
+    """loss [M] through puro_lm_head_distill_fwd; the backward recomputes the logits. With a ``main_grad`` FP32
+    buffer on W, dW is accumulated into it and W gets no .grad; otherwise W's .grad is dW in BF16."""
+
+    @staticmethod
+    def forward(ctx, X, W, ids, teacher, temperature, target):
+        if X.dtype != torch.bfloat16 or W.dtype != torch.bfloat16:
+            raise TypeError("the LM head takes BF16 X and W")
+        main_grad = getattr(W, "main_grad", None)
+        X, W = X.contiguous(), W.contiguous()
+        lse, loss, z_top = lm_head_distill_fwd(X, W, ids, teacher, temperature, target)
+        ctx.save_for_backward(X, W, ids, teacher, lse, z_top)
+        ctx.args = temperature, target, main_grad
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        X, W, ids, teacher, lse, z_top = ctx.saved_tensors
+        temperature, target, mg = ctx.args
+        want_dx, want_dw = ctx.needs_input_grad[:2]
+        dW = mg if mg is not None or not want_dw else torch.empty_like(W)
+        dX, dW = lm_head_distill_bwd(X, W, ids, teacher, lse, z_top, temperature, target, dloss.contiguous(),
+                                     want_dx=want_dx, want_dw=want_dw, dW=dW, accumulate_dw=want_dw and mg is not None)
+        return dX, dW if mg is None else None, None, None, None, None
+
+
+def lm_head_distill(X, W, ids, teacher, temperature=1.0, target=DISTILL_LOGITS):
+    """The distillation loss [M] of X [M, K] and W [V, K] (BF16) as an autograd operation (``lm_head_distill_fwd``);
+    no gradient flows to the teacher's values."""
+    return _DistillFn.apply(X, W, ids, teacher, temperature, target)
 
 
 # ------------------------------------------------------------------- MuonH

@@ -518,8 +518,9 @@ puro_status puro_lm_head_ce_bwd(const uint16_t* X, const uint16_t* W, const int3
  * No teacher beyond the entries is assumed (PROBS need not add up to 1).
  *
  * The logits are never stored (as puro_lm_head_ce_*): the forward keeps lse and
- * z_top for the backward, which recomputes the logits in chunks of 8192 vocabulary
- * columns. BF16 operands with binary32 accumulation, statistics and sums in
+ * z_top for the backward, which recomputes the logits and keeps two BF16 copies
+ * of dz, of as many vocabulary columns at a time as 2.5 GiB each hold, in its
+ * workspace. BF16 operands with binary32 accumulation, statistics and sums in
  * binary32; dz is rounded once to BF16, the operand type of its GEMMs. dX and
  * dW: either may be NULL to skip it. dw_type PURO_OUT_FP32, or PURO_OUT_BF16,
  * the type a gradient has when ranks exchange it (Appendix C); accumulate_dW

@@ -12,8 +12,8 @@
 //
 // As with the cross-entropy (lm_head.hip) the logits never reach memory: the
 // forward's GEMM reduces them to (max, sum exp) per row and 128 columns, the
-// backward recomputes them by chunks of the vocabulary, its GEMM writing the
-// dense part of dz. What differs from a one-hot target is sparse: the k
+// backward recomputes them (by chunks of the vocabulary, where there are very
+// many), its GEMM writing the dense part of dz. What differs from a one-hot target is sparse: the k
 // logits of a row that the loss needs are k dot products, and the gradient at
 // those places is written over the dense part's, from the same formula with
 // the entry's q, in one rounding.
@@ -226,6 +226,20 @@ constexpr size_t kAl = 256;
 size_t al(size_t v) { return (v + kAl - 1) / kAl * kAl; }
 int64_t pad128(int64_t v) { return (v + 127) / 128 * 128; }
 
+// Vocabulary columns per chunk of the backward: as few chunks as keep one copy
+// of a chunk's dz within 2.5 GiB (288 GB of memory make a chunk of the whole
+// vocabulary the usual case), of even width, a multiple of the 256-wide tiles.
+// Few columns at a time leave the grids of few rows half empty and add every
+// chunk's dX to binary32 sums; that a chunk of 8192 columns stays in the
+// last-level cache gains less. Backward of V 151936, K 1536 at 8192 columns, at
+// 32768 and at all: M 300 1842, 1106, 1029 us; M 2000 3646, 2953, 2823; M 4096
+// 6068, 5512, 5308; M 8192 11023, 10438 (30464), 10263.
+constexpr int64_t kDzBytes = (int64_t)5 << 29;
+int64_t chunk_of(int64_t Mp, int64_t Vp) {
+    const int64_t chunks = (Mp * Vp * 2 + kDzBytes - 1) / kDzBytes;
+    return std::min(((Vp + chunks - 1) / chunks + 255) / 256 * 256, Vp);
+}
+
 struct Layout {
     size_t stats;                                                  // forward
     size_t coef, val, xt, wt, dz, dzt, dxacc, gemm;                // backward
@@ -236,7 +250,7 @@ Layout layout(int64_t M, int64_t V, int64_t K, int64_t k, bool bwd) {
     size_t used = 0;
     auto take = [&](size_t b) { const size_t at = used; used = al(used + b); return at; };
     Layout l{};
-    const int64_t Mp = pad128(M), Vp = pad128(V), Vc = std::min<int64_t>(Vp, kLmChunk);
+    const int64_t Mp = pad128(M), Vp = pad128(V), Vc = chunk_of(Mp, Vp);
     if (!bwd) {
         l.stats = take((size_t)M * (Vp / 128) * sizeof(float2));
     } else {
@@ -246,7 +260,7 @@ Layout layout(int64_t M, int64_t V, int64_t K, int64_t k, bool bwd) {
         l.wt = take((size_t)Vp * K * 2);
         l.dz = take((size_t)Mp * Vc * 2);
         l.dzt = take((size_t)Mp * Vc * 2);
-        l.dxacc = take((size_t)M * K * 4);
+        if (Vc < V) l.dxacc = take((size_t)M * K * 4);
         // the split-K partials of the dX and dW GEMMs, for a full chunk and for the last one
         size_t g = 0;
         const int64_t last = V - (V - 1) / Vc * Vc;
@@ -300,7 +314,7 @@ void launch_lm_distill_fwd(const DistillArgs& a, float* lse, float* loss, float*
 void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* z_top, const float* dloss, float grad_scale,
                            uint16_t* dX, void* dW, bool dw_bf16, int accumulate_dw, void* ws, hipStream_t stream) {
     uint8_t* const w8 = reinterpret_cast<uint8_t*>(ws);
-    const int64_t M = a.M, V = a.V, K = a.K, Mp = pad128(M), Vp = pad128(V), Vc = std::min<int64_t>(Vp, kLmChunk);
+    const int64_t M = a.M, V = a.V, K = a.K, Mp = pad128(M), Vp = pad128(V), Vc = chunk_of(Mp, Vp);
     const Layout l = layout(M, V, K, a.k, true);
     float* const coef = reinterpret_cast<float*>(w8 + l.coef);
     float* const val = reinterpret_cast<float*>(w8 + l.val);
@@ -329,7 +343,9 @@ void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* 
             zero_columns_kernel<<<blocks(Mp * (np - n)), kThreads, 0, stream>>>(dz, Mp, np, (int)n, (int)(np - n));
         if (dX) {
             GemmProblem gx{};
-            gx.M = M; gx.N = K; gx.K = np; gx.out = kOutF32; gx.D = dxacc; gx.ldd = K; gx.accumulate = c0 > 0;
+            gx.M = M; gx.N = K; gx.K = np; gx.ldd = K;
+            if (Vc < V) { gx.out = kOutF32; gx.D = dxacc; gx.accumulate = c0 > 0; }
+            else { gx.out = kOutBF16; gx.D = dX; }
             gx.A = reinterpret_cast<const uint8_t*>(dz); gx.lda = np; gx.fa = kBF16; gx.sa_mode = kSNone;
             gx.B = reinterpret_cast<const uint8_t*>(wt + c0); gx.ldb = Vp; gx.fb = kBF16; gx.sb_mode = kSNone;
             launch_gemm(gx, gws, stream);
@@ -344,7 +360,7 @@ void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* 
             launch_gemm(gw, gws, stream);
         }
     }
-    if (dX) {
+    if (dX && Vc < V) {
         const int64_t n4 = M * K / 4;
         f32_to_bf16_kernel<<<blocks(n4), kThreads, 0, stream>>>(dxacc, dX, n4);
     }

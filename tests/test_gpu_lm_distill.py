@@ -104,8 +104,7 @@ def test_shapes(P, M, V, K, k, kind, tau):
 
 
 @pytest.mark.parametrize("M,V,K,k", [(65, 9000, 64, 20), (130, 8193, 40, 5), (33, 16384, 24, 9), (1, 20001, 16, 64)])
-def test_several_chunks(P, M, V, K, k):
-    """Vocabularies over more than one chunk of the backward, the last one full, ragged, or one column."""
+def test_wide_vocabularies(P, M, V, K, k):
     c = Case(V, M, V, K, k)
     c.ids[:, -1] = V - 1                                       # an entry in the last column
     c.ids[:, 0] = min(8191, V - 1)
@@ -113,6 +112,45 @@ def test_several_chunks(P, M, V, K, k):
     f, lse, loss, z_top = check_forward(P, c, 1.0)
     dX, dW = P.lm_head_distill_bwd(*c.dev, lse, z_top)
     check_gradients(c, f, 1.0, np.ones(M), 1.0, dX, dW)
+
+
+@pytest.mark.parametrize("M,V", [(16384, 90001), (30001, 131072)])
+def test_several_chunks(P, M, V):
+    """dz of more than 2.5 GiB: two and three chunks of the vocabulary, the last one ragged or whole. Sampled rows of
+    the losses and dX, and rows of dW on both sides of every chunk's border (from the forward's lse, itself checked)."""
+    import torch
+    K, k = 16, 4
+    c = Case(M, M, V, K, k, plain=True)
+    lse, loss, z_top = P.lm_head_distill_fwd(*c.dev)
+    dX, dW = P.lm_head_distill_bwd(*c.dev, lse, z_top, dloss=to_dev(c.dloss))
+    rows = np.unique(np.r_[0, M - 1, np.random.default_rng(2).integers(0, M, 30)])
+    f = ld.forward(c.X[rows], c.W, c.ids[rows], c.t[rows], 1.0, L)
+    for name, got in (("lse", lse), ("loss", loss)):
+        assert (np.abs(host(got)[rows] - f[name]) <= f["tol_" + name] + 2.0 ** -24 * np.abs(f[name])).all(), name
+    part = Case(0, 1, 1, 8, 1)
+    part.X, part.W = c.X[rows], c.W
+    check_gradients(part, f, 1.0, c.dloss[rows].astype(np.float64), 1.0, dX[torch.from_numpy(rows).cuda()], None)
+    chunks = -(-(M + 127) // 128 * 128 * ((V + 127) // 128 * 128) * 2 // (5 << 29))
+    assert chunks >= 2
+    width = (-(-(V + 127) // 128 * 128 // chunks) + 255) // 256 * 256
+    cols = np.unique(np.r_[0, V - 1, [b + d for b in range(width, V, width) for d in (-1, 0)],
+                           np.random.default_rng(3).integers(0, V, 12)])
+    # dz of those columns and all rows: the columns as a vocabulary of their own, with the whole one's lse
+    x, w = f64(c.X), f64(c.W[cols])
+    a, S = x @ w.T, np.abs(x) @ np.abs(w).T
+    place = np.full(V, -1, np.int64)
+    place[cols] = np.arange(cols.size)
+    q, _, tol_q = ld.teacher(c.ids, c.t, V, 1.0, L)
+    at = place[c.ids]
+    g = dict(a=a, tol_a=ld.TOL_Z * S, lse=host(lse).astype(np.float64), tol_lse=np.zeros(M), q=q, tol_q=tol_q,
+             ok=np.ones_like(at, bool), at=at)
+    # (entries elsewhere count for Q, but have no place here: a column of their own, dropped afterwards)
+    g["at"] = np.where(at >= 0, at, cols.size)
+    g["a"] = np.concatenate((a, np.zeros((M, 1))), 1)
+    g["tol_a"] = np.concatenate((g["tol_a"], np.zeros((M, 1))), 1)
+    mid, lo, hi = (f64(v)[:, :-1] for v in ld.dz_band(g, 1.0, c.dloss.astype(np.float64), 1.0))
+    check_fp32(host(dW[torch.from_numpy(cols).cuda()]), mid.T @ x, np.abs(mid).T @ np.abs(x), what="dW columns",
+               slack=(hi - lo).T @ np.abs(x))
 
 
 @pytest.mark.parametrize("k", [1, 63, 64, 65, 200, 1024])

@@ -18,7 +18,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 // Heads that a lane has in flight: their loads are issued together.
-constexpr int kUnroll = 4;
+// (backward, which loads two vectors a head: two heads take 90 registers and five
+// waves fit a SIMD; four took 126, 52.7 against 41.9 us at 8192 tokens of 16 + 8
+// heads of 128)
+constexpr int kUnroll = 4, kUnrollBwd = 2;
 
 // Table of cosines and sines: the angle in double precision (at position 10^6
 // a binary32 angle is off by 0.03), reduced and evaluated there.
@@ -111,10 +114,9 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
     const int waves = (int)gridDim.x * kWaves;
     const LaneRole role = lane_role<L>(a.D, a.rope.dim, a.rope.interleaved, lane);
     const bool turned = kind < 2 && a.rope.dim > 0, half = a.rope.dim == L * 8;
-    float g[8], sum[8];
+    float sum[8];
     uint4 gw{};
     if (gamma) gw = *reinterpret_cast<const uint4*>(gamma + role.col);
-    unpack8(gw, g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
     const float inv_d = 1.0f / (float)a.D;
@@ -126,17 +128,17 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
         uint16_t* const y = const_cast<uint16_t*>(head_at(out, tok)) + role.col;
         Turn turn{};
         if (turned) turn = load_turn(a.rope, role, a.rope.pos ? a.rope.pos[t] : tok.s, true);
-        for (int i = 0; i * GPW < heads; i += kUnroll) {
-            uint4 rd[kUnroll], rx[kUnroll];
+        for (int i = 0; i * GPW < heads; i += kUnrollBwd) {
+            uint4 rd[kUnrollBwd], rx[kUnrollBwd];
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
+            for (int u = 0; u < kUnrollBwd; ++u) {
                 const int h = min((i + u) * GPW + grp, heads - 1);
                 rd[u] = *reinterpret_cast<const uint4*>(d + h * grad.hs);
                 if (gamma) rx[u] = *reinterpret_cast<const uint4*>(x + h * in.hs);
                 else rx[u] = rd[u];
             }
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
+            for (int u = 0; u < kUnrollBwd; ++u) {
                 if ((i + u) * GPW >= heads) break;
                 const int h = (i + u) * GPW + grp;
                 const bool live = role.holds && h < heads;
@@ -149,6 +151,10 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
                 }
                 if (turned) turn8<L>(v, turn, role, a.rope.interleaved, half);
                 if (gamma) {
+                    // (unpacked anew for each head: kept, it would hold eight registers)
+                    float g[8];
+                    asm volatile("" : "+v"(gw.x), "+v"(gw.y), "+v"(gw.z), "+v"(gw.w));
+                    unpack8(gw, g);
                     norm_bwd8<L>(v, n, g, inv_d, a.eps, wg);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum[e] += live ? wg[e] : 0.0f;
@@ -172,37 +178,51 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
         a.part[((int64_t)kind * gridDim.x + blockIdx.x) * a.D + c] = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
 }
 
-// dgamma of 8 columns per block: 32 threads a column take every 32nd partial
-// sum, then add up in a tree.
+// dgamma of 8 columns per block: two lanes a row of partial sums (16 bytes
+// each), 128 rows at a time, four loads in flight per lane; then across the
+// wave and the four waves.
 __global__ __launch_bounds__(kThreads) void dgamma_sum_kernel(const float* __restrict__ pq, int64_t nq,
                                                               float* __restrict__ dgq, const float* __restrict__ pk,
-                                                              int64_t nk, float* __restrict__ dgk, int64_t ldp, int D) {
-    __shared__ float red[32][9];
-    const float* const p = blockIdx.y ? pk : pq;
+                                                              int64_t nk, float* __restrict__ dgk, int64_t ldp) {
+    __shared__ float4 red[kWaves][2];
+    const float* const p = (blockIdx.y ? pk : pq) + blockIdx.x * 8 + (threadIdx.x & 1) * 4;
     float* const out = blockIdx.y ? dgk : dgq;
     const int64_t n = blockIdx.y ? nk : nq;
-    const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
-    const int col = (int)blockIdx.x * 8 + c;
     if (!out) return;
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t i = r; i < n; i += 128) {
+    float4 s[4] = {};
+    for (int64_t i = threadIdx.x >> 1; i < n; i += 512) {
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (i + 32 * u < n) s[u] += p[(i + 32 * u) * ldp + col];
+            if (i + 128 * u < n) {
+                const float4 v = *reinterpret_cast<const float4*>(p + (i + 128 * u) * ldp);
+                s[u].x += v.x; s[u].y += v.y; s[u].z += v.z; s[u].w += v.w;
+            }
     }
-    red[r][c] = (s[0] + s[1]) + (s[2] + s[3]);
+    float t[4] = {(s[0].x + s[1].x) + (s[2].x + s[3].x), (s[0].y + s[1].y) + (s[2].y + s[3].y),
+                  (s[0].z + s[1].z) + (s[2].z + s[3].z), (s[0].w + s[1].w) + (s[2].w + s[3].w)};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        t[e] += lane_xor_f<2>(t[e]);
+        t[e] += lane_xor_f<4>(t[e]);
+        t[e] += lane_xor_f<8>(t[e]);
+        t[e] += lane_xor_f<16>(t[e]);
+        t[e] += lane_xor_f<32>(t[e]);
+    }
+    if ((threadIdx.x & 63) < 2) red[threadIdx.x >> 6][threadIdx.x & 1] = make_float4(t[0], t[1], t[2], t[3]);
     __syncthreads();
-    for (int o = 16; o >= 1; o >>= 1) {
-        if (r < o) red[r][c] += red[r + o][c];
-        __syncthreads();
+    if (threadIdx.x < 2) {
+        const float4 a = red[0][threadIdx.x], b = red[1][threadIdx.x], c = red[2][threadIdx.x], d = red[3][threadIdx.x];
+        float* const o = out + blockIdx.x * 8 + threadIdx.x * 4;
+        o[0] = (a.x + b.x) + (c.x + d.x); o[1] = (a.y + b.y) + (c.y + d.y);
+        o[2] = (a.z + b.z) + (c.z + d.z); o[3] = (a.w + b.w) + (c.w + d.w);
     }
-    if (r == 0) out[col] = red[0][c];
 }
 
 // Blocks of the backward per kind of heads: enough to fill the chip, each wave
-// with a token or more.
+// with a token or more, and few partial sums (8192 tokens as above: 512 blocks
+// 41.8 us, 768 41.1, 1024 41.2).
 int64_t bwd_blocks(int64_t tokens) {
-    return std::max<int64_t>(1, std::min<int64_t>((tokens + kWaves - 1) / kWaves, 512));
+    return std::max<int64_t>(1, std::min<int64_t>((tokens + kWaves - 1) / kWaves, 768));
 }
 
 // f(std::integral_constant<int, L>) with the lanes of a head of D values.
@@ -239,7 +259,7 @@ void launch_qk_norm_rope_fwd(const QkArgs& a, hipStream_t stream) {
 
 void launch_dgamma_sum(const float* part_q, int64_t nq, float* dgq, const float* part_k, int64_t nk, float* dgk,
                        int64_t ldp, int D, hipStream_t stream) {
-    dgamma_sum_kernel<<<dim3((unsigned)(D / 8), 2), kThreads, 0, stream>>>(part_q, nq, dgq, part_k, nk, dgk, ldp, D);
+    dgamma_sum_kernel<<<dim3((unsigned)(D / 8), 2), kThreads, 0, stream>>>(part_q, nq, dgq, part_k, nk, dgk, ldp);
 }
 
 size_t qk_bwd_ws_bytes(int64_t tokens, int D) {

@@ -9,9 +9,12 @@
 // dn x r over tokens and heads, and with g = dn gamma, h = x r,
 // dx = r (g - h mean(g h)).
 //
-// Layout: L = 1, 2, 4, .. 32 lanes hold a head, eight consecutive values (one
-// 16-byte vector) each; sums over a head and the exchange of the pairs stay
-// within those lanes.
+// Layout: L = 1, 2, 4, .. 32 lanes hold a head, eight values each: consecutive
+// ones (one 16-byte vector), the pairs' other values exchanged between lanes;
+// or, where whole heads that fill their lanes turn by pairs (i, i + D / 2), four
+// pairs (two 8-byte pieces D / 2 values apart), so that no value changes lanes
+// and no entry of the table is loaded twice. Sums over a head stay within its
+// lanes.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -49,14 +52,6 @@ __device__ __forceinline__ float head_sum(float v) {
     if constexpr (L >= 32) v += lane_xor_f<16>(v);
     return v;
 }
-
-// A lane's part of the rotation at one position: y_e = n_e c_e + p_e s_e with
-// p_e the pair's other value and the sign of the pair's first value in s.
-// Lanes past the rotated values keep theirs (not by c = 1, s = 0: an infinity
-// times 0 would be a NaN).
-struct Turn {
-    float c[8], s[8];
-};
 
 // A token's place: its sequence and its position there.
 struct Token {
@@ -96,53 +91,108 @@ __device__ __forceinline__ LaneRole lane_role(int D, int R, int interleaved, int
     return r;
 }
 
-// The table's row of a position, for this lane; back: turned the other way.
-// A position outside the table has no angle: NaN.
+// How a kernel's instance turns heads: not at all; pairs (i, i + D / 2) of
+// whole heads that fill their lanes, four pairs a lane; such pairs of any head,
+// eight consecutive values a lane; neighbours. (As types: with the table's
+// loads in branches the compiler split them into single words.)
+enum : int { kTurnNone = 0, kTurnHalf = 1, kTurnPart = 2, kTurnPairs = 3 };
+__host__ __device__ inline int turn_kind(const RopeArgs& a, int lanes) {
+    return a.dim == 0 ? kTurnNone : a.interleaved ? kTurnPairs : a.dim == lanes * 8 ? kTurnHalf : kTurnPart;
+}
+
+// The eight values of a lane, from the start of their head, as 16 bytes.
+template <int L, int TURN>
+__device__ __forceinline__ uint4 load8(const uint16_t* head, const LaneRole& r) {
+    if constexpr (TURN != kTurnHalf) return *reinterpret_cast<const uint4*>(head + r.col);
+    const uint2 lo = *reinterpret_cast<const uint2*>(head + r.col / 2);
+    const uint2 hi = *reinterpret_cast<const uint2*>(head + L * 4 + r.col / 2);
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
+}
+template <int L, int TURN>
+__device__ __forceinline__ void store8(uint16_t* head, const LaneRole& r, const uint4 v) {
+    if constexpr (TURN != kTurnHalf) {
+        *reinterpret_cast<uint4*>(head + r.col) = v;
+    } else {
+        *reinterpret_cast<uint2*>(head + r.col / 2) = make_uint2(v.x, v.y);
+        *reinterpret_cast<uint2*>(head + L * 4 + r.col / 2) = make_uint2(v.z, v.w);
+    }
+}
+// Their columns: e < 4 and e >= 4.
+template <int L, int TURN>
+__device__ __forceinline__ int column(const LaneRole& r, int e) {
+    return TURN == kTurnHalf ? (e < 4 ? r.col / 2 + e : L * 4 + r.col / 2 + e - 4) : r.col + e;
+}
+
+// A lane's factors at one position: y_e = n_e c_e + p_e s_e with p_e the pair's
+// other value and the sign of the pair's first value in s. With four pairs a
+// lane: the pairs' c and s, as they are. back: turned the other way. A position
+// outside the table has no angle: NaN.
+struct Turn {
+    float c[8], s[8];
+};
+template <int TURN>
 __device__ __forceinline__ Turn load_turn(const RopeArgs& a, const LaneRole& r, int pos, bool back) {
-    Turn t;
+    Turn t{};
+    if constexpr (TURN == kTurnNone) return t;
     const bool in = (unsigned)pos < (unsigned)a.len;
-    const float2* row = a.table + (int64_t)(in ? pos : 0) * (a.dim / 2) + r.pair;
-    const float4* v = reinterpret_cast<const float4*>(row);
-    const float nan = __builtin_nanf("");
-    if (a.interleaved) {
-        const float4 u[2] = {v[0], v[1]};
+    const float2* const row = a.table + (int64_t)(in ? pos : 0) * (a.dim / 2);
+    const float4* const v = reinterpret_cast<const float4*>(row + (TURN == kTurnHalf ? r.col / 2 : r.pair));
+    constexpr int N = TURN == kTurnPart ? 8 : 4;       // pairs that the lane needs
+    float4 u[N / 2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float c = in ? (i & 1 ? u[i / 2].z : u[i / 2].x) : nan;
-            const float s = in ? (i & 1 ? u[i / 2].w : u[i / 2].y) : nan;
+    for (int i = 0; i < N / 2; ++i) u[i] = v[i];
+    const uint32_t sign = r.first != back ? 0x80000000u : 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float c = i & 1 ? u[i / 2].z : u[i / 2].x, s = i & 1 ? u[i / 2].w : u[i / 2].y;
+        if constexpr (TURN == kTurnPairs) {
             t.c[2 * i] = t.c[2 * i + 1] = c;
             t.s[2 * i] = back ? s : -s;
             t.s[2 * i + 1] = back ? -s : s;
+        } else {
+            t.c[i] = c;
+            t.s[i] = TURN == kTurnHalf ? s : __uint_as_float(__float_as_uint(s) ^ sign);
         }
-    } else {
-        const float4 u[4] = {v[0], v[1], v[2], v[3]};
+    }
+    if (__builtin_amdgcn_ballot_w64(!in)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float c = i & 1 ? u[i / 2].z : u[i / 2].x, s = i & 1 ? u[i / 2].w : u[i / 2].y;
-            t.c[i] = in ? c : nan;
-            t.s[i] = in ? (r.first != back ? -s : s) : nan;
+            t.c[i] = in ? t.c[i] : __builtin_nanf("");
+            t.s[i] = in ? t.s[i] : __builtin_nanf("");
         }
     }
     return t;
 }
 
-// The eight values turned. HALF: the pairs' other values are L / 2 lanes away
-// (the whole head is rotated), else wherever LaneRole says.
-template <int L>
-__device__ __forceinline__ void turn8(float v[8], const Turn& t, const LaneRole& r, int interleaved, bool half) {
-    float p[8];
-    if (interleaved) {
+// Four pairs (v_e, v_4+e) turned by (c_e, s_e), or back.
+__device__ __forceinline__ void turn_pairs4(float v[8], const float c[4], const float s[4], bool back) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = v[i ^ 1];
-    } else if (L >= 2 && half) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = lane_xor_f<(L >= 2 ? L / 2 : 1)>(v[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = __shfl(v[i], r.partner, 64);
+    for (int e = 0; e < 4; ++e) {
+        const float a = v[e], b = v[4 + e];
+        v[e] = fmaf(b, back ? s[e] : -s[e], a * c[e]);
+        v[4 + e] = fmaf(a, back ? -s[e] : s[e], b * c[e]);
     }
+}
+
+// The eight values turned. (Lanes past the rotated values keep theirs, not by
+// c = 1, s = 0: an infinity times 0 would be a NaN. Where all of a head turns,
+// lanes that hold none of it turn their zeros.)
+template <int TURN>
+__device__ __forceinline__ void turn8(float v[8], const Turn& t, const LaneRole& r, const RopeArgs& a, int D, bool back) {
+    if constexpr (TURN == kTurnNone) return;
+    if constexpr (TURN == kTurnHalf) {
+        turn_pairs4(v, t.c, t.s, back);
+        return;
+    }
+    float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = r.turns ? fmaf(p[i], t.s[i], v[i] * t.c[i]) : v[i];
+    for (int i = 0; i < 8; ++i) {
+        const float p = TURN == kTurnPairs ? v[i ^ 1] : __shfl(v[i], r.partner, 64);
+        y[i] = fmaf(p, t.s[i], v[i] * t.c[i]);
+    }
+    const bool all = a.dim == D;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = all || r.turns ? y[i] : v[i];
 }
 
 __device__ __forceinline__ void unpack8(const uint4 w, float v[8]) {
@@ -155,13 +205,17 @@ __device__ __forceinline__ uint4 pack8(const float v[8]) {
 }
 
 // 1 / sqrt(mean(x^2) + eps) of the head whose eight values the lane holds
-// (zeros where it holds none).
+// (zeros where it holds none), by the reciprocal-root instruction (1 ulp),
+// which flushes numbers below the normal range: those are scaled by 2^64.
 template <int L>
 __device__ __forceinline__ float head_rstd(const float x[8], float inv_d, float eps) {
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-    return 1.0f / sqrtf(fmaf(head_sum<L>(ss), inv_d, eps));
+    const float m = fmaf(head_sum<L>(ss), inv_d, eps);
+    const bool tiny = m < 0x1p-100f;
+    const float r = __builtin_amdgcn_rsqf(tiny ? m * 0x1p64f : m);
+    return tiny ? r * 0x1p32f : r;
 }
 
 // The backward of the norm: d (the gradient of n, turned back) becomes dx, and

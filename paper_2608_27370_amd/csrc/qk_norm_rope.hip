@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kThreads) void rope_table_kernel(float2* __restrict
 
 // Forward: wave w takes steps [part * per, part * per + per) of 64 / L heads
 // of token w / parts. Few tokens are split over more waves.
-template <int L>
+template <int L, int TURN>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Divisor per_seq, int per) {
     constexpr int GPW = 64 / L;
     const bool key = blockIdx.y != 0;
@@ -58,20 +58,18 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Di
     const int lane = threadIdx.x & 63, grp = lane / L;
     const LaneRole role = lane_role<L>(a.D, a.rope.dim, a.rope.interleaved, lane);
     const Token tok = token_of(t, per_seq);
-    const bool turned = a.rope.dim > 0, half = a.rope.dim == L * 8;
-    const uint16_t* const x = head_at(in, tok) + role.col;
-    uint16_t* const y = const_cast<uint16_t*>(head_at(out, tok)) + role.col;
-    Turn turn{};
-    if (turned) turn = load_turn(a.rope, role, a.rope.pos ? a.rope.pos[t] : tok.s, false);
+    const uint16_t* const x = head_at(in, tok);
+    uint16_t* const y = const_cast<uint16_t*>(head_at(out, tok));
+    const Turn turn = load_turn<TURN>(a.rope, role, TURN && a.rope.pos ? a.rope.pos[t] : tok.s, false);
     uint4 gw{};
-    if (gamma) gw = *reinterpret_cast<const uint4*>(gamma + role.col);
+    if (gamma) gw = load8<L, TURN>(gamma, role);
     const float inv_d = 1.0f / (float)a.D;
     const int i1 = min(steps, part * per + per);
     for (int i = part * per; i < i1; i += kUnroll) {
         uint4 raw[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)     // (lanes past the last head read it again and store nothing)
-            raw[u] = *reinterpret_cast<const uint4*>(x + min((i + u) * GPW + grp, heads - 1) * in.hs);
+            raw[u] = load8<L, TURN>(x + min((i + u) * GPW + grp, heads - 1) * in.hs, role);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             if (i + u >= i1) break;
@@ -88,8 +86,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Di
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = v[e] * r * g[e];
             }
-            if (turned) turn8<L>(v, turn, role, a.rope.interleaved, half);
-            if (role.holds && h < heads) *reinterpret_cast<uint4*>(y + h * out.hs) = pack8(v);
+            turn8<TURN>(v, turn, role, a.rope, a.D, false);
+            if (role.holds && h < heads) store8<L, TURN>(y + h * out.hs, role, pack8(v));
         }
     }
 }
@@ -97,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Di
 // Backward: wave w takes tokens w, w + waves, ..; every lane keeps the sums of
 // dgamma of its eight columns in binary32, the block adds them up in a fixed
 // order and writes part[kind][block][D].
-template <int L>
+template <int L, int TURN>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Divisor per_seq) {
     constexpr int GPW = 64 / L;
     __shared__ float red[kWaves][L * 8];
@@ -113,28 +111,28 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
     const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * kWaves + wave);
     const int waves = (int)gridDim.x * kWaves;
     const LaneRole role = lane_role<L>(a.D, a.rope.dim, a.rope.interleaved, lane);
-    const bool turned = kind < 2 && a.rope.dim > 0, half = a.rope.dim == L * 8;
+    const bool turned = TURN != kTurnNone && kind < 2;
     float sum[8];
     uint4 gw{};
-    if (gamma) gw = *reinterpret_cast<const uint4*>(gamma + role.col);
+    if (gamma) gw = load8<L, TURN>(gamma, role);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
     const float inv_d = 1.0f / (float)a.D;
     for (int64_t t64 = w; heads > 0 && t64 < a.tokens; t64 += waves) {
         const int t = (int)t64;
         const Token tok = token_of(t, per_seq);
-        const uint16_t* const d = head_at(grad, tok) + role.col;
-        const uint16_t* const x = head_at(in, tok) + role.col;
-        uint16_t* const y = const_cast<uint16_t*>(head_at(out, tok)) + role.col;
+        const uint16_t* const d = head_at(grad, tok);
+        const uint16_t* const x = head_at(in, tok);
+        uint16_t* const y = const_cast<uint16_t*>(head_at(out, tok));
         Turn turn{};
-        if (turned) turn = load_turn(a.rope, role, a.rope.pos ? a.rope.pos[t] : tok.s, true);
+        if (turned) turn = load_turn<TURN>(a.rope, role, a.rope.pos ? a.rope.pos[t] : tok.s, true);
         for (int i = 0; i * GPW < heads; i += kUnrollBwd) {
             uint4 rd[kUnrollBwd], rx[kUnrollBwd];
 #pragma unroll
             for (int u = 0; u < kUnrollBwd; ++u) {
                 const int h = min((i + u) * GPW + grp, heads - 1);
-                rd[u] = *reinterpret_cast<const uint4*>(d + h * grad.hs);
-                if (gamma) rx[u] = *reinterpret_cast<const uint4*>(x + h * in.hs);
+                rd[u] = load8<L, TURN>(d + h * grad.hs, role);
+                if (gamma) rx[u] = load8<L, TURN>(x + h * in.hs, role);
                 else rx[u] = rd[u];
             }
 #pragma unroll
@@ -149,7 +147,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = n[e] = 0.0f;
                 }
-                if (turned) turn8<L>(v, turn, role, a.rope.interleaved, half);
+                if (turned) turn8<TURN>(v, turn, role, a.rope, a.D, true);
                 if (gamma) {
                     // (unpacked anew for each head: kept, it would hold eight registers)
                     float g[8];
@@ -160,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
                     for (int e = 0; e < 8; ++e) sum[e] += live ? wg[e] : 0.0f;
                 }
                 // (an untouched head as its bits are: a signalling NaN is not made quiet)
-                if (live) *reinterpret_cast<uint4*>(y + h * out.hs) = turned || gamma ? pack8(v) : rd[u];
+                if (live) store8<L, TURN>(y + h * out.hs, role, turned || gamma ? pack8(v) : rd[u]);
             }
         }
     }
@@ -171,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
         float s = sum[e];
 #pragma unroll
         for (int o = L; o < 64; o *= 2) s += __shfl_xor(s, o, 64);
-        if (grp == 0) red[wave][lane * 8 + e] = s;
+        if (grp == 0 && role.holds) red[wave][column<L, TURN>(role, e)] = s;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < a.D; c += kThreads)
@@ -225,15 +223,23 @@ int64_t bwd_blocks(int64_t tokens) {
     return std::max<int64_t>(1, std::min<int64_t>((tokens + kWaves - 1) / kWaves, 768));
 }
 
-// f(std::integral_constant<int, L>) with the lanes of a head of D values.
+// f(lanes of a head, how it turns), both as types.
 template <class F>
-void by_lanes(int D, F&& f) {
-    if (D <= 8) f(std::integral_constant<int, 1>{});
-    else if (D <= 16) f(std::integral_constant<int, 2>{});
-    else if (D <= 32) f(std::integral_constant<int, 4>{});
-    else if (D <= 64) f(std::integral_constant<int, 8>{});
-    else if (D <= 128) f(std::integral_constant<int, 16>{});
-    else f(std::integral_constant<int, 32>{});
+void by_lanes(int D, const RopeArgs& rope, F&& f) {
+    auto turns = [&](auto lanes) {
+        switch (turn_kind(rope, decltype(lanes)::value)) {
+        case kTurnNone: f(lanes, std::integral_constant<int, kTurnNone>{}); break;
+        case kTurnHalf: f(lanes, std::integral_constant<int, kTurnHalf>{}); break;
+        case kTurnPart: f(lanes, std::integral_constant<int, kTurnPart>{}); break;
+        default: f(lanes, std::integral_constant<int, kTurnPairs>{});
+        }
+    };
+    if (D <= 8) turns(std::integral_constant<int, 1>{});
+    else if (D <= 16) turns(std::integral_constant<int, 2>{});
+    else if (D <= 32) turns(std::integral_constant<int, 4>{});
+    else if (D <= 64) turns(std::integral_constant<int, 8>{});
+    else if (D <= 128) turns(std::integral_constant<int, 16>{});
+    else turns(std::integral_constant<int, 32>{});
 }
 
 }  // namespace
@@ -247,13 +253,13 @@ void launch_rope_table(float2* table, int64_t len, int dim, double theta, hipStr
 void launch_qk_norm_rope_fwd(const QkArgs& a, hipStream_t stream) {
     const int heads = std::max(a.hq, a.hk);
     if (a.tokens == 0 || heads == 0) return;
-    by_lanes(a.D, [&](auto lanes) {
+    by_lanes(a.D, a.rope, [&](auto lanes, auto turn) {
         constexpr int L = decltype(lanes)::value, GPW = 64 / L;
         const int steps = (heads + GPW - 1) / GPW;
         const int per = a.tokens * steps <= 4096 ? 1 : steps;
         const int64_t waves = a.tokens * ((steps + per - 1) / per);
-        qk_norm_rope_fwd_kernel<L><<<dim3((unsigned)((waves + kWaves - 1) / kWaves), a.hk > 0 ? 2 : 1), kThreads, 0, stream>>>(
-            a, Divisor::of((uint32_t)a.seq), per);
+        qk_norm_rope_fwd_kernel<L, decltype(turn)::value>
+            <<<dim3((unsigned)((waves + kWaves - 1) / kWaves), a.hk > 0 ? 2 : 1), kThreads, 0, stream>>>(a, Divisor::of((uint32_t)a.seq), per);
     });
 }
 
@@ -271,8 +277,8 @@ void launch_qk_norm_rope_bwd(QkArgs a, void* ws, hipStream_t stream) {
     const int64_t blocks = bwd_blocks(a.tokens);
     a.part = sums ? reinterpret_cast<float*>(ws) : nullptr;
     if (a.tokens > 0)
-        by_lanes(a.D, [&](auto lanes) {
-            qk_norm_rope_bwd_kernel<decltype(lanes)::value>
+        by_lanes(a.D, a.rope, [&](auto lanes, auto turn) {
+            qk_norm_rope_bwd_kernel<decltype(lanes)::value, decltype(turn)::value>
                 <<<dim3((unsigned)blocks, a.dv.p ? 3 : 2), kThreads, 0, stream>>>(a, Divisor::of((uint32_t)a.seq));
         });
     if (sums) {

@@ -15,75 +15,256 @@ namespace puro {
 
 namespace {
 
-// The thread's 8x8 block of [dq | dk | dv] (BF16 bits), and what its columns
-// add to dgamma, from the head of L lanes it belongs to; kind: 0 a query head,
-// 1 a key head, 2 a value head or none.
+// The heads of one kind, 0 query, 1 key, 2 value, as a tile takes them: the
+// first one's number, where the gradient and the head before the norm are
+// (heads that are not normalised are not read: the gradient stands in).
+struct Kind {
+    const uint16_t *g, *x, *gamma;
+    int64_t gbs, grs, ghs, xbs, xrs, xhs;
+    int64_t first;
+};
+struct Kinds {
+    Kind of[3];
+};
+
+Kinds kinds_of(const QkArgs& k) {
+    Kinds r;
+    const HeadsArg g[3] = {k.dq, k.dk, k.dv}, x[3] = {k.gq ? k.q : k.dq, k.gk ? k.k : k.dk, k.dv};
+    const uint16_t* const gamma[3] = {k.gq, k.gk, nullptr};
+    const int64_t first[3] = {0, k.hq, (int64_t)k.hq + k.hk};
+    for (int i = 0; i < 3; ++i)
+        r.of[i] = Kind{g[i].p, x[i].p, gamma[i], g[i].bs, g[i].rs, g[i].hs, x[i].bs, x[i].rs, x[i].hs, first[i]};
+    return r;
+}
+
+// What a thread takes of the head of L lanes that it belongs to; head0: the
+// tile's first head (one of 128 values, or two of 64). A head's kind is read
+// from the kernel's arguments (their first) by its number.
+struct HeadOf {
+    int kind;
+    bool none;                    // past the last head: the last one again, and zeros
+    int64_t gbs, grs, xbs, xrs;   // strides of the gradient and of the head
+    const uint16_t *gp, *xp;      // the head at token 0
+    const uint16_t* gamma;
+};
 template <int L>
-__device__ __forceinline__ void load_qk_bwd_8x8(const QkArgs& k, const Divisor& per_seq, const Tile& t, int head,
-                                                uint32_t w[8][4], float sum[8], int& kind) {
+__device__ __forceinline__ HeadOf head_of(const QkArgs& k, int head0) {
+    typedef const __attribute__((address_space(4))) Kinds* kinds_ptr;
+    const kinds_ptr kinds = (kinds_ptr)__builtin_amdgcn_kernarg_segment_ptr();
     const int hqk = k.hq + k.hk;
-    const bool none = head >= hqk + k.hk;      // the last head again, and zeros
-    head = min(head, hqk + k.hk - 1);
-    kind = head < k.hq ? 0 : (head < hqk ? 1 : 2);
-    const LaneRole role = lane_role<L>(k.D, k.rope.dim, k.rope.interleaved, threadIdx.x & 63);
-    const HeadsArg g = kind == 0 ? k.dq : (kind == 1 ? k.dk : k.dv);
-    const int first = kind == 0 ? 0 : (kind == 1 ? k.hq : hqk);
-    const uint16_t* gamma = kind == 0 ? k.gq : (kind == 1 ? k.gk : nullptr);
-    const bool norm = gamma != nullptr;
-    // (heads that are not normalised are not read: the gradient stands in)
-    const HeadsArg x = norm ? (kind == 0 ? k.q : k.k) : g;
-    const int64_t hc = head - first;
-    const uint16_t* const gp = g.p + hc * g.hs + role.col;
-    const uint16_t* const xp = x.p + hc * x.hs + role.col;
-    const int rows = (int)max((int64_t)0, min((int64_t)8, k.tokens - t.row0));   // of the thread's eight
-    uint4 rd[8], rx[8];
-    int pos[8];
-    const bool turned = k.rope.dim > 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        // rows past the last are the last one again, and zeros below
-        const int row = (int)min(t.row0 + i, k.tokens - 1);
-        const Token tok = token_of(row, per_seq);
-        rd[i] = *reinterpret_cast<const uint4*>(gp + tok.b * g.bs + tok.s * g.rs);
-        rx[i] = *reinterpret_cast<const uint4*>(xp + tok.b * x.bs + tok.s * x.rs);
-        pos[i] = tok.s;
-        if (turned && k.rope.pos) pos[i] = k.rope.pos[row];
+    auto one = [&](int head) __attribute__((always_inline)) {
+        HeadOf h;
+        h.none = head >= hqk + k.hk;
+        head = min(head, hqk + k.hk - 1);
+        h.kind = (head >= k.hq ? 1 : 0) + (head >= hqk ? 1 : 0);
+        const auto& c = kinds->of[h.kind];
+        const int64_t at = head - c.first;
+        h.gbs = c.gbs; h.grs = c.grs; h.xbs = c.xbs; h.xrs = c.xrs;
+        h.gp = c.g + at * c.ghs;
+        h.xp = c.x + at * c.xhs;
+        h.gamma = c.gamma;
+        return h;
+    };
+    HeadOf h = one(head0);
+    if constexpr (L == 8) {
+        const bool second = (threadIdx.x & 8) != 0;
+        const HeadOf b = one(head0 + 1);
+        // (into vector registers one field after the other: there are too few scalar ones)
+        auto pick = [&](auto x, auto y) __attribute__((always_inline)) {
+            auto v = second ? y : x;
+            asm volatile("" : "+v"(v));
+            return v;
+        };
+        h.kind = pick(h.kind, b.kind);
+        h.none = second ? b.none : h.none;
+        h.gp = pick(h.gp, b.gp); h.gbs = pick(h.gbs, b.gbs); h.grs = pick(h.grs, b.grs);
+        h.xp = pick(h.xp, b.xp); h.xbs = pick(h.xbs, b.xbs); h.xrs = pick(h.xrs, b.xrs);
+        h.gamma = pick(h.gamma, b.gamma);
     }
+    return h;
+}
+
+// (The sums are pinned after each row: the compiler moves their additions to
+// where the sums are used, behind a branch, and keeps 64 terms until then.)
+
+// Any case, two rows at a time.
+template <int L>
+__device__ __forceinline__ void load_qk_bwd_any(const QkArgs& k, const Divisor& per_seq, const Tile& t, int head0,
+                                                uint32_t w[8][4], float sum[8], int col[2]) {
+    const LaneRole role = lane_role<L>(k.D, k.rope.dim, k.rope.interleaved, threadIdx.x & 63);
+    HeadOf h = head_of<L>(k, head0);
+    h.gp += role.col;
+    h.xp += role.col;
+    const int kind = h.kind;
+    col[0] = t.cc * 8;
+    col[1] = t.cc * 8 + 4;
+    const bool norm = h.gamma != nullptr;
+    const float inv_d = 1.0f / (float)k.D;
+    uint4 gw{};
+    if (norm) gw = *reinterpret_cast<const uint4*>(h.gamma + role.col);
+    const int turn_as = turn_kind(k.rope, L);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+#pragma unroll
+    for (int i0 = 0; i0 < 8; i0 += 2) {
+        uint4 rd[2], rx[2];
+        int pos[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            // rows past the last one are the last one again, and zeros below
+            const int row = (int)min(t.row0 + i0 + u, k.tokens - 1);
+            const Token tok = token_of(row, per_seq);
+            rd[u] = *reinterpret_cast<const uint4*>(h.gp + tok.b * h.gbs + tok.s * h.grs);
+            rx[u] = *reinterpret_cast<const uint4*>(h.xp + tok.b * h.xbs + tok.s * h.xrs);
+            pos[u] = turn_as != kTurnNone && k.rope.pos ? k.rope.pos[row] : tok.s;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int i = i0 + u;
+            const bool live = t.row0 + i < k.tokens && !h.none;
+            float d[8], n[8], x8[8], gm[8], wg[8];
+            unpack8(rd[u], d);
+            auto turned = [&](auto as) __attribute__((always_inline)) {
+                constexpr int TURN = decltype(as)::value;
+                turn8<TURN>(d, load_turn<TURN>(k.rope, role, pos[u], true), role, k.rope, k.D, true);
+            };
+            if (turn_as == kTurnPart || turn_as == kTurnHalf) turned(std::integral_constant<int, kTurnPart>{});
+            else if (turn_as == kTurnPairs) turned(std::integral_constant<int, kTurnPairs>{});
+            unpack8(rx[u], x8);
+            unpack8(gw, gm);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) n[e] = d[e];
+            norm_bwd8<L>(n, x8, gm, inv_d, k.eps, wg);
+            uint4 o = rd[u];
+            if (kind != 2) o = pack8(norm ? n : d);
+            w[i][0] = live ? o.x : 0u; w[i][1] = live ? o.y : 0u;
+            w[i][2] = live ? o.z : 0u; w[i][3] = live ? o.w : 0u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sum[e] += live && norm ? wg[e] : 0.0f;
+                asm volatile("" : "+v"(sum[e]));
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// The usual case: both kinds of heads normalised, whole heads turned by pairs
+// (i, i + D / 2), sequences of whole groups of 8 tokens, so that a thread's rows
+// are one sequence's and all or none of them exist. Here lane l of a head holds
+// the pairs 4 l .. 4 l + 3, two 8-byte pieces D / 2 values apart: no value changes
+// lanes, and the lanes' cosines and sines are one run of the table (with eight
+// consecutive values a lane, every entry is loaded by two lanes and each of
+// four 16-byte loads touches all of the row's lines, which held up the loads: 70
+// against 54 us at 8192 tokens of 16 + 8 heads of 128). The results change to the
+// quantiser's columns through LDS, a row of a wave at a time. The tile's loads
+// are all issued before the first is waited for, a row's cosines and sines one
+// row ahead. (A wave with a position outside the table takes the way above.)
+template <int L>
+__device__ __forceinline__ void load_qk_bwd_usual(const QkArgs& k, const Divisor& per_seq, const Tile& t,
+                                                  int head0, uint8_t (*stage)[1024], uint32_t w[8][4], float sum[8],
+                                                  int col[2]) {
+    constexpr int D = L * 8;
+    const HeadOf h = head_of<L>(k, head0);
+    const int kind = h.kind;
+    const bool live = t.row0 < k.tokens && !h.none;
+    const int row0 = (int)min(t.row0, k.tokens - 8);
+    const Token tok = token_of(row0, per_seq);
+    const int lane = threadIdx.x & 63, l = lane % L;
+    col[0] = t.cc / L * D + 4 * l;
+    col[1] = col[0] + D / 2;
+    const uint16_t* const gp = h.gp + tok.b * h.gbs + tok.s * h.grs;
+    const uint16_t* const xp = h.xp + tok.b * h.xbs + tok.s * h.xrs + 4 * l;
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
     if (wave_none(kind != 2)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bool live = i < rows && !none;
-            w[i][0] = live ? rd[i].x : 0u; w[i][1] = live ? rd[i].y : 0u;
-            w[i][2] = live ? rd[i].z : 0u; w[i][3] = live ? rd[i].w : 0u;
+            const uint4 v = *reinterpret_cast<const uint4*>(gp + i * h.grs + 8 * l);
+            w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
         }
-        return;
+    } else {
+        int pos[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pos[i] = tok.s + i;
+        if (k.rope.pos) {
+            bool out = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                pos[i] = k.rope.pos[row0 + i];
+                out = out || (unsigned)pos[i] >= (unsigned)k.rope.len;
+            }
+            if (!wave_none(out)) {
+                load_qk_bwd_any<L>(k, per_seq, t, head0, w, sum, col);
+                return;
+            }
+        }
+        auto turn_row = [&](int p, float4 u[2]) __attribute__((always_inline)) {
+            const float4* const v = reinterpret_cast<const float4*>(k.rope.table + (int64_t)p * (D / 2) + 4 * l);
+            u[0] = v[0];
+            u[1] = v[1];
+        };
+        uint2 rd[8][2], rx[8][2];
+        float4 next[2];
+        turn_row(pos[0], next);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint16_t* const g = gp + i * h.grs + 4 * l;
+            rd[i][0] = *reinterpret_cast<const uint2*>(g);
+            rd[i][1] = *reinterpret_cast<const uint2*>(g + D / 2);
+            rx[i][0] = *reinterpret_cast<const uint2*>(xp + i * h.xrs);
+            rx[i][1] = *reinterpret_cast<const uint2*>(xp + i * h.xrs + D / 2);
+        }
+        uint2 gw[2] = {};
+        if (L == 16 || h.gamma) {
+            gw[0] = *reinterpret_cast<const uint2*>(h.gamma + 4 * l);
+            gw[1] = *reinterpret_cast<const uint2*>(h.gamma + D / 2 + 4 * l);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // a wave's four rows of 256 bytes, odd ones with their halves swapped
+        // (so that two rows' 8-byte pieces do not meet in a bank)
+        const int r = lane >> 4, swap = (r & 1) << 7, at = (lane & 15) / L * (D * 2) + 8 * l;
+        uint8_t* const mine = stage[threadIdx.x >> 6] + r * 256;
+        constexpr float inv_d = 1.0f / (float)D;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 u[2] = {next[0], next[1]};
+            if (i < 7) turn_row(pos[i + 1], next);
+            float d[8], x8[8], wg[8], gm[8];
+            unpack8(make_uint4(rd[i][0].x, rd[i][0].y, rd[i][1].x, rd[i][1].y), d);
+            unpack8(make_uint4(rx[i][0].x, rx[i][0].y, rx[i][1].x, rx[i][1].y), x8);
+            asm volatile("" : "+v"(gw[0].x), "+v"(gw[0].y), "+v"(gw[1].x), "+v"(gw[1].y));
+            unpack8(make_uint4(gw[0].x, gw[0].y, gw[1].x, gw[1].y), gm);
+const float c[4] = {u[0].x, u[0].z, u[1].x, u[1].z}, sn[4] = {u[0].y, u[0].w, u[1].y, u[1].w};
+            turn_pairs4(d, c, sn, true);
+            norm_bwd8<L>(d, x8, gm, inv_d, k.eps, wg);
+            const uint4 n = pack8(d);
+            uint2 lo = make_uint2(n.x, n.y), hi = make_uint2(n.z, n.w);
+            if constexpr (L == 8) {
+                lo.x = kind != 2 ? lo.x : rd[i][0].x; lo.y = kind != 2 ? lo.y : rd[i][0].y;
+                hi.x = kind != 2 ? hi.x : rd[i][1].x; hi.y = kind != 2 ? hi.y : rd[i][1].y;
+            }
+            __builtin_amdgcn_wave_barrier();
+            *reinterpret_cast<uint2*>(mine + (at ^ swap)) = lo;
+            *reinterpret_cast<uint2*>(mine + ((at + D) ^ swap)) = hi;
+            __builtin_amdgcn_wave_barrier();
+            const uint4 o = *reinterpret_cast<const uint4*>(mine + (((lane & 15) * 16) ^ swap));
+            w[i][0] = o.x; w[i][1] = o.y; w[i][2] = o.z; w[i][3] = o.w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sum[e] += wg[e];
+                asm volatile("" : "+v"(sum[e]));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = live ? sum[e] : 0.0f;
     }
-    float gm[8];
-    uint4 gw{};
-    if (norm) gw = *reinterpret_cast<const uint4*>(gamma + role.col);
-    unpack8(gw, gm);
-    const float inv_d = 1.0f / (float)k.D;
+    if (!wave_none(!live)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float d[8], n[8], x8[8], wg[8];
-        unpack8(rd[i], d);
-        if (turned) {
-            const Turn turn = load_turn(k.rope, role, pos[i], true);
-            turn8<L>(d, turn, role, k.rope.interleaved, k.rope.dim == L * 8);
-        }
-        unpack8(rx[i], x8);
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) n[e] = d[e];
-        norm_bwd8<L>(n, x8, gm, inv_d, k.eps, wg);
-        const bool live = i < rows && !none;
-        uint4 o = rd[i];
-        if (kind != 2) o = pack8(norm ? n : d);
-        w[i][0] = live ? o.x : 0u; w[i][1] = live ? o.y : 0u;
-        w[i][2] = live ? o.z : 0u; w[i][3] = live ? o.w : 0u;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += live && norm ? wg[e] : 0.0f;
+            for (int j = 0; j < 4; ++j) w[i][j] = live ? w[i][j] : 0u;
     }
 }
 
@@ -92,34 +273,37 @@ enum : int { kQkAmax = 0, kQkTensor = 1, kQkRow = 2, kQkRowCol = 3, kQkCol = 4 }
 // One tile per block. The block's sums for dgamma go to
 // k.part[tile row][head][D] (query and key heads), in the one pass that the
 // grouped modes take and in the amax pass of the per-tensor mode.
-template <int FMT, int MODE, int L, bool FLOOR = false>
-__global__ __launch_bounds__(kThreads) void qk_bwd_quant_kernel(QuantArgs a, QkArgs k, Divisor per_seq,
+template <int FMT, int MODE, int L, bool USUAL, bool FLOOR = false>
+__global__ __launch_bounds__(kThreads) void qk_bwd_quant_kernel(Kinds kinds, QuantArgs a, QkArgs k, Divisor per_seq,
                                                                 uint32_t* partial) {
     constexpr bool GROUPS = MODE >= kQkRow;
     constexpr bool ROWS = MODE == kQkRow || MODE == kQkRowCol, COLS = MODE == kQkRowCol || MODE == kQkCol;
+    (void)kinds;      // (read where they lie, by number)
     __shared__ uint32_t red[4];
     __shared__ uint32_t colmax[COLS ? 4 : 1][kTile / 2];
     __shared__ float sums[MODE == kQkTensor ? 1 : 4][kTile];
+    __shared__ __attribute__((aligned(16))) uint8_t stage[USUAL ? 4 : 1][1024];
     __shared__ __attribute__((aligned(16))) uint8_t tq[COLS || MODE == kQkTensor ? kTile * kTile : 16];
     const int bx = blockIdx.x;
     const int64_t by = blockIdx.y;
     const Tile t = tile_coords(a.cols, bx, by);
-    const int head = L == 16 ? bx : bx * 2 + (t.cc >> 3);
+    const int head0 = L == 16 ? bx : bx * 2;
     PartialShare ps;
     if constexpr (MODE == kQkTensor) ps = load_partials(a);
     uint32_t w[8][4];
     float sum[8];
-    int kind;
-    load_qk_bwd_8x8<L>(k, per_seq, t, head, w, sum, kind);
+    int col[2];
+    if constexpr (USUAL) load_qk_bwd_usual<L>(k, per_seq, t, head0, stage, w, sum, col);
+    else load_qk_bwd_any<L>(k, per_seq, t, head0, w, sum, col);
     if constexpr (MODE != kQkTensor) {
-        if (k.part && __builtin_amdgcn_readfirstlane(L == 16 ? head : bx * 2) < k.hq + k.hk) {
+        if (k.part && head0 < k.hq + k.hk) {
             // the wave's four row groups (16 lanes apart), then the four waves
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float s = sum[e];
                 s += __shfl_xor(s, 16, 64);
                 s += __shfl_xor(s, 32, 64);
-                if ((threadIdx.x & 63) < 16) sums[threadIdx.x >> 6][t.cc * 8 + e] = s;
+                if ((threadIdx.x & 63) < 16) sums[threadIdx.x >> 6][col[e / 4] + e % 4] = s;
             }
             __syncthreads();
             if (threadIdx.x < kTile) {
@@ -149,27 +333,28 @@ __global__ __launch_bounds__(kThreads) void qk_bwd_quant_kernel(QuantArgs a, QkA
     }
 }
 
-template <int FMT, int L>
+template <int FMT, int L, bool USUAL>
 void launch_fmt(int mode, QuantArgs a, const QkArgs& k, void* ws, hipStream_t stream) {
     const dim3 grid((unsigned)tiles_x(a.cols), (unsigned)tiles_y(a.rows));
     const Divisor per_seq = Divisor::of((uint32_t)k.seq);
+    const Kinds kinds = kinds_of(k);
     uint32_t* partial = reinterpret_cast<uint32_t*>(ws);
     switch (mode) {
     case kQTensor:
-        qk_bwd_quant_kernel<kE4M3, kQkAmax, L><<<grid, kThreads, 0, stream>>>(a, k, per_seq, partial);
+        qk_bwd_quant_kernel<kE4M3, kQkAmax, L, USUAL><<<grid, kThreads, 0, stream>>>(kinds, a, k, per_seq, partial);
         amax_source(a, (int)(grid.x * grid.y), ws, stream);
-        qk_bwd_quant_kernel<FMT, kQkTensor, L><<<grid, kThreads, 0, stream>>>(a, k, per_seq, partial);
+        qk_bwd_quant_kernel<FMT, kQkTensor, L, USUAL><<<grid, kThreads, 0, stream>>>(kinds, a, k, per_seq, partial);
         break;
     case kQRow:
         by_rule(a, [&](auto floor) {
             constexpr bool FLOOR = decltype(floor)::value;
-            if (a.qT) qk_bwd_quant_kernel<FMT, kQkRowCol, L, FLOOR><<<grid, kThreads, 0, stream>>>(a, k, per_seq, partial);
-            else qk_bwd_quant_kernel<FMT, kQkRow, L, FLOOR><<<grid, kThreads, 0, stream>>>(a, k, per_seq, partial);
+            if (a.qT) qk_bwd_quant_kernel<FMT, kQkRowCol, L, USUAL, FLOOR><<<grid, kThreads, 0, stream>>>(kinds, a, k, per_seq, partial);
+            else qk_bwd_quant_kernel<FMT, kQkRow, L, USUAL, FLOOR><<<grid, kThreads, 0, stream>>>(kinds, a, k, per_seq, partial);
         });
         break;
     case kQCol:
         by_rule(a, [&](auto floor) {
-            qk_bwd_quant_kernel<FMT, kQkCol, L, decltype(floor)::value><<<grid, kThreads, 0, stream>>>(a, k, per_seq, partial);
+            qk_bwd_quant_kernel<FMT, kQkCol, L, USUAL, decltype(floor)::value><<<grid, kThreads, 0, stream>>>(kinds, a, k, per_seq, partial);
         });
         break;
     }
@@ -202,8 +387,14 @@ void launch_qk_norm_rope_bwd_quantize(int fmt, int mode, QuantArgs a, QkArgs k, 
     }
     auto run = [&](auto fmt_c) {
         constexpr int FMT = decltype(fmt_c)::value;
-        if (k.D == 128) launch_fmt<FMT, 16>(mode, a, k, ws, stream);
-        else launch_fmt<FMT, 8>(mode, a, k, ws, stream);
+        const bool usual = k.gq && k.gk && turn_kind(k.rope, k.D / 8) == kTurnHalf && k.seq % 8 == 0;
+        if (k.D == 128) {
+            if (usual) launch_fmt<FMT, 16, true>(mode, a, k, ws, stream);
+            else launch_fmt<FMT, 16, false>(mode, a, k, ws, stream);
+        } else {
+            if (usual) launch_fmt<FMT, 8, true>(mode, a, k, ws, stream);
+            else launch_fmt<FMT, 8, false>(mode, a, k, ws, stream);
+        }
     };
     if (fmt == kE4M3) run(std::integral_constant<int, kE4M3>{});
     else run(std::integral_constant<int, kE5M2>{});

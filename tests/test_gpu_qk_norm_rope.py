@@ -346,6 +346,46 @@ def test_quantised_equals_quantising_the_gradient(P):
             torch.testing.assert_close(x, y, rtol=0, atol=2e-5 * float(x.abs().max()))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_quantised_with_positions_outside_the_table(P, D):
+    """In one wave's rows among many: NaN scales and codes of those tokens' turned heads, everything else as it was,
+    dgamma NaN."""
+    c = Case(P, 28, 256, 3, 1, D, D, positions="given")
+    cols, turned = 5 * D, 4 * D
+    if cols % 128:
+        c = Case(P, 28, 256, 4, 1, D, D, positions="given")
+        cols, turned = 6 * D, 5 * D
+    run = lambda pos: P.qk_norm_rope_bwd_quantize_fp8(*c.g, c.q, c.k, fmt=E4, mode=ROW, rnd=1,
+                                                      **dict(c.args, positions=pos))
+    good = run(c.p_dev)
+    bad = c.p_dev.clone()
+    bad[70], bad[201] = -5, c.rope.table.shape[0] + 3
+    got = run(bad)
+    keep = np.setdiff1d(np.arange(256), [70, 201])
+    q, w = host(got["q"]), host(good["q"])
+    assert (q[keep] == w[keep]).all() and (host(got["scale"])[keep] == host(good["scale"])[keep]).all()
+    whole = turned // 128                                      # groups of turned heads alone
+    assert np.isnan(host(got["scale"])[[70, 201]][:, :whole]).all() and (q[[70, 201]][:, :whole * 128] == 0x7F).all()
+    tail = -(-turned // 128) * 128
+    assert (q[[70, 201]][:, tail:] == w[[70, 201]][:, tail:]).all()
+    assert np.isnan(host(got["dgamma_q"])).all()
+
+
+@pytest.mark.parametrize("T,batch", [(152, 1), (136, 17), (1032, 3), (200, 25), (8, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_quantised_ragged_rows(P, T, batch, D):
+    """Sequences of whole groups of 8 tokens, and not; rows that end inside a tile; an odd number of heads of 64."""
+    c = Case(P, T + D, T, 2, 1, D, D, batch=batch)
+    got = P.qk_norm_rope_bwd_quantize_fp8(*c.g, c.q, c.k, fmt=E5, mode=TENSOR, rnd=0, **c.args)
+    parts = [c.backward(i)[:2] for i in range(2)]
+    ref = np.concatenate([p[0] for p in parts] + [f64(c.d[2])], 1).reshape(T, -1)
+    tol = np.concatenate([p[1] for p in parts] + [np.zeros(c.d[2].shape)], 1).reshape(T, -1)
+    mid, lo, hi = qk.band(ref, tol)
+    band_check.check(host(got["q"]), host(got["scale"]), mid, lo, hi, lo == hi, fp8.E5M2, "fp32", None, "ragged")
+    check_dgamma(got["dgamma_q"], c, 0, "ragged")
+    check_dgamma(got["dgamma_k"], c, 1, "ragged")
+
+
 def test_large_offsets(P):
     """Heads more than 2^31 elements after the first one of their tensor."""
     import torch

@@ -138,23 +138,45 @@ struct Teacher {
 };
 
 // lse and loss of a row, from its blocks' (max, sum exp(a - max)) and its
-// entries: one wave per row.
+// entries: a block per row. The pairs are read once, kHold of a thread's stay in
+// registers between the maximum and the sum (as many as a vocabulary of 262144
+// has; M 4096, V 151936: XXX us, a wave per row that read them twice 29). The
+// first wave then takes the entries.
+constexpr int kHold = 8;
 __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const float2* __restrict__ stats, int64_t ld, int nblk,
-                                                                int64_t M, Teacher tch, const float* __restrict__ z_top,
+                                                                Teacher tch, const float* __restrict__ z_top,
                                                                 float* __restrict__ lse, float* __restrict__ loss) {
-    const int lane = threadIdx.x & 63;
-    const int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (m >= M) return;
+    __shared__ float red[8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t m = blockIdx.x;
     const float2* const st = stats + m * ld;
+    float2 v[kHold];
     float mx = -kInf;
-    for (int b = lane; b < nblk; b += 64) mx = fmaxf(mx, st[b].x);
-    mx = wave_max(mx);
-    float s = 0.0f;
-    for (int b = lane; b < nblk; b += 64) {
-        const float2 v = st[b];
-        if (v.y != 0.0f) s += v.y * exp_f32(v.x - mx);   // NaN sums propagate
+#pragma unroll
+    for (int u = 0; u < kHold; ++u) {
+        const int b = (int)threadIdx.x + kThreads * u;
+        v[u] = b < nblk ? st[b] : make_float2(-kInf, 0.0f);
     }
-    const float l = mx + logf(wave_sum(s));
+#pragma unroll
+    for (int u = 0; u < kHold; ++u) mx = fmaxf(mx, v[u].x);
+    for (int b = (int)threadIdx.x + kThreads * kHold; b < nblk; b += kThreads) mx = fmaxf(mx, st[b].x);
+    mx = wave_max(mx);
+    if (lane == 0) red[wave] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float s = 0.0f;
+#pragma unroll
+    for (int u = 0; u < kHold; ++u)
+        if (v[u].y != 0.0f) s += v[u].y * exp_f32(v[u].x - mx);   // NaN sums propagate
+    for (int b = (int)threadIdx.x + kThreads * kHold; b < nblk; b += kThreads) {
+        const float2 w = st[b];
+        if (w.y != 0.0f) s += w.y * exp_f32(w.x - mx);
+    }
+    s = wave_sum(s);
+    if (lane == 0) red[4 + wave] = s;
+    __syncthreads();
+    if (wave > 0) return;
+    const float l = mx + logf((red[4] + red[5]) + (red[6] + red[7]));
     tch.ids += m * tch.k;
     tch.t += m * tch.k;
     z_top += m * tch.k;
@@ -307,8 +329,8 @@ void launch_lm_distill_fwd(const DistillArgs& a, float* lse, float* loss, float*
     g.stats_ld = pad128(a.V) / 128;
     g.ldd = a.V;
     launch_gemm(g, nullptr, stream);
-    distill_rows_kernel<<<(unsigned)((a.M + 3) / 4), kThreads, 0, stream>>>(g.stats, g.stats_ld, (int)g.stats_ld, a.M,
-                                                                          teacher_of(a), z_top, lse, loss);
+    distill_rows_kernel<<<(unsigned)a.M, kThreads, 0, stream>>>(g.stats, g.stats_ld, (int)g.stats_ld, teacher_of(a), z_top,
+                                                              lse, loss);
 }
 
 void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* z_top, const float* dloss, float grad_scale,

@@ -240,6 +240,7 @@ void run_plan(const GemmProblem& g, const Plan& pl, void* ws, hipStream_t stream
     prm.lse = g.lse; prm.grad_scale = g.grad_scale; prm.row_scale = g.row_scale;
     prm.rows_a = (int)(g.rows_a ? g.rows_a : g.M);
     prm.rows_b = (int)(g.rows_b ? g.rows_b : g.N);
+    prm.dzt = g.dzt; prm.ld_dzt = g.ld_dzt;
     prm.q8 = g.q8; prm.q8_scale = g.q8_scale; prm.q8t = g.q8t; prm.q8t_scale = g.q8t_scale;
     const bool grouped = grouped_scales(g);
     const int out = pl.splits > 1 ? 2 : g.out;
@@ -302,9 +303,13 @@ void gemm_plan(int64_t M, int64_t N, int64_t K, bool grouped, int* tile_m, int* 
     *splits = p.splits;
 }
 
+static bool lm_head_kind(int out) {
+    return out == kOutLseStats || out == kOutSoftmaxGrad || out == kOutSoftmaxGradQ || out == kOutSoftmaxGradT;
+}
+
 void launch_gemm(const GemmProblem& g, void* ws, hipStream_t stream) {
     const int64_t kb = g.K * elem_bytes(g);
-    if (g.out == kOutLseStats || g.out == kOutSoftmaxGrad || g.out == kOutSoftmaxGradQ) {
+    if (lm_head_kind(g.out)) {
         // the LM-head epilogues reduce over 128-column wave tiles: the
         // 256 x 256 configuration, unsplit
         run_plan(g, Plan{0, 1, (int)((kb + kBK - 1) / kBK)}, ws, stream);
@@ -314,7 +319,7 @@ void launch_gemm(const GemmProblem& g, void* ws, hipStream_t stream) {
 }
 
 int gemm_tile(const GemmProblem& g) {
-    if (g.out == kOutLseStats || g.out == kOutSoftmaxGrad || g.out == kOutSoftmaxGradQ) return kTiles[0].bm;
+    if (lm_head_kind(g.out)) return kTiles[0].bm;
     return kTiles[make_plan(g.M, g.N, g.K * elem_bytes(g), grouped_scales(g), g.batch, g.upper != 0).cfg].bm;
 }
 

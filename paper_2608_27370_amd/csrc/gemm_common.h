@@ -54,6 +54,8 @@ struct Params {
     float grad_scale;
     const float* row_scale;    // kOutSoftmaxGrad: a factor per row in place of grad_scale, or NULL
     int rows_a, rows_b;        // rows that A and B have (M and N, or fewer)
+    uint16_t* dzt;             // kOutSoftmaxGradT: the transposed copy [N, M] and its row pitch
+    int64_t ld_dzt;
     uint8_t* q8;               // kOutSoftmaxGradQ: dz's FP8 copies (the GemmProblem fields)
     float* q8_scale;
     uint8_t* q8t;

@@ -287,6 +287,59 @@ __device__ __forceinline__ void quantize_staged_dz(const P& p, const uint8_t* ep
     }
 }
 
+// The transposed copy of a wave's staged 128 x 128 BF16 tile (row r at ep +
+// 256 r, its 16-byte chunk c at position c ^ (r & 15)): row c of the copy, 128
+// values, leaves in one run of 256 bytes, sixteen lanes of 16 bytes. A lane
+// reads 8 x 8 blocks (rows 8 b .., chunk cb: a phase's sixteen lanes one row, all
+// banks), transposes them in registers and writes them over the tile as the
+// copy's rows, row c at ep + 256 c, its chunk b at position b ^ (c >> 3) (sixteen
+// lanes, sixteen positions), to read them back a row at a time. The region
+// belongs to this wave alone and LDS takes a wave's accesses in order.
+template <class P>
+__device__ __forceinline__ void store_transposed_dz(const P& p, uint8_t* ep, int64_t mrow0, int64_t ncol0, int lane) {
+    typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+    const int cb = lane & 15, b0 = lane >> 4;
+    uint32_t t[4][8][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int b = b0 + 4 * k;
+        uint32_t w[8][4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = b * 8 + i;
+            const v4u v = *reinterpret_cast<const v4u*>(ep + r * 256 + ((cb ^ (r & 15)) << 4));
+            w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
+        }
+        transpose8x8_b16(w, t[k]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int b = b0 + 4 * k;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<v4u*>(ep + (cb * 8 + j) * 256 + ((b ^ cb) << 4)) = v4u{t[k][j][0], t[k][j][1], t[k][j][2], t[k][j][3]};
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const uint32_t pitch = (uint32_t)(p.ld_dzt * 2);
+    const __amdgpu_buffer_rsrc_t rt = __builtin_amdgcn_make_buffer_rsrc(p.dzt + ncol0 * p.ld_dzt + mrow0, 0,
+                                                                        (int)(127 * pitch + 256), 0x00020000);
+    // chunk lane & 15 of rows 4 it + (lane >> 4)
+    const int voff = (int)((uint32_t)(lane >> 4) * pitch) + (lane & 15) * 16;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        v4u d[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = (g * 8 + e) * 4 + (lane >> 4);
+            d[e] = *reinterpret_cast<const v4u*>(ep + c * 256 + (((lane & 15) ^ (c >> 3)) << 4));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            __builtin_amdgcn_raw_buffer_store_b128(d[e], rt, voff, (int)((uint32_t)(g * 8 + e) * 4 * pitch), 0);
+    }
+}
+
 // PROD: the workgroup has NW more waves that only issue the global->LDS
 // loads (producers); the NW MFMA waves (consumers) then only read LDS and
 // multiply, so a load that cannot issue (the texture unit's queue full)
@@ -913,7 +966,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     // Its dz kinds take every wave tile this way (M and N are multiples of
     // 128, so a wave tile lies wholly inside the output or wholly outside):
     // kOutSoftmaxGradQ quantises the staged tile (below).
-    constexpr bool kDz = OUT == kOutSoftmaxGrad || OUT == kOutSoftmaxGradQ;
+    constexpr bool kDz = OUT == kOutSoftmaxGrad || OUT == kOutSoftmaxGradQ || OUT == kOutSoftmaxGradT;
     static_assert(!kDz || (ECPR == 32 && WTM == 128 && WTM * 256 <= REGION), "dz kinds: 128 x 128 wave tiles");
     if constexpr ((OUT == kOutBF16 || OUT == kOutBF16Epi || kDz) && ECPR == 32 && WTM * 256 <= REGION) {
         if constexpr (kDz) {
@@ -1105,6 +1158,13 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                     (const __attribute__((address_space(4))) Params*)__builtin_amdgcn_kernarg_segment_ptr();
                 asm volatile("" : "+s"(kp));
                 quantize_staged_dz(*kp, ep, mrow0, ncol0, lane);
+            }
+            if constexpr (OUT == kOutSoftmaxGradT) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                const __attribute__((address_space(4))) Params* kp =
+                    (const __attribute__((address_space(4))) Params*)__builtin_amdgcn_kernarg_segment_ptr();
+                asm volatile("" : "+s"(kp));
+                store_transposed_dz(*kp, ep, mrow0, ncol0, lane);
             }
             return;
         }
@@ -1373,6 +1433,9 @@ void launch_tile(const Params& prm, int out, int grid, hipStream_t stream) {
         // the blockwise E4M3 recipe's backward, 128 x 128 wave tiles
         if constexpr (FA == kE4M3 && FB == kE4M3 && GROUPED && BM / WM == 128 && BN / WN == 128)
             launch_cfg<BM, BN, WM, WN, SL, NST, XA, PROD, FA, FB, GROUPED, kOutSoftmaxGradQ>(prm, grid, stream);
+    } else if (out == kOutSoftmaxGradT) {
+        if constexpr (FA == kBF16 && FB == kBF16 && !GROUPED && BM / WM == 128 && BN / WN == 128)
+            launch_cfg<BM, BN, WM, WN, SL, NST, XA, PROD, FA, FB, GROUPED, kOutSoftmaxGradT>(prm, grid, stream);
     } else launch_cfg<BM, BN, WM, WN, SL, NST, XA, PROD, FA, FB, GROUPED, kOutBF16>(prm, grid, stream);
 }
 

@@ -150,8 +150,9 @@ enum ScaleMode : int { kSTensor = 0, kSRow = 1, kSBlock = 2, kSNone = 3 };
 // 128x1 column groups with power-of-two scales, as the quantiser makes them
 // from the BF16 dz (E4M3 block-scaled operands). Both dz kinds need M and N
 // to be multiples of 128.
+// kOutSoftmaxGradT writes that dz and its transposed copy (BF16 operands).
 enum OutKind : int { kOutBF16 = 0, kOutF32 = 1, kOutBF16Epi = 3, kOutLseStats = 4, kOutSoftmaxGrad = 5,
-                     kOutSoftmaxGradQ = 6 };
+                     kOutSoftmaxGradQ = 6, kOutSoftmaxGradT = 7 };
 
 // K, lda and ldb count operand elements (FP8 codes, or BF16 values when fa
 // and fb are kBF16, with scale modes kSNone).
@@ -204,13 +205,16 @@ struct GemmProblem {
     float* zt;
     const float* lse;
     float grad_scale;
-    // kOutSoftmaxGrad: a factor per row [rows_a] in place of grad_scale; the
+    // kOutSoftmaxGrad (T): a factor per row [rows_a] in place of grad_scale; the
     // rows that A and B have (0: M and N), fewer than the output, whose M and
     // N are multiples of 128: dz of rows past them is zero, that of columns
     // past them is left to be cleared. targets NULL: no one-hot term (nor, in
     // kOutLseStats, a target's logit)
     const float* row_scale = nullptr;
     int64_t rows_a = 0, rows_b = 0;
+    // kOutSoftmaxGradT: the transposed copy [N, M] (row pitch ld_dzt)
+    uint16_t* dzt = nullptr;
+    int64_t ld_dzt = 0;
     // kOutSoftmaxGradQ: dz's row-grouped codes [M, N] (ld N) with scales
     // [N / 128][M], and its transposed column-grouped codes [N, M] (ld M)
     // with scales [M / 128][N] (scale arrays k-block-major)

@@ -170,6 +170,34 @@ Plan make_plan(int64_t M, int64_t N, int64_t K, bool grouped, int batch = 1, boo
     return e.plan;
 }
 
+// The plan of a long reduction whose operands come from memory, each tile's
+// panels read once per unit (GemmProblem::long_k): the large tiles, 256x256 or
+// 256x192, whichever leaves fewer CUs idle with one unit each. make_plan's
+// constants are those of operands that the L2s mostly hold: it takes 128x128
+// tiles for such a problem, which read twice the panels. The distillation
+// loss's dX (its whole backward timed, vocabulary 80000, 50257, 36000, 24000
+// columns): 1000 rows of 1024 676 -> 596 us, 481 -> 440, 366 -> 347, 219 -> 228;
+// 500 of 1536 604 -> 553, 398 -> 367, 330 -> 306, 193 -> 198; 300 of 1536 at
+// 151936 989 -> 880; four tiles (200 of 1024) lose, 196 -> 208 at 50257, and at
+// 4096 rows both are within 1%. Hence the limits.
+bool long_k_plan(int64_t M, int64_t N, int64_t K, Plan* best) {
+    constexpr int64_t kLongBytes = 65536;
+    if (K < kLongBytes || N % 4 != 0) return false;
+    const int ksteps = (int)((K + kBK - 1) / kBK);
+    int64_t most = 0;
+    for (int c = 0; c < 2; ++c) {
+        const int64_t tiles = ((M + kTiles[c].bm - 1) / kTiles[c].bm) * ((N + kTiles[c].bn - 1) / kTiles[c].bn);
+        if (tiles < 8 || tiles > kCUs / 2) return false;
+        const int64_t s = kCUs / tiles;
+        if (s * tiles > most) {
+            most = s * tiles;
+            const int kps = (int)((ksteps + s - 1) / s);
+            *best = Plan{c, (ksteps + kps - 1) / kps, kps};
+        }
+    }
+    return true;
+}
+
 // Tile rows per group of an XCD's contiguous range of tiles (the order in
 // which that XCD's CUs take them): 4 (the QKV Wgrad's 24-tile ranges become
 // 4 x 6 tiles, 10 operand panels per XCD instead of 11 at 8). On the
@@ -294,6 +322,11 @@ size_t gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int out, int batch)
     return w;
 }
 
+size_t gemm_long_k_workspace_bytes(int64_t M, int64_t N, int64_t K, int out) {
+    Plan pl;
+    return long_k_plan(M, N, K, &pl) ? plan_workspace_bytes(M, N, pl) : gemm_workspace_bytes(M, N, K, out);
+}
+
 void gemm_plan(int64_t M, int64_t N, int64_t K, bool grouped, int* tile_m, int* tile_n, int* stages,
                int* splits) {
     const Plan p = make_plan(M, N, K, grouped);
@@ -304,7 +337,8 @@ void gemm_plan(int64_t M, int64_t N, int64_t K, bool grouped, int* tile_m, int* 
 }
 
 static bool lm_head_kind(int out) {
-    return out == kOutLseStats || out == kOutSoftmaxGrad || out == kOutSoftmaxGradQ || out == kOutSoftmaxGradT;
+    return out == kOutLseStats || out == kOutSoftmaxGrad || out == kOutSoftmaxGradQ || out == kOutSoftmaxGradT ||
+           out == kOutLseAny;
 }
 
 void launch_gemm(const GemmProblem& g, void* ws, hipStream_t stream) {
@@ -315,7 +349,9 @@ void launch_gemm(const GemmProblem& g, void* ws, hipStream_t stream) {
         run_plan(g, Plan{0, 1, (int)((kb + kBK - 1) / kBK)}, ws, stream);
         return;
     }
-    run_plan(g, make_plan(g.M, g.N, kb, grouped_scales(g), g.batch, g.upper != 0), ws, stream);
+    Plan pl;
+    if (!g.long_k || !long_k_plan(g.M, g.N, kb, &pl)) pl = make_plan(g.M, g.N, kb, grouped_scales(g), g.batch, g.upper != 0);
+    run_plan(g, pl, ws, stream);
 }
 
 int gemm_tile(const GemmProblem& g) {

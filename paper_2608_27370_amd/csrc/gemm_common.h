@@ -50,11 +50,11 @@ struct Params {
     float2* stats;             // [M][stats_ld]: (max, sum exp(z - max)) per 128-column block
     int64_t stats_ld;
     float* zt;                 // [M]: the target's logit
-    const float* lse;          // [rows_a]
+    const float* lse;          // [M] (kOutSoftmaxGradT: [rows_a])
     float grad_scale;
-    const float* row_scale;    // kOutSoftmaxGrad: a factor per row in place of grad_scale, or NULL
+    const float* row_scale;    // kOutSoftmaxGradT: a factor per row in place of grad_scale
     int rows_a, rows_b;        // rows that A and B have (M and N, or fewer)
-    uint16_t* dzt;             // kOutSoftmaxGradT: the transposed copy [N, M] and its row pitch
+    uint16_t* dzt;             // kOutSoftmaxGradT: the transposed copy [N, M], or NULL, and its row pitch
     int64_t ld_dzt;
     uint8_t* q8;               // kOutSoftmaxGradQ: dz's FP8 copies (the GemmProblem fields)
     float* q8_scale;

@@ -838,7 +838,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     // one FMA, z log2(e) - max log2(e), fed to the exp2 instruction. Its
     // rounding errs by a relative 2^-24 of |z| on each term and of |max| on
     // all of them alike, far inside the error of a binary32 log-sum-exp.
-    if constexpr (OUT == kOutLseStats) {
+    if constexpr (OUT == kOutLseStats || OUT == kOutLseAny) {
         static_assert(!PROD && FN == 4 && WTN == 128, "LM-head statistics: 128-column wave tiles");
         const int mrow0 = m0 + wm * WTM, ncol0 = n0 + wn * WTN;
         if (ncol0 >= p.N) return;      // a wave tile wholly past N (the ragged last tile) has no block
@@ -849,10 +849,11 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int64_t m = (int64_t)mrow0 + i * 32 + (lane & 31);
-            tcol[i] = p.targets && m < p.M ? p.targets[m] - p.col0 - ncol0 - 4 * hl : INT_MIN;
+            tcol[i] = OUT == kOutLseStats && m < p.M ? p.targets[m] - p.col0 - ncol0 - 4 * hl : INT_MIN;
         }
         // columns of the lane past the last one (a ragged last block) count as minus infinity
         const int past = p.N - ncol0 - 4 * hl;
+        (void)past;
         constexpr float kLog2e = 1.44269504088896340736f;
         static_for<FM>([&](auto i_c) __attribute__((always_inline)) {
             constexpr int i = decltype(i_c)::value;
@@ -863,11 +864,13 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
 #pragma unroll
                 for (int e = 0; e < FN * 16; ++e) v[e] *= alpha;
             }
-            if (ncol0 + WTN > p.N) {
+            if constexpr (OUT == kOutLseAny) {
+                if (ncol0 + WTN > p.N) {
 #pragma unroll
-                for (int e = 0; e < FN * 16; ++e) {
-                    const int c = e / 16 * 32 + 8 * (e % 16 / 4) + e % 4;
-                    v[e] = c < past ? v[e] : -__builtin_inff();
+                    for (int e = 0; e < FN * 16; ++e) {
+                        const int c = e / 16 * 32 + 8 * (e % 16 / 4) + e % 4;
+                        v[e] = c < past ? v[e] : -__builtin_inff();
+                    }
                 }
             }
             float mq[4] = {v[0], v[1], v[2], v[3]};
@@ -886,6 +889,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             // the target's logit, where this wave tile holds it: entry
             // (j, g, t) of fragment row i is column j*32 + 8g + t past the
             // lane's first (rare: a branch taken by the whole wave or not)
+            if constexpr (OUT == kOutLseAny) return;
             const int tc = tcol[i];
             const bool mine = tc >= 0 && tc < WTN && ((tc >> 2) & 1) == 0;
             if (__builtin_amdgcn_ballot_w64(mine)) {
@@ -966,6 +970,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     // Its dz kinds take every wave tile this way (M and N are multiples of
     // 128, so a wave tile lies wholly inside the output or wholly outside):
     // kOutSoftmaxGradQ quantises the staged tile (below).
+    constexpr bool kAny = OUT == kOutSoftmaxGradT;
     constexpr bool kDz = OUT == kOutSoftmaxGrad || OUT == kOutSoftmaxGradQ || OUT == kOutSoftmaxGradT;
     static_assert(!kDz || (ECPR == 32 && WTM == 128 && WTM * 256 <= REGION), "dz kinds: 128 x 128 wave tiles");
     if constexpr ((OUT == kOutBF16 || OUT == kOutBF16Epi || kDz) && ECPR == 32 && WTM * 256 <= REGION) {
@@ -980,17 +985,23 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             constexpr float kL2eLo = 1.925962989e-8f;                // log2(e) - kL2eHi
             constexpr float kLn2 = 0.693147180559945309f;
             constexpr float kL2eLoLn2 = kL2eLo * kLn2;
-            float row_p[kDz ? FM : 1], row_k[kDz ? FM : 1], row_g[kDz ? FM : 1];
+            float row_p[kDz ? FM : 1], row_k[kDz ? FM : 1], row_g[kAny ? FM : 1];
             int row_tgt[kDz ? FM : 1];
             if constexpr (kDz) {
 #pragma unroll
                 for (int i = 0; i < FM; ++i) {
                     const int64_t m = (int64_t)mrow0 + i * 32 + (lane & 31);
-                    // (rows that A does not have: z = 0, and a gradient of 0 (e^0))
-                    const bool has = m < p.rows_a;
-                    row_tgt[i] = p.targets ? p.targets[m] - p.col0 - ncol0 - 4 * (lane >> 5) : INT_MIN;
-                    const float l = has ? p.lse[m] : 0.0f;
-                    row_g[i] = p.row_scale ? (has ? p.row_scale[m] : 0.0f) : p.grad_scale;
+                    float l;
+                    if constexpr (kAny) {
+                        // (rows that A does not have: z = 0, and a gradient of 0 (e^0))
+                        const bool has = m < p.rows_a;
+                        row_tgt[i] = INT_MIN;
+                        l = has ? p.lse[m] : 0.0f;
+                        row_g[i] = has ? p.row_scale[m] : 0.0f;
+                    } else {
+                        row_tgt[i] = p.targets[m] - p.col0 - ncol0 - 4 * (lane >> 5);
+                        l = p.lse[m];
+                    }
                     row_p[i] = l * kL2eHi;
                     row_k[i] = 1.0f - (fmaf(l, kL2eHi, -row_p[i]) + l * kL2eLo) * kLn2;
                 }
@@ -1061,7 +1072,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                         // the four sums are columns j*32 + 8g + {0..3} past the
                         // lane's first: tr is the target's position among them
                         const int tr = row_tgt[i] - (j * 32 + 8 * g);
-                        const float P = row_p[i], K = row_k[i], gs = row_g[i];
+                        const float P = row_p[i], K = row_k[i], gs = kAny ? row_g[kAny ? i : 0] : p.grad_scale;
                         auto dz = [&](float z, int c) __attribute__((always_inline)) {
                             // 2^(z log2 e - lse log2 e) = 2^t (1 + c)
                             const float e = __builtin_amdgcn_exp2f(fmaf(z, kL2eHi, -P)) * fmaf(z, kL2eLoLn2, K);
@@ -1123,7 +1134,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             auto stage = [&](auto scaled, auto epi) __attribute__((always_inline)) {
                 static_for<FM + 1>([&](auto i_c) __attribute__((always_inline)) {
                     constexpr int i = decltype(i_c)::value;
-                    if constexpr (kDz && i < FM) {
+                    if constexpr (kDz && !kAny && i < FM) {
                         // set for the lane that holds its row's target (and
                         // maybe for its partner lane): a wave-uniform branch
                         if (__builtin_amdgcn_ballot_w64((unsigned)row_tgt[i] < (unsigned)WTN))
@@ -1164,7 +1175,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                 const __attribute__((address_space(4))) Params* kp =
                     (const __attribute__((address_space(4))) Params*)__builtin_amdgcn_kernarg_segment_ptr();
                 asm volatile("" : "+s"(kp));
-                store_transposed_dz(*kp, ep, mrow0, ncol0, lane);
+                if (kp->dzt) store_transposed_dz(*kp, ep, mrow0, ncol0, lane);
             }
             return;
         }
@@ -1433,9 +1444,11 @@ void launch_tile(const Params& prm, int out, int grid, hipStream_t stream) {
         // the blockwise E4M3 recipe's backward, 128 x 128 wave tiles
         if constexpr (FA == kE4M3 && FB == kE4M3 && GROUPED && BM / WM == 128 && BN / WN == 128)
             launch_cfg<BM, BN, WM, WN, SL, NST, XA, PROD, FA, FB, GROUPED, kOutSoftmaxGradQ>(prm, grid, stream);
-    } else if (out == kOutSoftmaxGradT) {
-        if constexpr (FA == kBF16 && FB == kBF16 && !GROUPED && BM / WM == 128 && BN / WN == 128)
-            launch_cfg<BM, BN, WM, WN, SL, NST, XA, PROD, FA, FB, GROUPED, kOutSoftmaxGradT>(prm, grid, stream);
+    } else if (out == kOutSoftmaxGradT || out == kOutLseAny) {
+        if constexpr (FA == kBF16 && FB == kBF16 && !GROUPED && BM / WM == 128 && BN / WN == 128) {
+            if (out == kOutLseAny) launch_cfg<BM, BN, WM, WN, SL, NST, XA, PROD, FA, FB, GROUPED, kOutLseAny>(prm, grid, stream);
+            else launch_cfg<BM, BN, WM, WN, SL, NST, XA, PROD, FA, FB, GROUPED, kOutSoftmaxGradT>(prm, grid, stream);
+        }
     } else launch_cfg<BM, BN, WM, WN, SL, NST, XA, PROD, FA, FB, GROUPED, kOutBF16>(prm, grid, stream);
 }
 

@@ -150,9 +150,11 @@ enum ScaleMode : int { kSTensor = 0, kSRow = 1, kSBlock = 2, kSNone = 3 };
 // 128x1 column groups with power-of-two scales, as the quantiser makes them
 // from the BF16 dz (E4M3 block-scaled operands). Both dz kinds need M and N
 // to be multiples of 128.
-// kOutSoftmaxGradT writes that dz and its transposed copy (BF16 operands).
+// With a teacher instead of targets (BF16 operands): kOutLseAny writes those
+// (max, sum) alone, for any N; kOutSoftmaxGradT dz = row_scale exp(z - lse) and,
+// with dzt, its transposed copy, for operands of fewer rows than M and N.
 enum OutKind : int { kOutBF16 = 0, kOutF32 = 1, kOutBF16Epi = 3, kOutLseStats = 4, kOutSoftmaxGrad = 5,
-                     kOutSoftmaxGradQ = 6, kOutSoftmaxGradT = 7 };
+                     kOutSoftmaxGradQ = 6, kOutSoftmaxGradT = 7, kOutLseAny = 8 };
 
 // K, lda and ldb count operand elements (FP8 codes, or BF16 values when fa
 // and fb are kBF16, with scale modes kSNone).
@@ -185,6 +187,10 @@ struct GemmProblem {
     // above the diagonal (square tiles); the tiles below are left unwritten
     // (gemm_tile returns the tile edge for filling them in)
     int upper = 0;
+    // an unbatched product with a long reduction over operands larger than the
+    // caches: long_k_plan's plan where it applies (gemm.hip), its workspace
+    // gemm_long_k_workspace_bytes
+    int long_k = 0;
     // a binary32 D is not read back soon: store it with non-temporal
     // (streaming) stores, which shorten the output-heavy epilogues (a BF16 D
     // is streamed or not by the operands' format, in every tile)
@@ -205,14 +211,12 @@ struct GemmProblem {
     float* zt;
     const float* lse;
     float grad_scale;
-    // kOutSoftmaxGrad (T): a factor per row [rows_a] in place of grad_scale; the
-    // rows that A and B have (0: M and N), fewer than the output, whose M and
-    // N are multiples of 128: dz of rows past them is zero, that of columns
-    // past them is left to be cleared. targets NULL: no one-hot term (nor, in
-    // kOutLseStats, a target's logit)
+    // kOutSoftmaxGradT: a factor per row [rows_a]; the rows that A and B have (0:
+    // M and N), fewer than the output, whose M and N are multiples of 128: dz of
+    // rows past them is zero, that of columns past them is left to be cleared
     const float* row_scale = nullptr;
     int64_t rows_a = 0, rows_b = 0;
-    // kOutSoftmaxGradT: the transposed copy [N, M] (row pitch ld_dzt)
+    // the transposed copy [N, M] (row pitch ld_dzt), or NULL
     uint16_t* dzt = nullptr;
     int64_t ld_dzt = 0;
     // kOutSoftmaxGradQ: dz's row-grouped codes [M, N] (ld N) with scales
@@ -227,6 +231,7 @@ struct GemmProblem {
 // Workspace the GEMM needs for split-K partial sums (0 when it runs unsplit);
 // K in bytes of an operand row (2 K for BF16 operands).
 size_t gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int out, int batch = 1);
+size_t gemm_long_k_workspace_bytes(int64_t M, int64_t N, int64_t K, int out);
 // The plan launch_gemm takes: tile, ring depth, k ranges.
 void gemm_plan(int64_t M, int64_t N, int64_t K, bool grouped, int* tile_m, int* tile_n, int* stages,
                int* splits);

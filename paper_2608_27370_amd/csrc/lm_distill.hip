@@ -293,7 +293,7 @@ Layout layout(int64_t M, int64_t V, int64_t K, int64_t k, bool bwd) {
         size_t g = 0;
         const int64_t last = V - (V - 1) / Vc * Vc;
         for (const int64_t n : {std::min(V, Vc), last}) {
-            g = std::max(g, gemm_workspace_bytes(M, K, pad128(n) * 2, kOutF32));
+            g = std::max(g, gemm_long_k_workspace_bytes(M, K, pad128(n) * 2, kOutF32));
             g = std::max(g, gemm_workspace_bytes(n, K, Mp * 2, kOutF32));
         }
         l.gemm = take(g);
@@ -330,7 +330,7 @@ void launch_lm_distill_fwd(const DistillArgs& a, float* lse, float* loss, float*
     uint8_t* const w8 = reinterpret_cast<uint8_t*>(ws);
     const Layout l = layout(a.M, a.V, a.K, a.k, false);
     top_logits_kernel<<<(unsigned)a.M, kThreads, 0, stream>>>(a.X, a.W, a.ids, a.V, a.K, (int)a.k, z_top);
-    GemmProblem g = logits(a, 0, a.V, kOutLseStats);
+    GemmProblem g = logits(a, 0, a.V, kOutLseAny);
     g.stats = reinterpret_cast<float2*>(w8 + l.stats);
     g.stats_ld = pad128(a.V) / 128;
     g.ldd = a.V;
@@ -359,7 +359,7 @@ void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* 
     if (dX) transpose_bf16(a.W, V, K, K, wt, Vp, stream, 1, 0, 0, Vp);
     for (int64_t c0 = 0; c0 < V; c0 += Vc) {
         const int64_t n = std::min(V - c0, Vc), np = pad128(n);
-        GemmProblem g = logits(a, c0, n, dW ? kOutSoftmaxGradT : kOutSoftmaxGrad);
+        GemmProblem g = logits(a, c0, n, kOutSoftmaxGradT);
         g.M = Mp; g.N = np;
         g.rows_a = M; g.rows_b = n;
         g.lse = lse;
@@ -373,7 +373,7 @@ void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* 
             zero_columns_kernel<<<blocks(Mp * (np - n)), kThreads, 0, stream>>>(dz, Mp, np, (int)n, (int)(np - n));
         if (dX) {
             GemmProblem gx{};
-            gx.M = M; gx.N = K; gx.K = np; gx.ldd = K;
+            gx.M = M; gx.N = K; gx.K = np; gx.ldd = K; gx.long_k = 1;
             if (Vc < V) { gx.out = kOutF32; gx.D = dxacc; gx.accumulate = c0 > 0; }
             else { gx.out = kOutBF16; gx.D = dX; }
             gx.A = reinterpret_cast<const uint8_t*>(dz); gx.lda = np; gx.fa = kBF16; gx.sa_mode = kSNone;

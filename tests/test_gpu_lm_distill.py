@@ -114,6 +114,14 @@ def test_wide_vocabularies(P, M, V, K, k):
     check_gradients(c, f, 1.0, np.ones(M), 1.0, dX, dW)
 
 
+def test_long_reduction(P):
+    """A vocabulary and a size of dX whose product takes the large tiles, split over the vocabulary."""
+    c = Case(15, 300, 33001, 1024, 8)
+    f, lse, loss, z_top = check_forward(P, c, 1.0)
+    dX, _ = P.lm_head_distill_bwd(*c.dev, lse, z_top, want_dw=False)
+    check_gradients(c, f, 1.0, np.ones(300), 1.0, dX, None)
+
+
 @pytest.mark.parametrize("M,V", [(16384, 90001), (30001, 131072)])
 def test_several_chunks(P, M, V):
     """dz of more than 2.5 GiB: two and three chunks of the vocabulary, the last one ragged or whole. Sampled rows of

@@ -902,7 +902,7 @@ puro_status check_distill_sizes(int64_t M, int64_t V, int64_t K, int64_t topk) {
     // BF16 operand pitches (2 M, 2 V, 2 K bytes, padded to 128 values) within 2^22
     const int64_t lim = (int64_t)1 << 21;
     if (M < 0 || V <= 0 || K <= 0 || M > lim || V > lim || K > lim) return PURO_ERR_SHAPE;
-    if (topk < 1 || topk > 1024) return PURO_ERR_SHAPE;
+    if (topk < 1 || topk > kDistillMaxTop) return PURO_ERR_SHAPE;
     if ((K % 8) != 0) return PURO_ERR_ALIGN;
     return PURO_OK;
 }

@@ -277,6 +277,8 @@ void launch_lm_head_bwd(const uint16_t* X, const uint16_t* W, const int32_t* tar
 
 // ---- LM head with a teacher's top logits (lm_distill.hip) -----------------------
 
+constexpr int kDistillMaxTop = 1024;      // entries per row
+
 struct DistillArgs {
     const uint16_t *X, *W;     // [M, K], [V, K] BF16, dense rows
     const int32_t* ids;        // [M, k]: entries outside [0, V) do not count

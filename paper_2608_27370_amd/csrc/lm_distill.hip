@@ -14,10 +14,10 @@
 // forward's GEMM reduces them to (max, sum exp) per row and 128 columns, the
 // backward recomputes them (by chunks of the vocabulary, where there are very
 // many), its GEMM writing the dense part of dz and of its transposed copy (a
-// transpose of its own moved the 5 GB of M 8192, V 151936 in 0.97 ms). What differs from a one-hot target is sparse: the k
-// logits of a row that the loss needs are k dot products, and the gradient at
-// those places is written over the dense part's, from the same formula with
-// the entry's q, in one rounding.
+// transpose of its own moved the 5 GB of M 8192, V 151936 in 0.97 ms). What
+// differs from a one-hot target is sparse: the k logits of a row that the loss
+// needs are k dot products, and the gradient at those places is written over
+// the dense part's, from the same formula with the entry's q, in one rounding.
 
 #include <math.h>
 
@@ -57,24 +57,27 @@ __global__ __launch_bounds__(kThreads) void zero_kernel(uint16_t* __restrict__ d
     if (i < n8) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// z_top[m][j] = X[m] . W[id], 0 for an entry that does not count: four waves
-// share a row, each takes kIds entries at a time, its lanes 16-byte pieces of
-// the K values (K % 8 == 0), summed in binary32 and across the wave.
+// z_top[j] = x . W[id_j] of a row's k entries, 0 for one that does not count,
+// by the four waves of a block: kIds entries at a time each, its lanes 16-byte
+// pieces of the K values (K % 8 == 0), summed in binary32 and across the wave.
+// (64 entries of 4096 rows of 1536: 805 MB of W's rows at 7.7 TB/s, from the
+// caches as far as tokens recur; in the GEMM's epilogue each lane would pick
+// them from its 64 sums by as many comparisons per entry.)
 constexpr int kIds = 4;
-__global__ __launch_bounds__(kThreads) void top_logits_kernel(const uint16_t* __restrict__ X, const uint16_t* __restrict__ W,
-                                                              const int32_t* __restrict__ ids, int64_t V, int64_t K, int k,
-                                                              float* __restrict__ z_top) {
-    const int64_t m = blockIdx.x;
+__device__ __forceinline__ void top_logits(const uint16_t* __restrict__ x, const uint16_t* __restrict__ W,
+                                           const int32_t* __restrict__ ids, int64_t V, int64_t K, int k, float* sz,
+                                           float* __restrict__ z_top) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint16_t* const x = X + m * K;
     for (int j0 = wave * kIds; j0 < k; j0 += kIds * 4) {
         const uint16_t* w[kIds];
         float s[kIds];
+        bool in[kIds];
 #pragma unroll
         for (int u = 0; u < kIds; ++u) {
-            const int id = j0 + u < k ? ids[m * k + j0 + u] : -1;
+            const int id = j0 + u < k ? ids[j0 + u] : -1;
             // (an entry that does not count reads row 0 and is dropped below)
-            w[u] = W + ((unsigned)id < (uint64_t)V ? id : 0) * K;
+            in[u] = (unsigned)id < (uint64_t)V;
+            w[u] = W + (in[u] ? id : 0) * K;
             s[u] = 0.0f;
         }
         for (int64_t c = lane * 8; c < K; c += 512) {
@@ -94,8 +97,7 @@ __global__ __launch_bounds__(kThreads) void top_logits_kernel(const uint16_t* __
 #pragma unroll
         for (int u = 0; u < kIds; ++u) {
             const float v = wave_sum(s[u]);
-            if (lane == 0 && j0 + u < k)
-                z_top[m * k + j0 + u] = (unsigned)ids[m * k + j0 + u] < (uint64_t)V ? v : 0.0f;
+            if (lane == 0 && j0 + u < k) sz[j0 + u] = z_top[j0 + u] = in[u] ? v : 0.0f;
         }
     }
 }
@@ -138,16 +140,19 @@ struct Teacher {
     }
 };
 
-// lse and loss of a row, from its blocks' (max, sum exp(a - max)) and its
-// entries: a block per row. The pairs are read once, kHold of a thread's stay in
+// lse, z_top and loss of a row, from its blocks' (max, sum exp(a - max)) and
+// its entries: a block per row. The pairs are read once, kHold of a thread's stay in
 // registers between the maximum and the sum (as many as a vocabulary of 262144
-// has; M 4096, V 151936: 13.7 us, a wave per row that read them twice 29.7). The
-// first wave then takes the entries.
+// has; M 4096, V 151936: 13.7 us, a wave per row that read them twice 29.7), their
+// loads in flight during the entries' dot products.
 constexpr int kHold = 8;
 __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const float2* __restrict__ stats, int64_t ld, int nblk,
-                                                                Teacher tch, const float* __restrict__ z_top,
-                                                                float* __restrict__ lse, float* __restrict__ loss) {
+                                                                const uint16_t* __restrict__ X,
+                                                                const uint16_t* __restrict__ W, int64_t K, Teacher tch,
+                                                                float* __restrict__ z_top, float* __restrict__ lse,
+                                                                float* __restrict__ loss) {
     __shared__ float red[8];
+    __shared__ float sz[kDistillMaxTop];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t m = blockIdx.x;
     const float2* const st = stats + m * ld;
@@ -158,6 +163,9 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const float2* __
         const int b = (int)threadIdx.x + kThreads * u;
         v[u] = b < nblk ? st[b] : make_float2(-kInf, 0.0f);
     }
+    tch.ids += m * tch.k;
+    tch.t += m * tch.k;
+    top_logits(X + m * K, W, tch.ids, tch.V, K, tch.k, sz, z_top + m * tch.k);
 #pragma unroll
     for (int u = 0; u < kHold; ++u) mx = fmaxf(mx, v[u].x);
     for (int b = (int)threadIdx.x + kThreads * kHold; b < nblk; b += kThreads) mx = fmaxf(mx, st[b].x);
@@ -178,14 +186,11 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const float2* __
     __syncthreads();
     if (wave > 0) return;
     const float l = mx + logf((red[4] + red[5]) + (red[6] + red[7]));
-    tch.ids += m * tch.k;
-    tch.t += m * tch.k;
-    z_top += m * tch.k;
     tch.begin(lane);
     float sum = 0.0f;
     for (int j = lane; j < tch.k; j += 64) {
         const float q = tch.q(j);
-        if (q != 0.0f) sum += q * (tch.log_q(j) - (z_top[j] * tch.inv_tau - l));
+        if (q != 0.0f) sum += q * (tch.log_q(j) - (sz[j] * tch.inv_tau - l));
     }
     sum = wave_sum(sum);
     if (lane == 0) {
@@ -329,14 +334,13 @@ size_t lm_distill_ws_bytes(int64_t M, int64_t V, int64_t K, int64_t k, bool bwd)
 void launch_lm_distill_fwd(const DistillArgs& a, float* lse, float* loss, float* z_top, void* ws, hipStream_t stream) {
     uint8_t* const w8 = reinterpret_cast<uint8_t*>(ws);
     const Layout l = layout(a.M, a.V, a.K, a.k, false);
-    top_logits_kernel<<<(unsigned)a.M, kThreads, 0, stream>>>(a.X, a.W, a.ids, a.V, a.K, (int)a.k, z_top);
     GemmProblem g = logits(a, 0, a.V, kOutLseAny);
     g.stats = reinterpret_cast<float2*>(w8 + l.stats);
     g.stats_ld = pad128(a.V) / 128;
     g.ldd = a.V;
     launch_gemm(g, nullptr, stream);
-    distill_rows_kernel<<<(unsigned)a.M, kThreads, 0, stream>>>(g.stats, g.stats_ld, (int)g.stats_ld, teacher_of(a), z_top,
-                                                              lse, loss);
+    distill_rows_kernel<<<(unsigned)a.M, kThreads, 0, stream>>>(g.stats, g.stats_ld, (int)g.stats_ld, a.X, a.W, a.K,
+                                                              teacher_of(a), z_top, lse, loss);
 }
 
 void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* z_top, const float* dloss, float grad_scale,

@@ -511,10 +511,12 @@ puro_status puro_lm_head_ce_bwd(const uint16_t* X, const uint16_t* W, const int3
  *     Q = sum_j q_j;  dX = dz W (BF16), dW = dz^T X (FP32 or BF16)
  * An entry whose id lies outside [0, V) (-1, say: fewer than topk are known)
  * does not count and has z_top 0; a row without entries (a padding token) has
- * loss 0 and gradient 0, and so has one whose teacher logits are all -infinity. An id
- * given twice counts twice: both q are added, which also mixes a hard target
- * into PURO_DISTILL_PROBS. A NaN among the entries that count, or a teacher
- * logit of +infinity, makes the row's loss and gradient NaN.
+ * loss 0 and gradient 0, and so has one whose teacher logits are all -infinity.
+ * A row whose dloss is 0 or whose q are all 0 adds nothing to dW and has dX 0
+ * whatever its hidden state holds, NaN included. An id given twice counts twice:
+ * both q are added, which also mixes a hard target into PURO_DISTILL_PROBS. A
+ * NaN among the entries that count, or a teacher logit of +infinity, makes the
+ * row's loss and gradient NaN.
  * No teacher beyond the entries is assumed (PROBS need not add up to 1).
  *
  * The logits are never stored (as puro_lm_head_ce_*): the forward keeps lse and

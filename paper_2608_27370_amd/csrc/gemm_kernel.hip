@@ -986,6 +986,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             constexpr float kLn2 = 0.693147180559945309f;
             constexpr float kL2eLoLn2 = kL2eLo * kLn2;
             float row_p[kDz ? FM : 1], row_k[kDz ? FM : 1], row_g[kAny ? FM : 1];
+            uint32_t row_on[kAny ? FM : 1];
             int row_tgt[kDz ? FM : 1];
             if constexpr (kDz) {
 #pragma unroll
@@ -998,6 +999,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                         row_tgt[i] = INT_MIN;
                         l = has ? p.lse[m] : 0.0f;
                         row_g[i] = has ? p.row_scale[m] : 0.0f;
+                        row_on[i] = row_g[i] != 0.0f ? ~0u : 0u;
                     } else {
                         row_tgt[i] = p.targets[m] - p.col0 - ncol0 - 4 * (lane >> 5);
                         l = p.lse[m];
@@ -1006,7 +1008,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                     row_k[i] = 1.0f - (fmaf(l, kL2eHi, -row_p[i]) + l * kL2eLo) * kLn2;
                 }
             }
-            (void)row_p; (void)row_k; (void)row_tgt; (void)row_g;
+            (void)row_p; (void)row_k; (void)row_tgt; (void)row_g; (void)row_on;
             // The bias / residual epilogue in the same one pass: the wave's
             // residual block arrives in its LDS region by DMA, each 16-byte
             // chunk already where the staged output chunk will sit (the lane
@@ -1096,7 +1098,13 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                             v2 = fmaf(rs, bf16lo(rv.y), v2); v3 = fmaf(rs, bf16hi(rv.y), v3);
                         }
                     }
-                    *pos = make_uint2(pack_bf16x2(v0, v1), pack_bf16x2(v2, v3));
+                    uint2 out2 = make_uint2(pack_bf16x2(v0, v1), pack_bf16x2(v2, v3));
+                    if constexpr (kAny) {
+                        // a row whose factor is 0 gets zeros, whatever its logits are
+                        out2.x &= row_on[kAny ? i : 0];
+                        out2.y &= row_on[kAny ? i : 0];
+                    }
+                    *pos = out2;
                 }
             };
             // Fragment row i is staged while row i - 1 leaves: after each

@@ -247,9 +247,11 @@ int gemm_tile(const GemmProblem& p);
 // one's. R, C, the pitches and the strides are multiples of 8, the pointers
 // 16-byte aligned (most callers' shapes are multiples of 128). With Rp > 0 (a
 // multiple of 8, Rp >= R) dst is [C, Rp], zeros from column R on, and R may be
-// any number.
+// any number. factor [R] (not batched): rows of src whose factor is 0 are not
+// read, zeros stand for them.
 void transpose_bf16(const uint16_t* src, int64_t R, int64_t C, int64_t lds, uint16_t* dst, int64_t ldd,
-                    hipStream_t stream, int batch = 1, int64_t bs_src = 0, int64_t bs_dst = 0, int64_t Rp = 0);
+                    hipStream_t stream, int batch = 1, int64_t bs_src = 0, int64_t bs_dst = 0, int64_t Rp = 0,
+                    const float* factor = nullptr);
 // The lower triangle of tiles of a symmetric A [R, R] (pitch ld, R a
 // multiple of 64 and of tg) from the upper one: element (i, j) = (j, i)
 // wherever i / tg > j / tg; `batch` matrices bs elements apart.

@@ -203,6 +203,8 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const float2* __
 // the factor of the dense part, and for each entry the whole gradient at its
 // place, coef exp(a - lse) - dloss g / tau * (the sum of q over all entries of
 // that id): entries of the same id have the same value, whichever is written.
+// A row whose coef is 0 (no entries, dloss 0) has no gradient: its hidden state,
+// and with it lse, may be anything.
 __global__ __launch_bounds__(64) void distill_coef_kernel(Teacher tch, const float* __restrict__ z_top,
                                                           const float* __restrict__ lse, const float* __restrict__ dloss,
                                                           float g_tau, float* __restrict__ coef, float* __restrict__ val) {
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(64) void distill_coef_kernel(Teacher tch, const flo
         const int32_t id = sid[j];
         float qs = 0.0f;
         for (int i = 0; i < tch.k; ++i) qs += sid[i] == id ? sq[i] : 0.0f;
-        val[m * tch.k + j] = c * exp_f32(z_top[m * tch.k + j] * tch.inv_tau - l) - dl * qs;
+        val[m * tch.k + j] = c == 0.0f ? 0.0f : c * exp_f32(z_top[m * tch.k + j] * tch.inv_tau - l) - dl * qs;
     }
 }
 
@@ -358,8 +360,9 @@ void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* 
     void* const gws = w8 + l.gemm;
     distill_coef_kernel<<<(unsigned)M, 64, (size_t)a.k * 8, stream>>>(teacher_of(a), z_top, lse, dloss, grad_scale / a.tau,
                                                                      coef, val);
-    // the operands whose reduction runs down their columns, zeros past the last row
-    if (dW) transpose_bf16(a.X, M, K, K, xt, Mp, stream, 1, 0, 0, Mp);
+    // the operands whose reduction runs down their columns, zeros past the last
+    // row and in rows without a gradient (whose X may hold anything)
+    if (dW) transpose_bf16(a.X, M, K, K, xt, Mp, stream, 1, 0, 0, Mp, coef);
     if (dX) transpose_bf16(a.W, V, K, K, wt, Vp, stream, 1, 0, 0, Vp);
     for (int64_t c0 = 0; c0 < V; c0 += Vc) {
         const int64_t n = std::min(V - c0, Vc), np = pad128(n);

@@ -1,6 +1,6 @@
 // RMSNorm of each query and key head with the position rotation: what the
 // forward and backward kernels (qk_norm_rope.hip) and the backward's fused
-// quantisation (quant.hip) share.
+// quantisation (qk_quant.hip) share.
 //
 // A head x of D values: n = x r gamma with r = 1 / sqrt(mean(x^2) + eps), and
 // the pairs (a, b) of its first R values turned by the position's angle:

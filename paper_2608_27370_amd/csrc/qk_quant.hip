@@ -235,7 +235,7 @@ __device__ __forceinline__ void load_qk_bwd_usual(const QkArgs& k, const Divisor
             unpack8(make_uint4(rx[i][0].x, rx[i][0].y, rx[i][1].x, rx[i][1].y), x8);
             asm volatile("" : "+v"(gw[0].x), "+v"(gw[0].y), "+v"(gw[1].x), "+v"(gw[1].y));
             unpack8(make_uint4(gw[0].x, gw[0].y, gw[1].x, gw[1].y), gm);
-const float c[4] = {u[0].x, u[0].z, u[1].x, u[1].z}, sn[4] = {u[0].y, u[0].w, u[1].y, u[1].w};
+            const float c[4] = {u[0].x, u[0].z, u[1].x, u[1].z}, sn[4] = {u[0].y, u[0].w, u[1].y, u[1].w};
             turn_pairs4(d, c, sn, true);
             norm_bwd8<L>(d, x8, gm, inv_d, k.eps, wg);
             const uint4 n = pack8(d);

@@ -13,13 +13,16 @@ constexpr int kT = 64;   // tile edge
 
 // dst [C, R] (pitch ldd) = src [R, C] (pitch lds) of problem blockIdx.z, in
 // 64 x 64 tiles; R, C and both pitches are multiples of 8 (a 16-byte chunk
-// never straddles an edge). Each thread moves two 16-byte chunks in and two
-// out; columns of dst from R up to Rp become zeros. The tile sits in LDS as 64 rows of 33 words (one padding word): a
-// wave's column reads (8 source rows x 8 columns, the lanes' chunks) then
-// fall on 32 distinct banks, two lanes sharing each word.
+// never straddles an edge). Columns of dst from R up to Rp become zeros, and
+// (SOME) those of rows whose factor is 0. Each thread moves two 16-byte chunks
+// in and two out. The tile sits in LDS as 64 rows of 33 words (one padding
+// word): a wave's column reads (8 source rows x 8 columns, the lanes' chunks)
+// then fall on 32 distinct banks, two lanes sharing each word.
+template <bool SOME>
 __global__ __launch_bounds__(256) void transpose_bf16_kernel(const uint16_t* __restrict__ src, int64_t R, int64_t C,
                                                              int64_t lds, uint16_t* __restrict__ dst, int64_t ldd,
-                                                             int64_t bs_src, int64_t bs_dst, int64_t Rp) {
+                                                             int64_t bs_src, int64_t bs_dst, int64_t Rp,
+                                                             const float* __restrict__ factor) {
     constexpr int kW = kT / 2 + 1;       // words per LDS row
     __shared__ uint32_t t[kT * kW];
     src += blockIdx.z * bs_src;
@@ -31,7 +34,7 @@ __global__ __launch_bounds__(256) void transpose_bf16_kernel(const uint16_t* __r
         const int row = q >> 3, ch = q & 7;
         const int64_t r = r0 + row, c = c0 + ch * 8;
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (r < R && c < C) v = *reinterpret_cast<const uint4*>(src + r * lds + c);
+        if (r < R && c < C && (!SOME || factor[r] != 0.0f)) v = *reinterpret_cast<const uint4*>(src + r * lds + c);
         uint32_t* w = t + row * kW + ch * 4;
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
     }
@@ -93,11 +96,13 @@ __global__ __launch_bounds__(256) void mirror_lower_bf16_kernel(uint16_t* __rest
 }  // namespace
 
 void transpose_bf16(const uint16_t* src, int64_t R, int64_t C, int64_t lds, uint16_t* dst, int64_t ldd,
-                    hipStream_t stream, int batch, int64_t bs_src, int64_t bs_dst, int64_t Rp) {
+                    hipStream_t stream, int batch, int64_t bs_src, int64_t bs_dst, int64_t Rp,
+                    const float* factor) {
     if (R <= 0 || C <= 0 || batch <= 0) return;
     if (Rp == 0) Rp = R;
     const dim3 grid((unsigned)((C + kT - 1) / kT), (unsigned)((Rp + kT - 1) / kT), (unsigned)batch);
-    transpose_bf16_kernel<<<grid, 256, 0, stream>>>(src, R, C, lds, dst, ldd, bs_src, bs_dst, Rp);
+    if (factor) transpose_bf16_kernel<true><<<grid, 256, 0, stream>>>(src, R, C, lds, dst, ldd, bs_src, bs_dst, Rp, factor);
+    else transpose_bf16_kernel<false><<<grid, 256, 0, stream>>>(src, R, C, lds, dst, ldd, bs_src, bs_dst, Rp, nullptr);
 }
 
 void mirror_lower_bf16(uint16_t* A, int64_t R, int64_t ld, int tg, hipStream_t stream, int batch, int64_t bs) {

@@ -219,6 +219,35 @@ def test_padding_rows_change_nothing(P):
     torch.testing.assert_close(dW2, dW3, rtol=0, atol=1e-5 * float(dW3.abs().max()))
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_padding_rows_may_hold_anything(P, value):
+    """Hidden states of rows without a gradient (no entries, dloss 0, probabilities 0) are never part of one."""
+    import torch
+    c = Case(9, 150, 700, 72, 5, PR, plain=True)
+    X, W, ids, t = c.dev
+    ids[3], ids[140:] = -1, -1
+    t[20] = 0
+    dloss = to_dev(c.dloss)
+    dloss[60:64] = 0
+    idle = [3, 20, *range(60, 64), *range(140, 150)]
+    lse, loss, z_top = P.lm_head_distill_fwd(X, W, ids, t, target=PR)
+    want = P.lm_head_distill_bwd(X, W, ids, t, lse, z_top, target=PR, dloss=dloss)
+    assert not want[0][idle].any()
+    bad = X.clone()
+    bad[idle] = value
+    lse2, loss2, z2 = P.lm_head_distill_fwd(bad, W, ids, t, target=PR)
+    empty = [3, 20, *range(140, 150)]
+    assert torch.isfinite(loss2[empty]).all() and not loss2[empty].any()
+    live = [i for i in range(150) if i not in idle]
+    assert torch.equal(lse[live], lse2[live]) and torch.equal(loss[live], loss2[live]) and torch.equal(z_top[live], z2[live])
+    got = P.lm_head_distill_bwd(bad, W, ids, t, lse2, z2, target=PR, dloss=dloss)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    # a NaN upstream gradient reaches every value of its row, underflowed exponentials' too
+    lse[7] += 1000
+    dloss[7] = float("nan")
+    assert torch.isnan(P.lm_head_distill_bwd(X, W, ids, t, lse, z_top, target=PR, dloss=dloss)[1]).all()
+
+
 @pytest.mark.parametrize("kind,value", [(L, np.nan), (L, np.inf), (PR, np.nan)])
 def test_special_values_stay_in_their_row(P, kind, value):
     import torch

@@ -274,7 +274,7 @@ puro_status puro_rmsnorm_quantize_fp8(const uint16_t* x, const uint16_t* gamma, 
  * outside the table.
  *
  * head_dim: a multiple of 8 from 8 to 256. heads_q and heads_k (heads_k also
- * counts the value heads of the backward): at most 65535; batch * seq < 2^31.
+ * counts the value heads of the backward): at most 65535; batch * seq at most 2^25.
  * batch * seq = 0 is a valid empty call. gamma_q, gamma_k: BF16 [head_dim],
  * 16-byte aligned. eps finite and >= 0 (with eps = 0 a head of zeros gives
  * NaN, as the formula does); heads whose sum of squares overflows binary32
@@ -293,7 +293,8 @@ typedef struct {
 
 /* The table of angles p * theta^(-2 i / dim), position p in [0, len), pair
  * i < dim / 2: computed in double precision, rounded to binary32. dim a
- * multiple of 16 (0: nothing is written) up to 256, len < 2^31, theta > 0 and finite. */
+ * multiple of 16 (0: nothing is written) up to 256, len < 2^31 of at most 2^31
+ * pairs in all, theta > 0 and finite. */
 puro_status puro_rope_table(float* table, int64_t len, int dim, double theta, hipStream_t stream);
 
 puro_status puro_qk_norm_rope_fwd(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim,
@@ -330,7 +331,7 @@ puro_status puro_qk_norm_rope_bwd(int64_t batch, int64_t seq, int heads_q, int h
  * requirements (rows = batch * seq, cols = the heads' width); BLOCK_128x128 is
  * PURO_ERR_UNSUPPORTED, and so is a head_dim other than 64 and 128 (a 128-column
  * tile then holds no whole heads: use the call above and puro_quantize_fp8).
- * dv is required when heads_k > 0. ws: its *_workspace_size bytes, 16-byte
+ * batch * seq is at most 2^22 here; dv is required when heads_k > 0. ws: its *_workspace_size bytes, 16-byte
  * aligned (needed in TENSOR mode and for dgamma). */
 size_t puro_qk_norm_rope_bwd_quantize_workspace_size(int64_t batch, int64_t seq, int heads_q, int heads_k,
                                                      int head_dim);

@@ -319,6 +319,9 @@ puro_status puro_rmsnorm_quantize_fp8(const uint16_t* x, const uint16_t* gamma, 
 namespace {
 
 constexpr int kMaxHeadDim = 256;
+// Tokens of a call: a launch holds fewer than 2^32 threads (the forward has a
+// wave per token) and at most 65535 block rows (the quantiser's, of 128 tokens).
+constexpr int64_t kMaxTokens = (int64_t)1 << 25, kMaxTokensQuant = (int64_t)1 << 22;
 
 bool finite_nonneg(float v) { return v >= 0.0f && v <= 3.4028235e38f; }
 
@@ -326,7 +329,7 @@ bool finite_nonneg(float v) { return v >= 0.0f && v <= 3.4028235e38f; }
 puro_status check_qk_sizes(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim, int64_t* tokens) {
     if (batch < 0 || seq < 0 || heads_q < 0 || heads_k < 0) return PURO_ERR_SHAPE;
     if (heads_q > 65535 || heads_k > 65535) return PURO_ERR_SHAPE;
-    if (batch > INT32_MAX || seq > INT32_MAX || batch * seq > INT32_MAX) return PURO_ERR_SHAPE;
+    if (batch > INT32_MAX || seq > INT32_MAX || batch * seq > kMaxTokens) return PURO_ERR_SHAPE;
     if (head_dim < 8 || head_dim > kMaxHeadDim) return PURO_ERR_SHAPE;
     if ((head_dim % 8) != 0) return PURO_ERR_ALIGN;
     *tokens = batch * seq;
@@ -418,6 +421,7 @@ puro_status puro_rope_table(float* table, int64_t len, int dim, double theta, hi
     if (len < 0 || len > INT32_MAX || dim < 0 || dim > kMaxHeadDim) return PURO_ERR_SHAPE;
     if ((dim % 16) != 0) return PURO_ERR_ALIGN;
     if (!(theta > 0.0) || !(theta <= 1.7976931348623157e308)) return PURO_ERR_UNSUPPORTED;
+    if (len * (dim / 2) > (int64_t)1 << 31) return PURO_ERR_SHAPE;
     if (len == 0 || dim == 0) return PURO_OK;
     if (!table) return PURO_ERR_NULL;
     if (!aligned16(table)) return PURO_ERR_ALIGN;
@@ -496,6 +500,7 @@ puro_status puro_qk_norm_rope_bwd_quantize_fp8(int64_t batch, int64_t seq, int h
     puro_status st = check_qk(batch, seq, heads_q, heads_k, head_dim, q, k, gamma_q, gamma_k, eps, rope, true, &a);
     if (st != PURO_OK) return st;
     if (head_dim != 64 && head_dim != 128) return PURO_ERR_UNSUPPORTED;
+    if (a.tokens > kMaxTokensQuant) return PURO_ERR_SHAPE;
     if ((st = check_heads(dq, batch, seq, heads_q, head_dim, false, &a.dq)) != PURO_OK) return st;
     if ((st = check_heads(dk, batch, seq, heads_k, head_dim, false, &a.dk)) != PURO_OK) return st;
     if ((st = check_heads(dv, batch, seq, heads_k, head_dim, false, &a.dv)) != PURO_OK) return st;

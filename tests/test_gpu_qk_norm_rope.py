@@ -399,6 +399,28 @@ def test_large_offsets(P):
     check_forward(P, c, q_out=q, k_out=k)
 
 
+def test_most_tokens(P):
+    """The largest call, 2^25 tokens of one head of 8 (a wave each forward); first, last and drawn tokens against the
+    formula in float64. Errors: one rounding to BF16 (2^-8 relative) and a few of 2^-24 of the terms' sizes."""
+    import torch
+    n, D = 1 << 25, 8
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, dy = (torch.randn(n, 1, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    gamma = torch.randn(D, generator=g, device="cuda").to(torch.bfloat16)
+    none = x[:, :0]
+    y, _ = P.qk_norm_rope_fwd(x, none, gamma_q=gamma)
+    dx = P.qk_norm_rope_bwd(dy, none, none, x, none, gamma_q=gamma, want_dgamma=False)[0]
+    at = torch.cat((torch.arange(1000, device="cuda"), torch.arange(n - 1000, n, device="cuda"),
+                    torch.randint(0, n, (100000,), generator=g, device="cuda")))
+    xs, ds, gm = x[at, 0].double(), dy[at, 0].double(), gamma.double()
+    r = 1 / (xs.square().mean(1, keepdim=True) + 1e-6).sqrt()
+    h, gg = xs * r, ds * gm
+    ref = h * gm
+    assert ((y[at, 0].double() - ref).abs() <= ref.abs() * (2.0 ** -8 + 2.0 ** -18)).all()
+    ref, size = r * (gg - h * (gg * h).mean(1, keepdim=True)), r * (gg.abs() + h.abs() * (gg * h).abs().mean(1, keepdim=True))
+    assert ((dx[at].double() - ref).abs() <= ref.abs() * 2.0 ** -8 + size * 2.0 ** -18).all()
+
+
 # ----------------------------------------------------------- streams and graphs
 def test_graph_replays_and_another_stream(P):
     """Captured forward and backwards, replayed on changed inputs, against eager calls in between; one workspace per

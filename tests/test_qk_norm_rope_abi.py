@@ -97,6 +97,17 @@ def test_sizes_and_empty_calls(call, puro):  # noqa: F811
         assert call("quant", mode=1, rnd=1, dgq=None, dgk=None, ws=None, nb=0, q8=None, scale=None, **size, **none) == OK
 
 
+def test_largest_calls(call, puro):  # noqa: F811
+    """More tokens than a launch takes are refused, not left to the launch to fail."""
+    L = puro.lib()
+    far = dict(rope=(FAKE, 16, 64, 0, FAKE))
+    for which in ("fwd", "bwd"):
+        assert call(which, batch=1, seq=(1 << 25) + 1, **far) == ERR_SHAPE
+    assert call("quant", batch=1, seq=(1 << 22) + 16, **far) == ERR_SHAPE
+    assert L.puro_qk_norm_rope_bwd_workspace_size(1, 1 << 25, 64) > 0 == L.puro_qk_norm_rope_bwd_workspace_size(1, (1 << 25) + 1, 64)
+    assert L.puro_rope_table(FAKE, 1 << 28, 128, 1e4, None) == ERR_SHAPE
+
+
 def test_table(puro):  # noqa: F811
     f = puro.lib().puro_rope_table
     assert f(FAKE, -1, 64, 1e4, None) == f(FAKE, 1 << 31, 64, 1e4, None) == f(FAKE, 4, 272, 1e4, None) == ERR_SHAPE

@@ -5,7 +5,9 @@
 // byte leave them bound by memory. A wave takes one token and walks its heads
 // (64 / L at a time, L lanes a head), so that the position's cosines and sines
 // are loaded once per token instead of once per head: as binary32 they are
-// four times the size of a head's own BF16 values.
+// four times the size of a head's own BF16 values. 8192 tokens of 16 + 8 heads
+// of 128: forward 18 to 19 us for 103 MB (5.4 TB/s; a large copy reaches 5.15),
+// backward 34 us for 187 MB (5.4) and 4 for the sum of dgamma; one token 2.5 us.
 
 #include <algorithm>
 

@@ -8,7 +8,7 @@
 // exchange its pairs and its sums by lane moves. Bound by memory: 4 bytes read
 // and 1 byte a copy written per query and key value, 2 and 1 per value head's.
 // 8192 tokens of 16 + 8 heads of 128, E4M3 rows and columns: 50 us for 187 MB
-// (3.7 TB/s; the BF16 backward and the quantiser one after the other move 337 MB).
+// (3.7 TB/s; the BF16 backward and the quantiser one after the other move 321 MB).
 // 166 registers let three blocks share a CU, and each of them loads, computes
 // and stores its one tile in that order: 2048 tiles are 2.7 rounds of the chip.
 

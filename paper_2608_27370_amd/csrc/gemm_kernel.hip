@@ -398,6 +398,9 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     const int T = gridDim.x;
     const int b = blockIdx.x;
     int lt = (T % 8 == 0) ? (b % 8) * (T / 8) + b / 8 : b;
+    // (the distillation loss's kinds: any number of tiles, the first T % 8 XCDs one
+    // more; a backward whose logits have 788 tiles, 431 -> 425 us)
+    if constexpr (OUT == kOutSoftmaxGradT || OUT == kOutLseAny) lt = (b % 8) * (T / 8) + min(b % 8, T % 8) + b / 8;
     // (divisions by host-made multipliers, skipped where the quotient is
     // zero: integer division is a long dependent chain, and a tile's first
     // loads wait for this index; a symmetric product has only the tiles on or
@@ -1464,6 +1467,11 @@ void launch_tile(const Params& prm, int out, int grid, hipStream_t stream) {
 
 template <int FA, int FB, bool GROUPED>
 void launch_variant(const Params& prm, int cfg, int out, int grid, hipStream_t stream) {
+    if constexpr (FA == kBF16 && FB == kBF16 && !GROUPED) {
+        constexpr TileCfg d = kLseTiles[0], e = kLseTiles[1];
+        if (cfg == kLseDeep) return launch_cfg<d.bm, d.bn, d.wm, d.wn, d.sl, d.nst, 0, 0, FA, FB, GROUPED, kOutLseAny>(prm, grid, stream);
+        if (cfg == kLsePair) return launch_cfg<e.bm, e.bn, e.wm, e.wn, e.sl, e.nst, 0, 0, FA, FB, GROUPED, kOutLseAny>(prm, grid, stream);
+    }
 #define PURO_TILE_CASE(i, bm, bn, wm, wn, sl, nst, xa, prod, f, s, g) \
     case i: launch_tile<bm, bn, wm, wn, sl, nst, xa, prod, FA, FB, GROUPED>(prm, out, grid, stream); break;
     switch (cfg) { PURO_TILE_LIST(PURO_TILE_CASE) }

@@ -114,6 +114,13 @@ def test_wide_vocabularies(P, M, V, K, k):
     check_gradients(c, f, 1.0, np.ones(M), 1.0, dX, dW)
 
 
+# one tile of 128 x 128 a CU (256 of them) and one more, two a CU (512) and more, up to 128 rows and more of them
+@pytest.mark.parametrize("M,V,K", [(129, 16384, 24), (257, 10900, 72), (128, 32769, 8), (255, 32768, 16), (256, 32769, 136),
+                                   (100, 65601, 16)])
+def test_tiles_of_the_forward(P, M, V, K):
+    check_forward(P, Case(M + K, M, V, K, 6), 1.5)
+
+
 def test_long_reduction(P):
     """A vocabulary and a size of dX whose product takes the large tiles, split over the vocabulary."""
     c = Case(15, 300, 33001, 1024, 8)

@@ -352,9 +352,11 @@ def _rope_args(rope, positions, tokens, device):
     n, half, two = t.shape
     if two != 2 or not t.is_contiguous():
         raise ValueError("the rotation's table is a contiguous [length, dim / 2, 2] tensor")
-    _check_tensor(t, "table", _FP32, device)
+    if t.dtype != torch.float32 or t.get_device() != device:
+        _check_tensor(t, "table", _FP32, device)
     if positions is not None:
-        _check_tensor(positions, "positions", _INT32, device)
+        if positions.dtype != torch.int32 or positions.get_device() != device:
+            _check_tensor(positions, "positions", _INT32, device)
         if positions.numel() != tokens or not positions.is_contiguous():
             raise ValueError("positions: one for each of the %d tokens, contiguous" % tokens)
         positions = positions.data_ptr()
@@ -367,10 +369,16 @@ def _heads(t, what, shape, device):
         raise ValueError("%s: shape %s expected, got %s" % (what, tuple(shape), tuple(t.shape)))
     if t.dtype not in _BF16_BITS or t.get_device() != device:
         _check_tensor(t, what, _BF16_BITS, device)
-    st = t.stride()
-    if st[-1] != 1 and t.numel() > 0 and shape[-1] > 1:
+    *batch, row, head, one = t.stride()
+    if one != 1 and t.numel() > 0 and shape[-1] > 1:
         raise ValueError("%s: the values of a head are contiguous" % what)
-    return Heads(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
+    return Heads(t.data_ptr(), batch[0] if batch else 0, row, head)
+
+
+def _new_heads(like, seq, heads, d):
+    """A new contiguous tensor of the shape of `like`, and its Heads."""
+    t = torch.empty_like(like, memory_format=torch.contiguous_format)
+    return t, Heads(t.data_ptr(), seq * heads * d, heads * d, d)
 
 
 def _qk_sizes(q, k):
@@ -380,15 +388,18 @@ def _qk_sizes(q, k):
         a, b = (1, *a), (1, *b)
     if len(a) != 4 or len(b) != 4:
         raise ValueError("heads are [S, H, D] or [B, S, H, D], both kinds alike")
-    if a[0] != b[0] or a[1] != b[1] or a[3] != b[3]:
+    batch, seq, hq, d = a
+    batch_k, seq_k, hk, d_k = b
+    if batch != batch_k or seq != seq_k or d != d_k:
         raise ValueError("q %s and k %s differ in more than their heads" % (tuple(q.shape), tuple(k.shape)))
-    return a[0], a[1], a[2], b[2], a[3]
+    return batch, seq, hq, hk, d
 
 
 def _gamma(g, what, d, device):
     if g is None:
         return None
-    _check_tensor(g, what, _BF16_BITS, device)
+    if g.dtype not in _BF16_BITS or g.get_device() != device:
+        _check_tensor(g, what, _BF16_BITS, device)
     if g.numel() != d or not g.is_contiguous():
         raise ValueError("%s: %d contiguous values" % (what, d))
     return g.data_ptr()
@@ -402,12 +413,11 @@ def qk_norm_rope_fwd(q, k, gamma_q=None, gamma_k=None, rope=None, positions=None
     batch, seq, hq, hk, d = _qk_sizes(q, k)
     dev = _current()
     a, b = _heads(q, "q", q.shape, dev), _heads(k, "k", k.shape, dev)
-    q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
-    k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
+    q_out, aq = _new_heads(q, seq, hq, d) if q_out is None else (q_out, _heads(q_out, "q_out", q.shape, dev))
+    k_out, ak = _new_heads(k, seq, hk, d) if k_out is None else (k_out, _heads(k_out, "k_out", k.shape, dev))
     _check("puro_qk_norm_rope_fwd", lib().puro_qk_norm_rope_fwd(
         batch, seq, hq, hk, d, a, b, _gamma(gamma_q, "gamma_q", d, dev), _gamma(gamma_k, "gamma_k", d, dev), eps,
-        _rope_args(rope, positions, batch * seq, dev), _heads(q_out, "q_out", q.shape, dev),
-        _heads(k_out, "k_out", k.shape, dev), _stream()))
+        _rope_args(rope, positions, batch * seq, dev), aq, ak, _stream()))
     return q_out, k_out
 
 
@@ -417,10 +427,9 @@ def _dgamma(gamma, want, d, device):
 
 def _qk_grads(dq, dk, dv, q, k, gamma_q, gamma_k, rope, positions, eps, sizes, dev):
     """The leading arguments of both backward calls."""
-    d = sizes[4]
-    return (*sizes, _heads(dq, "dq", dq.shape, dev), _heads(dk, "dk", dk.shape, dev),
-            _heads(dv, "dv", dk.shape, dev) if dv is not None else None, _heads(q, "q", dq.shape, dev),
-            _heads(k, "k", dk.shape, dev), _gamma(gamma_q, "gamma_q", d, dev), _gamma(gamma_k, "gamma_k", d, dev), eps,
+    d, sq, sk = sizes[4], dq.shape, dk.shape
+    return (*sizes, _heads(dq, "dq", sq, dev), _heads(dk, "dk", sk, dev),
+            _heads(dv, "dv", sk, dev) if dv is not None else None, _heads(q, "q", sq, dev), _heads(k, "k", sk, dev), _gamma(gamma_q, "gamma_q", d, dev), _gamma(gamma_k, "gamma_k", d, dev), eps,
             _rope_args(rope, positions, sizes[0] * sizes[1], dev))
 
 
@@ -434,11 +443,13 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, gamma_q=None, gamma_k=None, rope=None, po
     args = _qk_grads(dq, dk, dv, q, k, gamma_q, gamma_k, rope, positions, eps, sizes, dev)
     tokens, width = batch * seq, (hq + (2 if dv is not None else 1) * hk) * d
     if out is None:
-        out = torch.empty(tokens, width, dtype=dq.dtype, device=dq.device)
-    elif tuple(out.shape) != (tokens, width):
-        raise ValueError("out: shape %s expected, got %s" % ((tokens, width), tuple(out.shape)))
-    _check_tensor(out, "out", _BF16_BITS, dev)
-    ld, at = _ld(out), out.data_ptr()
+        out, ld = dq.new_empty(tokens, width), width
+    else:
+        if out.shape != (tokens, width):
+            raise ValueError("out: shape %s expected, got %s" % ((tokens, width), tuple(out.shape)))
+        _check_tensor(out, "out", _BF16_BITS, dev)
+        ld = _ld(out)
+    at = out.data_ptr()
     dgq, dgk = _dgamma(gamma_q, want_dgamma, d, dq.device), _dgamma(gamma_k, want_dgamma, d, dq.device)
     nb = 0
     if dgq is not None or dgk is not None:
@@ -756,17 +767,19 @@ def lm_head_distill_workspace_size(M, V, K, topk, backward):
 
 
 def _dense(t, what, dtypes, shape, device):
-    _check_tensor(t, what, dtypes, device)
-    if tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype not in dtypes or t.get_device() != device:
+        _check_tensor(t, what, dtypes, device)
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: a contiguous %s tensor expected, got %s" % (what, shape, tuple(t.shape)))
     return t.data_ptr()
 
 
 def _distill_args(X, W, ids, teacher, dev):
     """Sizes and the pointers of the inputs that both passes take."""
-    if X.dim() != 2 or W.dim() != 2 or ids.dim() != 2:
+    x, w, i = X.shape, W.shape, ids.shape
+    if len(x) != 2 or len(w) != 2 or len(i) != 2:
         raise ValueError("X [M, K], W [V, K], ids and teacher [M, topk]")
-    (M, K), V, k = X.shape, W.shape[0], ids.shape[1]
+    (M, K), V, k = x, w[0], i[1]
     return M, V, K, k, (_dense(X, "X", _BF16_BITS, (M, K), dev), _dense(W, "W", _BF16_BITS, (V, K), dev),
                         _dense(ids, "ids", _INT32, (M, k), dev), _dense(teacher, "teacher", _FP32, (M, k), dev))
 
@@ -778,8 +791,8 @@ def lm_head_distill_fwd(X, W, ids, teacher, temperature=1.0, target=DISTILL_LOGI
     Returns (lse, loss, z_top): [M], [M] and the student's logits [M, topk]; the logits X W^T are never stored."""
     dev = _current()
     M, V, K, k, inputs = _distill_args(X, W, ids, teacher, dev)
-    new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=X.device)      # noqa: E731
-    lse, loss, z_top = new(M) if lse is None else lse, new(M) if loss is None else loss, new(M, k) if z_top is None else z_top
+    lse, loss, z_top = (teacher.new_empty(*shape) if t is None else t
+                        for t, shape in ((lse, (M,)), (loss, (M,)), (z_top, (M, k))))
     w, nb = _ws(lm_head_distill_workspace_size(M, V, K, k, False), ws, X.device)
     _check("puro_lm_head_distill_fwd", lib().puro_lm_head_distill_fwd(
         *inputs, M, V, K, k, target, temperature, _dense(lse, "lse", _FP32, (M,), dev), _dense(loss, "loss", _FP32, (M,), dev),

@@ -219,7 +219,7 @@ bool grouped_scales(const GemmProblem& g) {
 }
 
 void run_plan(const GemmProblem& g, const Plan& pl, void* ws, hipStream_t stream) {
-    const TileCfg t = pl.cfg >= kLseDeep ? kLseTiles[pl.cfg - kLseDeep] : kTiles[pl.cfg];
+    const TileCfg t = pl.cfg >= kLmDeep ? kLmTiles[pl.cfg - kLmDeep] : kTiles[pl.cfg];
     // the kernel walks k in bytes of an operand row
     const int eb = elem_bytes(g);
     Params prm{};
@@ -336,16 +336,18 @@ void gemm_plan(int64_t M, int64_t N, int64_t K, bool grouped, int* tile_m, int* 
     *splits = p.splits;
 }
 
-// The distillation forward's tiles: 256 x 256, or 128 x 128 where those leave CUs
+// The distillation logits' tiles: 256 x 256, or 128 x 128 where those leave CUs
 // idle. A wave of the large tile holds 256 sums a lane, whose products and
 // exponentials alone take 20 to 40 us (K 512, 1536). Whole forward, large against
 // small tiles: 77 rows, V 5003, K 1536 40.8 -> 23.8 us; 300 rows, V 16000 39.6 ->
 // 33.6 (two workgroups a CU; one, with the deep ring, 36.9); one row, V 151936 124
 // -> 98 (up to 128 rows the large tile is half empty; two a CU 106). More than
-// two tiles a CU lose: 256 rows, V 151936 146 -> 197.
-static int lse_cfg(int64_t M, int64_t N) {
+// two tiles a CU lose: 256 rows, V 151936 146 -> 197. Whole backward: 77 rows,
+// V 5003, K 1536 72 -> 54 us; 300 rows, V 16000 141 -> 130; one row, V 151936 646 ->
+// 623; 1500 rows, V 4000 107 -> 96.
+static int lm_cfg(int64_t M, int64_t N) {
     const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128);
-    return tiles <= kCUs ? kLseDeep : tiles <= 2 * kCUs ? kLsePair : M <= 128 ? kLseDeep : 0;
+    return tiles <= kCUs ? kLmDeep : tiles <= 2 * kCUs ? kLmPair : M <= 128 ? kLmDeep : 0;
 }
 
 static bool lm_head_kind(int out) {
@@ -357,8 +359,8 @@ void launch_gemm(const GemmProblem& g, void* ws, hipStream_t stream) {
     const int64_t kb = g.K * elem_bytes(g);
     if (lm_head_kind(g.out)) {
         // the LM-head epilogues reduce over 128-column wave tiles: the
-        // 256 x 256 configuration (or the ones of lse_cfg), unsplit
-        run_plan(g, Plan{g.out == kOutLseAny ? lse_cfg(g.M, g.N) : 0, 1, (int)((kb + kBK - 1) / kBK)}, ws, stream);
+        // 256 x 256 configuration (or the ones of lm_cfg), unsplit
+        run_plan(g, Plan{g.out == kOutLseAny || g.out == kOutSoftmaxGradT ? lm_cfg(g.M, g.N) : 0, 1, (int)((kb + kBK - 1) / kBK)}, ws, stream);
         return;
     }
     Plan pl;

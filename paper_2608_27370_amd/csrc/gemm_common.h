@@ -116,10 +116,10 @@ struct TileCfg {
     X(5, 256, 128, 2, 2, 128, 2, 3, 0, 6.577f, 0.7372f, 1.20f)
 #define PURO_TILE_ROW(i, bm, bn, wm, wn, sl, nst, xa, prod, f, s, g) {bm, bn, wm, wn, sl, nst, xa, prod, f, s, g},
 
-// The distillation forward's small tiles, beside the list (lse_cfg in gemm.hip):
+// The distillation loss's small tiles, beside the list (lm_cfg in gemm.hip):
 // four waves of 32 x 128, a ring of four slices or, two workgroups a CU, of two.
-constexpr int kLseDeep = 6, kLsePair = 7;
-constexpr TileCfg kLseTiles[] = {{128, 128, 4, 1, 128, 4, 0, 0, 0.0f, 0.0f, 0.0f}, {128, 128, 4, 1, 128, 2, 0, 0, 0.0f, 0.0f, 0.0f}};
+constexpr int kLmDeep = 6, kLmPair = 7;
+constexpr TileCfg kLmTiles[] = {{128, 128, 4, 1, 128, 4, 0, 0, 0.0f, 0.0f, 0.0f}, {128, 128, 4, 1, 128, 2, 0, 0, 0.0f, 0.0f, 0.0f}};
 
 constexpr int kLdsBytes = 160 * 1024;
 // LDS bytes of a configuration with xa spare A units, and the spare units

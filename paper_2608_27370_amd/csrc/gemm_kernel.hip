@@ -340,6 +340,28 @@ __device__ __forceinline__ void store_transposed_dz(const P& p, uint8_t* ep, int
     }
 }
 
+// The same of a 128 x 128 tile that four waves staged, 32 rows each (row r of the
+// tile at base + (r >> 5) region + 256 (r & 31)): wave w takes chunks 4 w .. 4 w + 3
+// of all rows, a lane one 8 x 8 block, which leaves from its registers (a column's
+// 128 values from sixteen lanes). Called when all waves have staged their rows.
+template <class P>
+__device__ __forceinline__ void store_transposed_dz32(const P& p, const uint8_t* base, int region, int64_t mrow0, int64_t ncol0,
+                                                      int wave, int lane) {
+    typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+    const int b = lane & 15, cb = wave * 4 + (lane >> 4);
+    uint32_t w[8][4], t[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = b * 8 + i;
+        const v4u v = *reinterpret_cast<const v4u*>(base + (r >> 5) * region + (r & 31) * 256 + ((cb ^ (r & 15)) << 4));
+        w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
+    }
+    transpose8x8_b16(w, t);
+    uint16_t* const out = p.dzt + (ncol0 + cb * 8) * p.ld_dzt + mrow0 + b * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) *reinterpret_cast<v4u*>(out + j * p.ld_dzt) = v4u{t[j][0], t[j][1], t[j][2], t[j][3]};
+}
+
 // PROD: the workgroup has NW more waves that only issue the global->LDS
 // loads (producers); the NW MFMA waves (consumers) then only read LDS and
 // multiply, so a load that cannot issue (the texture unit's queue full)
@@ -975,7 +997,8 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     // kOutSoftmaxGradQ quantises the staged tile (below).
     constexpr bool kAny = OUT == kOutSoftmaxGradT;
     constexpr bool kDz = OUT == kOutSoftmaxGrad || OUT == kOutSoftmaxGradQ || OUT == kOutSoftmaxGradT;
-    static_assert(!kDz || (ECPR == 32 && WTM == 128 && WTM * 256 <= REGION), "dz kinds: 128 x 128 wave tiles");
+    constexpr bool kDz32 = kAny && BM == 128 && BN == 128 && WTM == 32;     // four waves of 32 x 128
+    static_assert(!kDz || (ECPR == 32 && (WTM == 128 || kDz32) && WTM * 256 <= REGION), "dz kinds: 128 x 128 wave tiles");
     if constexpr ((OUT == kOutBF16 || OUT == kOutBF16Epi || kDz) && ECPR == 32 && WTM * 256 <= REGION) {
         if constexpr (kDz) {
             if (mrow0 + WTM > p.M || ncol0 + WTN > p.N) return;
@@ -1186,7 +1209,12 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                 const __attribute__((address_space(4))) Params* kp =
                     (const __attribute__((address_space(4))) Params*)__builtin_amdgcn_kernarg_segment_ptr();
                 asm volatile("" : "+s"(kp));
-                if (kp->dzt) store_transposed_dz(*kp, ep, mrow0, ncol0, lane);
+                if constexpr (kDz32) {
+                    __syncthreads();     // (M and N are whole tiles: no wave has left)
+                    if (kp->dzt) store_transposed_dz32(*kp, smem, REGION, m0, n0, wave, lane);
+                } else {
+                    if (kp->dzt) store_transposed_dz(*kp, ep, mrow0, ncol0, lane);
+                }
             }
             return;
         }
@@ -1468,9 +1496,17 @@ void launch_tile(const Params& prm, int out, int grid, hipStream_t stream) {
 template <int FA, int FB, bool GROUPED>
 void launch_variant(const Params& prm, int cfg, int out, int grid, hipStream_t stream) {
     if constexpr (FA == kBF16 && FB == kBF16 && !GROUPED) {
-        constexpr TileCfg d = kLseTiles[0], e = kLseTiles[1];
-        if (cfg == kLseDeep) return launch_cfg<d.bm, d.bn, d.wm, d.wn, d.sl, d.nst, 0, 0, FA, FB, GROUPED, kOutLseAny>(prm, grid, stream);
-        if (cfg == kLsePair) return launch_cfg<e.bm, e.bn, e.wm, e.wn, e.sl, e.nst, 0, 0, FA, FB, GROUPED, kOutLseAny>(prm, grid, stream);
+        constexpr TileCfg d = kLmTiles[0], e = kLmTiles[1];
+        auto small = [&](auto kind) {
+            constexpr int OUT = decltype(kind)::value;
+            if (cfg == kLmDeep) launch_cfg<d.bm, d.bn, d.wm, d.wn, d.sl, d.nst, 0, 0, FA, FB, GROUPED, OUT>(prm, grid, stream);
+            else launch_cfg<e.bm, e.bn, e.wm, e.wn, e.sl, e.nst, 0, 0, FA, FB, GROUPED, OUT>(prm, grid, stream);
+        };
+        if (cfg >= kLmDeep) {
+            if (out == kOutLseAny) small(std::integral_constant<int, kOutLseAny>{});
+            else small(std::integral_constant<int, kOutSoftmaxGradT>{});
+            return;
+        }
     }
 #define PURO_TILE_CASE(i, bm, bn, wm, wn, sl, nst, xa, prod, f, s, g) \
     case i: launch_tile<bm, bn, wm, wn, sl, nst, xa, prod, FA, FB, GROUPED>(prm, out, grid, stream); break;

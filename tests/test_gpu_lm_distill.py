@@ -121,6 +121,15 @@ def test_tiles_of_the_forward(P, M, V, K):
     check_forward(P, Case(M + K, M, V, K, 6), 1.5)
 
 
+# the same of the backward's logits: one tile a CU, two, and up to 128 rows of more
+@pytest.mark.parametrize("M,V,K", [(255, 1000, 72), (300, 11000, 40), (513, 6500, 16), (128, 65601, 8)])
+def test_tiles_of_the_backward(P, M, V, K):
+    c = Case(M + V, M, V, K, 6)
+    f, lse, loss, z_top = check_forward(P, c, 1.5)
+    dX, dW = P.lm_head_distill_bwd(*c.dev, lse, z_top, temperature=1.5, dloss=to_dev(c.dloss))
+    check_gradients(c, f, 1.5, c.dloss.astype(np.float64), 1.0, dX, dW)
+
+
 def test_long_reduction(P):
     """A vocabulary and a size of dX whose product takes the large tiles, split over the vocabulary."""
     c = Case(15, 300, 33001, 1024, 8)

@@ -464,7 +464,10 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     const int s0 = ks * p.ksteps_per_split;
     const int s1 = min((ks + 1) * p.ksteps_per_split, p.ksteps);
 
-    const int valid_m = min(BM, p.rows_a - m0), valid_n = min(BN, p.rows_b - n0);
+    // (only kOutSoftmaxGradT's operands have fewer rows than the output: two more
+    // scalar loads here, ahead of a tile's first vector loads, are its alone)
+    constexpr bool kFewer = OUT == kOutSoftmaxGradT;
+    const int valid_m = min(BM, (kFewer ? p.rows_a : p.M) - m0), valid_n = min(BN, (kFewer ? p.rows_b : p.N) - n0);
     const v4i ra = make_rsrc(p.A + (int64_t)m0 * p.lda, (uint32_t)(valid_m * p.lda));
     const v4i rb = make_rsrc(p.B + (int64_t)n0 * p.ldb, (uint32_t)(valid_n * p.ldb));
 

@@ -308,11 +308,12 @@ puro_status puro_qk_norm_rope_fwd(int64_t batch, int64_t seq, int heads_q, int h
  * dn the gradient turned back, r = 1 / sqrt(mean(x^2) + eps), h = x r,
  * g = dn gamma:  dx = r (g - h mean(g h)).  dgamma_q, dgamma_k (FP32
  * [head_dim], overwritten, either NULL: not wanted) = the sums over tokens and
- * heads of dn h, in binary32 in a fixed order. dv, dv_in (both or neither):
- * the value heads' gradients, copied, so that one call assembles the gradient
- * of the projection's output. The statistics are recomputed from the heads,
- * which the call reads anyway: nothing is kept from the forward but its
- * inputs. ws: the matching *_workspace_size bytes (for dgamma; 16-byte aligned). */
+ * heads of dn h, in a fixed order, in binary32 and, beyond 64 additions in a
+ * row, in binary64. dv, dv_in (both or neither): the value heads' gradients,
+ * copied, so that one call assembles the gradient of the projection's output.
+ * The statistics are recomputed from the heads, which the call reads anyway:
+ * nothing is kept from the forward but its inputs. ws: the matching
+ * *_workspace_size bytes (for dgamma; 16-byte aligned). */
 size_t puro_qk_norm_rope_bwd_workspace_size(int64_t batch, int64_t seq, int head_dim);
 puro_status puro_qk_norm_rope_bwd(int64_t batch, int64_t seq, int heads_q, int heads_k, int head_dim,
                                   const puro_heads* dq, const puro_heads* dk, const puro_heads* dv,

@@ -94,13 +94,21 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Di
     }
 }
 
+// Sums of dgamma: a binary32 sum of n terms of one sign is off by up to n / 2
+// units in the last place (2^20 tokens of 16 heads of 128 are 1366 a lane), so
+// after kDeep additions it moves to a binary64 one, rounded once at the end.
+// (Fewer terms never leave binary32; 8192 tokens of 16 + 8 heads: 6 a lane.)
+constexpr int kDeep = 64;
+
 // Backward: wave w takes tokens w, w + waves, ..; every lane keeps the sums of
-// dgamma of its eight columns in binary32, the block adds them up in a fixed
-// order and writes part[kind][block][D].
+// dgamma of its eight columns in binary32 (the long ones' binary64 parts in
+// LDS, each lane its own), the block adds them up in a fixed order and writes
+// part[kind][block][D].
 template <int L, int TURN>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Divisor per_seq) {
     constexpr int GPW = 64 / L;
     __shared__ float red[kWaves][L * 8];
+    __shared__ double deep[8][kThreads];
     const int kind = blockIdx.y;
     const HeadsArg grad = kind == 0 ? a.dq : (kind == 1 ? a.dk : a.dv);
     const HeadsArg out = kind == 0 ? a.oq : (kind == 1 ? a.ok : a.ov);
@@ -120,6 +128,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
     const float inv_d = 1.0f / (float)a.D;
+    int adds = 0;
+    bool folded = false;
     for (int64_t t64 = w; heads > 0 && t64 < a.tokens; t64 += waves) {
         const int t = (int)t64;
         const Token tok = token_of(t, per_seq);
@@ -162,9 +172,23 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
                 // (an untouched head as its bits are: a signalling NaN is not made quiet)
                 if (live) store8<L, TURN>(y + h * out.hs, role, turned || gamma ? pack8(v) : rd[u]);
             }
+            adds += kUnrollBwd;
+            if (adds >= kDeep) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    deep[e][threadIdx.x] = (folded ? deep[e][threadIdx.x] : 0.0) + (double)sum[e];
+                    sum[e] = 0.0f;
+                }
+                adds = 0;
+                folded = true;
+            }
         }
     }
     if (!a.part || kind == 2) return;
+    if (folded) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = (float)(deep[e][threadIdx.x] + (double)sum[e]);
+    }
     // the groups of a wave, then the block's waves
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -180,7 +204,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
 
 // dgamma of 8 columns per block: two lanes a row of partial sums (16 bytes
 // each), 128 rows at a time, four loads in flight per lane; then across the
-// wave and the four waves.
+// wave and the four waves. Every kDeep rounds the lane's sums move to binary64
+// ones, as above (32768 rows and fewer, 2^18 tokens of 16 heads quantised, never).
 __global__ __launch_bounds__(kThreads) void dgamma_sum_kernel(const float* __restrict__ pq, int64_t nq,
                                                               float* __restrict__ dgq, const float* __restrict__ pk,
                                                               int64_t nk, float* __restrict__ dgk, int64_t ldp) {
@@ -189,17 +214,31 @@ __global__ __launch_bounds__(kThreads) void dgamma_sum_kernel(const float* __res
     float* const out = blockIdx.y ? dgk : dgq;
     const int64_t n = blockIdx.y ? nk : nq;
     if (!out) return;
-    float4 s[4] = {};
-    for (int64_t i = threadIdx.x >> 1; i < n; i += 512) {
+    double deep[4] = {};
+    float t[4];
+    for (int64_t i0 = threadIdx.x >> 1;; i0 += 512 * kDeep) {
+        float4 s[4] = {};
+        const int64_t end = min(n, i0 + 512 * kDeep);
+        for (int64_t i = i0; i < end; i += 512) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (i + 128 * u < n) {
-                const float4 v = *reinterpret_cast<const float4*>(p + (i + 128 * u) * ldp);
-                s[u].x += v.x; s[u].y += v.y; s[u].z += v.z; s[u].w += v.w;
-            }
+            for (int u = 0; u < 4; ++u)
+                if (i + 128 * u < n) {
+                    const float4 v = *reinterpret_cast<const float4*>(p + (i + 128 * u) * ldp);
+                    s[u].x += v.x; s[u].y += v.y; s[u].z += v.z; s[u].w += v.w;
+                }
+        }
+        t[0] = (s[0].x + s[1].x) + (s[2].x + s[3].x);
+        t[1] = (s[0].y + s[1].y) + (s[2].y + s[3].y);
+        t[2] = (s[0].z + s[1].z) + (s[2].z + s[3].z);
+        t[3] = (s[0].w + s[1].w) + (s[2].w + s[3].w);
+        if (n <= 512 * kDeep) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            deep[e] += (double)t[e];
+            t[e] = (float)deep[e];
+        }
+        if (i0 + 512 * kDeep >= n) break;
     }
-    float t[4] = {(s[0].x + s[1].x) + (s[2].x + s[3].x), (s[0].y + s[1].y) + (s[2].y + s[3].y),
-                  (s[0].z + s[1].z) + (s[2].z + s[3].z), (s[0].w + s[1].w) + (s[2].w + s[3].w)};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         t[e] += lane_xor_f<2>(t[e]);

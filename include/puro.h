@@ -277,8 +277,9 @@ puro_status puro_rmsnorm_quantize_fp8(const uint16_t* x, const uint16_t* gamma, 
  * counts the value heads of the backward): at most 65535; batch * seq at most 2^25.
  * batch * seq = 0 is a valid empty call. gamma_q, gamma_k: BF16 [head_dim],
  * 16-byte aligned. eps finite and >= 0 (with eps = 0 a head of zeros gives
- * NaN, as the formula does); heads whose sum of squares overflows binary32
- * are outside the statement. */
+ * NaN, as the formula does; any other head, down to the smallest values that
+ * BF16 has, its norm); heads whose sum of squares overflows binary32 are
+ * outside the statement. */
 typedef struct {
     uint16_t* data;
     int64_t batch_stride, row_stride, head_stride;

@@ -205,26 +205,39 @@ __device__ __forceinline__ uint4 pack8(const float v[8]) {
 }
 
 // 1 / sqrt(mean(x^2) + eps) of the head whose eight values the lane holds
-// (zeros where it holds none), by the reciprocal-root instruction (1 ulp),
-// which flushes numbers below the normal range: those are scaled by 2^64.
+// (zeros where it holds none), by the reciprocal-root instruction (1 ulp, which
+// flushes numbers below the normal range). Where the mean and eps are so small
+// that squares have lost bits or vanished (a binary32 square below 2^-126; from
+// 2^-100 on what is lost is less than 2^-40 of the mean), the head is scaled:
+// x becomes x s and the result r / s with s = 2^96, otherwise s = 1; x r stays.
 template <int L>
-__device__ __forceinline__ float head_rstd(const float x[8], float inv_d, float eps) {
+__device__ __forceinline__ float head_rstd(float x[8], float inv_d, float eps, float& s) {
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-    const float m = fmaf(head_sum<L>(ss), inv_d, eps);
+    float m = fmaf(head_sum<L>(ss), inv_d, eps);
     const bool tiny = m < 0x1p-100f;
-    const float r = __builtin_amdgcn_rsqf(tiny ? m * 0x1p64f : m);
-    return tiny ? r * 0x1p32f : r;
+    s = tiny ? 0x1p96f : 1.0f;
+    if (__builtin_amdgcn_ballot_w64(tiny)) {
+        ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] *= s;
+            ss = fmaf(x[i], x[i], ss);
+        }
+        m = fmaf(head_sum<L>(ss), inv_d, eps * s * s);
+    }
+    return __builtin_amdgcn_rsqf(m);
 }
 
 // The backward of the norm: d (the gradient of n, turned back) becomes dx, and
 // what the lane's columns add to dgamma is returned in w. (x: zeros where the
 // lane holds none; d is zero there too.)
 template <int L>
-__device__ __forceinline__ void norm_bwd8(float d[8], const float x[8], const float g[8], float inv_d, float eps,
+__device__ __forceinline__ void norm_bwd8(float d[8], float x[8], const float g[8], float inv_d, float eps,
                                           float w[8]) {
-    const float r = head_rstd<L>(x, inv_d, eps);
+    float s;
+    const float r = head_rstd<L>(x, inv_d, eps, s);
     float m = 0.0f, h[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -235,7 +248,7 @@ __device__ __forceinline__ void norm_bwd8(float d[8], const float x[8], const fl
     }
     m = head_sum<L>(m) * inv_d;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) d[i] = r * fmaf(-h[i], m, d[i]);
+    for (int i = 0; i < 8; ++i) d[i] = r * fmaf(-h[i], m, d[i]) * s;
 }
 
 }  // namespace puro

@@ -83,7 +83,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Di
                 for (int e = 0; e < 8; ++e) v[e] = 0.0f;
             }
             if (gamma) {
-                const float r = head_rstd<L>(v, inv_d, a.eps);
+                float s;
+                const float r = head_rstd<L>(v, inv_d, a.eps, s);
                 unpack8(gw, g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = v[e] * r * g[e];

@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads) void rope_table_kernel(float2* __restrict
 
 // Forward: wave w takes steps [part * per, part * per + per) of 64 / L heads
 // of token w / parts. Few tokens are split over more waves.
-template <int L, int TURN>
+template <int L, int TURN, bool SMALL>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Divisor per_seq, int per) {
     constexpr int GPW = 64 / L;
     const bool key = blockIdx.y != 0;
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_fwd_kernel(QkArgs a, Di
             }
             if (gamma) {
                 float s;
-                const float r = head_rstd<L>(v, inv_d, a.eps, s);
+                const float r = head_rstd<L, SMALL>(v, inv_d, a.eps, s);
                 unpack8(gw, g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = v[e] * r * g[e];
@@ -105,7 +105,7 @@ constexpr int kDeep = 64;
 // dgamma of its eight columns in binary32 (the long ones' binary64 parts in
 // LDS, each lane its own), the block adds them up in a fixed order and writes
 // part[kind][block][D].
-template <int L, int TURN>
+template <int L, int TURN, bool SMALL>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Divisor per_seq) {
     constexpr int GPW = 64 / L;
     __shared__ float red[kWaves][L * 8];
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
                     float g[8];
                     asm volatile("" : "+v"(gw.x), "+v"(gw.y), "+v"(gw.z), "+v"(gw.w));
                     unpack8(gw, g);
-                    norm_bwd8<L>(v, n, g, inv_d, a.eps, wg);
+                    norm_bwd8<L, SMALL>(v, n, g, inv_d, a.eps, wg);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum[e] += live ? wg[e] : 0.0f;
                 }
@@ -265,15 +265,21 @@ int64_t bwd_blocks(int64_t tokens) {
     return std::max<int64_t>(1, std::min<int64_t>((tokens + kWaves - 1) / kWaves, 768));
 }
 
-// f(lanes of a head, how it turns), both as types.
+// f(lanes of a head, how it turns, whether heads may be too small for their
+// squares), as types.
 template <class F>
-void by_lanes(int D, const RopeArgs& rope, F&& f) {
+void by_lanes(const QkArgs& a, F&& f) {
+    const int D = a.D;
+    auto small = [&](auto lanes, auto turn) {
+        if ((a.gq || a.gk) && a.eps < kLeastMean) f(lanes, turn, std::integral_constant<bool, true>{});
+        else f(lanes, turn, std::integral_constant<bool, false>{});
+    };
     auto turns = [&](auto lanes) {
-        switch (turn_kind(rope, decltype(lanes)::value)) {
-        case kTurnNone: f(lanes, std::integral_constant<int, kTurnNone>{}); break;
-        case kTurnHalf: f(lanes, std::integral_constant<int, kTurnHalf>{}); break;
-        case kTurnPart: f(lanes, std::integral_constant<int, kTurnPart>{}); break;
-        default: f(lanes, std::integral_constant<int, kTurnPairs>{});
+        switch (turn_kind(a.rope, decltype(lanes)::value)) {
+        case kTurnNone: small(lanes, std::integral_constant<int, kTurnNone>{}); break;
+        case kTurnHalf: small(lanes, std::integral_constant<int, kTurnHalf>{}); break;
+        case kTurnPart: small(lanes, std::integral_constant<int, kTurnPart>{}); break;
+        default: small(lanes, std::integral_constant<int, kTurnPairs>{});
         }
     };
     if (D <= 8) turns(std::integral_constant<int, 1>{});
@@ -295,12 +301,12 @@ void launch_rope_table(float2* table, int64_t len, int dim, double theta, hipStr
 void launch_qk_norm_rope_fwd(const QkArgs& a, hipStream_t stream) {
     const int heads = std::max(a.hq, a.hk);
     if (a.tokens == 0 || heads == 0) return;
-    by_lanes(a.D, a.rope, [&](auto lanes, auto turn) {
+    by_lanes(a, [&](auto lanes, auto turn, auto small) {
         constexpr int L = decltype(lanes)::value, GPW = 64 / L;
         const int steps = (heads + GPW - 1) / GPW;
         const int per = a.tokens * steps <= 4096 ? 1 : steps;
         const int64_t waves = a.tokens * ((steps + per - 1) / per);
-        qk_norm_rope_fwd_kernel<L, decltype(turn)::value>
+        qk_norm_rope_fwd_kernel<L, decltype(turn)::value, decltype(small)::value>
             <<<dim3((unsigned)((waves + kWaves - 1) / kWaves), a.hk > 0 ? 2 : 1), kThreads, 0, stream>>>(a, Divisor::of((uint32_t)a.seq), per);
     });
 }
@@ -319,8 +325,8 @@ void launch_qk_norm_rope_bwd(QkArgs a, void* ws, hipStream_t stream) {
     const int64_t blocks = bwd_blocks(a.tokens);
     a.part = sums ? reinterpret_cast<float*>(ws) : nullptr;
     if (a.tokens > 0)
-        by_lanes(a.D, a.rope, [&](auto lanes, auto turn) {
-            qk_norm_rope_bwd_kernel<decltype(lanes)::value, decltype(turn)::value>
+        by_lanes(a, [&](auto lanes, auto turn, auto small) {
+            qk_norm_rope_bwd_kernel<decltype(lanes)::value, decltype(turn)::value, decltype(small)::value>
                 <<<dim3((unsigned)blocks, a.dv.p ? 3 : 2), kThreads, 0, stream>>>(a, Divisor::of((uint32_t)a.seq));
         });
     if (sums) {

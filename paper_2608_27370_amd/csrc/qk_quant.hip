@@ -138,7 +138,7 @@ __device__ __forceinline__ void load_qk_bwd_any(const QkArgs& k, const Divisor& 
             unpack8(gw, gm);
 #pragma unroll
             for (int e = 0; e < 8; ++e) n[e] = d[e];
-            norm_bwd8<L>(n, x8, gm, inv_d, k.eps, wg);
+            norm_bwd8<L, true>(n, x8, gm, inv_d, k.eps, wg);
             uint4 o = rd[u];
             if (kind != 2) o = pack8(norm ? n : d);
             w[i][0] = live ? o.x : 0u; w[i][1] = live ? o.y : 0u;
@@ -153,9 +153,10 @@ __device__ __forceinline__ void load_qk_bwd_any(const QkArgs& k, const Divisor& 
     }
 }
 
-// The usual case: both kinds of heads normalised, whole heads turned by pairs
-// (i, i + D / 2), sequences of whole groups of 8 tokens, so that a thread's rows
-// are one sequence's and all or none of them exist. Here lane l of a head holds
+// The usual case: both kinds of heads normalised with an eps that stands over
+// the smallest heads, whole heads turned by pairs (i, i + D / 2), sequences of
+// whole groups of 8 tokens, so that a thread's rows are one sequence's and all
+// or none of them exist. Here lane l of a head holds
 // the pairs 4 l .. 4 l + 3, two 8-byte pieces D / 2 values apart: no value changes
 // lanes, and the lanes' cosines and sines are one run of the table (with eight
 // consecutive values a lane, every entry is loaded by two lanes and each of
@@ -241,7 +242,7 @@ __device__ __forceinline__ void load_qk_bwd_usual(const QkArgs& k, const Divisor
             unpack8(make_uint4(gw[0].x, gw[0].y, gw[1].x, gw[1].y), gm);
             const float c[4] = {u[0].x, u[0].z, u[1].x, u[1].z}, sn[4] = {u[0].y, u[0].w, u[1].y, u[1].w};
             turn_pairs4(d, c, sn, true);
-            norm_bwd8<L>(d, x8, gm, inv_d, k.eps, wg);
+            norm_bwd8<L, false>(d, x8, gm, inv_d, k.eps, wg);
             const uint4 n = pack8(d);
             uint2 lo = make_uint2(n.x, n.y), hi = make_uint2(n.z, n.w);
             if constexpr (L == 8) {
@@ -391,7 +392,7 @@ void launch_qk_norm_rope_bwd_quantize(int fmt, int mode, QuantArgs a, QkArgs k, 
     }
     auto run = [&](auto fmt_c) {
         constexpr int FMT = decltype(fmt_c)::value;
-        const bool usual = k.gq && k.gk && turn_kind(k.rope, k.D / 8) == kTurnHalf && k.seq % 8 == 0;
+        const bool usual = k.gq && k.gk && k.eps >= kLeastMean && turn_kind(k.rope, k.D / 8) == kTurnHalf && k.seq % 8 == 0;
         if (k.D == 128) {
             if (usual) launch_fmt<FMT, 16, true>(mode, a, k, ws, stream);
             else launch_fmt<FMT, 16, false>(mode, a, k, ws, stream);

@@ -205,8 +205,11 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(QkArgs a, Di
 
 // dgamma of 8 columns per block: two lanes a row of partial sums (16 bytes
 // each), 128 rows at a time, four loads in flight per lane; then across the
-// wave and the four waves. Every kDeep rounds the lane's sums move to binary64
-// ones, as above (32768 rows and fewer, 2^18 tokens of 16 heads quantised, never).
+// wave and the four waves. LONG: every kDeep rounds the lane's sums move to
+// binary64 ones, as above; kLongRows rows (2^18 tokens of 16 heads quantised)
+// are the most that never would.
+constexpr int64_t kLongRows = 512 * kDeep;
+template <bool LONG>
 __global__ __launch_bounds__(kThreads) void dgamma_sum_kernel(const float* __restrict__ pq, int64_t nq,
                                                               float* __restrict__ dgq, const float* __restrict__ pk,
                                                               int64_t nk, float* __restrict__ dgk, int64_t ldp) {
@@ -217,9 +220,9 @@ __global__ __launch_bounds__(kThreads) void dgamma_sum_kernel(const float* __res
     if (!out) return;
     double deep[4] = {};
     float t[4];
-    for (int64_t i0 = threadIdx.x >> 1;; i0 += 512 * kDeep) {
+    for (int64_t i0 = threadIdx.x >> 1;; i0 += kLongRows) {
         float4 s[4] = {};
-        const int64_t end = min(n, i0 + 512 * kDeep);
+        const int64_t end = LONG ? min(n, i0 + kLongRows) : n;
         for (int64_t i = i0; i < end; i += 512) {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
@@ -232,13 +235,13 @@ __global__ __launch_bounds__(kThreads) void dgamma_sum_kernel(const float* __res
         t[1] = (s[0].y + s[1].y) + (s[2].y + s[3].y);
         t[2] = (s[0].z + s[1].z) + (s[2].z + s[3].z);
         t[3] = (s[0].w + s[1].w) + (s[2].w + s[3].w);
-        if (n <= 512 * kDeep) break;
+        if constexpr (!LONG) break;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             deep[e] += (double)t[e];
             t[e] = (float)deep[e];
         }
-        if (i0 + 512 * kDeep >= n) break;
+        if (i0 + kLongRows >= n) break;
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -313,7 +316,9 @@ void launch_qk_norm_rope_fwd(const QkArgs& a, hipStream_t stream) {
 
 void launch_dgamma_sum(const float* part_q, int64_t nq, float* dgq, const float* part_k, int64_t nk, float* dgk,
                        int64_t ldp, int D, hipStream_t stream) {
-    dgamma_sum_kernel<<<dim3((unsigned)(D / 8), 2), kThreads, 0, stream>>>(part_q, nq, dgq, part_k, nk, dgk, ldp);
+    const dim3 grid((unsigned)(D / 8), 2);
+    if (std::max(nq, nk) > kLongRows) dgamma_sum_kernel<true><<<grid, kThreads, 0, stream>>>(part_q, nq, dgq, part_k, nk, dgk, ldp);
+    else dgamma_sum_kernel<false><<<grid, kThreads, 0, stream>>>(part_q, nq, dgq, part_k, nk, dgk, ldp);
 }
 
 size_t qk_bwd_ws_bytes(int64_t tokens, int D) {

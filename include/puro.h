@@ -532,8 +532,9 @@ puro_status puro_lm_head_ce_bwd(const uint16_t* X, const uint16_t* W, const int3
  * != 0 adds to an FP32 dW (with BF16: PURO_ERR_UNSUPPORTED).
  *
  * Any M >= 0 (0: dW is cleared), V >= 1, K a positive multiple of 8, each at
- * most 2^21; topk from 1 to 1024; tau and 1 / tau positive and normal; X, W, dX, dW
- * and ws 16-byte aligned. Nothing is allocated or synchronised. */
+ * most 2^21, M V at most 2^39; topk from 1 to 1024; tau and 1 / tau positive
+ * and normal; X, W, dX, dW and ws 16-byte aligned. Nothing is allocated or
+ * synchronised. */
 typedef enum { PURO_DISTILL_LOGITS = 0, PURO_DISTILL_PROBS = 1 } puro_distill_target;
 size_t puro_lm_head_distill_workspace_size(int64_t M, int64_t V, int64_t K, int64_t topk, int backward);
 puro_status puro_lm_head_distill_fwd(const uint16_t* X, const uint16_t* W, const int32_t* ids, const float* teacher,

@@ -907,6 +907,8 @@ puro_status check_distill_sizes(int64_t M, int64_t V, int64_t K, int64_t topk) {
     // BF16 operand pitches (2 M, 2 V, 2 K bytes, padded to 128 values) within 2^22
     const int64_t lim = (int64_t)1 << 21;
     if (M < 0 || V <= 0 || K <= 0 || M > lim || V > lim || K > lim) return PURO_ERR_SHAPE;
+    // the logits' grid: a launch holds fewer than 2^32 threads, 2^24 tiles of 256 x 256
+    if (M * V > (int64_t)1 << 39) return PURO_ERR_SHAPE;
     if (topk < 1 || topk > kDistillMaxTop) return PURO_ERR_SHAPE;
     if ((K % 8) != 0) return PURO_ERR_ALIGN;
     return PURO_OK;

@@ -51,17 +51,21 @@ __device__ __forceinline__ float wave_max(float v) {
     return v;
 }
 
+// (element passes over matrices of any size: a launch holds fewer than 2^32
+// threads, so from kMaxBlocks blocks on each takes several pieces)
+constexpr int64_t kMaxBlocks = 1 << 20;
+
 __global__ __launch_bounds__(kThreads) void f32_to_bf16_kernel(const float* __restrict__ src, uint16_t* __restrict__ dst,
                                                                int64_t n4) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= n4) return;
-    const float4 v = reinterpret_cast<const float4*>(src)[i];
-    reinterpret_cast<uint2*>(dst)[i] = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n4; i += kMaxBlocks * kThreads) {
+        const float4 v = reinterpret_cast<const float4*>(src)[i];
+        reinterpret_cast<uint2*>(dst)[i] = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    }
 }
 
 __global__ __launch_bounds__(kThreads) void zero_kernel(uint16_t* __restrict__ dst, int64_t n8) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i < n8) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n8; i += kMaxBlocks * kThreads)
+        reinterpret_cast<uint4*>(dst)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // z_top[j] = x . W[id_j] of a row's k entries, 0 for one that does not count,
@@ -401,12 +405,14 @@ void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* 
     }
     if (dX && Vc < V) {
         const int64_t n4 = M * K / 4;
-        f32_to_bf16_kernel<<<blocks(n4), kThreads, 0, stream>>>(dxacc, dX, n4);
+        f32_to_bf16_kernel<<<(unsigned)std::min((n4 + kThreads - 1) / kThreads, kMaxBlocks), kThreads, 0, stream>>>(dxacc, dX, n4);
     }
 }
 
 void launch_zero(void* dst, int64_t bytes, hipStream_t stream) {
-    if (bytes > 0) zero_kernel<<<blocks(bytes / 16), kThreads, 0, stream>>>(reinterpret_cast<uint16_t*>(dst), bytes / 16);
+    const int64_t n8 = bytes / 16;
+    if (n8 > 0) zero_kernel<<<(unsigned)std::min((n8 + kThreads - 1) / kThreads, kMaxBlocks), kThreads, 0, stream>>>(
+        reinterpret_cast<uint16_t*>(dst), n8);
 }
 
 }  // namespace puro

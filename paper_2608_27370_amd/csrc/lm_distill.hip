@@ -272,7 +272,8 @@ int64_t pad128(int64_t v) { return (v + 127) / 128 * 128; }
 
 // Vocabulary columns per chunk of the backward: as few chunks as keep one copy
 // of a chunk's dz within 2.5 GiB (288 GB of memory make a chunk of the whole
-// vocabulary the usual case), of even width, a multiple of the 256-wide tiles.
+// vocabulary the usual case), of even width, a multiple of the 256-wide tiles
+// (256 columns of the most rows, 2^21, are 1 GiB).
 // Few columns at a time leave the grids of few rows half empty and add every
 // chunk's dX to binary32 sums; that a chunk of 8192 columns stays in the
 // last-level cache gains less. Backward of V 151936, K 1536 at 8192 columns, at
@@ -280,7 +281,7 @@ int64_t pad128(int64_t v) { return (v + 127) / 128 * 128; }
 // 6068, 5512, 5308; M 8192 11023, 10438 (30464), 10263.
 constexpr int64_t kDzBytes = (int64_t)5 << 29;
 int64_t chunk_of(int64_t Mp, int64_t Vp) {
-    const int64_t chunks = (Mp * Vp * 2 + kDzBytes - 1) / kDzBytes;
+    const int64_t most = kDzBytes / (2 * Mp) / 256 * 256, chunks = (Vp + most - 1) / most;
     return std::min(((Vp + chunks - 1) / chunks + 255) / 256 * 256, Vp);
 }
 

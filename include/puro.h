@@ -516,11 +516,12 @@ puro_status puro_lm_head_ce_bwd(const uint16_t* X, const uint16_t* W, const int3
  * does not count and has z_top 0; a row without entries (a padding token) has
  * loss 0 and gradient 0, and so has one whose teacher logits are all -infinity.
  * A row whose dloss is 0 or whose q are all 0 adds nothing to dW and has dX 0
- * whatever its hidden state holds, NaN included. An id given twice counts twice:
- * both q are added, which also mixes a hard target into PURO_DISTILL_PROBS. A
- * NaN among the entries that count, or a teacher logit of +infinity, makes the
- * row's loss and gradient NaN.
- * No teacher beyond the entries is assumed (PROBS need not add up to 1).
+ * whatever its hidden state holds, NaN included, and a row whose q are all 0
+ * also whatever its dloss is. An id given twice counts twice: both q are added,
+ * which also mixes a hard target into PURO_DISTILL_PROBS. A NaN among the
+ * entries that count, or a teacher logit of +infinity, makes the row's loss and
+ * gradient NaN. No teacher beyond the entries is assumed (PROBS need not add up
+ * to 1).
  *
  * The logits are never stored (as puro_lm_head_ce_*): the forward keeps lse and
  * z_top for the backward, which recomputes the logits and keeps two BF16 copies

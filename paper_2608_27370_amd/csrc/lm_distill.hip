@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const float2* __
 // place, coef exp(a - lse) - dloss g / tau * (the sum of q over all entries of
 // that id): entries of the same id have the same value, whichever is written.
 // A row whose coef is 0 (no entries, dloss 0) has no gradient: its hidden state,
-// and with it lse, may be anything.
+// and with it lse, may be anything, and so may the dloss of one without entries.
 __global__ __launch_bounds__(64) void distill_coef_kernel(Teacher tch, const float* __restrict__ z_top,
                                                           const float* __restrict__ lse, const float* __restrict__ dloss,
                                                           float g_tau, float* __restrict__ coef, float* __restrict__ val) {
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(64) void distill_coef_kernel(Teacher tch, const flo
     Q = wave_sum(Q);
     __syncthreads();
     const float dl = (dloss ? dloss[m] : 1.0f) * g_tau;
-    const float c = dl * Q, l = lse[m];
+    const float c = Q == 0.0f ? 0.0f : dl * Q, l = lse[m];      // (dl infinite or NaN in a padding token's row)
     if (lane == 0) coef[m] = c;
     for (int j = lane; j < tch.k; j += 64) {
         const int32_t id = sid[j];

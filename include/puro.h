@@ -521,7 +521,8 @@ puro_status puro_lm_head_ce_bwd(const uint16_t* X, const uint16_t* W, const int3
  * which also mixes a hard target into PURO_DISTILL_PROBS. A NaN among the
  * entries that count, or a teacher logit of +infinity, makes the row's loss and
  * gradient NaN. No teacher beyond the entries is assumed (PROBS need not add up
- * to 1).
+ * to 1). grad_scale and grad_scale / tau are finite; logits whose quotient by
+ * tau overflows binary32 are outside the statement.
  *
  * The logits are never stored (as puro_lm_head_ce_*): the forward keeps lse and
  * z_top for the backward, which recomputes the logits and keeps two BF16 copies

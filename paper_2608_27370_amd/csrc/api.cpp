@@ -962,6 +962,9 @@ puro_status puro_lm_head_distill_bwd(const uint16_t* X, const uint16_t* W, const
     DistillArgs a;
     const puro_status st = check_distill(X, W, ids, teacher, M, V, K, topk, target, temperature, &a);
     if (st != PURO_OK) return st;
+    // (an infinite factor times a dloss of 0 would be NaN)
+    const float factor = grad_scale / temperature;
+    if (!(factor >= -3.4028235e38f) || !(factor <= 3.4028235e38f)) return PURO_ERR_UNSUPPORTED;
     if (!(grad_scale >= -3.4028235e38f) || !(grad_scale <= 3.4028235e38f)) return PURO_ERR_UNSUPPORTED;
     if (dw_type != PURO_OUT_BF16 && dw_type != PURO_OUT_FP32) return PURO_ERR_UNSUPPORTED;
     if (dW && accumulate_dW && dw_type != PURO_OUT_FP32) return PURO_ERR_UNSUPPORTED;

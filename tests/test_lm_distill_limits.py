@@ -36,3 +36,17 @@ def test_copies_of_the_gradient_within_what_is_stated(puro, M, V):  # noqa: F811
     rest = 4 * Mp + 4 * M * k + 2 * Mp * K + 2 * Vp * K + 4 * M * K + 256 * 256 * 256 * 4 + (1 << 20)
     used = puro.lib().puro_lm_head_distill_workspace_size(M, V, K, k, 1)
     assert used <= 2 * min(5 << 29, 2 * Mp * Vp) + rest
+
+
+def test_factors_of_the_gradient(puro):  # noqa: F811
+    """grad_scale and its quotient by the temperature are finite: times a dloss of 0 they have to be 0."""
+    from test_abi import ERR_UNSUPPORTED
+
+    def f(g, tau):
+        return puro.lib().puro_lm_head_distill_bwd(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 100, 500, 64, 8, 0, tau, None, g, FAKE, FAKE,
+                                                   1, 0, FAKE, 16, None)
+
+    for g, tau in ((1e3, 1e-37), (-1e3, 1e-37), (3e38, 0.5), (float("nan"), 1.0), (float("inf"), 1e10)):
+        assert f(g, tau) == ERR_UNSUPPORTED
+    for g, tau in ((1.0, 1e-37), (3e38, 2.0), (0.0, 1e-37), (1e-38, 1e10)):
+        assert f(g, tau) == ERR_WORKSPACE

@@ -307,7 +307,12 @@ void launch_qk_norm_rope_fwd(const QkArgs& a, hipStream_t stream) {
     by_lanes(a, [&](auto lanes, auto turn, auto small) {
         constexpr int L = decltype(lanes)::value, GPW = 64 / L;
         const int steps = (heads + GPW - 1) / GPW;
-        const int per = a.tokens * steps <= 4096 ? 1 : steps;
+        // a wave a step up to 2048 of them, and a wave a token beyond (us, split
+        // and whole; 16 + 8 heads of 128, four steps: 1 token 2.33 and 2.74, 256
+        // 2.89 and 3.32, 512 3.67 and 3.52, 1024 5.29 and 4.13, 4096 13.3 and 10.1;
+        // 16 + 4 of 256, eight steps: 256 tokens 3.59 and 4.86, 512 5.01 and 5.20,
+        // 1024 7.60 and 7.22): the split's waves load the position's row anew
+        const int per = a.tokens * steps <= 2048 ? 1 : steps;
         const int64_t waves = a.tokens * ((steps + per - 1) / per);
         qk_norm_rope_fwd_kernel<L, decltype(turn)::value, decltype(small)::value>
             <<<dim3((unsigned)((waves + kWaves - 1) / kWaves), a.hk > 0 ? 2 : 1), kThreads, 0, stream>>>(a, Divisor::of((uint32_t)a.seq), per);

@@ -20,9 +20,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 // Heads that a lane has in flight: their loads are issued together.
-// (backward, which loads two vectors a head: two heads take 90 registers and five
-// waves fit a SIMD; four took 126, 52.7 against 41.9 us at 8192 tokens of 16 + 8
-// heads of 128)
+// (backward, which loads two vectors a head: two heads take 64 to 95 registers and
+// five waves or more fit a SIMD; four took 126, 52.7 against 41.9 us at 8192
+// tokens of 16 + 8 heads of 128)
 constexpr int kUnroll = 4, kUnrollBwd = 2;
 
 // Table of cosines and sines: the angle in double precision (at position 10^6

@@ -9,8 +9,13 @@
 // and 1 byte a copy written per query and key value, 2 and 1 per value head's.
 // 8192 tokens of 16 + 8 heads of 128, E4M3 rows and columns: 50 us for 187 MB
 // (3.7 TB/s; the BF16 backward and the quantiser one after the other move 321 MB).
-// 166 registers let three blocks share a CU, and each of them loads, computes
-// and stores its one tile in that order: 2048 tiles are 2.7 rounds of the chip.
+// 163 to 166 registers (heads of 128, the usual case below) let three blocks
+// share a CU, 171 to 174 (heads of 64) two, 96 to 140 (any other case) five to
+// three, and each of them loads, computes and stores its one tile in that order:
+// 2048 tiles are 2.7 rounds of three a CU. With the sum of dgamma, us at 8192
+// tokens, in groups and per tensor: 16 + 8 heads of 128 turned by halves 54 to 56
+// and 77, by neighbours 60 and 82, 48 of their values 63 and 83, query heads alone
+// normalised 64 and 83; 32 + 8 of 64 51 and 70.
 
 #include "qk_norm_rope.h"
 #include "quant_tile.h"

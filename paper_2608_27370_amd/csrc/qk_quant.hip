@@ -10,12 +10,12 @@
 // 8192 tokens of 16 + 8 heads of 128, E4M3 rows and columns: 50 us for 187 MB
 // (3.7 TB/s; the BF16 backward and the quantiser one after the other move 321 MB).
 // 163 to 166 registers (heads of 128, the usual case below) let three blocks
-// share a CU, 171 to 174 (heads of 64) two, 96 to 140 (any other case) five to
-// three, and each of them loads, computes and stores its one tile in that order:
-// 2048 tiles are 2.7 rounds of three a CU. With the sum of dgamma, us at 8192
-// tokens, in groups and per tensor: 16 + 8 heads of 128 turned by halves 54 to 56
-// and 77, by neighbours 60 and 82, 48 of their values 63 and 83, query heads alone
-// normalised 64 and 83; 32 + 8 of 64 51 and 70.
+// share a CU, 171 to 174 (heads of 64) two, 101 to 128 (any other case) four,
+// and each of them loads, computes and stores its one tile in that order: 2048
+// tiles are 2.7 rounds of three a CU. With the sum of dgamma, us at 8192 tokens,
+// in groups and per tensor: 16 + 8 heads of 128 turned by halves 54 to 56 and 76,
+// by neighbours 59 and 82, 48 of their values 58 and 82, query heads alone
+// normalised 56 and 80; 32 + 8 of 64 51 and 70, half turned by neighbours 48 and 67.
 
 #include "qk_norm_rope.h"
 #include "quant_tile.h"
@@ -97,7 +97,7 @@ __device__ __forceinline__ HeadOf head_of(const QkArgs& k, int head0) {
 // where the sums are used, behind a branch, and keeps 64 terms until then.)
 
 // Any case, two rows at a time.
-template <int L>
+template <int L, bool SMALL>
 __device__ __forceinline__ void load_qk_bwd_any(const QkArgs& k, const Divisor& per_seq, const Tile& t, int head0,
                                                 uint32_t w[8][4], float sum[8], int col[2]) {
     const LaneRole role = lane_role<L>(k.D, k.rope.dim, k.rope.interleaved, threadIdx.x & 63);
@@ -143,7 +143,7 @@ __device__ __forceinline__ void load_qk_bwd_any(const QkArgs& k, const Divisor& 
             unpack8(gw, gm);
 #pragma unroll
             for (int e = 0; e < 8; ++e) n[e] = d[e];
-            norm_bwd8<L, true>(n, x8, gm, inv_d, k.eps, wg);
+            norm_bwd8<L, SMALL>(n, x8, gm, inv_d, k.eps, wg);
             uint4 o = rd[u];
             if (kind != 2) o = pack8(norm ? n : d);
             w[i][0] = live ? o.x : 0u; w[i][1] = live ? o.y : 0u;
@@ -205,7 +205,7 @@ __device__ __forceinline__ void load_qk_bwd_usual(const QkArgs& k, const Divisor
                 out = out || (unsigned)pos[i] >= (unsigned)k.rope.len;
             }
             if (!wave_none(out)) {
-                load_qk_bwd_any<L>(k, per_seq, t, head0, w, sum, col);
+                load_qk_bwd_any<L, false>(k, per_seq, t, head0, w, sum, col);
                 return;
             }
         }
@@ -304,7 +304,10 @@ __global__ __launch_bounds__(kThreads) void qk_bwd_quant_kernel(Kinds kinds, Qua
     float sum[8];
     int col[2];
     if constexpr (USUAL) load_qk_bwd_usual<L>(k, per_seq, t, head0, stage, w, sum, col);
-    else load_qk_bwd_any<L>(k, per_seq, t, head0, w, sum, col);
+    // (twice: one that always looks for tiny heads takes 137 to 140 registers in
+    // groups, 56 -> 64 us where query heads alone are normalised)
+    else if (k.eps < kLeastMean) load_qk_bwd_any<L, true>(k, per_seq, t, head0, w, sum, col);
+    else load_qk_bwd_any<L, false>(k, per_seq, t, head0, w, sum, col);
     if constexpr (MODE != kQkTensor) {
         if (k.part && head0 < k.hq + k.hk) {
             // the wave's four row groups (16 lanes apart), then the four waves

@@ -53,7 +53,7 @@ struct Params {
     const float* lse;          // [M] (kOutSoftmaxGradT: [rows_a])
     float grad_scale;
     const float* row_scale;    // kOutSoftmaxGradT: a factor per row in place of grad_scale
-    int rows_a, rows_b;        // rows that A and B have (M and N, or fewer)
+    int rows_a, rows_b;        // kOutSoftmaxGradT: rows that A and B have, M and N or fewer (M and N in every other kind)
     uint16_t* dzt;             // kOutSoftmaxGradT: the transposed copy [N, M], or NULL, and its row pitch
     int64_t ld_dzt;
     uint8_t* q8;               // kOutSoftmaxGradQ: dz's FP8 copies (the GemmProblem fields)

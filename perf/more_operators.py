@@ -1,0 +1,356 @@
+"""The 8-bit integer path of a trained model and the verification of a draft model's tokens, as cases to time and compare.
+
+Each case is one pass through an operator of ``paper_2608_27370_amd.puro`` (``own``), or the same operator in plain
+torch operations in binary32 (the verification in binary64: its choice of a token moves with the last bits), rounded
+once at the end. Operators (``op``):
+
+* ``gemm``       -- Y = X W^T of int8 codes with a scale per token and per output channel, bias and residual.
+* ``quant``      -- int8 codes of a BF16 tensor, of its RMSNorm or of a gate/up output's SwiGLU, with a scale per token;
+                    with a transposed copy with a scale per channel, as the backward's products read it.
+* ``linear_bwd`` -- the linear layer's backward in int8: the gradient quantised both ways, dX and dW.
+* ``verify``     -- drafted tokens accepted or replaced, from the target's and the draft's logits or probabilities and
+                    given random numbers.
+
+Sizes are those of Qwen2-1.5B (hidden size 1536, QKV 2048, gate/up 17920, MLP 8960, 151936 tokens), and generic ones
+around them.
+"""
+
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-6
+
+
+def listed():
+    return [
+        # one token through the QKV projection with its bias: the smallest product, bound by its latency
+        dict(name="gemm_decode_1", op="gemm", M=1, N=2048, K=1536, out="bf16", bias=True, res=False),
+        # the LM head over one sequence's four drafted tokens and the next: 233 MB of weights for five rows
+        dict(name="gemm_draft_head_5", op="gemm", M=5, N=151936, K=1536, out="fp32", bias=False, res=False),
+        # a ragged batch's down projection into the residual stream, odd sizes in M and N
+        dict(name="gemm_ragged_77", op="gemm", M=77, N=1531, K=8960, out="bf16", bias=False, res=True),
+        # the gate/up projection of one 8192-token micro-batch: the largest
+        dict(name="gemm_gate_up_8192", op="gemm", M=8192, N=17920, K=1536, out="bf16", bias=False, res=False),
+        # one token's norm ahead of the QKV projection
+        dict(name="quant_norm_1", op="quant", src="rmsnorm", M=1, C=1536, both=False),
+        # the down projection's input of half a micro-batch
+        dict(name="quant_swiglu_4096", op="quant", src="swiglu", M=4096, C=8960, both=False),
+        # a training step's activations for the forward and the weight gradient, a ragged number of tokens
+        dict(name="quant_both_8187", op="quant", src="plain", M=8187, C=1536, both=True),
+        # the QKV projection's backward of a short ragged micro-batch, and of a whole one
+        dict(name="linear_bwd_333", op="linear_bwd", M=333, N=2048, K=1536),
+        dict(name="linear_bwd_8192", op="linear_bwd", M=8192, N=2048, K=1536),
+        # one sequence, four drafts, probabilities as a sampler's filters leave them
+        dict(name="verify_1", op="verify", B=1, G=4, V=151936, kind="probs", dtype="fp32", draft="full", tau=1.0, same=True),
+        # a serving batch from the two models' logits, up to seven drafts each
+        dict(name="verify_logits_96", op="verify", B=96, G=7, V=151936, kind="logits", dtype="bf16", draft="full", tau=0.8, same=False),
+        # drafts looked up in the prompt (no probabilities of their own), an odd vocabulary
+        dict(name="verify_lookup_33", op="verify", B=33, G=3, V=50257, kind="logits", dtype="fp32", draft="none", tau=1.0, same=False),
+    ]
+
+
+def _log(rng, lo, hi, step=1):
+    """A size between lo and hi, even over its logarithm, a multiple of step."""
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    return max(-(-lo // step) * step, min(hi // step * step, int(round(v / step)) * step))
+
+
+def draw(rng):
+    op = rng.choice(["gemm", "gemm", "quant", "linear_bwd", "verify", "verify"])
+    if op == "gemm":
+        M, K = _log(rng, 1, 8192), _log(rng, 64, 17920, 16)
+        N = _log(rng, 64, min(151936, max(64, 8192 * 17920 * 1536 // (M * K))))
+        out = rng.choice(["bf16", "bf16", "fp32"])
+        return dict(op=op, M=M, N=N, K=K, out=out, bias=out == "bf16" and rng.random() < 0.4,
+                    res=out == "bf16" and rng.random() < 0.4)
+    if op == "quant":
+        src = rng.choice(["plain", "rmsnorm", "swiglu"])
+        C = _log(rng, 64, 17920, 16)
+        return dict(op=op, src=src, M=_log(rng, 1, max(1, min(8192, 8192 * 4096 // C))), C=C,
+                    both=src == "plain" and rng.random() < 0.6)
+    if op == "linear_bwd":
+        M, K = _log(rng, 1, 8192), _log(rng, 64, 8960, 16)
+        return dict(op=op, M=M, N=_log(rng, 64, min(17920, max(64, 8192 * 8192 * 1536 // (M * K))), 16), K=K)
+    V = _log(rng, 1000, 151936)
+    G = rng.choice([0, 1, 2, 3, 4, 5, 7, 8])
+    return dict(op=op, B=_log(rng, 1, max(1, min(96, 96 * 4 * 151936 // (V * (G + 1))))), G=G, V=V, kind=rng.choice(["logits", "probs"]),
+                dtype=rng.choice(["bf16", "fp32"]), draft=rng.choice(["full", "full", "none"]),
+                tau=rng.choice([1.0, 0.7, 1.3]), same=rng.random() < 0.3)
+
+
+# ------------------------------------------------------------------- inputs
+def _gen(seed, t):
+    return torch.Generator(device="cuda").manual_seed(seed * 16 + t)
+
+
+def _normal(seed, t, shape, std=1.0):
+    return torch.randn(shape, generator=_gen(seed, t), device="cuda") * std
+
+
+def _activations(seed, t, M, C):
+    """Tokens of unlike sizes over channels of unlike sizes, a few of them large, as a residual stream has them."""
+    x = _normal(seed, t, (M, C)) * torch.exp(0.5 * _normal(seed, t + 1, (1, C))) * torch.exp(0.3 * _normal(seed, t + 2, (M, 1)))
+    large = torch.rand((1, C), generator=_gen(seed, t + 3), device="cuda") < 0.01
+    return torch.where(large, 15.0 * x, x).to(torch.bfloat16)
+
+
+def _codes(x):
+    """int8 codes of the rows of x, the nearest to 127 x / amax (ties to even), and the rows' scales amax / 127; a row of
+    zeros has scale 1. In binary64: half of a row's largest value, 63.5 steps, is a tie and not to be lost by rounding."""
+    x = x.double()
+    amax = x.abs().amax(dim=1)
+    full = amax > 0
+    q = torch.round(x * 127.0 / torch.where(full, amax, 1.0)[:, None])
+    return q.to(torch.int8), torch.where(full, amax / 127.0, 1.0).float()
+
+
+def _padded(q):
+    """Codes [C, M] with zeros behind each row up to a multiple of 16."""
+    out = torch.zeros((q.shape[0], -(-q.shape[1] // 16) * 16), dtype=torch.int8, device=q.device)
+    out[:, : q.shape[1]] = q
+    return out
+
+
+def _prepare_gemm(c, seed):
+    M, N, K = c["M"], c["N"], c["K"]
+    A, sa = _codes(_activations(seed, 1, M, K).float())
+    B, sb = _codes(_normal(seed, 5, (N, K), 0.02).to(torch.bfloat16).float())
+    s = dict(case=c, A=A, sa=sa, B=B, sb=sb, bias=None, res=None)
+    if c["bias"]:
+        s["bias"] = _normal(seed, 6, (N,), 0.5).to(torch.bfloat16)
+    pitch = -(-N // 8) * 8
+    if c["res"]:
+        s["res"] = _normal(seed, 7, (M, pitch)).to(torch.bfloat16)[:, :N]
+    s["D"] = torch.empty((M, pitch), dtype=torch.float32 if c["out"] == "fp32" else torch.bfloat16, device="cuda")[:, :N]
+    return s
+
+
+def _prepare_quant(c, seed):
+    M, C = c["M"], c["C"]
+    s = dict(case=c, x=_activations(seed, 1, M, 2 * C if c["src"] == "swiglu" else C), gamma=None)
+    if c["src"] == "rmsnorm":
+        s["gamma"] = (1 + 0.2 * _normal(seed, 5, (C,))).to(torch.bfloat16)
+    s["values"] = torch.empty((M, C), dtype=torch.bfloat16, device="cuda")
+    s["valuesT"] = torch.empty((C, M), dtype=torch.bfloat16, device="cuda")
+    return s
+
+
+def _prepare_linear_bwd(c, seed):
+    M, N, K = c["M"], c["N"], c["K"]
+    xT, sx = _codes(_activations(seed, 1, M, K).float().t().contiguous())
+    wT, sw = _codes(_normal(seed, 5, (N, K), 0.02).to(torch.bfloat16).float().t().contiguous())
+    dY = _normal(seed, 6, (M, N), 1e-3) * torch.exp(0.7 * _normal(seed, 7, (M, 1)))
+    return dict(case=c, dY=dY.to(torch.bfloat16), xT=_padded(xT), sx=sx, wT=_padded(wT), sw=sw)
+
+
+def _rows(c):
+    """Rows of each sequence: 1 + its drafts, 0 to G of them in turn (same: G)."""
+    b = torch.arange(c["B"], dtype=torch.int64)
+    return torch.full((c["B"],), c["G"] + 1, dtype=torch.int64) if c["same"] else 1 + (5 * b + 3) % (c["G"] + 1)
+
+
+def _prepare_verify(c, seed):
+    B, V = c["B"], c["V"]
+    n = _rows(c)
+    T = int(n.sum())
+    offsets = torch.zeros(B + 1, dtype=torch.int64)
+    offsets[1:] = n.cumsum(0)
+    dtype = torch.bfloat16 if c["dtype"] == "bf16" else torch.float32
+    # frequent tokens have larger logits; the padding of the vocabulary is masked
+    rank = torch.randperm(V, generator=_gen(seed, 1), device="cuda")
+    z = _normal(seed, 2, (T, V), 2.0)
+    z -= 1.1 * torch.log1p(rank.float())
+    z[:, V - V // 500:] = -math.inf
+    last = torch.zeros(T, dtype=torch.bool)
+    last[offsets[1:] - 1] = True
+    drafted = (~last).cuda()
+    zq = z[drafted]
+    zq += 0.6 * torch.randn(zq.shape, generator=_gen(seed, 3), device="cuda")
+    # the draft model's own choices (the largest of its logits plus Gumbel noise)
+    noise = -torch.log(-torch.log(torch.rand(zq.shape, generator=_gen(seed, 4), device="cuda").clamp_(1e-12, 1 - 1e-7)))
+    ids = torch.zeros(T, dtype=torch.int32, device="cuda")
+    ids[drafted] = (zq / c["tau"] + noise).argmax(dim=1).to(torch.int32) if len(zq) else 0
+    del noise
+    if c["kind"] == "probs":
+        z, zq = torch.softmax(z / c["tau"], dim=1), torch.softmax(zq / c["tau"], dim=1)
+    return dict(case=c, target=z.to(dtype), draft=zq.to(dtype) if c["draft"] == "full" else None, ids=ids,
+                offsets=offsets.to(torch.int32).cuda(), u=torch.rand(T, generator=_gen(seed, 5), device="cuda"),
+                us=torch.rand(B, generator=_gen(seed, 6), device="cuda"))
+
+
+def prepare(case, seed):
+    return {"gemm": _prepare_gemm, "quant": _prepare_quant, "linear_bwd": _prepare_linear_bwd,
+            "verify": _prepare_verify}[case["op"]](case, seed)
+
+
+# -------------------------------------------------------------- plain forms
+def _product(a, sa, b, sb):
+    return (a.float() @ b.float().t()) * sa[:, None] * sb[None, :]
+
+
+def _plain_gemm(s):
+    y = _product(s["A"], s["sa"], s["B"], s["sb"])
+    if s["bias"] is not None:
+        y = y + s["bias"].float()
+    if s["res"] is not None:
+        y = y + s["res"].float()
+    return y.to(s["D"].dtype)
+
+
+def _plain_quant(s):
+    c = s["case"]
+    x = s["x"].float()
+    if c["src"] == "rmsnorm":
+        x = x * (1.0 / (x.square().mean(dim=1, keepdim=True) + EPS).sqrt()) * s["gamma"].float()
+    elif c["src"] == "swiglu":
+        g, u = x.split(c["C"], dim=1)
+        x = g / (1.0 + torch.exp(-g)) * u
+    q, scale = _codes(x)
+    if not c["both"]:
+        return ((q.float() * scale[:, None]).to(torch.bfloat16),)
+    qT, scaleT = _codes(x.t().contiguous())
+    return (q.float() * scale[:, None]).to(torch.bfloat16), (qT.float() * scaleT[:, None]).to(torch.bfloat16)
+
+
+def _plain_linear_bwd(s):
+    M = s["case"]["M"]
+    dy = s["dY"].float()
+    q, sq = _codes(dy)
+    qT, sqT = _codes(dy.t().contiguous())
+    dX = _product(q, sq, s["wT"][:, : s["case"]["N"]], s["sw"]).to(torch.bfloat16)
+    return dX, _product(qT, sqT, s["xT"][:, :M], s["sx"])
+
+
+def _plain_verify(s):
+    c = s["case"]
+    B, V = c["B"], c["V"]
+    at = s["offsets"].long()
+    start, n = at[:-1], at[1:] - at[:-1]
+    T = s["target"].shape[0]
+    t = torch.arange(T, device="cuda")
+    seq = torch.repeat_interleave(torch.arange(B, device="cuda"), n, output_size=T)
+    i = t - start[seq]
+    last = i == n[seq] - 1
+    p, q = s["target"].double(), s["draft"].double() if s["draft"] is not None else None
+    if c["kind"] == "logits":
+        p = torch.exp((p - p.amax(dim=1, keepdim=True)) / c["tau"])
+        p = p / p.sum(dim=1, keepdim=True)
+        if q is not None and len(q):
+            q = torch.exp((q - q.amax(dim=1, keepdim=True)) / c["tau"])
+            q = q / q.sum(dim=1, keepdim=True)
+    ids = s["ids"].long()
+    pd = p.gather(1, ids[:, None]).squeeze(1)
+    qd = torch.ones_like(pd)
+    row_q = (t - seq).clamp(max=max(0, T - B - 1))          # the draft's row of each target row that has one
+    if q is not None and len(q):
+        qd = q[row_q].gather(1, ids[:, None]).squeeze(1)
+    taken = (s["u"].double() * qd < pd) & ~last
+    stop = torch.where(taken, n[seq], i)
+    accepted = n.scatter_reduce(0, seq, stop, "amin")
+    row = start + accepted
+    pr = p[row]
+    rest = pr
+    if q is None:
+        rest = pr.scatter(1, ids[row][:, None], 0.0)
+    elif len(q):
+        rest = (pr - q[row_q[row]]).clamp_min(0.0)
+    rest = torch.where(last[row][:, None], pr, rest)
+    total = rest.sum(dim=1, keepdim=True)
+    rest = torch.where(total > 0, rest, pr)
+    cum = rest.cumsum(dim=1)
+    hit = cum > s["us"].double()[:, None] * cum[:, -1:]
+    pick = torch.where(hit.any(dim=1), hit.int().argmax(dim=1), V - 1 - (rest.flip(1) > 0).int().argmax(dim=1))
+    tokens = torch.where(i < accepted[seq], ids, torch.where(i == accepted[seq], pick[seq], -1))
+    return tokens.to(torch.int32), accepted.to(torch.int32)
+
+
+# ---------------------------------------------------------------- the calls
+def _own_run(s):
+    from paper_2608_27370_amd import puro as P
+    c = s["case"]
+    if c["op"] == "gemm":
+        return P.int8_gemm(s["A"], s["sa"], s["B"], s["sb"], D=s["D"], bias=s["bias"], residual=s["res"])
+    if c["op"] == "linear_bwd":
+        saved = dict(xq_t=s["xT"], x_scale=s["sx"], wq_t=s["wT"], w_scale=s["sw"])
+        return P.int8_linear_bwd(s["dY"], saved)
+    if c["op"] == "verify":
+        kind = P.VERIFY_LOGITS if c["kind"] == "logits" else P.VERIFY_PROBS
+        return P.verify_drafts(s["target"], s["draft"], s["ids"], s["offsets"], s["u"], s["us"], kind=kind,
+                               temperature=c["tau"])
+    if c["src"] == "rmsnorm":
+        r = P.rmsnorm_quantize_int8(s["x"], s["gamma"], EPS)
+    elif c["src"] == "swiglu":
+        r = P.swiglu_quantize_int8(s["x"], c["C"])
+    else:
+        r = P.quantize_int8(s["x"], want_qT=c["both"])
+    # (what the codes stand for, in one elementwise pass each)
+    values = torch.mul(r["q"], r["scale"][:, None], out=s["values"])
+    if not c["both"]:
+        return (values,)
+    return values, torch.mul(r["qT"][:, : c["M"]], r["scaleT"][:, None], out=s["valuesT"])
+
+
+def run(state):
+    if own:
+        return _own_run(state)
+    return {"gemm": _plain_gemm, "quant": _plain_quant, "linear_bwd": _plain_linear_bwd,
+            "verify": _plain_verify}[state["case"]["op"]](state)
+
+
+def work(case):
+    if case["op"] == "gemm":
+        M, N, K = case["M"], case["N"], case["K"]
+        e = 4 if case["out"] == "fp32" else 2
+        side = 2 * N * case["bias"] + 2 * M * N * case["res"]
+        return {"bytes": (M + N) * (K + 4) + M * N * e + side, "flops": 2.0 * M * N * K}
+    if case["op"] == "linear_bwd":
+        M, N, K = case["M"], case["N"], case["K"]
+        # dY, the two saved copies, dX and dW; what lies between the steps is not counted
+        return {"bytes": 2 * M * N + K * (M + N) + 8 * K + 2 * M * K + 4 * N * K, "flops": 4.0 * M * N * K}
+    if case["op"] == "quant":
+        M, C = case["M"], case["C"]
+        reads = M * C * (4 if case["src"] == "swiglu" else 2) + (2 * C if case["src"] == "rmsnorm" else 0)
+        return {"bytes": reads + (M * C + 4 * M) + (M * C + 4 * C if case["both"] else 0), "flops": 4.0 * M * C}
+    T, B, V = int(_rows(case).sum()), case["B"], case["V"]
+    e = 2 if case["dtype"] == "bf16" else 4
+    full = case["draft"] == "full"
+    # logits: every row's normaliser; probabilities: the row that a token is taken from
+    rows = T + (T - B if full else 0) if case["kind"] == "logits" else B * (2 if full and case["G"] else 1)
+    return {"bytes": rows * V * e + 16 * T + 12 * B, "flops": 4.0 * rows * V}
+
+
+# ------------------------------------------------- the definition, in 64 bits
+def _nearest(x):
+    """What x [R, C] is in steps of a 127th of its rows' largest magnitudes."""
+    top = x.abs().max(dim=1, keepdim=True).values
+    unit = torch.where(top > 0, top, 1.0)
+    return torch.round(127.0 * x / unit) / 127.0 * unit
+
+
+def exact(case, seed):
+    if case["op"] == "verify":
+        return None                # whole numbers
+    s = prepare(case, seed)
+    if case["op"] == "gemm":
+        y = (s["A"].double() * s["sa"].double()[:, None]) @ (s["B"].double() * s["sb"].double()[:, None]).t()
+        for k in ("bias", "res"):
+            if s[k] is not None:
+                y += s[k].double()
+        return y
+    if case["op"] == "linear_bwd":
+        dy = s["dY"].double()
+        w = s["wT"][:, : case["N"]].double() * s["sw"].double()[:, None]
+        x = s["xT"][:, : case["M"]].double() * s["sx"].double()[:, None]
+        return _nearest(dy) @ w.t(), _nearest(dy.t().contiguous()) @ x.t()
+    x = s["x"].double()
+    if case["src"] == "rmsnorm":
+        x = x / torch.sqrt((x * x).sum(dim=1, keepdim=True) / case["C"] + EPS) * s["gamma"].double()
+    elif case["src"] == "swiglu":
+        g, u = x[:, : case["C"]], x[:, case["C"]:]
+        x = g * torch.sigmoid(g) * u
+    if not case["both"]:
+        return (_nearest(x),)
+    return _nearest(x), _nearest(x.t().contiguous())

@@ -98,13 +98,13 @@ def _activations(seed, t, M, C):
 
 
 def _codes(x):
-    """int8 codes of the rows of x, the nearest to 127 x / amax (ties to even), and the rows' scales amax / 127; a row of
-    zeros has scale 1. In binary64: half of a row's largest value, 63.5 steps, is a tie and not to be lost by rounding."""
-    x = x.double()
-    amax = x.abs().amax(dim=1)
+    """int8 codes of the rows of x (binary32 values): the nearest integers to x r, r = 127 / amax rounded to binary32,
+    and the rows' scales amax / 127; a row of zeros has scale 1. The products in binary64, where they are exact: half of a
+    row's largest value lies next to the border of 63.5."""
+    amax = x.abs().amax(dim=1).double()
     full = amax > 0
-    q = torch.round(x * 127.0 / torch.where(full, amax, 1.0)[:, None])
-    return q.to(torch.int8), torch.where(full, amax / 127.0, 1.0).float()
+    r = (127.0 / torch.where(full, amax, 1.0)).float()
+    return torch.round(x.double() * r.double()[:, None]).to(torch.int8), torch.where(full, amax / 127.0, 1.0).float()
 
 
 def _padded(q):
@@ -324,10 +324,11 @@ def work(case):
 
 # ------------------------------------------------- the definition, in 64 bits
 def _nearest(x):
-    """What x [R, C] is in steps of a 127th of its rows' largest magnitudes."""
+    """What x [R, C] is in steps of a 127th of its rows' largest magnitudes (the encoding's factor is a binary32 number)."""
     top = x.abs().max(dim=1, keepdim=True).values
-    unit = torch.where(top > 0, top, 1.0)
-    return torch.round(127.0 * x / unit) / 127.0 * unit
+    unit = torch.where(top > 0, top, 127.0)
+    factor = (127.0 / unit).to(torch.float32).to(torch.float64)
+    return torch.round(factor * x) * (unit / 127.0)
 
 
 def exact(case, seed):

@@ -70,7 +70,7 @@ __device__ __forceinline__ float exp_f32(float x) {
     return __builtin_amdgcn_exp2f(t) * (1.0f + err * kLn2);
 }
 
-// e^x as m * 2^n, m in [1, 2) within about 2 ulp, n an integer: the exp2
+// e^x as m * 2^n, m in [1, 2] within about 2 ulp, n an integer: the exp2
 // instruction only ever sees the fraction of x log2 e, so results that lie
 // below binary32's normal range (where that instruction flushes to zero) keep
 // their significand. For finite x with |x| < 2^24.
@@ -78,11 +78,12 @@ __device__ __forceinline__ float exp_split(float x, int& n) {
     constexpr float kL2eHi = 1.44269502162933349609375f;
     constexpr float kL2eLo = 1.925962989e-8f;
     constexpr float kLn2 = 0.693147180559945309f;
-    const float t = x * kL2eHi;
-    const float err = fmaf(x, kL2eHi, -t) + x * kL2eLo;
-    const float fl = floorf(t);
+    // (the fraction is taken from the exact product: written as t - floor(t) with
+    // t's own error applied afterwards, the compiler fuses the difference with t's
+    // product and that error counts twice, a relative 2^-18.5 at x = -80)
+    const float fl = floorf(x * kL2eHi);
     n = (int)fl;
-    return __builtin_amdgcn_exp2f(t - fl) * (1.0f + err * kLn2);
+    return __builtin_amdgcn_exp2f(fmaf(x, kL2eHi, -fl)) * (1.0f + x * kL2eLo * kLn2);
 }
 
 // Gate values below kDeepGate take the scaled evaluation: there 1 + e^-g equals

@@ -550,6 +550,116 @@ puro_status puro_lm_head_distill_bwd(const uint16_t* X, const uint16_t* W, const
                                      puro_out_dtype dw_type, int accumulate_dW, void* ws, size_t ws_bytes,
                                      hipStream_t stream);
 
+/* ------------------------------------------- 8-bit integer linear layers ---
+ * The other 8-bit operand type of the matrix cores: a trained model served (or
+ * trained on) with int8 weights and activations, a scale for each token and
+ * each output channel instead of the FP8 recipe's groups. The paper trains in
+ * FP8 (Section 3.2) and states no integer format; the readings here follow the
+ * FP8 encoding above.
+ *
+ * Encoding of a row of values x with amax = max |x|:
+ *     s = fl32(amax / 127),  r = fl32(127 / amax),  code = the integer nearest
+ *     to x r (the exact product; ties to even), in [-127, 127];
+ *     amax = 0: s = 1, codes 0;  a NaN or an infinity among x: s = NaN, codes 0
+ *     (so that a product with the row is NaN). r does not overflow: rows below
+ *     2^-100 are scaled by 2^64 with their amax first, which changes no code.
+ *
+ * puro_quantize_int8: of the BF16 tensor x [rows, cols] (row pitch ld) the codes
+ * q [rows, cols] (dense) with a scale per row, scale [rows], and / or a transposed
+ * copy with a scale per column: qT [cols, rows], row pitch ld_qT, scaleT [cols],
+ * encoded from the BF16 values. The copy's columns from `rows` up to the next
+ * multiple of 16 are filled with zeros, so that any number of tokens can be a
+ * product's reduction dimension; what lies beyond is left alone. Either of q and
+ * qT may be NULL (not wanted), each comes with its scales.
+ * Requirements: cols % 16 == 0, ld % 8 == 0, ld < 2^23, x, q and qT 16-byte
+ * aligned, ld_qT % 16 == 0 and >= rows; rows at most 65535 * 128. ws (16-byte
+ * aligned): *_workspace_size(rows, cols) bytes, needed for qT only. */
+size_t puro_quantize_int8_workspace_size(int64_t rows, int64_t cols);
+puro_status puro_quantize_int8(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, int8_t* q, float* scale,
+                               int8_t* qT, int64_t ld_qT, float* scaleT, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+
+/* The same encoding of a linear layer's input where it is formed (the places of
+ * puro_rmsnorm_quantize_fp8 and puro_swiglu_quantize_fp8), a scale per row:
+ *   rmsnorm:  y = x rstd gamma, rstd = 1 / sqrt(mean(x^2) + eps) (written to
+ *             rstd [rows] unless that is NULL), of x [rows, cols];
+ *   swiglu:   h = silu(gate) up of gu [rows, 2 cols].
+ * The values are encoded as binary32 has them, without a rounding to BF16
+ * between. Requirements as puro_quantize_int8; gamma BF16 [cols], 16-byte
+ * aligned; eps finite and >= 0; gu's pitch ld >= 2 cols. */
+puro_status puro_rmsnorm_quantize_int8(const uint16_t* x, const uint16_t* gamma, int64_t rows, int64_t cols,
+                                       int64_t ld, float eps, int8_t* q, float* scale, float* rstd,
+                                       hipStream_t stream);
+puro_status puro_swiglu_quantize_int8(const uint16_t* gu, int64_t rows, int64_t cols, int64_t ld, int8_t* q,
+                                      float* scale, hipStream_t stream);
+
+/* D[m, n] = (sum_k A[m, k] B[n, k]) a_scale[m] b_scale[n] (+ bias[n] + residual[m, n])
+ * of int8 codes A [M, K] (pitch lda) and B [N, K] (pitch ldb), a_scale [M] and
+ * b_scale [N]. The sum is exact (32-bit integers; K at most 131056), rounded to
+ * binary32, multiplied by a_scale and then by b_scale, the other terms added in
+ * binary32, and rounded once to D's type (BF16 or FP32, pitch ldd). accumulate
+ * != 0: D += result (FP32 only). bias: BF16 [N]; residual: BF16 [M, N], pitch ldr,
+ * may be D itself (ldr == ldd) and must not overlap it otherwise; either may be
+ * NULL; both for a BF16 D only. (Other combinations: PURO_ERR_UNSUPPORTED.)
+ * A linear layer's three products have this form: Y from X's and W's rows,
+ * dX from dY's rows and W's transposed copy, dW from the transposed copies of dY
+ * and X (K then is the number of tokens rounded up to 16).
+ * Requirements: K % 16 == 0; lda, ldb % 16 == 0, at least K and at most 2^22;
+ * ldd, ldr % 4 == 0 and at least N, ldr at most 2^22; data pointers, a_scale and
+ * b_scale 16-byte aligned; M and N at most 2^22, M N at most 2^38; ws (16-byte
+ * aligned): puro_int8_gemm_workspace_size(M, N, K) bytes. M = 0 or N = 0 is a
+ * valid empty call; K = 0 is an empty sum. */
+size_t puro_int8_gemm_workspace_size(int64_t M, int64_t N, int64_t K);
+puro_status puro_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* A, int64_t lda, const float* a_scale,
+                           const int8_t* B, int64_t ldb, const float* b_scale, void* D, puro_out_dtype d_type,
+                           int64_t ldd, int accumulate, const uint16_t* bias, const uint16_t* residual, int64_t ldr,
+                           void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* --------------------------------------- verification of drafted tokens ---
+ * A distilled student (puro_lm_head_distill_*) proposes tokens; the model itself
+ * scores them all in one pass, and each is kept with the probability that leaves
+ * the model's own distribution unchanged. For B sequences whose rows lie one
+ * after another: sequence b has the target rows offsets[b] .. offsets[b + 1] - 1,
+ * the i-th of them the target's prediction of the place where the draft put
+ * draft_ids[offsets[b] + i]; the last row has no draft (its id is not read). The
+ * draft's own prediction for target row t is row t - b of `draft`; draft NULL:
+ * the drafts were chosen without probabilities (q = 1 at the id).
+ *     p, q: softmax of row / temperature (PURO_VERIFY_LOGITS), or the row as it
+ *           stands, not negative (PURO_VERIFY_PROBS)
+ *     draft i is kept while uniform[t] q[id] < p[id]; at the first that is not,
+ *     or after all, the token drawn from max(p - q, 0) (from p in the last row,
+ *     and where that is 0 everywhere): the least v with
+ *     sum_{w <= v} rest[w] > uniform_sample[b] sum_w rest[w]
+ *     (the last v with rest[v] > 0 where rounding leaves none).
+ * tokens[offsets[b] ..]: the kept ids, the drawn token, then -1; accepted[b]: how
+ * many were kept. temperature 0 (LOGITS): the row's largest logit, the lowest id
+ * among equals, is the token, and a draft is kept where it is that; draft,
+ * uniform and uniform_sample are not read then.
+ * Exponentials and sums in binary64, in a fixed order: over 10^5 entries the
+ * drawn token moves with differences of 10^-8.
+ * Special values: logits of -infinity have probability 0; an id outside [0, V) is
+ * not kept, nor is one whose p or q is NaN; a row of logits with a NaN or a
+ * +infinity, or with no probability at all, keeps nothing; a token that would be
+ * drawn from such a row, or from one with a NaN or an infinity in its rest, is -1.
+ * A sequence without rows has accepted 0 and no token (as behind the last one
+ * of a batch with room to spare: rows behind the last sequence are neither read
+ * nor written); one whose offsets decrease or leave [0, T], or whose draft rows
+ * leave [0, draft_rows), has accepted -1 and no token.
+ * dtype: PURO_OUT_BF16 or PURO_OUT_FP32 for both target [T, V] (pitch ld_target)
+ * and draft [draft_rows, V] (pitch ld_draft); any V from 1 to 2^21 and pitches
+ * from V to 2^22 (rows need no more than their element's alignment); T and B at
+ * most 2^20, T V and B V at most 2^35, draft_rows at most T. offsets [B + 1], draft_ids [T],
+ * tokens [T], accepted [B]: int32; uniform [T], uniform_sample [B]: FP32 in
+ * [0, 1). temperature finite and >= 0, if not 0 between 2^-20 and 2^20 (PROBS:
+ * not used). ws (16-byte aligned): *_workspace_size bytes. */
+typedef enum { PURO_VERIFY_LOGITS = 0, PURO_VERIFY_PROBS = 1 } puro_verify_kind;
+size_t puro_verify_drafts_workspace_size(int64_t B, int64_t T, int64_t draft_rows, int64_t V);
+puro_status puro_verify_drafts(int64_t B, int64_t T, int64_t draft_rows, int64_t V, puro_verify_kind kind,
+                               puro_out_dtype dtype, const void* target, int64_t ld_target, const void* draft,
+                               int64_t ld_draft, const int32_t* draft_ids, const int32_t* offsets,
+                               const float* uniform, const float* uniform_sample, double temperature,
+                               int32_t* tokens, int32_t* accepted, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------------- MuonH ---
  * Section 3.3 (Hyperball Optimization), equation hyperball-update: a wrapped
  * matrix keeps its initial Frobenius radius R; with the Muon update u and the

@@ -985,6 +985,177 @@ puro_status puro_lm_head_distill_bwd(const uint16_t* X, const uint16_t* W, const
 
 }  // extern "C"
 
+// --------------------------------------------- 8-bit integer linear layers
+namespace {
+
+// The int32 sums of a product are exact: 2^14 K < 2^31 (codes of -128 too).
+constexpr int64_t kMaxInt8K = 131056;
+
+// x [rows, width] and its int8 copy's columns, as the quantisers take them.
+puro_status check_int8_source(const uint16_t* x, int64_t rows, int64_t cols, int64_t width, int64_t ld) {
+    if (cols < 0 || cols > ((int64_t)1 << 30)) return PURO_ERR_SHAPE;
+    const puro_status st = check_bf16_matrix(x, rows, width, ld);
+    if (st != PURO_OK) return st;
+    if ((cols % 16) != 0) return PURO_ERR_ALIGN;
+    return ld < ((int64_t)1 << 23) ? PURO_OK : PURO_ERR_SHAPE;
+}
+
+// The rows' codes and scales.
+puro_status check_int8_rows(const int8_t* q, const float* scale) {
+    if (!q || !scale) return PURO_ERR_NULL;
+    return aligned16(q) && ((uintptr_t)scale & 3) == 0 ? PURO_OK : PURO_ERR_ALIGN;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t puro_quantize_int8_workspace_size(int64_t rows, int64_t cols) {
+    if (rows <= 0 || cols <= 0 || rows > (int64_t)65535 * kGroup || cols > ((int64_t)1 << 23)) return 0;
+    return quant_int8_ws_bytes(rows, cols);
+}
+
+puro_status puro_quantize_int8(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, int8_t* q, float* scale,
+                               int8_t* qT, int64_t ld_qT, float* scaleT, void* ws, size_t ws_bytes,
+                               hipStream_t stream) {
+    puro_status st = check_int8_source(x, rows, cols, cols, ld);
+    if (st != PURO_OK) return st;
+    if (qT && (ld_qT < rows || ld_qT > kMaxPitch)) return PURO_ERR_SHAPE;
+    if (qT && ((ld_qT % 16) != 0 || !aligned16(qT) || ((uintptr_t)scaleT & 3) != 0)) return PURO_ERR_ALIGN;
+    if (rows == 0 || cols == 0) return PURO_OK;
+    if (!q && !qT) return PURO_ERR_NULL;
+    if (q && (st = check_int8_rows(q, scale)) != PURO_OK) return st;
+    if (qT) {
+        if (!scaleT || !ws) return PURO_ERR_NULL;
+        if (!aligned16(ws)) return PURO_ERR_ALIGN;
+        if (ws_bytes < quant_int8_ws_bytes(rows, cols)) return PURO_ERR_WORKSPACE;
+    }
+    if (q) launch_quantize_int8(QuantInt8Args{x, rows, cols, ld, q, scale, nullptr, 0.0f, nullptr, 0}, stream);
+    if (qT) launch_quantize_int8_t(x, rows, cols, ld, qT, ld_qT, scaleT, ws, stream);
+    return launched();
+}
+
+puro_status puro_rmsnorm_quantize_int8(const uint16_t* x, const uint16_t* gamma, int64_t rows, int64_t cols,
+                                       int64_t ld, float eps, int8_t* q, float* scale, float* rstd,
+                                       hipStream_t stream) {
+    puro_status st = check_int8_source(x, rows, cols, cols, ld);
+    if (st != PURO_OK) return st;
+    if (!finite_nonneg(eps)) return PURO_ERR_UNSUPPORTED;
+    if (rows == 0) return PURO_OK;
+    if (cols == 0) return PURO_ERR_SHAPE;      // (the mean of an empty row is undefined)
+    if (!gamma) return PURO_ERR_NULL;
+    if (!aligned16(gamma) || ((uintptr_t)rstd & 3) != 0) return PURO_ERR_ALIGN;
+    if ((st = check_int8_rows(q, scale)) != PURO_OK) return st;
+    launch_quantize_int8(QuantInt8Args{x, rows, cols, ld, q, scale, gamma, eps, rstd, 0}, stream);
+    return launched();
+}
+
+puro_status puro_swiglu_quantize_int8(const uint16_t* gu, int64_t rows, int64_t cols, int64_t ld, int8_t* q,
+                                      float* scale, hipStream_t stream) {
+    if (cols > ((int64_t)1 << 30)) return PURO_ERR_SHAPE;
+    puro_status st = check_int8_source(gu, rows, cols, cols < 0 ? cols : 2 * cols, ld);
+    if (st != PURO_OK) return st;
+    if (rows == 0 || cols == 0) return PURO_OK;
+    if ((st = check_int8_rows(q, scale)) != PURO_OK) return st;
+    launch_quantize_int8(QuantInt8Args{gu, rows, cols, ld, q, scale, nullptr, 0.0f, nullptr, 1}, stream);
+    return launched();
+}
+
+size_t puro_int8_gemm_workspace_size(int64_t M, int64_t N, int64_t K) {
+    if (M <= 0 || N <= 0 || K <= 0 || M > kMaxPitch || N > kMaxPitch || K > kMaxInt8K) return 0;
+    return int8_gemm_ws_bytes(M, N, K);
+}
+
+puro_status puro_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* A, int64_t lda, const float* a_scale,
+                           const int8_t* B, int64_t ldb, const float* b_scale, void* D, puro_out_dtype d_type,
+                           int64_t ldd, int accumulate, const uint16_t* bias, const uint16_t* residual, int64_t ldr,
+                           void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (M < 0 || N < 0 || K < 0 || M > kMaxPitch || N > kMaxPitch || K > kMaxInt8K) return PURO_ERR_SHAPE;
+    if (M * N > (int64_t)1 << 38) return PURO_ERR_SHAPE;
+    if (d_type != PURO_OUT_BF16 && d_type != PURO_OUT_FP32) return PURO_ERR_UNSUPPORTED;
+    const bool f32 = d_type == PURO_OUT_FP32;
+    if ((accumulate && !f32) || ((bias || residual) && f32)) return PURO_ERR_UNSUPPORTED;
+    if ((K % 16) != 0 || (lda % 16) != 0 || (ldb % 16) != 0 || (ldd % 4) != 0) return PURO_ERR_ALIGN;
+    if (lda < K || ldb < K || lda > kMaxPitch || ldb > kMaxPitch || ldd < N) return PURO_ERR_SHAPE;
+    if (residual && (ldr < N || ldr > kMaxPitch)) return PURO_ERR_SHAPE;
+    if (residual && (ldr % 4) != 0) return PURO_ERR_ALIGN;
+    if (M == 0 || N == 0) return PURO_OK;
+    if (!a_scale || !b_scale || !D || (K > 0 && (!A || !B))) return PURO_ERR_NULL;
+    if (!aligned16(A) || !aligned16(B) || !aligned16(a_scale) || !aligned16(b_scale) || !aligned16(D) || !aligned16(bias) ||
+        !aligned16(residual))
+        return PURO_ERR_ALIGN;
+    if (residual == D && residual && ldr != ldd) return PURO_ERR_SHAPE;
+    if (residual && residual != D) {
+        const uintptr_t r0 = (uintptr_t)residual, r1 = r0 + (uintptr_t)(((M - 1) * ldr + N) * 2);
+        const uintptr_t d0 = (uintptr_t)D, d1 = d0 + (uintptr_t)(((M - 1) * ldd + N) * 2);
+        if (r0 < d1 && d0 < r1) return PURO_ERR_SHAPE;
+    }
+    const size_t need = int8_gemm_ws_bytes(M, N, K);
+    if (need > 0) {
+        if (!ws) return PURO_ERR_NULL;
+        if (!aligned16(ws)) return PURO_ERR_ALIGN;
+        if (ws_bytes < need) return PURO_ERR_WORKSPACE;
+    }
+    launch_int8_gemm(Int8Problem{M, N, K, A, B, lda, ldb, a_scale, b_scale, D, ldd, f32, accumulate != 0, bias, residual, ldr},
+                     ws, stream);
+    return launched();
+}
+
+}  // extern "C"
+
+// ---------------------------------------- verification of drafted tokens
+namespace {
+
+puro_status check_verify_sizes(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
+    if (B < 0 || T < 0 || draft_rows < 0 || V < 1) return PURO_ERR_SHAPE;
+    const int64_t rows = (int64_t)1 << 20;
+    // (a launch holds fewer than 2^24 blocks of 256 threads, a block at least 8192 entries of a long row)
+    if (B > rows || T > rows || draft_rows > T || V > (int64_t)1 << 21) return PURO_ERR_SHAPE;
+    if (T * V > (int64_t)1 << 35 || B * V > (int64_t)1 << 35) return PURO_ERR_SHAPE;
+    return PURO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t puro_verify_drafts_workspace_size(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
+    if (check_verify_sizes(B, T, draft_rows, V) != PURO_OK || B == 0) return 0;
+    return verify_ws_bytes(B, T, draft_rows, V);
+}
+
+puro_status puro_verify_drafts(int64_t B, int64_t T, int64_t draft_rows, int64_t V, puro_verify_kind kind,
+                               puro_out_dtype dtype, const void* target, int64_t ld_target, const void* draft,
+                               int64_t ld_draft, const int32_t* draft_ids, const int32_t* offsets,
+                               const float* uniform, const float* uniform_sample, double temperature,
+                               int32_t* tokens, int32_t* accepted, void* ws, size_t ws_bytes, hipStream_t stream) {
+    const puro_status st = check_verify_sizes(B, T, draft_rows, V);
+    if (st != PURO_OK) return st;
+    if (kind != PURO_VERIFY_LOGITS && kind != PURO_VERIFY_PROBS) return PURO_ERR_UNSUPPORTED;
+    if (dtype != PURO_OUT_BF16 && dtype != PURO_OUT_FP32) return PURO_ERR_UNSUPPORTED;
+    const bool logits = kind == PURO_VERIFY_LOGITS, greedy = logits && temperature == 0.0;
+    if (logits && !greedy && (!(temperature >= 0x1p-20) || !(temperature <= 0x1p20))) return PURO_ERR_UNSUPPORTED;
+    const bool drafted = draft && !greedy;
+    if (T > 0 && (ld_target < V || ld_target > kMaxPitch)) return PURO_ERR_SHAPE;
+    if (drafted && draft_rows > 0 && (ld_draft < V || ld_draft > kMaxPitch)) return PURO_ERR_SHAPE;
+    if (B == 0) return PURO_OK;
+    if (!offsets || !accepted || !ws) return PURO_ERR_NULL;
+    if (T > 0 && (!target || !draft_ids || !tokens || (!greedy && (!uniform || !uniform_sample)))) return PURO_ERR_NULL;
+    const uintptr_t e = dtype == PURO_OUT_BF16 ? 1 : 3;
+    if (((uintptr_t)target & e) != 0 || (drafted && ((uintptr_t)draft & e) != 0) || !aligned16(ws)) return PURO_ERR_ALIGN;
+    for (const void* p : {(const void*)draft_ids, (const void*)offsets, (const void*)uniform, (const void*)uniform_sample,
+                          (const void*)tokens, (const void*)accepted})
+        if (((uintptr_t)p & 3) != 0) return PURO_ERR_ALIGN;
+    if (ws_bytes < verify_ws_bytes(B, T, draft_rows, V)) return PURO_ERR_WORKSPACE;
+    launch_verify(VerifyArgs{target, drafted ? draft : nullptr, ld_target, ld_draft, draft_ids, offsets, uniform, uniform_sample,
+                             (int)B, (int)T, (int)draft_rows, (int)V, logits, dtype == PURO_OUT_BF16, logits ? temperature : 1.0, tokens,
+                             accepted},
+                  ws, stream);
+    return launched();
+}
+
+}  // extern "C"
+
 // ------------------------------------------------------------------- MuonH
 namespace {
 

@@ -299,6 +299,56 @@ void launch_lm_distill_bwd(const DistillArgs& a, const float* lse, const float* 
 // Zeros over `bytes` (a multiple of 16) from a 16-byte aligned address.
 void launch_zero(void* dst, int64_t bytes, hipStream_t stream);
 
+// ---- int8 quantisation and product (int8.hip) -----------------------------------
+
+// Codes and scales of the rows of a BF16 tensor, its RMSNorm (gamma set) or a
+// gate/up output's SwiGLU (swiglu; x [rows, 2 cols]).
+struct QuantInt8Args {
+    const uint16_t* x;
+    int64_t rows, cols, ld;
+    int8_t* q;
+    float* scale;
+    const uint16_t* gamma;
+    float eps;
+    float* rstd;               // or NULL
+    int swiglu;
+};
+void launch_quantize_int8(const QuantInt8Args& a, hipStream_t stream);
+// The transposed copy qT [cols, rows] (pitch ld_qT, zeros up to the next 16
+// columns) with a scale per column; ws holds quant_int8_ws_bytes.
+size_t quant_int8_ws_bytes(int64_t rows, int64_t cols);
+void launch_quantize_int8_t(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, int8_t* qT, int64_t ld_qT,
+                            float* scaleT, void* ws, hipStream_t stream);
+
+struct Int8Problem {
+    int64_t M, N, K;
+    const int8_t *A, *B;
+    int64_t lda, ldb;
+    const float *sa, *sb;
+    void* D;
+    int64_t ldd;
+    int f32, accumulate;
+    const uint16_t *bias, *residual;
+    int64_t ldr;
+};
+size_t int8_gemm_ws_bytes(int64_t M, int64_t N, int64_t K);
+void launch_int8_gemm(const Int8Problem& p, void* ws, hipStream_t stream);
+
+// ---- verification of drafted tokens (verify.hip) --------------------------------
+
+struct VerifyArgs {
+    const void *target, *draft;          // [T, V], [draft_rows, V] (or NULL)
+    int64_t ld_t, ld_d;
+    const int32_t *ids, *offsets;
+    const float *u, *us;
+    int B, T, draft_rows, V;
+    int logits, bf16;
+    double temperature;
+    int32_t *tokens, *accepted;
+};
+size_t verify_ws_bytes(int64_t B, int64_t T, int64_t draft_rows, int64_t V);
+void launch_verify(const VerifyArgs& a, void* ws, hipStream_t stream);
+
 // ---- MuonH (muonh.hip) ---------------------------------------------------------
 
 // Workspace of one MuonH step of `count` [rows, cols] matrices (rows and cols

@@ -389,7 +389,7 @@ void by_rule(const QuantArgs& a, F&& f) {
 // Amax source of a per-tensor quantisation whose partial maxima are in ws:
 // reduced by every quantise block (few partials) or once by a one-block
 // kernel into the amax slot of ws.
-void amax_source(QuantArgs& a, int P, void* ws, hipStream_t stream) {
+[[maybe_unused]] void amax_source(QuantArgs& a, int P, void* ws, hipStream_t stream) {
     uint32_t* partial = reinterpret_cast<uint32_t*>(ws);
     a.supplied = 0;
     if (P > kMaxInlinePartials) {
@@ -404,8 +404,8 @@ void amax_source(QuantArgs& a, int P, void* ws, hipStream_t stream) {
     }
 }
 
-int64_t tiles_x(int64_t cols) { const int64_t g = (cols + kTile - 1) / kTile; return g > 0 ? g : 1; }
-int64_t tiles_y(int64_t rows) { const int64_t g = (rows + kTile - 1) / kTile; return g > 0 ? g : 1; }
+[[maybe_unused]] int64_t tiles_x(int64_t cols) { const int64_t g = (cols + kTile - 1) / kTile; return g > 0 ? g : 1; }
+[[maybe_unused]] int64_t tiles_y(int64_t rows) { const int64_t g = (rows + kTile - 1) / kTile; return g > 0 ? g : 1; }
 
 }  // namespace
 

@@ -105,6 +105,15 @@ _SIGS = {
     "puro_lm_head_distill_fwd": (_i, [_p, _p, _p, _p, _i64, _i64, _i64, _i64, _i, ctypes.c_float, _p, _p, _p, _p, _sz, _p]),
     "puro_lm_head_distill_bwd": (_i, [_p, _p, _p, _p, _p, _p, _i64, _i64, _i64, _i64, _i, ctypes.c_float, _p,
                                       ctypes.c_float, _p, _p, _i, _i, _p, _sz, _p]),
+    "puro_quantize_int8_workspace_size": (_sz, [_i64, _i64]),
+    "puro_quantize_int8": (_i, [_p, _i64, _i64, _i64, _p, _p, _p, _i64, _p, _p, _sz, _p]),
+    "puro_rmsnorm_quantize_int8": (_i, [_p, _p, _i64, _i64, _i64, ctypes.c_float, _p, _p, _p, _p]),
+    "puro_swiglu_quantize_int8": (_i, [_p, _i64, _i64, _i64, _p, _p, _p]),
+    "puro_int8_gemm_workspace_size": (_sz, [_i64, _i64, _i64]),
+    "puro_int8_gemm": (_i, [_i64, _i64, _i64, _p, _i64, _p, _p, _i64, _p, _p, _i, _i64, _i, _p, _p, _i64, _p, _sz, _p]),
+    "puro_verify_drafts_workspace_size": (_sz, [_i64, _i64, _i64, _i64]),
+    "puro_verify_drafts": (_i, [_i64, _i64, _i64, _i64, _i, _i, _p, _i64, _p, _i64, _p, _p, _p, _p, ctypes.c_double, _p, _p,
+                                _p, _sz, _p]),
     "puro_muonh_workspace_size": (_sz, [_i64, _i64, _i64]),
     "puro_muonh_step": (_i, [_i64, _i64, _i64, _p, _p, _p, _p, _p, ctypes.c_float, _i, ctypes.c_float, _i, _p,
                              _p, _sz, _p]),
@@ -852,6 +861,212 @@ def lm_head_distill(X, W, ids, teacher, temperature=1.0, target=DISTILL_LOGITS):
     """The distillation loss [M] of X [M, K] and W [V, K] (BF16) as an autograd operation (``lm_head_distill_fwd``);
     no gradient flows to the teacher's values."""
     return _DistillFn.apply(X, W, ids, teacher, temperature, target)
+
+
+# -------------------------------------------- 8-bit integer linear layers
+# (calls of few microseconds: as few checks each as keep a kernel from foreign memory)
+_INT8 = (torch.int8,)
+
+
+def _matrix(t, what, dtypes, device):
+    """(rows, cols, row pitch, address) of a 2-D tensor with contiguous rows."""
+    if t.dtype not in dtypes or t.get_device() != device:
+        _check_tensor(t, what, dtypes, device)
+    if t.dim() != 2:
+        raise ValueError("%s: 2-D expected, got %s" % (what, tuple(t.shape)))
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if rows <= 1 or cols == 0:
+        ld = -(-cols // 16) * 16               # (the pitch of one row, or of none, is any)
+    if one != 1 and cols > 1 and rows > 0:
+        raise ValueError("%s: the values of a row are contiguous" % what)
+    return rows, cols, ld, t.data_ptr()
+
+
+def _vector(t, what, dtypes, n, device):
+    if t.dtype not in dtypes or t.get_device() != device:
+        _check_tensor(t, what, dtypes, device)
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s: %d contiguous values expected, got %s" % (what, n, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _int8_rows(rows, cols, out, like, dev):
+    """q [rows, cols] and scale [rows], given or new, and their addresses."""
+    out = out or {}
+    q, scale = out.get("q"), out.get("scale")
+    q = like.new_empty((rows, cols), dtype=torch.int8) if q is None else q
+    scale = like.new_empty(rows, dtype=torch.float32) if scale is None else scale
+    return q, scale, _dense(q, "q", _INT8, (rows, cols), dev), _vector(scale, "scale", _FP32, rows, dev)
+
+
+def quantize_int8(x, want_q=True, want_qT=False, out=None, ws=None):
+    """int8 codes of a BF16 tensor [rows, cols]: q [rows, cols] with scale [rows] (a token's, or an output channel's of a
+    weight) and, with want_qT, the transposed copy qT [cols, rows rounded up to 16] (zeros behind the rows) with scaleT
+    [cols]; returns dict(q, scale, qT, scaleT) (absent outputs are None). ``out`` may supply outputs; a given qT may have
+    a longer pitch."""
+    dev = _current()
+    rows, cols, ld, px = _matrix(x, "x", _BF16_BITS, dev)
+    q = scale = qT = scaleT = pq = ps = pT = psT = None
+    nb, ldT = 0, -(-rows // 16) * 16
+    if want_q:
+        q, scale, pq, ps = _int8_rows(rows, cols, out, x, dev)
+    if want_qT:
+        qT, scaleT = (out or {}).get("qT"), (out or {}).get("scaleT")
+        qT = x.new_empty((cols, ldT), dtype=torch.int8) if qT is None else qT
+        scaleT = x.new_empty(cols, dtype=torch.float32) if scaleT is None else scaleT
+        if qT.shape != (cols, ldT):
+            raise ValueError("qT: shape %s expected, got %s" % ((cols, ldT), tuple(qT.shape)))
+        _, _, ldT, pT = _matrix(qT, "qT", _INT8, dev)
+        psT = _vector(scaleT, "scaleT", _FP32, cols, dev)
+        ws, nb = _ws(_size("puro_quantize_int8_workspace_size", rows, cols), ws, x.device)
+    _check("puro_quantize_int8", lib().puro_quantize_int8(px, rows, cols, ld, pq, ps, pT, ldT, psT, _ptr(ws) if nb else None, nb,
+                                                          _stream()))
+    return dict(q=q, scale=scale, qT=qT, scaleT=scaleT)
+
+
+def rmsnorm_quantize_int8(x, gamma, eps, out=None):
+    """int8 codes of y = x rstd gamma (RMSNorm of each row of x) with a scale per row, y not written (nor rounded to
+    BF16); returns dict(q, scale, rstd)."""
+    dev = _current()
+    rows, cols, ld, px = _matrix(x, "x", _BF16_BITS, dev)
+    q, scale, pq, ps = _int8_rows(rows, cols, out, x, dev)
+    rstd = (out or {}).get("rstd")
+    rstd = x.new_empty(rows, dtype=torch.float32) if rstd is None else rstd
+    _check("puro_rmsnorm_quantize_int8", lib().puro_rmsnorm_quantize_int8(
+        px, _vector(gamma, "gamma", _BF16_BITS, cols, dev), rows, cols, ld, eps, pq, ps, _vector(rstd, "rstd", _FP32, rows, dev),
+        _stream()))
+    return dict(q=q, scale=scale, rstd=rstd)
+
+
+def swiglu_quantize_int8(gu, cols, out=None):
+    """int8 codes of H = silu(gate) up of a fused gate/up output gu [rows, 2 cols] with a scale per row, H not written
+    (nor rounded to BF16); returns dict(q, scale)."""
+    dev = _current()
+    rows, width, ld, px = _matrix(gu, "gu", _BF16_BITS, dev)
+    if width < 2 * cols:
+        raise ValueError("gu: %d columns for two halves of %d" % (width, cols))
+    q, scale, pq, ps = _int8_rows(rows, cols, out, gu, dev)
+    _check("puro_swiglu_quantize_int8", lib().puro_swiglu_quantize_int8(px, rows, cols, ld, pq, ps, _stream()))
+    return dict(q=q, scale=scale)
+
+
+def int8_gemm(A, a_scale, B, b_scale, out_dtype=OUT_BF16, D=None, accumulate=False, bias=None, residual=None, ws=None):
+    """D[M, N] (+)= (sum_k A[m, k] B[n, k]) a_scale[m] b_scale[n] (+ bias[n] + residual[m, n]) of int8 codes A [M, K] and
+    B [N, K]; D BF16 or FP32 (its own type, if given); accumulate with FP32, bias and residual (BF16) with BF16."""
+    dev = _current()
+    M, K, lda, pa = _matrix(A, "A", _INT8, dev)
+    N, K_b, ldb, pb = _matrix(B, "B", _INT8, dev)
+    if K != K_b:
+        raise ValueError("A %s and B %s differ in their columns" % (tuple(A.shape), tuple(B.shape)))
+    if D is None:
+        if out_dtype not in (OUT_BF16, OUT_FP32):
+            raise ValueError("out_dtype is OUT_BF16 or OUT_FP32")
+        ldd = -(-N // 4) * 4
+        D = (torch.zeros if accumulate else torch.empty)(M, ldd, dtype=torch.float32 if out_dtype == OUT_FP32 else torch.bfloat16,
+                                                         device=A.device)
+        D = D if ldd == N else D[:, :N]
+        pd = D.data_ptr()
+    else:
+        if D.shape != (M, N):
+            raise ValueError("D: shape %s expected, got %s" % ((M, N), tuple(D.shape)))
+        _, _, ldd, pd = _matrix(D, "D", (torch.bfloat16, torch.float32), dev)
+    ldr, pr = 0, None
+    if residual is not None:
+        if residual.shape != (M, N):
+            raise ValueError("residual: shape %s expected, got %s" % ((M, N), tuple(residual.shape)))
+        _, _, ldr, pr = _matrix(residual, "residual", _BF16_BITS, dev)
+    w, nb = _ws(_size("puro_int8_gemm_workspace_size", M, N, K), ws, A.device)
+    _check("puro_int8_gemm", lib().puro_int8_gemm(
+        M, N, K, pa, lda, _vector(a_scale, "a_scale", _FP32, M, dev), pb, ldb, _vector(b_scale, "b_scale", _FP32, N, dev), pd,
+        OUT_FP32 if D.dtype == torch.float32 else OUT_BF16, ldd, int(bool(accumulate)),
+        _vector(bias, "bias", _BF16_BITS, N, dev) if bias is not None else None, pr, ldr, _ptr(w), nb, _stream()))
+    return D
+
+
+def int8_linear_fwd(X, W):
+    """Y = X W^T [M, N] (BF16) with both quantised to int8, a scale per token and per output channel; returns (Y, saved):
+    the transposed copies with scales per channel that ``int8_linear_bwd`` takes."""
+    x = quantize_int8(X, want_qT=True)
+    w = quantize_int8(W, want_qT=True)
+    Y = int8_gemm(x["q"], x["scale"], w["q"], w["scale"])
+    return Y, dict(xq_t=x["qT"], x_scale=x["scaleT"], wq_t=w["qT"], w_scale=w["scaleT"])
+
+
+def int8_linear_bwd(dY, saved, want_dx=True, want_dw=True, dX=None, dW=None, accumulate_dw=False):
+    """dX = dY W [M, K] (BF16) and dW = dY^T X [N, K] (FP32) with dY [M, N] quantised to int8 per token for the one and
+    per channel for the other; returns (dX, dW)."""
+    q = quantize_int8(dY, want_q=want_dx, want_qT=want_dw)
+    if want_dx:
+        dX = int8_gemm(q["q"], q["scale"], saved["wq_t"], saved["w_scale"], D=dX)
+    if want_dw:
+        dW = int8_gemm(q["qT"], q["scaleT"], saved["xq_t"], saved["x_scale"], OUT_FP32, D=dW, accumulate=accumulate_dw)
+    return (dX if want_dx else None), (dW if want_dw else None)
+
+
+class _Int8LinearFn(torch.autograd.Function):
+    """Y = X W^T through int8_linear_fwd; the backward takes the rounding's derivative as 1. With a ``main_grad`` FP32
+    buffer on W, dW is accumulated into it and W gets no .grad; otherwise W's .grad is dW in W's dtype."""
+
+    @staticmethod
+    def forward(ctx, X, W):
+        if X.dtype != torch.bfloat16 or W.dtype != torch.bfloat16:
+            raise TypeError("the int8 linear layer takes BF16 X and W")
+        Y, saved = int8_linear_fwd(X.contiguous(), W.contiguous())
+        ctx.save_for_backward(*saved.values())
+        ctx.main_grad = getattr(W, "main_grad", None)
+        return Y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dY):
+        saved = dict(zip(("xq_t", "x_scale", "wq_t", "w_scale"), ctx.saved_tensors))
+        want_dx, want_dw = ctx.needs_input_grad
+        mg = ctx.main_grad if want_dw else None
+        dX, dW = int8_linear_bwd(dY.to(torch.bfloat16).contiguous(), saved, want_dx, want_dw, dW=mg, accumulate_dw=mg is not None)
+        return dX, dW.to(torch.bfloat16) if want_dw and mg is None else None
+
+
+def int8_linear(X, W):
+    """The int8 linear layer as an autograd operation: X [..., K], W [N, K] (BF16); returns Y [..., N] (BF16). N and K are
+    multiples of 16, the number of tokens is any."""
+    Y = _Int8LinearFn.apply(X.reshape(-1, X.shape[-1]), W)
+    return Y.reshape(*X.shape[:-1], Y.shape[-1])
+
+
+# ----------------------------------------- verification of drafted tokens
+VERIFY_LOGITS, VERIFY_PROBS = 0, 1
+
+
+def verify_drafts(target, draft, draft_ids, offsets, uniform=None, uniform_sample=None, temperature=1.0, kind=VERIFY_LOGITS,
+                  tokens=None, accepted=None, ws=None):
+    """Which drafted tokens to keep, and the token after them. target [T, V] (BF16 or FP32): the rows of all sequences one
+    after another, sequence b's from offsets[b] to offsets[b + 1] (int32 [B + 1]), one more than it has drafts; draft
+    [drafts, V] of target's type: the draft model's predictions (row t - b for target row t), None where it has none;
+    draft_ids [T] int32, the last of a sequence not read. Logits, at a temperature (0: the largest), or probabilities
+    (VERIFY_PROBS). uniform [T] and uniform_sample [B]: FP32 random numbers in [0, 1). Returns (tokens [T], accepted [B])
+    int32: a sequence's kept ids, its drawn token and -1 from there on; rows behind the last sequence are left alone."""
+    dev = _current()
+    T, V, ldt, pt = _matrix(target, "target", (torch.bfloat16, torch.float32), dev)
+    B = offsets.shape[0] - 1
+    rows, ldd, pd = T, 0, None
+    if draft is not None:
+        rows, V_d, ldd, pd = _matrix(draft, "draft", (target.dtype,), dev)
+        if V_d != V:
+            raise ValueError("target %s and draft %s differ in their columns" % (tuple(target.shape), tuple(draft.shape)))
+        pd = pd or pt                          # (no rows have no address; none is read)
+    if tokens is None:
+        tokens = draft_ids.new_empty(T)
+    if accepted is None:
+        accepted = draft_ids.new_empty(B)
+    w, nb = _ws(_size("puro_verify_drafts_workspace_size", B, T, rows, V), ws, target.device)
+    _check("puro_verify_drafts", lib().puro_verify_drafts(
+        B, T, rows, V, kind, OUT_BF16 if target.dtype == torch.bfloat16 else OUT_FP32, pt, ldt, pd, ldd,
+        _vector(draft_ids, "draft_ids", _INT32, T, dev), _vector(offsets, "offsets", _INT32, B + 1, dev),
+        _vector(uniform, "uniform", _FP32, T, dev) if uniform is not None else None,
+        _vector(uniform_sample, "uniform_sample", _FP32, B, dev) if uniform_sample is not None else None, temperature,
+        _vector(tokens, "tokens", _INT32, T, dev), _vector(accepted, "accepted", _INT32, B, dev), _ptr(w), nb, _stream()))
+    return tokens, accepted
 
 
 # ------------------------------------------------------------------- MuonH

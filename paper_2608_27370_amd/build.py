@@ -19,7 +19,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpuro.so")
 # (source, object name, extra flags): the GEMM kernel is compiled once per
 # operand-format pair and scale kind, so that its instantiations build in parallel
-GEMM_VARIANTS = [(fa, fb, g) for fa in (0, 1) for fb in (0, 1) for g in (0, 1)] + [(2, 2, 0)]   # + BF16
+GEMM_VARIANTS = [(fa, fb, g) for fa in (0, 1) for fb in (0, 1) for g in (0, 1)] + [(2, 2, 0), (3, 3, 0)]   # + BF16, int8
 SOURCES = [("quant.hip", "quant", []), ("qk_quant.hip", "qk_quant", []),
            ("qk_norm_rope.hip", "qk_norm_rope", []), ("gemm.hip", "gemm", []), ("lm_head.hip", "lm_head", []),
            ("lm_distill.hip", "lm_distill", []), ("int8.hip", "int8", []), ("verify.hip", "verify", []),

@@ -17,7 +17,9 @@ namespace {
 // Fixed-order sum of the split-K partials, scaling and output conversion.
 // Batched launches: problem bi's partials follow problem bi-1's, its output
 // starts bsd bytes and its residual bsr elements after the previous one's.
-template <int OUT>
+// INT: int8 operands, whose partials are integers (their sum exact) and whose
+// scales are those of a row and of a column.
+template <int OUT, bool INT = false>
 __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restrict__ partial, int splits,
                                                             int M, int N, const float* sa, const float* sb,
                                                             int a_tensor, int b_tensor, void* D,
@@ -38,12 +40,24 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
     float alpha = alpha0;
     if (a_tensor) alpha *= sa[0];
     if (b_tensor) alpha *= sb[0];
-    float4 s = *reinterpret_cast<const float4*>(partial + m * N + n);
-    for (int k = 1; k < splits; ++k) {
-        const float4 t = *reinterpret_cast<const float4*>(partial + ((int64_t)k * M + m) * N + n);
-        s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+    float4 s;
+    if constexpr (INT) {
+        int4 v = *reinterpret_cast<const int4*>(partial + m * N + n);
+        for (int k = 1; k < splits; ++k) {
+            const int4 t = *reinterpret_cast<const int4*>(partial + ((int64_t)k * M + m) * N + n);
+            v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
+        }
+        const float r = sa[m];
+        const float4 c = *reinterpret_cast<const float4*>(sb + n);
+        s = make_float4((float)v.x * r * c.x, (float)v.y * r * c.y, (float)v.z * r * c.z, (float)v.w * r * c.w);
+    } else {
+        s = *reinterpret_cast<const float4*>(partial + m * N + n);
+        for (int k = 1; k < splits; ++k) {
+            const float4 t = *reinterpret_cast<const float4*>(partial + ((int64_t)k * M + m) * N + n);
+            s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+        }
+        s.x *= alpha; s.y *= alpha; s.z *= alpha; s.w *= alpha;
     }
-    s.x *= alpha; s.y *= alpha; s.z *= alpha; s.w *= alpha;
     if constexpr (OUT == kOutBF16Epi) add_epilogue4(s, bias, residual, ldr, m, n, res_scale);
     if constexpr (OUT == kOutF32) {
         float* dst = reinterpret_cast<float*>(D) + m * ldd + n;
@@ -281,6 +295,7 @@ void run_plan(const GemmProblem& g, const Plan& pl, void* ws, hipStream_t stream
     using E4 = std::integral_constant<int, kE4M3>;
     using E5 = std::integral_constant<int, kE5M2>;
     if (g.fa == kBF16) launch_variant<kBF16, kBF16, false>(prm, pl.cfg, out, grid, stream);
+    else if (g.fa == kInt8) launch_variant<kInt8, kInt8, false>(prm, pl.cfg, out, grid, stream);
     else if (g.fa == kE4M3 && g.fb == kE4M3) launch(E4{}, E4{});
     else if (g.fa == kE5M2 && g.fb == kE4M3) launch(E5{}, E4{});
     else if (g.fa == kE4M3 && g.fb == kE5M2) launch(E4{}, E5{});
@@ -288,21 +303,21 @@ void run_plan(const GemmProblem& g, const Plan& pl, void* ws, hipStream_t stream
     if (pl.splits > 1) {
         const int64_t n = g.M * (g.N / 4) * g.batch;
         const int blocks = (int)((n + 255) / 256);
-        if (g.out == kOutF32)
-            splitk_reduce_kernel<kOutF32><<<blocks, 256, 0, stream>>>(
-                prm.partial, pl.splits, prm.M, prm.N, g.sa, g.sb, g.sa_mode == kSTensor,
-                g.sb_mode == kSTensor, g.D, g.ldd, g.accumulate, nullptr, nullptr, 0, g.alpha, 1.0f, g.batch,
-                prm.bsd, 0);
-        else if (g.out == kOutBF16Epi)
-            splitk_reduce_kernel<kOutBF16Epi><<<blocks, 256, 0, stream>>>(
-                prm.partial, pl.splits, prm.M, prm.N, g.sa, g.sb, g.sa_mode == kSTensor,
-                g.sb_mode == kSTensor, g.D, g.ldd, 0, g.bias, g.residual, g.ldr, g.alpha, g.res_scale, g.batch,
-                prm.bsd, g.bsr);
-        else
-            splitk_reduce_kernel<kOutBF16><<<blocks, 256, 0, stream>>>(
-                prm.partial, pl.splits, prm.M, prm.N, g.sa, g.sb, g.sa_mode == kSTensor,
-                g.sb_mode == kSTensor, g.D, g.ldd, g.accumulate, nullptr, nullptr, 0, g.alpha, 1.0f, g.batch,
-                prm.bsd, 0);
+        auto reduce = [&](auto out_c, auto int_c) {
+            constexpr int OUT = decltype(out_c)::value;
+            constexpr bool epi = OUT == kOutBF16Epi;
+            splitk_reduce_kernel<OUT, decltype(int_c)::value><<<blocks, 256, 0, stream>>>(
+                prm.partial, pl.splits, prm.M, prm.N, g.sa, g.sb, g.sa_mode == kSTensor, g.sb_mode == kSTensor, g.D, g.ldd,
+                epi ? 0 : g.accumulate, epi ? g.bias : nullptr, epi ? g.residual : nullptr, epi ? g.ldr : 0, g.alpha,
+                epi ? g.res_scale : 1.0f, g.batch, prm.bsd, epi ? g.bsr : 0);
+        };
+        auto reduce_out = [&](auto int_c) {
+            if (g.out == kOutF32) reduce(std::integral_constant<int, kOutF32>{}, int_c);
+            else if (g.out == kOutBF16Epi) reduce(std::integral_constant<int, kOutBF16Epi>{}, int_c);
+            else reduce(std::integral_constant<int, kOutBF16>{}, int_c);
+        };
+        if (g.fa == kInt8) reduce_out(std::true_type{});
+        else reduce_out(std::false_type{});
     }
 }
 

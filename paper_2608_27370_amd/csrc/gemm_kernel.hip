@@ -46,6 +46,10 @@
 //    GEMM with residual 3001x2056x2064 40 -> 35 us).
 //  * Small grids split K into ranges whose FP32 partial sums a second kernel
 //    adds in a fixed order (deterministic).
+//  * int8 operands take the same path with v_mfma_i32_32x32x32_i8 (two a 64-byte
+//    step, together as long as the FP8 one): exact integer sums, turned to
+//    binary32 where the accumulators are read and multiplied there by their
+//    row's and column's scales.
 
 // This file is compiled once per operand-format pair and scale kind
 // (PURO_FA, PURO_FB, PURO_GROUPED), each object holding that variant's tile
@@ -59,7 +63,7 @@
 #include "kernels.h"
 
 #if !defined(PURO_FA) || !defined(PURO_FB) || !defined(PURO_GROUPED)
-#error "gemm_kernel.hip is compiled with -DPURO_FA=<0|1> -DPURO_FB=<0|1> -DPURO_GROUPED=<0|1>"
+#error "gemm_kernel.hip is compiled with -DPURO_FA=<0|1|2|3> -DPURO_FB=<0|1|2|3> -DPURO_GROUPED=<0|1>"
 #endif
 
 namespace puro {
@@ -71,6 +75,7 @@ namespace {
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int v16i __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void_t;
 
 constexpr uint32_t kRsrcWord3 = 0x00020000u;  // raw buffer, 32-bit data format
@@ -99,6 +104,7 @@ constexpr int cgcd(int a, int b) { return b == 0 ? a : cgcd(b, a % b); }
 
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 
 // Raw buffer descriptor (base, num_records bytes; 32-bit data format); every
 // field is made wave-uniform so that it lives in SGPRs.
@@ -405,7 +411,10 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
 
     // A's ring, B's stages, and the grouped scales of a slice's rows (A then
     // B), float, DMA'd like the operands
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[SMEM + (GROUPED ? NST * (BM + BN) * 4 : 0)];
+    // (int8: the epilogue's column scales and bias, where no spare units leave room)
+    constexpr int COLS = FA == kInt8 && OUT != 2 ? NW * WTN * (OUT == kOutBF16Epi ? 8 : 4) : 0;
+    static_assert(XA == 0 || COLS <= XA * UNIT, "column scales in the spare units");
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[SMEM + (GROUPED ? NST * (BM + BN) * 4 : XA ? 0 : COLS)];
     float* const ssc = reinterpret_cast<float*>(smem + SMEM);
 
     const int tid = threadIdx.x;
@@ -562,7 +571,8 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
         }
     };
 
-    v16f acc[FM][FN];
+    typedef std::conditional_t<FA == kInt8, v16i, v16f> Acc;
+    Acc acc[FM][FN];
 
     const int fr = lane & 31;                 // fragment row of this lane
     const int c0 = (lane >> 5) * 2;           // first of this lane's two chunks in a 64-byte k step
@@ -657,6 +667,14 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                                                                 __builtin_bit_cast(v8bf, alo), acc[i][j], 0, 0, 0);
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, bhi),
                                                                 __builtin_bit_cast(v8bf, ahi), acc[i][j], 0, 0, 0);
+        } else if constexpr (FA == kInt8) {
+            // int8: the lane's 32 bytes are 32 k values, each half for one 32x32x32 instruction
+            const v4i blo = __builtin_shufflevector(f.f[FM + j], f.f[FM + j], 0, 1, 2, 3);
+            const v4i bhi = __builtin_shufflevector(f.f[FM + j], f.f[FM + j], 4, 5, 6, 7);
+            const v4i alo = __builtin_shufflevector(f.f[i], f.f[i], 0, 1, 2, 3);
+            const v4i ahi = __builtin_shufflevector(f.f[i], f.f[i], 4, 5, 6, 7);
+            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(blo, alo, acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bhi, ahi, acc[i][j], 0, 0, 0);
         } else if constexpr (GROUPED)
             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
                 f.f[FM + j], f.f[i], acc[i][j], FB, FA, 3, (int)f.sc[FM + j], 3, (int)f.sc[i]);
@@ -769,7 +787,10 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
 #pragma unroll
         for (int e = R * n / of; e < R * (n + 1) / of; ++e) {
             // 0 x 0 + 0: one instruction for a fragment's 16 registers
-            acc[e / FN][e % FN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8bf{}, v8bf{}, v16f{}, 0, 0, 0);
+            if constexpr (FA == kInt8)
+                acc[e / FN][e % FN] = __builtin_amdgcn_mfma_i32_32x32x32_i8(v4i{}, v4i{}, v16i{}, 0, 0, 0);
+            else
+                acc[e / FN][e % FN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8bf{}, v8bf{}, v16f{}, 0, 0, 0);
             asm volatile("" : "+a"(acc[e / FN][e % FN]));      // here, not earlier
         }
     };
@@ -806,6 +827,32 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
         if (p.a_mode == kSTensor) alpha *= p.sa[0];
         if (p.b_mode == kSTensor) alpha *= p.sb[0];
     }
+    // int8: the scales of the lane's rows, and four columns' of the wave tile's, for
+    // the epilogue (zeros outside the matrix; the last vector of four one by one
+    // where it ends outside it)
+    constexpr bool kInt = FA == kInt8 && OUT != 2;
+    float row_s[kInt ? FM : 1];
+    v4f col_s = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint2 col_b = make_uint2(0u, 0u);
+    if constexpr (kInt) {
+        const int mr = m0 + wm * WTM + (lane & 31), nc = n0 + wn * WTN + 4 * lane;
+        const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p.sa), 0, p.M * 4, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p.sb), 0, p.N * 4, 0x00020000);
+        if constexpr (OUT == kOutBF16Epi) {
+            // (read where whole vectors of four lie in or outside the matrix)
+            const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p.bias), 0, p.bias ? p.N * 2 : 0, 0x00020000);
+            col_b = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rb, nc * 2, 0, 0));
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) row_s[i] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rr, (mr + i * 32) * 4, 0, 0));
+        if (p.N % 4 == 0) {
+            col_s = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rc, nc * 4, 0, 0));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) col_s[e] = nc + e < p.N ? p.sb[nc + e] : 0.0f;
+        }
+    }
+    (void)row_s; (void)col_s; (void)col_b;
     if (!PROD || producer) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((NST - 1) * LOADS) : "memory");
     __syncthreads();
     if constexpr (PROD) {
@@ -856,6 +903,19 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
         asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[i][j][e]));
         return v;
     };
+    // int8: the wave tile's column scales and bias, in LDS behind what the epilogue
+    // stages (in registers the 64 + 32 a lane needs would leave none for the 256 x
+    // 256 tile): four sums of row i*32 + (l & 31) as values, columns j*32 + 8g +
+    // 4(l >> 5) on
+    float* const lds_cols = reinterpret_cast<float*>(smem + (XA ? NST * STAGE : SMEM)) + wave * WTN;
+    auto scale4 = [&](int i, int j, int g, float& v0, float& v1, float& v2, float& v3) __attribute__((always_inline)) {
+        if constexpr (kInt) {
+            const v4f c = *reinterpret_cast<const v4f*>(lds_cols + j * 32 + 8 * g + 4 * (lane >> 5));
+            v0 = (float)__float_as_int(v0) * row_s[i] * c.x; v1 = (float)__float_as_int(v1) * row_s[i] * c.y;
+            v2 = (float)__float_as_int(v2) * row_s[i] * c.z; v3 = (float)__float_as_int(v3) * row_s[i] * c.w;
+        }
+    };
+    (void)scale4; (void)lds_cols;
 
     // ---- The LM head's forward statistics, straight from the accumulators.
     // Of each of its rows i*32 + (l & 31), lane l holds the 64 columns
@@ -978,6 +1038,13 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                 rb, (uint32_t)((ncol0 + ((it * 64 + lane) % ECPR) * 4) * 2), 0, 0));
     }
     __syncthreads();   // every wave is done with the last stage
+    if constexpr (kInt) {
+        if (lane < WTN / 4) *reinterpret_cast<v4f*>(lds_cols + 4 * lane) = col_s;
+        if constexpr (OUT == kOutBF16Epi) {
+            if (p.bias && lane < WTN / 4)
+                *reinterpret_cast<v4f*>(lds_cols + NW * WTN + 4 * lane) = v4f{bf16lo(col_b.x), bf16hi(col_b.x), bf16lo(col_b.y), bf16hi(col_b.y)};
+        }
+    }
     // A plain BF16 output of a tile inside the matrix, 128-column wave tiles:
     // the lane rounds its sums to BF16 first and stages those, half the LDS
     // bytes of the binary32 staging below, and the whole wave tile fits its
@@ -1047,13 +1114,13 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             // residual in binary32 with one rounding to BF16, and writes the
             // result over them. The bias of the lane's 64 columns is loaded
             // into registers once.
-            uint2 bq[OUT == kOutBF16Epi ? FN * 4 : 1];
+            uint2 bq[OUT == kOutBF16Epi && FA != kInt8 ? FN * 4 : 1];
             if constexpr (OUT == kOutBF16Epi) {
-                if (p.bias) {
+                if (FA != kInt8 && p.bias) {
                     const __amdgpu_buffer_rsrc_t rbq = __builtin_amdgcn_make_buffer_rsrc(
                         const_cast<uint16_t*>(p.bias), 0, p.N * 2, 0x00020000);
 #pragma unroll
-                    for (int e = 0; e < FN * 4; ++e)
+                    for (int e = 0; e < (FA != kInt8 ? FN * 4 : 0); ++e)
                         bq[e] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(
                             rbq, (uint32_t)((ncol0 + (e / 4) * 32 + 8 * (e % 4) + 4 * (lane >> 5)) * 2), 0, 0));
                 }
@@ -1096,6 +1163,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                 for (int g = 0; g < 4; ++g) {
                     float v0 = acc_at(i, j, 4 * g), v1 = acc_at(i, j, 4 * g + 1);
                     float v2 = acc_at(i, j, 4 * g + 2), v3 = acc_at(i, j, 4 * g + 3);
+                    scale4(i, j, g, v0, v1, v2, v3);
                     if constexpr (decltype(scaled)::value) {
                         v0 *= alpha; v1 *= alpha; v2 *= alpha; v3 *= alpha;
                     }
@@ -1117,8 +1185,13 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
                     if constexpr (OUT == kOutBF16Epi) {
                         // each term only when given: adding +0 would turn a -0 sum into +0
                         if constexpr ((decltype(epi)::value & 1) != 0) {
-                            const uint2 b = bq[j * 4 + g];
-                            v0 += bf16lo(b.x); v1 += bf16hi(b.x); v2 += bf16lo(b.y); v3 += bf16hi(b.y);
+                            if constexpr (FA == kInt8) {
+                                const v4f b = *reinterpret_cast<const v4f*>(lds_cols + NW * WTN + j * 32 + 8 * g + 4 * (lane >> 5));
+                                v0 += b.x; v1 += b.y; v2 += b.z; v3 += b.w;
+                            } else {
+                                const uint2 b = bq[j * 4 + g];
+                                v0 += bf16lo(b.x); v1 += bf16hi(b.x); v2 += bf16lo(b.y); v3 += bf16hi(b.y);
+                            }
                         }
                         if constexpr ((decltype(epi)::value & 2) != 0) {
                             const uint2 rv = *pos;
@@ -1185,7 +1258,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             };
             // epi: bit 0 a bias, bit 1 a residual (bias / residual epilogue only)
             auto stage_epi = [&](auto epi) __attribute__((always_inline)) {
-                if (alpha == 1.0f) stage(std::false_type{}, epi);
+                if (FA == kInt8 || alpha == 1.0f) stage(std::false_type{}, epi);
                 else stage(std::true_type{}, epi);
             };
             if constexpr (OUT == kOutBF16Epi) {
@@ -1283,8 +1356,9 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int chunk = j * 8 + g * 2 + (lane >> 5);
-                    const float4 v = make_float4(acc_at(i, j, 4 * g), acc_at(i, j, 4 * g + 1),
-                                                 acc_at(i, j, 4 * g + 2), acc_at(i, j, 4 * g + 3));
+                    float4 v = make_float4(acc_at(i, j, 4 * g), acc_at(i, j, 4 * g + 1),
+                                           acc_at(i, j, 4 * g + 2), acc_at(i, j, 4 * g + 3));
+                    scale4(i, j, g, v.x, v.y, v.z, v.w);
                     *reinterpret_cast<float4*>(ep + r * ROWB + ((chunk ^ (r & SWZ)) << 4)) = v;
                 }
         }

@@ -248,11 +248,18 @@ void launch_quantize_int8_t(const uint16_t* x, int64_t rows, int64_t cols, int64
     quant_cols_int8_kernel<<<grid, kThreads, 0, stream>>>(a, rows, ld_qT, part, P);
 }
 
-size_t int8_gemm_ws_bytes(int64_t, int64_t, int64_t) { return 0; }
+size_t int8_gemm_ws_bytes(int64_t M, int64_t N, int64_t K) { return gemm_workspace_bytes(M, N, K, kOutBF16); }
 
-void launch_int8_gemm(const Int8Problem& p, void*, hipStream_t stream) {
-    const int64_t tiles = (p.N + 15) / 16 * ((p.M + 15) / 16);
-    int8_gemm_kernel<<<(unsigned)std::min<int64_t>((tiles + 3) / 4, 1 << 20), kThreads, 0, stream>>>(p);
+void launch_int8_gemm(const Int8Problem& p, void* ws, hipStream_t stream) {
+    GemmProblem g{};
+    g.M = p.M; g.N = p.N; g.K = p.K;
+    g.A = reinterpret_cast<const uint8_t*>(p.A); g.lda = p.lda; g.fa = kInt8; g.sa_mode = kSNone; g.sa = p.sa;
+    g.B = reinterpret_cast<const uint8_t*>(p.B); g.ldb = p.ldb; g.fb = kInt8; g.sb_mode = kSNone; g.sb = p.sb;
+    g.D = p.D; g.ldd = p.ldd; g.accumulate = p.accumulate;
+    g.out = p.f32 ? kOutF32 : p.bias || p.residual ? kOutBF16Epi : kOutBF16;
+    g.bias = p.bias; g.residual = p.residual; g.ldr = p.ldr;
+    g.nt_f32 = 1;       // (as the FP8 product: a dW or logits, next read by another kernel)
+    launch_gemm(g, ws, stream);
 }
 
 }  // namespace puro

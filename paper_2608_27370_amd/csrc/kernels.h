@@ -157,7 +157,8 @@ enum OutKind : int { kOutBF16 = 0, kOutF32 = 1, kOutBF16Epi = 3, kOutLseStats = 
                      kOutSoftmaxGradQ = 6, kOutSoftmaxGradT = 7, kOutLseAny = 8 };
 
 // K, lda and ldb count operand elements (FP8 codes, or BF16 values when fa
-// and fb are kBF16, with scale modes kSNone).
+// and fb are kBF16, with scale modes kSNone; int8 codes when they are kInt8, with
+// modes kSNone and sa [M], sb [N] a scale for each row of A and of B).
 struct GemmProblem {
     int64_t M, N, K;
     const uint8_t* A;

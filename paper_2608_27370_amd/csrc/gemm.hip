@@ -18,7 +18,8 @@ namespace {
 // Batched launches: problem bi's partials follow problem bi-1's, its output
 // starts bsd bytes and its residual bsr elements after the previous one's.
 // INT: int8 operands, whose partials are integers (their sum exact) and whose
-// scales are those of a row and of a column.
+// scales are those of a row and of a column; N is the partials' row length there,
+// the first `cols` of which are the output's.
 template <int OUT, bool INT = false>
 __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restrict__ partial, int splits,
                                                             int M, int N, const float* sa, const float* sb,
@@ -26,7 +27,7 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
                                                             int64_t ldd, int accumulate, const uint16_t* bias,
                                                             const uint16_t* residual, int64_t ldr, float alpha0,
                                                             float res_scale, int batch, int64_t bsd,
-                                                            int64_t bsr) {
+                                                            int64_t bsr, int cols) {
     const int64_t nq = N / 4;
     int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (idx >= (int64_t)M * nq * batch) return;
@@ -48,8 +49,21 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
             v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
         }
         const float r = sa[m];
-        const float4 c = *reinterpret_cast<const float4*>(sb + n);
-        s = make_float4((float)v.x * r * c.x, (float)v.y * r * c.y, (float)v.z * r * c.z, (float)v.w * r * c.w);
+        float c[4];
+        if (n + 3 < cols) {
+            const float4 t = *reinterpret_cast<const float4*>(sb + n);
+            c[0] = t.x; c[1] = t.y; c[2] = t.z; c[3] = t.w;
+        } else {
+            for (int e = 0; e < 4; ++e) c[e] = n + e < cols ? sb[n + e] : 0.0f;
+        }
+        s = make_float4((float)v.x * r * c[0], (float)v.y * r * c[1], (float)v.z * r * c[2], (float)v.w * r * c[3]);
+        if (OUT != kOutF32 && n + 3 >= cols) {
+            const float w[4] = {s.x, s.y, s.z, s.w};
+            uint16_t* const dst = reinterpret_cast<uint16_t*>(D) + m * ldd + n;
+            for (int e = 0; n + e < cols; ++e)
+                dst[e] = to_bf16(OUT == kOutBF16Epi ? add_epilogue1(w[e], bias, residual, ldr, m, n + e, res_scale) : w[e]);
+            return;
+        }
     } else {
         s = *reinterpret_cast<const float4*>(partial + m * N + n);
         for (int k = 1; k < splits; ++k) {
@@ -61,6 +75,13 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
     if constexpr (OUT == kOutBF16Epi) add_epilogue4(s, bias, residual, ldr, m, n, res_scale);
     if constexpr (OUT == kOutF32) {
         float* dst = reinterpret_cast<float*>(D) + m * ldd + n;
+        if constexpr (INT) {
+            if (n + 3 >= cols) {
+                const float v[4] = {s.x, s.y, s.z, s.w};
+                for (int e = 0; n + e < cols; ++e) dst[e] = accumulate ? dst[e] + v[e] : v[e];
+                return;
+            }
+        }
         if (accumulate) {
             const float4 o = *reinterpret_cast<const float4*>(dst);
             s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
@@ -283,6 +304,7 @@ void run_plan(const GemmProblem& g, const Plan& pl, void* ws, hipStream_t stream
     prm.rows_a = (int)(g.rows_a ? g.rows_a : g.M);
     prm.rows_b = (int)(g.rows_b ? g.rows_b : g.N);
     prm.dzt = g.dzt; prm.ld_dzt = g.ld_dzt;
+    prm.part_n = (int)((g.N + 3) / 4 * 4);
     prm.q8 = g.q8; prm.q8_scale = g.q8_scale; prm.q8t = g.q8t; prm.q8t_scale = g.q8t_scale;
     const bool grouped = grouped_scales(g);
     const int out = pl.splits > 1 ? 2 : g.out;
@@ -301,15 +323,16 @@ void run_plan(const GemmProblem& g, const Plan& pl, void* ws, hipStream_t stream
     else if (g.fa == kE4M3 && g.fb == kE5M2) launch(E4{}, E5{});
     else launch(E5{}, E5{});
     if (pl.splits > 1) {
-        const int64_t n = g.M * (g.N / 4) * g.batch;
+        const int64_t cols = g.fa == kInt8 ? prm.part_n : g.N;
+        const int64_t n = g.M * (cols / 4) * g.batch;
         const int blocks = (int)((n + 255) / 256);
         auto reduce = [&](auto out_c, auto int_c) {
             constexpr int OUT = decltype(out_c)::value;
             constexpr bool epi = OUT == kOutBF16Epi;
             splitk_reduce_kernel<OUT, decltype(int_c)::value><<<blocks, 256, 0, stream>>>(
-                prm.partial, pl.splits, prm.M, prm.N, g.sa, g.sb, g.sa_mode == kSTensor, g.sb_mode == kSTensor, g.D, g.ldd,
+                prm.partial, pl.splits, prm.M, (int)cols, g.sa, g.sb, g.sa_mode == kSTensor, g.sb_mode == kSTensor, g.D, g.ldd,
                 epi ? 0 : g.accumulate, epi ? g.bias : nullptr, epi ? g.residual : nullptr, epi ? g.ldr : 0, g.alpha,
-                epi ? g.res_scale : 1.0f, g.batch, prm.bsd, epi ? g.bsr : 0);
+                epi ? g.res_scale : 1.0f, g.batch, prm.bsd, epi ? g.bsr : 0, prm.N);
         };
         auto reduce_out = [&](auto int_c) {
             if (g.out == kOutF32) reduce(std::integral_constant<int, kOutF32>{}, int_c);
@@ -379,7 +402,8 @@ void launch_gemm(const GemmProblem& g, void* ws, hipStream_t stream) {
         return;
     }
     Plan pl;
-    if (!g.long_k || !long_k_plan(g.M, g.N, kb, &pl)) pl = make_plan(g.M, g.N, kb, grouped_scales(g), g.batch, g.upper != 0);
+    const int64_t N = g.fa == kInt8 ? (g.N + 3) / 4 * 4 : g.N;
+    if (!g.long_k || !long_k_plan(g.M, g.N, kb, &pl)) pl = make_plan(g.M, N, kb, grouped_scales(g), g.batch, g.upper != 0);
     run_plan(g, pl, ws, stream);
 }
 

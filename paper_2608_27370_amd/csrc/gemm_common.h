@@ -56,6 +56,7 @@ struct Params {
     int rows_a, rows_b;        // kOutSoftmaxGradT: rows that A and B have, M and N or fewer (M and N in every other kind)
     uint16_t* dzt;             // kOutSoftmaxGradT: the transposed copy [N, M], or NULL, and its row pitch
     int64_t ld_dzt;
+    int part_n;                // int8: row length of the partial sums, N rounded up to 4
     uint8_t* q8;               // kOutSoftmaxGradQ: dz's FP8 copies (the GemmProblem fields)
     float* q8_scale;
     uint8_t* q8t;

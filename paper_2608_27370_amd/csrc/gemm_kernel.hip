@@ -445,7 +445,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
         p.B += bi * p.bsb;
         p.D = reinterpret_cast<uint8_t*>(p.D) + bi * p.bsd;
         if (p.residual) p.residual += bi * p.bsr;
-        p.partial += (int64_t)bi * p.splits * p.M * p.N;
+        p.partial += (int64_t)bi * p.splits * p.M * p.N;      // (int8 products are not batched)
     }
     const int ks = p.splits > 1 ? (int)p.per_split.quotient((uint32_t)lt) : 0;
     const int rem = lt - ks * per_split;
@@ -1014,15 +1014,18 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     uint8_t* ep = smem + wave * REGION;
     const int mrow0 = m0 + wm * WTM;
     const int ncol0 = n0 + wn * WTN;
-    float* const part = p.partial + (int64_t)ks * p.M * p.N;
+    // columns of what is stored (int8 partial sums have rows of whole vectors of
+    // four: any N may be split over k)
+    const int out_n = FA == kInt8 && OUT == 2 ? p.part_n : p.N;
+    float* const part = p.partial + (int64_t)ks * p.M * out_n;
     // a tile inside the matrix whose sums overwrite the output (or, binary32,
     // add to it) stores whole 4-column vectors everywhere: a branch-free path
     // that issues all of a pass's LDS reads before its stores
     constexpr int ES = (OUT == kOutF32 || OUT == 2) ? 4 : 2;    // bytes per output element
-    const int64_t ldo = OUT == 2 ? (int64_t)p.N : p.ldd;          // output pitch (elements)
+    const int64_t ldo = OUT == 2 ? (int64_t)out_n : p.ldd;          // output pitch (elements)
     // (and whose rows, and residual rows, lie within 2^31 bytes of its first:
     // the fast path addresses them with 32-bit buffer offsets)
-    const bool fast = m0 + BM <= p.M && n0 + BN <= p.N && (OUT == 2 || OUT == kOutF32 || !p.accumulate) &&
+    const bool fast = m0 + BM <= p.M && n0 + BN <= out_n && (OUT == 2 || OUT == kOutF32 || !p.accumulate) &&
                       (int64_t)WTM * ldo * ES <= INT32_MAX &&
                       (OUT != kOutBF16Epi || (int64_t)WTM * p.ldr * 2 <= INT32_MAX);
     // the bias of the lane's columns in the fast path below: lane chunk
@@ -1301,9 +1304,9 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     // columns lie outside get an offset out of range, and the row offsets go
     // into the lane offsets (as scalar operands they could exceed a buffer's
     // size, which the range check must not see).
-    const int vrows = min(WTM, p.M - mrow0), vcols = min(WTN, p.N - ncol0);
+    const int vrows = min(WTM, p.M - mrow0), vcols = min(WTN, out_n - ncol0);
     if (vrows <= 0 || vcols <= 0) return;
-    const bool edge = !fast && p.N % 4 == 0 && (OUT == 2 || OUT == kOutF32 || !p.accumulate) &&
+    const bool edge = !fast && out_n % 4 == 0 && (OUT == 2 || OUT == kOutF32 || !p.accumulate) &&
                       (int64_t)WTM * ldo * ES <= INT32_MAX &&
                       (OUT != kOutBF16Epi || (int64_t)WTM * p.ldr * 2 <= INT32_MAX);
     const bool sized = fast || edge;
@@ -1336,7 +1339,7 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     // the wave tile's output (and residual) rows as buffers: base at its
     // first element, range to its last valid row's last valid element
     const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
-        OUT == 2 ? (void*)(part + (int64_t)mrow0 * p.N + ncol0)
+        OUT == 2 ? (void*)(part + (int64_t)mrow0 * out_n + ncol0)
                  : (void*)(reinterpret_cast<uint8_t*>(p.D) + ((int64_t)mrow0 * p.ldd + ncol0) * ES),
         0, sized ? (int)((vrows - 1) * row_bytes + vcols * ES) : 0, 0x00020000);
     const __amdgpu_buffer_rsrc_t rres = __builtin_amdgcn_make_buffer_rsrc(
@@ -1491,10 +1494,10 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             float4 v = *reinterpret_cast<const float4*>(ep + r * ROWB + ((c ^ (r & SWZ)) << 4));
             const int m = mrow0 + pass * RPP + r;
             const int n = ncol0 + c * 4;
-            if (m >= p.M || n >= p.N) continue;
+            if (m >= p.M || n >= out_n) continue;
             if constexpr (OUT == 2) {
                 // split-K partial sums, dense [splits][M][N] FP32 (N % 4 == 0)
-                *reinterpret_cast<float4*>(part + (int64_t)m * p.N + n) = v;
+                *reinterpret_cast<float4*>(part + (int64_t)m * out_n + n) = v;
                 continue;
             }
             v.x *= alpha; v.y *= alpha; v.z *= alpha; v.w *= alpha;

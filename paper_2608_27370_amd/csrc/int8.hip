@@ -2,9 +2,13 @@
 // channels) and of columns (transposed copies) to int8, and the product of int8
 // codes with a scale for each row of either operand.
 
+#include "gemm_common.h"
 #include "quant_tile.h"
 
 namespace puro {
+
+using gemm_detail::add_epilogue1;
+using gemm_detail::add_epilogue4;
 
 namespace {
 
@@ -40,40 +44,159 @@ __device__ __forceinline__ uint2 encode_int8(const float v[8], const Int8Scale& 
 }
 
 // ---------------------------------------------------------------- rows ---
-// One block per row: the row's values are formed twice, for its largest
-// magnitude and for the codes.
+// TPR threads (a wave or the block) per row, whose NC chunks of 8 values a thread
+// are loaded once, all together, and stay in registers between the row's largest
+// magnitude and its codes. Bound by memory: a row is read once and its codes
+// written.
 enum : int { kRowBf16 = 0, kRowNorm = 1, kRowSwiglu = 2 };
 
 __device__ __forceinline__ void words(const uint4& v, uint32_t w[4]) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+__device__ __forceinline__ void floats(const uint32_t w[4], float v[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = bf16lo(w[i]); v[2 * i + 1] = bf16hi(w[i]); }
+}
+__device__ __forceinline__ uint32_t max_bits(const float v[8], uint32_t m) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return m;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+__device__ __forceinline__ float sum_squares(const uint32_t w[4], float ss) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        ss = fmaf(bf16lo(w[i]), bf16lo(w[i]), ss);
+        ss = fmaf(bf16hi(w[i]), bf16hi(w[i]), ss);
+    }
+    return ss;
+}
+__device__ __forceinline__ void norm_values(const uint32_t x[4], float rstd, const uint32_t g[4], float v[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bf16lo(x[i]) * rstd * bf16lo(g[i]);
+        v[2 * i + 1] = bf16hi(x[i]) * rstd * bf16hi(g[i]);
+    }
+}
+__device__ __forceinline__ void swiglu_values(const uint32_t g[4], const uint32_t u[4], float v[8]) {
+    auto all = [&](auto near_c) __attribute__((always_inline)) {
+        constexpr bool NEAR = decltype(near_c)::value;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = swiglu1<NEAR>(bf16lo(g[i]), bf16lo(u[i]));
+            v[2 * i + 1] = swiglu1<NEAR>(bf16hi(g[i]), bf16hi(u[i]));
+        }
+    };
+    if (wave_none(absmax_bits8(g) > kNearGateBits)) all(std::true_type{});
+    else all(std::false_type{});
+}
 
+template <int SRC, int TPR, int NC>
+__global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args a) {
+    __shared__ uint32_t red[4];
+    __shared__ float sums[4];
+    constexpr bool WAVE = TPR == 64;
+    const int t = WAVE ? threadIdx.x & 63 : threadIdx.x;
+    const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+    if (WAVE && row >= a.rows) return;          // (a whole wave; its block meets at no barrier)
+    const int cpr = (int)(a.cols / 8);
+    const uint16_t* xr = a.x + row * a.ld;
+    constexpr int SECOND = SRC == kRowBf16 ? 0 : NC;
+    uint4 x[NC], y[SECOND > 0 ? SECOND : 1];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = t + i * TPR;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if constexpr (SECOND > 0) y[i] = x[i];
+        if (c < cpr) {
+            x[i] = *reinterpret_cast<const uint4*>(xr + c * 8);
+            if constexpr (SRC == kRowNorm) y[i] = *reinterpret_cast<const uint4*>(a.gamma + c * 8);
+            if constexpr (SRC == kRowSwiglu) y[i] = *reinterpret_cast<const uint4*>(xr + a.cols + c * 8);
+        }
+    }
+    float rstd = 1.0f;
+    if constexpr (SRC == kRowNorm) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            uint32_t w[4];
+            words(x[i], w);
+            ss = sum_squares(w, ss);
+        }
+        ss = wave_sum(ss);
+        if constexpr (!WAVE) {
+            if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
+            __syncthreads();
+            ss = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+        }
+        rstd = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+        if (a.rstd && t == 0) a.rstd[row] = rstd;
+    }
+    // the row's values: as they are loaded, formed twice (two products a value), or
+    // formed once and kept
+    float h[SRC == kRowSwiglu ? NC : 1][8];
+    auto values = [&](int i, float v[8]) __attribute__((always_inline)) {
+        uint32_t w[4], z[4];
+        words(x[i], w);
+        if constexpr (SRC == kRowBf16) floats(w, v);
+        if constexpr (SRC == kRowNorm) { words(y[i], z); norm_values(w, rstd, z, v); }
+        if constexpr (SRC == kRowSwiglu) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = h[i][e];
+        }
+    };
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        if constexpr (SRC == kRowBf16) {
+            uint32_t w[4];
+            words(x[i], w);
+            m = max(m, absmax_bits8(w) << 16);
+        } else {
+            float v[8];
+            if constexpr (SRC == kRowSwiglu) {
+                uint32_t w[4], z[4];
+                words(x[i], w);
+                words(y[i], z);
+                swiglu_values(w, z, h[i]);
+            }
+            values(i, v);
+            m = max_bits(v, m);
+        }
+    }
+    m = WAVE ? wave_max(m) : block_max(m, red);
+    const Int8Scale s = int8_scale(m);
+    if (t == 0) a.scale[row] = s.s;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = t + i * TPR;
+        float v[8];
+        values(i, v);
+        if (c < cpr) *reinterpret_cast<uint2*>(a.q + row * a.cols + c * 8) = encode_int8(v, s);
+    }
+}
+
+// Rows longer than the registers hold: one block per row, the values formed twice
+// (the second time from the caches).
 template <int SRC>
 __device__ __forceinline__ void row_values(const QuantInt8Args& a, const uint16_t* xr, int64_t c, float rstd, float v[8]) {
-    uint32_t w[4];
+    uint32_t w[4], z[4];
     words(*reinterpret_cast<const uint4*>(xr + c * 8), w);
-    if constexpr (SRC == kRowBf16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = bf16lo(w[i]); v[2 * i + 1] = bf16hi(w[i]); }
-    } else if constexpr (SRC == kRowNorm) {
-        uint32_t g[4];
-        words(*reinterpret_cast<const uint4*>(a.gamma + c * 8), g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = bf16lo(w[i]) * rstd * bf16lo(g[i]);
-            v[2 * i + 1] = bf16hi(w[i]) * rstd * bf16hi(g[i]);
-        }
-    } else {
-        uint32_t u[4];
-        words(*reinterpret_cast<const uint4*>(xr + a.cols + c * 8), u);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = swiglu1<false>(bf16lo(w[i]), bf16lo(u[i]));
-            v[2 * i + 1] = swiglu1<false>(bf16hi(w[i]), bf16hi(u[i]));
-        }
+    if constexpr (SRC == kRowBf16) floats(w, v);
+    if constexpr (SRC == kRowNorm) {
+        words(*reinterpret_cast<const uint4*>(a.gamma + c * 8), z);
+        norm_values(w, rstd, z, v);
+    }
+    if constexpr (SRC == kRowSwiglu) {
+        words(*reinterpret_cast<const uint4*>(xr + a.cols + c * 8), z);
+        swiglu_values(w, z, v);
     }
 }
 
 template <int SRC>
-__global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args a) {
+__global__ __launch_bounds__(kThreads) void quant_long_rows_int8_kernel(QuantInt8Args a) {
     __shared__ uint32_t red[4];
     __shared__ float sums[4];
     const int64_t row = blockIdx.x, cpr = a.cols / 8;
@@ -84,14 +207,9 @@ __global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args
         for (int64_t c = threadIdx.x; c < cpr; c += kThreads) {
             uint32_t w[4];
             words(*reinterpret_cast<const uint4*>(xr + c * 8), w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                ss = fmaf(bf16lo(w[i]), bf16lo(w[i]), ss);
-                ss = fmaf(bf16hi(w[i]), bf16hi(w[i]), ss);
-            }
+            ss = sum_squares(w, ss);
         }
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
+        ss = wave_sum(ss);
         if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
         __syncthreads();
         rstd = 1.0f / sqrtf(((sums[0] + sums[1]) + (sums[2] + sums[3])) / (float)a.cols + a.eps);
@@ -101,8 +219,7 @@ __global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args
     for (int64_t c = threadIdx.x; c < cpr; c += kThreads) {
         float v[8];
         row_values<SRC>(a, xr, c, rstd, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        m = max_bits(v, m);
     }
     const Int8Scale s = int8_scale(block_max(m, red));
     if (threadIdx.x == 0) a.scale[row] = s.s;
@@ -115,27 +232,54 @@ __global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args
 
 // ---------------------------------------------------------------- columns ---
 // Largest magnitude patterns of the columns over P ranges of rows: part [P][cols].
+// A block has 512 columns (a lane 8 of them), its four waves take the range's rows
+// in turn, eight rows' loads in flight each.
+constexpr int kColBlock = 512;
 __global__ __launch_bounds__(kThreads) void col_max_kernel(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, int P,
                                                            uint16_t* part) {
-    const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (c >= cols / 8) return;
+    __shared__ uint4 red[kThreads];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * kColBlock + lane * 8;
     const int64_t r0 = rows * blockIdx.y / P, r1 = rows * (blockIdx.y + 1) / P;
-    uint32_t m[4] = {0u, 0u, 0u, 0u};
-    for (int64_t r = r0; r < r1; ++r) {
-        uint32_t w[4];
-        words(*reinterpret_cast<const uint4*>(x + r * ld + c * 8), w);
+    uint4 m = make_uint4(0, 0, 0, 0);
+    if (col < cols) {
+        constexpr int U = 8;
+        for (int64_t r = r0 + wave; r < r1; r += 4 * U) {
+            uint4 v[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m[i] = pk_max_u16(m[i], mag2(w[i]));
+            for (int u = 0; u < U; ++u) {
+                // (past the range: the row that is there anyway)
+                const int64_t ru = r + 4 * u < r1 ? r + 4 * u : r;
+                v[u] = *reinterpret_cast<const uint4*>(x + ru * ld + col);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                m.x = pk_max_u16(m.x, mag2(v[u].x)); m.y = pk_max_u16(m.y, mag2(v[u].y));
+                m.z = pk_max_u16(m.z, mag2(v[u].z)); m.w = pk_max_u16(m.w, mag2(v[u].w));
+            }
+        }
     }
-    *reinterpret_cast<uint4*>(part + (int64_t)blockIdx.y * cols + c * 8) = make_uint4(m[0], m[1], m[2], m[3]);
+    red[threadIdx.x] = m;
+    __syncthreads();
+    if (wave == 0 && col < cols) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+            const uint4 v = red[w * 64 + lane];
+            m.x = pk_max_u16(m.x, v.x); m.y = pk_max_u16(m.y, v.y); m.z = pk_max_u16(m.z, v.z); m.w = pk_max_u16(m.w, v.w);
+        }
+        *reinterpret_cast<uint4*>(part + (int64_t)blockIdx.y * cols + col) = m;
+    }
 }
 
-// The transposed copy by 128x128 tiles: each thread an 8x8 block, the columns'
-// scales from the partial maxima. `a`: x, its rows rounded up to 16 (which are
-// written; the rows behind `rows` read as zeros), ld, qT, scaleT.
+// The transposed copy by 128x128 tiles, each thread an 8x8 block. The tile's
+// values are on their way while the partial maxima of its columns are read, 16
+// threads a chunk of 8 columns, and 64 threads make the scales of two columns
+// each. `a`: x, its rows rounded up to 16 (which are written; the rows behind
+// `rows` read as zeros), ld, qT, scaleT.
 __global__ __launch_bounds__(kThreads) void quant_cols_int8_kernel(QuantArgs a, int64_t rows, int64_t ld_qT,
                                                                    const uint16_t* part, int P) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[kTile * kTile];
+    __shared__ __attribute__((aligned(16))) float factor[kTile], before[kTile];
     const Tile t = tile_coords(a.cols);
     const int64_t tr0 = (int64_t)blockIdx.y * kTile;
     const int64_t vr = max((int64_t)0, min((int64_t)kTile, rows - tr0));
@@ -144,94 +288,282 @@ __global__ __launch_bounds__(kThreads) void quant_cols_int8_kernel(QuantArgs a, 
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         w[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, t.col_ok ? (uint32_t)(((t.rg * 8 + i) * a.ld + t.col) * 2) : kOOB, 0, 0);
-    uint32_t m[4] = {0u, 0u, 0u, 0u};
-    if (t.col_ok)
-        for (int p = 0; p < P; ++p) {
-            uint32_t v[4];
-            words(*reinterpret_cast<const uint4*>(part + (int64_t)p * a.cols + t.col), v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) m[i] = pk_max_u16(m[i], v[i]);
+    uint4 m = make_uint4(0, 0, 0, 0);
+    if (t.col_ok) {
+#pragma unroll 4
+        for (int p = t.rg; p < P; p += 16) {
+            const uint4 v = *reinterpret_cast<const uint4*>(part + (int64_t)p * a.cols + t.col);
+            m.x = pk_max_u16(m.x, v.x); m.y = pk_max_u16(m.y, v.y); m.z = pk_max_u16(m.z, v.z); m.w = pk_max_u16(m.w, v.w);
         }
-    Int8Scale s[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        s[j] = int8_scale((j & 1 ? m[j / 2] >> 16 : m[j / 2] & 0xFFFFu) << 16);
-        if (t.rg == 0 && blockIdx.y == 0 && t.col_ok) a.scaleT[t.col + j] = s[j].s;
     }
+    uint32_t* const maxima = reinterpret_cast<uint32_t*>(lds);      // [16 groups][64 words of two columns]
+    *reinterpret_cast<uint4*>(maxima + t.rg * 64 + t.cc * 4) = m;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        uint32_t v = maxima[threadIdx.x];
+#pragma unroll
+        for (int g = 1; g < 16; ++g) v = pk_max_u16(v, maxima[g * 64 + threadIdx.x]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int j = 2 * threadIdx.x + e;
+            const Int8Scale s = int8_scale((e ? v >> 16 : v & 0xFFFFu) << 16);
+            factor[j] = s.r;
+            before[j] = s.pre;
+            const int64_t col = (int64_t)blockIdx.x * kTile + j;
+            if (blockIdx.y == 0 && col < a.cols) a.scaleT[col] = s.s;
+        }
+    }
+    __syncthreads();
+    float r[8], pre[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { r[j] = factor[t.cc * 8 + j]; pre[j] = before[t.cc * 8 + j]; }
     uint2 c[8], ct[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t x[4] = {(uint32_t)w[i].x, (uint32_t)w[i].y, (uint32_t)w[i].z, (uint32_t)w[i].w};
+        float v[8];
+        floats(x, v);
         uint32_t b[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = code_bits((j & 1 ? bf16hi(x[j / 2]) : bf16lo(x[j / 2])) * s[j].pre, s[j].r);
+        for (int j = 0; j < 8; ++j) b[j] = code_bits(v[j] * pre[j], r[j]);
         c[i] = make_uint2(pack_codes(b[0], b[1], b[2], b[3]), pack_codes(b[4], b[5], b[6], b[7]));
     }
     transpose8x8(c, ct);
     // LDS row r = column r of the tile, its 16-byte chunk h (rows 16 h ..) at h ^ ((r >> 3) & 7)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int r = t.cc * 8 + j;
-        *reinterpret_cast<uint2*>(lds + r * kTile + (((t.rg >> 1) ^ (r >> 3 & 7)) << 4) + ((t.rg & 1) << 3)) = ct[j];
+        const int r8 = t.cc * 8 + j;
+        *reinterpret_cast<uint2*>(lds + r8 * kTile + (((t.rg >> 1) ^ (r8 >> 3 & 7)) << 4) + ((t.rg & 1) << 3)) = ct[j];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kTile * kTile / 16 / kThreads; ++i) {
         const int q = i * kThreads + threadIdx.x;
-        const int r = q >> 3, h = q & 7;
-        const uint4 v = *reinterpret_cast<const uint4*>(lds + r * kTile + ((h ^ (r >> 3 & 7)) << 4));
-        const int64_t col = (int64_t)blockIdx.x * kTile + r, row = tr0 + h * 16;
+        const int r8 = q >> 3, h = q & 7;
+        const uint4 v = *reinterpret_cast<const uint4*>(lds + r8 * kTile + ((h ^ (r8 >> 3 & 7)) << 4));
+        const int64_t col = (int64_t)blockIdx.x * kTile + r8, row = tr0 + h * 16;
         if (col < a.cols && row < a.rows) *reinterpret_cast<uint4*>(a.qT + col * ld_qT + row) = v;
     }
 }
 
 int col_ranges(int64_t rows) { return (int)std::min<int64_t>(64, (rows + 31) / 32); }
 
-// ---------------------------------------------------------------- product ---
-// One wave per 16 x 16 tile of D, operands straight from memory: per 64 values
-// of k one v_mfma_i32_16x16x64_i8, B's rows as its first operand, so that lane l
-// holds columns 4 (l >> 4) + 0..3 of row l & 15.
+// ---------------------------------------------------------------- product of few rows ---
+// Up to 64 rows of A: the time is that of reading B once. A block has 16 NT columns
+// and WK waves that take steps of 128 values of k in turn, straight from memory
+// into registers (a lane 32 bytes of its row, four lanes a whole cache line), U
+// steps' loads in flight; nothing but the rows of A that exist is read of A, from
+// the caches. (16 columns, 8 waves, 2 steps: 1x2048x1536 3.9 us, 5x151936x1536 52.0;
+// 32 columns 4.6 and 56.1, 4 waves 3.9 and 52.6, 4 steps 4.3 and 73.9, 16 waves with
+// one step 4.1 and 68.7.) Per step and 16 x 16 tile two v_mfma_i32_16x16x64_i8 with B's rows as
+// the first operand, so that lane l holds columns 4 (l >> 4) + 0..3 of row l & 15
+// (A and B split k alike). The waves' integer sums meet in LDS.
 typedef int v4i32 __attribute__((ext_vector_type(4)));
 
-__global__ __launch_bounds__(kThreads) void int8_gemm_kernel(Int8Problem p) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t tiles_n = (p.N + 15) / 16, tiles = tiles_n * ((p.M + 15) / 16);
-    for (int64_t tile = (int64_t)blockIdx.x * 4 + wave; tile < tiles; tile += (int64_t)gridDim.x * 4) {
-        const int64_t m0 = tile / tiles_n * 16, n0 = tile % tiles_n * 16;
-        const int64_t m = m0 + (lane & 15), nr = n0 + (lane & 15);
-        v4i32 acc = {0, 0, 0, 0};
-        for (int64_t k = (lane >> 4) * 16; k < (p.K + 63) / 64 * 64; k += 64) {
-            v4i32 x = {0, 0, 0, 0}, w = {0, 0, 0, 0};
-            if (k < p.K && m < p.M) x = *reinterpret_cast<const v4i32*>(p.A + m * p.lda + k);
-            if (k < p.K && nr < p.N) w = *reinterpret_cast<const v4i32*>(p.B + nr * p.ldb + k);
-            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc, 0, 0, 0);
+// Outputs [m, n .. n + 3]: the scaled sums, bias, residual, one rounding.
+__device__ __forceinline__ void store_int8_outputs(const Int8Problem& p, int64_t m, int64_t n, v4i32 acc, float sa, const float sb[4]) {
+    float4 v = make_float4((float)acc.x * sa * sb[0], (float)acc.y * sa * sb[1], (float)acc.z * sa * sb[2], (float)acc.w * sa * sb[3]);
+    if (m >= p.M || n >= p.N) return;
+    if (p.N % 4 == 0) {
+        if (!p.f32) {
+            if (p.bias || p.residual) add_epilogue4(v, p.bias, p.residual, p.ldr, m, n, 1.0f);
+            *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.D) + m * p.ldd + n) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+            return;
         }
-        if (m >= p.M) continue;
-        const float sa = p.sa[m];
+        float4* d = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.D) + m * p.ldd + n);
+        if (p.accumulate) {
+            const float4 o = *d;
+            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        }
+        *d = v;
+        return;
+    }
+    const float w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t n = n0 + 4 * (lane >> 4) + e;
-            if (n >= p.N) continue;
-            float v = (float)acc[e] * sa * p.sb[n];
-            if (p.bias) v += __uint_as_float((uint32_t)p.bias[n] << 16);
-            if (p.residual) v += __uint_as_float((uint32_t)p.residual[m * p.ldr + n] << 16);
-            if (p.f32) {
-                float* d = reinterpret_cast<float*>(p.D) + m * p.ldd + n;
-                *d = p.accumulate ? *d + v : v;
-            } else {
-                reinterpret_cast<uint16_t*>(p.D)[m * p.ldd + n] = to_bf16(v);
-            }
+    for (int e = 0; e < 4; ++e) {
+        if (n + e >= p.N) continue;
+        if (p.f32) {
+            float* d = reinterpret_cast<float*>(p.D) + m * p.ldd + n + e;
+            *d = p.accumulate ? *d + w[e] : w[e];
+        } else {
+            reinterpret_cast<uint16_t*>(p.D)[m * p.ldd + n + e] = to_bf16(add_epilogue1(w[e], p.bias, p.residual, p.ldr, m, n + e, 1.0f));
         }
     }
+}
+
+template <int MT, int NT, int WK, int U>
+__global__ __launch_bounds__(WK * 64) void int8_rows_kernel(Int8Problem p) {
+    __shared__ v4i32 sums[WK > 1 ? WK * MT * NT * 64 : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = lane & 15, q = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * NT), m0 = (int64_t)blockIdx.y * (16 * MT);
+    const int K = (int)p.K;
+    const int rows_n = (int)min((int64_t)16 * NT, p.N - n0), rows_m = (int)min((int64_t)16 * MT, p.M - m0);
+    const __amdgpu_buffer_rsrc_t rb = buffer_rsrc(p.B + n0 * p.ldb, (uint32_t)((rows_n - 1) * p.ldb + K));
+    const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(p.A + m0 * p.lda, (uint32_t)((rows_m - 1) * p.lda + K));
+    uint32_t ob[NT], oa[MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) ob[j] = j * 16 + r < rows_n ? (uint32_t)((j * 16 + r) * p.ldb) : kOOB;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) oa[i] = i * 16 + r < rows_m ? (uint32_t)((i * 16 + r) * p.lda) : kOOB;
+    v4i32 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = v4i32{0, 0, 0, 0};
+    for (int k0 = wave * 128; k0 < K; k0 += WK * 128 * U) {
+        v4i32 b[U][NT][2], a[U][MT][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = k0 + u * (WK * 128) + q * 32 + h * 16;
+                // (past the reduction's end, and of rows that are not there: zeros)
+                const bool in = k < K;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) b[u][j][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, in ? ob[j] + k : kOOB, 0, 0);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) a[u][i][h] = __builtin_amdgcn_raw_buffer_load_b128(ra, in ? oa[i] + k : kOOB, 0, 0);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[u][j][h], a[u][i][h], acc[i][j], 0, 0, 0);
+    }
+    if constexpr (WK > 1) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) sums[((i * NT + j) * WK + wave) * 64 + lane] = acc[i][j];
+        __syncthreads();
+    }
+    for (int t = wave; t < MT * NT; t += WK) {
+        const int i = t / NT, j = t % NT;
+        const int64_t m = m0 + i * 16 + r, n = n0 + j * 16 + q * 4;
+        float sb[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sb[e] = n + e < p.N ? p.sb[n + e] : 0.0f;
+        const float sa = m < p.M ? p.sa[m] : 0.0f;
+        v4i32 v;
+        if constexpr (WK > 1) {
+            v = sums[t * WK * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < WK; ++w) v += sums[(t * WK + w) * 64 + lane];
+        } else {
+            v = acc[i][j];
+        }
+        store_int8_outputs(p, m, n, v, sa, sb);
+    }
+}
+
+// The same for at most 16 rows and a reduction of at most 2048, N % 4 == 0: A's
+// values stay in registers (a wave has two steps of k at most) and a block goes
+// through many groups of 16 columns, the next one's loads (and scales) in flight
+// while one is summed. Two LDS buffers and one barrier a group; the waves take
+// turns in storing.
+constexpr int kStreamWaves = 8, kStreamK = kStreamWaves * 2 * 128;
+__global__ __launch_bounds__(kStreamWaves * 64, 4) void int8_stream_kernel(Int8Problem p) {
+    __shared__ v4i32 sums[2][kStreamWaves * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = lane & 15, q = lane >> 4;
+    const int K = (int)p.K;
+    const int groups = (int)((p.N + 15) / 16);
+    struct Set {
+        v4i32 b[4];
+        float4 s;
+    };
+    // the lane's places in a row of the operands (past the reduction's end: none)
+    uint32_t ok[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int k = wave * 128 + (e >> 1) * (kStreamWaves * 128) + q * 32 + (e & 1) * 16;
+        ok[e] = k < K ? (uint32_t)k : kOOB;
+    }
+    v4i32 a[4];
+    const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(p.A, (uint32_t)((p.M - 1) * p.lda + K));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        a[e] = __builtin_amdgcn_raw_buffer_load_b128(ra, r < p.M && ok[e] != kOOB ? (uint32_t)(r * p.lda) + ok[e] : kOOB, 0, 0);
+    const float sa = r < p.M ? p.sa[r] : 0.0f;
+    const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(p.sb, (uint32_t)(p.N * 4));
+    auto load = [&](Set& t, int g) __attribute__((always_inline)) {
+        const int64_t n0 = (int64_t)g * 16;
+        const int rows = g < groups ? (int)min((int64_t)16, p.N - n0) : 0;
+        const __amdgpu_buffer_rsrc_t rb = buffer_rsrc(rows > 0 ? p.B + n0 * p.ldb : p.B, rows > 0 ? (uint32_t)((rows - 1) * p.ldb + K) : 0u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            t.b[e] = __builtin_amdgcn_raw_buffer_load_b128(rb, r < rows && ok[e] != kOOB ? (uint32_t)(r * p.ldb) + ok[e] : kOOB, 0, 0);
+        t.s = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(rs, g < groups ? (uint32_t)((g * 16 + q * 4) * 4) : kOOB, 0, 0));
+    };
+    auto take = [&](const Set& t, int g, int turn) __attribute__((always_inline)) {
+        v4i32 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.b[e], a[e], acc, 0, 0, 0);
+        v4i32* const buf = sums[turn & 1];
+        buf[wave * 64 + lane] = acc;
+        __syncthreads();
+        if (wave != (turn & (kStreamWaves - 1))) return;
+        v4i32 v = buf[lane];
+#pragma unroll
+        for (int w = 1; w < kStreamWaves; ++w) v += buf[w * 64 + lane];
+        const float sb[4] = {t.s.x, t.s.y, t.s.z, t.s.w};
+        store_int8_outputs(p, r, (int64_t)g * 16 + q * 4, v, sa, sb);
+    };
+    Set t0, t1;
+    int g = blockIdx.x;
+    const int step = gridDim.x;
+    load(t0, g);
+    for (int turn = 0; g < groups; turn += 2) {
+        load(t1, g + step);
+        take(t0, g, turn);
+        g += step;
+        if (g >= groups) break;
+        load(t0, g + step);
+        take(t1, g, turn + 1);
+        g += step;
+    }
+}
+
+// A wave per row where there are rows enough to fill the chip with four a block,
+// else a block; in as few chunks a thread as hold the row.
+template <int N> using Int = std::integral_constant<int, N>;
+template <int SRC>
+void launch_rows(const QuantInt8Args& a, hipStream_t stream) {
+    const int64_t cpr = a.cols / 8;
+    auto run = [&](auto tpr, auto nc) {
+        constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
+        quant_rows_int8_kernel<SRC, TPR, NC><<<(unsigned)(TPR == 64 ? (a.rows + 3) / 4 : a.rows), kThreads, 0, stream>>>(a);
+    };
+    auto fit = [&](auto tpr, auto... nc) {
+        constexpr int TPR = decltype(tpr)::value;
+        bool done = false;
+        auto one = [&](auto n) {
+            if (!done && cpr <= TPR * decltype(n)::value) { run(tpr, n); done = true; }
+        };
+        (one(nc), ...);
+        return done;
+    };
+    if (a.rows >= 1024 && fit(Int<64>{}, Int<1>{}, Int<2>{},
+                              Int<4>{}))
+        return;
+    if (fit(Int<256>{}, Int<1>{}, Int<2>{},
+            Int<3>{}, Int<5>{}, Int<8>{},
+            Int<12>{}))
+        return;
+    quant_long_rows_int8_kernel<SRC><<<(unsigned)a.rows, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
 
 void launch_quantize_int8(const QuantInt8Args& a, hipStream_t stream) {
-    const int grid = (int)a.rows;
-    if (a.swiglu) quant_rows_int8_kernel<kRowSwiglu><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.gamma) quant_rows_int8_kernel<kRowNorm><<<grid, kThreads, 0, stream>>>(a);
-    else quant_rows_int8_kernel<kRowBf16><<<grid, kThreads, 0, stream>>>(a);
+    if (a.swiglu) launch_rows<kRowSwiglu>(a, stream);
+    else if (a.gamma) launch_rows<kRowNorm>(a, stream);
+    else launch_rows<kRowBf16>(a, stream);
 }
 
 size_t quant_int8_ws_bytes(int64_t rows, int64_t cols) { return (size_t)col_ranges(rows) * cols * 2; }
@@ -240,7 +572,7 @@ void launch_quantize_int8_t(const uint16_t* x, int64_t rows, int64_t cols, int64
                             float* scaleT, void* ws, hipStream_t stream) {
     const int P = col_ranges(rows);
     uint16_t* part = reinterpret_cast<uint16_t*>(ws);
-    col_max_kernel<<<dim3((unsigned)((cols / 8 + kThreads - 1) / kThreads), P), kThreads, 0, stream>>>(x, rows, cols, ld, P, part);
+    col_max_kernel<<<dim3((unsigned)((cols + kColBlock - 1) / kColBlock), P), kThreads, 0, stream>>>(x, rows, cols, ld, P, part);
     QuantArgs a{};
     a.x = x; a.rows = (rows + 15) / 16 * 16; a.cols = cols; a.ld = ld;
     a.qT = reinterpret_cast<uint8_t*>(qT); a.scaleT = scaleT;
@@ -248,9 +580,39 @@ void launch_quantize_int8_t(const uint16_t* x, int64_t rows, int64_t cols, int64
     quant_cols_int8_kernel<<<grid, kThreads, 0, stream>>>(a, rows, ld_qT, part, P);
 }
 
-size_t int8_gemm_ws_bytes(int64_t M, int64_t N, int64_t K) { return gemm_workspace_bytes(M, N, K, kOutBF16); }
+// Whether a product takes the kernels of few rows: those read A's fragments from
+// the caches for every 16 columns, which from 17 rows on costs more than the tiled
+// kernel's LDS unless the whole product is small (in a graph, weights not in a
+// cache: 1x2048x1536 3.8 us against 6.9 tiled, 1x1536x8960 8.3 against 11.0, 5x151936x
+// 1536 48.1 against 60.4; 20x2048x1536 4.7 against 6.7, 64x2048x1536 6.7 against 7.1,
+// but 20x17920x1536 13.3 against 12.4 and 64x151936x1536 164 against 65).
+static bool few_rows(int64_t M, int64_t N, int64_t K) { return M <= 16 || (M <= 64 && N * K <= (int64_t)1 << 22); }
+
+// Blocks of the streaming kernel: two a CU, as many as its registers allow (5x151936x
+// 1536: 512 blocks 48.1 us, 768 49.2, 1536 50.1; the other kernel 52.0). Where a
+// block would have few groups, the other kernel's many blocks are faster (1x17920x1536
+// 8.3 us against 8.6).
+constexpr int kStreamBlocks = 512;
+constexpr int64_t kStreamColumns = 32768;
+
+template <int MT>
+static void launch_few(const Int8Problem& p, hipStream_t stream) {
+    int8_rows_kernel<MT, 1, 8, 2><<<(unsigned)((p.N + 15) / 16), 512, 0, stream>>>(p);
+}
+
+size_t int8_gemm_ws_bytes(int64_t M, int64_t N, int64_t K) {
+    return few_rows(M, N, K) ? 0 : gemm_workspace_bytes(M, (N + 3) / 4 * 4, K, kOutBF16);
+}
 
 void launch_int8_gemm(const Int8Problem& p, void* ws, hipStream_t stream) {
+    if (few_rows(p.M, p.N, p.K)) {
+        if (p.M <= 16 && p.K <= kStreamK && p.N % 4 == 0 && p.N >= kStreamColumns)
+            int8_stream_kernel<<<kStreamBlocks, kStreamWaves * 64, 0, stream>>>(p);
+        else if (p.M <= 16) launch_few<1>(p, stream);
+        else if (p.M <= 32) launch_few<2>(p, stream);
+        else launch_few<4>(p, stream);
+        return;
+    }
     GemmProblem g{};
     g.M = p.M; g.N = p.N; g.K = p.K;
     g.A = reinterpret_cast<const uint8_t*>(p.A); g.lda = p.lda; g.fa = kInt8; g.sa_mode = kSNone; g.sa = p.sa;

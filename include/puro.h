@@ -642,13 +642,13 @@ puro_status puro_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* A, int
  * +infinity, or with no probability at all, keeps nothing; a token that would be
  * drawn from such a row, or from one with a NaN or an infinity in its rest, is -1.
  * A sequence without rows has accepted 0 and no token (as behind the last one
- * of a batch with room to spare: rows behind the last sequence are neither read
- * nor written); one whose offsets decrease or leave [0, T], or whose draft rows
- * leave [0, draft_rows), has accepted -1 and no token.
+ * of a batch with room to spare: rows behind the last sequence are not written);
+ * one whose offsets decrease or leave [0, T], that begins before an earlier
+ * offset, or whose draft rows leave [0, draft_rows), has accepted -1 and no token.
  * dtype: PURO_OUT_BF16 or PURO_OUT_FP32 for both target [T, V] (pitch ld_target)
  * and draft [draft_rows, V] (pitch ld_draft); any V from 1 to 2^21 and pitches
- * from V to 2^22 (rows need no more than their element's alignment); T and B at
- * most 2^20, T V and B V at most 2^35, draft_rows at most T. offsets [B + 1], draft_ids [T],
+ * from V to 2^22 (rows need no more than their element's alignment); T at
+ * most 2^20, B at most 2^16, T V and B V at most 2^35, draft_rows at most T. offsets [B + 1], draft_ids [T],
  * tokens [T], accepted [B]: int32; uniform [T], uniform_sample [B]: FP32 in
  * [0, 1). temperature finite and >= 0, if not 0 between 2^-20 and 2^20 (PROBS:
  * not used). ws (16-byte aligned): *_workspace_size bytes. */

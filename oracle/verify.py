@@ -67,7 +67,7 @@ def verify(target, draft, ids, offsets, u, us, kind, tau, tokens):
     accepted = np.zeros(B, np.int32)
     for b in range(B):
         lo, hi = int(offsets[b]), int(offsets[b + 1])
-        if lo < 0 or hi < lo or hi > T or (draft is not None and hi - lo > 1 and (lo - b < 0 or hi - 1 - b > len(draft))):
+        if lo < 0 or hi < lo or hi > T or max(offsets[:b + 1]) > lo or (draft is not None and hi - lo > 1 and (lo - b < 0 or hi - 1 - b > len(draft))):
             accepted[b] = -1
             continue
         if lo == hi:

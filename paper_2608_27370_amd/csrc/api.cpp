@@ -1110,7 +1110,7 @@ puro_status check_verify_sizes(int64_t B, int64_t T, int64_t draft_rows, int64_t
     if (B < 0 || T < 0 || draft_rows < 0 || V < 1) return PURO_ERR_SHAPE;
     const int64_t rows = (int64_t)1 << 20;
     // (a launch holds fewer than 2^24 blocks of 256 threads, a block at least 8192 entries of a long row)
-    if (B > rows || T > rows || draft_rows > T || V > (int64_t)1 << 21) return PURO_ERR_SHAPE;
+    if (B > (int64_t)1 << 16 || T > rows || draft_rows > T || V > (int64_t)1 << 21) return PURO_ERR_SHAPE;
     if (T * V > (int64_t)1 << 35 || B * V > (int64_t)1 << 35) return PURO_ERR_SHAPE;
     return PURO_OK;
 }

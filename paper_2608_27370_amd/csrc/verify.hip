@@ -6,18 +6,20 @@
 // draw from max(p - q, 0) / sum max(p - q, 0): the kept or drawn token is then
 // distributed as p.
 //
-// A vocabulary row is worked on by blocks of a chunk each; every sum over a row is
-// one of its chunks' sums, in order, so that all blocks see the same values.
-//  * LOGITS: the chunks' largest logits and sums of exponentials of every row;
-//  * every sequence's chunks of the row where its drafts end: the block finds that
-//    row (each draft's probability from the rows' sums), and sums what is left over;
-//  * one block per sequence: the chunk, then the entry where the running sum passes
+// A vocabulary row is worked on in pieces of 2048 entries, a wave each; every sum
+// over a row is made of its pieces' sums, in a fixed order.
+//  * LOGITS: of every row the pieces' largest logits and sums of exponentials, then
+//    of every sequence, by a block of 16 waves (a row each), the row where its
+//    drafts end and that row's sums. PROBS: the drafts' entries alone say that row;
+//  * the pieces of that row: what is left over of each, and of p;
+//  * a block per sequence: the piece, then the entry where the running sum passes
 //    the random number's share.
 // Exponentials, probabilities and sums are binary64: with 10^5 entries a running
 // sum that errs by 10^-8 moves the drawn token once in 10^3 draws.
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "device_common.h"
 #include "kernels.h"
@@ -27,36 +29,110 @@ namespace puro {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 8192;       // entries per block
+constexpr int kWaves = kThreads / 64;
+constexpr int kPiece = 2048;       // entries per wave
 constexpr double kInf = __builtin_huge_val();
 
-// Values of a row: four consecutive words, of any alignment that the elements have.
+struct Args : VerifyArgs {
+    int pieces;           // of a row
+    double c;             // log2(e) / temperature
+    double2* stats;       // [T + draft_rows][pieces]: largest logit; sum of 2^((z - largest) c) (greedy: its id)
+    double2* left;        // [B][pieces]: sums of max(p - q, 0) and of p
+    double4* row;         // [B]: the end row's largest logits and reciprocal sums, target and draft
+    int* kept;            // [B]: drafts kept
+};
+
+// ---- values of a row ---------------------------------------------------------
+
 __device__ __forceinline__ float value(const uint16_t* p, int64_t v) { return __uint_as_float((uint32_t)p[v] << 16); }
 __device__ __forceinline__ float value(const float* p, int64_t v) { return p[v]; }
 
-__device__ __forceinline__ double shfl_xor(double v, int o) { return __shfl_xor(v, o, 64); }
-
-// Sums over a block in a fixed order, in every thread.
-__device__ __forceinline__ double block_sum(double v, double* red) {
+// E entries in 16 bytes; a row begins at any element, so that the 16-byte loads are
+// of no more than its alignment.
+template <typename E> constexpr int kPerVector = 16 / (int)sizeof(E);
+__device__ __forceinline__ void unpack(const uint4& w, float x[8], const uint16_t*) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += shfl_xor(v, o);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (red[0] + red[1]) + (red[2] + red[3]);
+    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16lo(u[i]); x[2 * i + 1] = bf16hi(u[i]); }
+}
+__device__ __forceinline__ void unpack(const uint4& w, float x[4], const float*) {
+    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
 }
 
-// The larger of two values, NaN if either is.
-__device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }
-
-struct Args : VerifyArgs {
-    int chunks;
-    double c;             // log2(e) / temperature
-    double2* stats;       // [T + draft_rows][chunks]: largest logit (greedy: and its id), sum of exponentials
-    double2* left;        // [B][chunks]: sums of max(p - q, 0) and of p
-    double4* row;         // [B]: the row's largest logits and reciprocal sums, target and draft
-    int* kept;            // [B]: drafts kept (-1: invalid)
+// The lane's entries of a piece, vector i at v0 + (i 64 + lane) * kPerVector, `fill`
+// past the row's end.
+template <typename E>
+struct Piece {
+    static constexpr int N = kPiece / 64 / kPerVector<E>;
+    float x[N][kPerVector<E>];
+    __device__ __forceinline__ static int at(int v0, int i) { return v0 + (i * 64 + (threadIdx.x & 63)) * kPerVector<E>; }
+    __device__ __forceinline__ void load(const E* row, int v0, int V, float fill) {
+        if (v0 + kPiece <= V) {
+            uint4 w[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) __builtin_memcpy(&w[i], row + at(v0, i), 16);
+#pragma unroll
+            for (int i = 0; i < N; ++i) unpack(w[i], x[i], row);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int v = at(v0, i);
+                if (v + kPerVector<E> <= V) {
+                    uint4 w;
+                    __builtin_memcpy(&w, row + v, 16);
+                    unpack(w, x[i], row);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kPerVector<E>; ++e) x[i][e] = v + e < V ? value(row, v + e) : fill;
+                }
+            }
+        }
+    }
 };
+
+// ---- arithmetic ----------------------------------------------------------------
+
+// 2^t in binary64 within 2^-45 relative, 0 far below: 2^n by the exponent, n the
+// nearest integer, times a polynomial of the rest f in [-1/2, 1/2] (interpolation
+// of degree 9 at the Chebyshev nodes, relative error 1.9e-14). t finite or
+// -infinity, at most 1000.
+__device__ __forceinline__ double exp2_f64(double t) {
+    t = fmax(t, -2000.0);
+    const double n = __builtin_rint(t), f = t - n;
+    double p = 0x1.b6571d9fbc782p-24;
+    p = __builtin_fma(p, f, 0x1.63ef9699f65f0p-20);
+    p = __builtin_fma(p, f, 0x1.ffcb7678dfe12p-17);
+    p = __builtin_fma(p, f, 0x1.43088e257f900p-13);
+    p = __builtin_fma(p, f, 0x1.5d87fe908f6f7p-10);
+    p = __builtin_fma(p, f, 0x1.3b2ab72b175e9p-7);
+    p = __builtin_fma(p, f, 0x1.c6b08d704411ap-5);
+    p = __builtin_fma(p, f, 0x1.ebfbdff8149f2p-3);
+    p = __builtin_fma(p, f, 0x1.62e42fefa39f7p-1);
+    p = __builtin_fma(p, f, 0x1.000000000003dp+0);
+    return __builtin_ldexp(p, (int)n);
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+// The larger of two values, NaN if either is.
+template <typename F>
+__device__ __forceinline__ F max_nan(F a, F b) { return a > b || a != a ? a : b; }
+
+// A row's normaliser: its largest logit m and the reciprocal of its sum; not finite
+// (then NaN) for a row with a NaN or an infinity, or without any probability.
+struct Norm {
+    double m, inv;
+};
+// The probability of a logit x, or x itself.
+__device__ __forceinline__ double prob(const Args& a, float x, const Norm& n) {
+    return a.logits ? exp2_f64(__builtin_fma((double)x, a.c, -(n.m * a.c))) * n.inv : (double)x;
+}
+__device__ __forceinline__ bool bad(const Norm& n) { return !(n.inv < kInf); }
+
+// ---- sequences -------------------------------------------------------------------
 
 // Rows of sequence b: its first, and how many (0: none; -1: invalid).
 struct Rows {
@@ -70,150 +146,202 @@ __device__ __forceinline__ Rows rows_of(const Args& a, int b) {
     if (a.draft && n > 1 && (start - b < 0 || end - 1 - b > a.draft_rows)) return {0, -1};
     return {(int)start, n};
 }
-
-// ---- LOGITS: (largest, sum of 2^((z - largest) c)) of every chunk of every row.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void chunk_sums_kernel(Args a) {
-    __shared__ double red[4];
-    __shared__ float redm[4];
-    const int chunk = (int)(blockIdx.x % (unsigned)a.chunks), r = (int)(blockIdx.x / (unsigned)a.chunks);
-    const E* z = r < a.T ? (const E*)a.target + (int64_t)r * a.ld_t : (const E*)a.draft + (int64_t)(r - a.T) * a.ld_d;
-    const int v0 = chunk * kChunk, v1 = min(a.V, v0 + kChunk);
+__device__ __forceinline__ const E* target_row(const Args& a, int64_t t) { return (const E*)a.target + t * a.ld_t; }
+template <typename E>
+__device__ __forceinline__ const E* draft_row(const Args& a, int64_t t) { return (const E*)a.draft + t * a.ld_d; }
+
+// ---- LOGITS: (largest, sum of 2^((z - largest) c)) of every piece of every row.
+// Bound by memory and, as closely, by its arithmetic: some 17 binary64 instructions
+// an entry.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void piece_sums_kernel(Args a, int total) {
+    const int at = (int)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (at >= total) return;
+    const int r = at / a.pieces, v0 = (at - r * a.pieces) * kPiece;
+    const E* z = r < a.T ? target_row<E>(a, r) : draft_row<E>(a, r - a.T);
+    Piece<E> x;
+    x.load(z, v0, a.V, -INFINITY);
     float m = -INFINITY;
-    for (int v = v0 + threadIdx.x; v < v1; v += kThreads) m = max_nan(m, value(z, v));
+#pragma unroll
+    for (int i = 0; i < x.N; ++i)
+#pragma unroll
+        for (int e = 0; e < kPerVector<E>; ++e) m = max_nan(m, x.x[i][e]);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) m = max_nan(m, __shfl_xor(m, o, 64));
-    if ((threadIdx.x & 63) == 0) redm[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = max_nan(max_nan(redm[0], redm[1]), max_nan(redm[2], redm[3]));
     double s = 0.0;
-    if (m != -INFINITY)
-        for (int v = v0 + threadIdx.x; v < v1; v += kThreads) s += exp2(((double)value(z, v) - (double)m) * a.c);
-    s = block_sum(s, red);
-    if (threadIdx.x == 0) a.stats[(int64_t)r * a.chunks + chunk] = make_double2((double)m, s);
+    if (m > -INFINITY && m < INFINITY) {
+        const double mc = (double)m * a.c;
+#pragma unroll
+        for (int i = 0; i < x.N; ++i)
+#pragma unroll
+            for (int e = 0; e < kPerVector<E>; ++e) s += exp2_f64(__builtin_fma((double)x.x[i][e], a.c, -mc));
+        s = wave_sum(s);
+    } else if (m != -INFINITY) {
+        s = __builtin_nan("");
+    }
+    if ((threadIdx.x & 63) == 0) a.stats[at] = make_double2((double)m, s);
 }
 
-// A row's largest logit and the reciprocal of its sum, by one wave.
-__device__ __forceinline__ double2 row_norm(const Args& a, int64_t r) {
-    const double2* st = a.stats + r * a.chunks;
+// A row's normaliser from its pieces, by one wave.
+__device__ __forceinline__ Norm row_norm(const Args& a, int64_t r) {
+    const double2* st = a.stats + r * a.pieces;
     const int lane = threadIdx.x & 63;
     double m = -kInf;
-    for (int c = lane; c < a.chunks; c += 64) m = st[c].x > m || st[c].x != st[c].x ? st[c].x : m;
+    for (int c = lane; c < a.pieces; c += 64) m = max_nan(m, st[c].x);
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const double t = shfl_xor(m, o);
-        m = t > m || t != t ? t : m;
-    }
+    for (int o = 32; o >= 1; o >>= 1) m = max_nan(m, __shfl_xor(m, o, 64));
+    if (!(m > -kInf && m < kInf)) return {m, __builtin_nan("")};
     double s = 0.0;
-    for (int c = lane; c < a.chunks; c += 64) {
+    for (int c = lane; c < a.pieces; c += 64) {
         const double2 v = st[c];
-        if (v.y != 0.0) s += v.y * exp2((v.x - m) * a.c);
+        s += v.y * exp2_f64(__builtin_fma(v.x, a.c, -(m * a.c)));
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) s += shfl_xor(s, o);
-    return make_double2(m, 1.0 / s);
+    return {m, 1.0 / wave_sum(s)};
 }
 
-// The probability of a row's value x.
-__device__ __forceinline__ double prob(const Args& a, float x, double m, double inv) {
-    return a.logits ? exp2(((double)x - m) * a.c) * inv : (double)x;
-}
-
-// Drafts kept of a sequence's n rows, by the whole block: four at a time.
+// Where a sequence's drafts end, by a block of 16 waves: eight rows at a time, a
+// wave for each one's normaliser and for its draft's.
+constexpr int kEndWaves = 16, kEndRows = kEndWaves / 2;
 template <typename E>
-__device__ __forceinline__ int kept_drafts(const Args& a, int b, Rows rows, int* ok) {
-    const int wave = threadIdx.x >> 6;
-    for (int i0 = 0; i0 < rows.n - 1; i0 += 4) {
-        const int i = i0 + wave;
+__global__ __launch_bounds__(kEndWaves * 64) void end_rows_kernel(Args a) {
+    __shared__ Norm norms[kEndWaves];
+    __shared__ int ok[kEndRows];
+    const int b = blockIdx.x, wave = threadIdx.x >> 6;
+    const Rows rows = rows_of(a, b);
+    if (rows.n <= 0) return;
+    for (int i0 = 0;; i0 += kEndRows) {
+        const int i = i0 + (wave & (kEndRows - 1));
+        const int64_t t = rows.start + i;
+        const bool drafted = i < rows.n - 1;
+        if (wave < kEndRows ? i < rows.n : drafted && a.draft) {
+            const Norm n = row_norm(a, wave < kEndRows ? t : a.T + t - b);
+            if ((threadIdx.x & 63) == 0) norms[wave] = n;
+        }
+        __syncthreads();
+        if (wave < kEndRows && (threadIdx.x & 63) == 0) {
+            bool keep = false;
+            const int d = drafted ? a.ids[t] : -1;
+            if (d >= 0 && d < a.V && !bad(norms[wave])) {
+                const double p = prob(a, value(target_row<E>(a, t), d), norms[wave]);
+                const double q = a.draft ? prob(a, value(draft_row<E>(a, t - b), d), norms[wave + kEndRows]) : 1.0;
+                keep = (double)a.u[t] * q < p;
+            }
+            ok[wave] = keep;
+        }
+        __syncthreads();
+        int w = 0;
+        while (w < kEndRows && ok[w]) ++w;
+        if (w < kEndRows) {              // (the last row is not kept, at the latest)
+            if (threadIdx.x == 0) {
+                const bool last = i0 + w == rows.n - 1;
+                const Norm p = norms[w], q = last || !a.draft ? Norm{0.0, 0.0} : norms[w + kEndRows];
+                a.kept[b] = i0 + w;
+                a.row[b] = make_double4(p.m, p.inv, q.m, q.inv);
+            }
+            return;
+        }
+        __syncthreads();
+    }
+}
+
+// The same of probabilities, whose entries say it alone: by one wave, 64 drafts at a
+// time (every wave of every block that needs it, rather than a launch of its own).
+template <typename E>
+__device__ __forceinline__ int kept_of_probs(const Args& a, int b, Rows rows) {
+    for (int i0 = 0;; i0 += 64) {
+        const int i = i0 + (threadIdx.x & 63);
+        const int64_t t = rows.start + i;
         bool keep = false;
         if (i < rows.n - 1) {
-            const int64_t t = rows.start + i;
             const int d = a.ids[t];
             if (d >= 0 && d < a.V) {
-                double2 np = make_double2(0.0, 0.0), nq = np;
-                if (a.logits) np = row_norm(a, t);
-                const double p = prob(a, value((const E*)a.target + t * a.ld_t, d), np.x, np.y);
-                double q = 1.0;
-                if (a.draft) {
-                    if (a.logits) nq = row_norm(a, a.T + t - b);
-                    q = prob(a, value((const E*)a.draft + (t - b) * a.ld_d, d), nq.x, nq.y);
-                }
+                const double p = (double)value(target_row<E>(a, t), d);
+                const double q = a.draft ? (double)value(draft_row<E>(a, t - b), d) : 1.0;
                 keep = (double)a.u[t] * q < p;
             }
         }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) ok[wave] = keep;
-        __syncthreads();
-        for (int w = 0; w < 4; ++w)
-            if (!ok[w]) return min(i0 + w, rows.n - 1);
+        const uint64_t not_kept = __builtin_amdgcn_ballot_w64(!keep);
+        if (not_kept) return i0 + __builtin_ctzll(not_kept);        // (the last row's at the latest)
     }
-    return max(rows.n - 1, 0);
 }
 
-// What is left over of entry v: (max(p - q, 0), p), NaN where p or q is.
-template <typename E>
-__device__ __forceinline__ double2 left_over(const Args& a, const E* zp, const E* zq, int onehot, const double4& n, int v) {
-    const double p = prob(a, value(zp, v), n.x, n.y);
-    double q = v == onehot ? 1.0 : 0.0;
-    if (zq) q = prob(a, value(zq, v), n.z, n.w);
-    const double d = p - q;
-    return make_double2(d <= 0.0 ? 0.0 : d, p);
-}
-
-// The row where a sequence's drafts end: its values, the draft's (or the id that
-// stands for them) unless it is the last one.
+// The row where a sequence's drafts end: its values, and the draft's (or the id
+// that stands for them) unless it is the last one.
 template <typename E>
 struct EndRow {
     const E *zp, *zq;
     int onehot;
-};
-template <typename E>
-__device__ __forceinline__ EndRow<E> end_row(const Args& a, int b, Rows rows, int kept) {
-    const int64_t t = rows.start + kept;
-    EndRow<E> r{(const E*)a.target + t * a.ld_t, nullptr, -1};
-    if (kept < rows.n - 1) {
-        if (a.draft) r.zq = (const E*)a.draft + (t - b) * a.ld_d;
-        else r.onehot = a.ids[t];
+    Norm np, nq;
+    __device__ __forceinline__ EndRow(const Args& a, int b, Rows rows, int kept) : zq(nullptr), onehot(-1), np{0.0, 1.0}, nq{0.0, 1.0} {
+        const int64_t t = rows.start + kept;
+        zp = target_row<E>(a, t);
+        if (kept < rows.n - 1) {
+            if (a.draft) zq = draft_row<E>(a, t - b);
+            else onehot = a.ids[t];
+        }
+        if (a.logits) {
+            const double4 n = a.row[b];
+            np = {n.x, n.y};
+            nq = {n.z, n.w};
+        }
     }
-    return r;
+    // (max(p - q, 0), p) of entry v with the values x and y, NaN where p or q is
+    __device__ __forceinline__ double2 left(const Args& a, int v, float x, float y) const {
+        const double p = prob(a, x, np);
+        const double q = zq ? prob(a, y, nq) : v == onehot ? 1.0 : 0.0;
+        const double d = p - q;
+        return make_double2(d <= 0.0 ? 0.0 : d, p);
+    }
+};
+
+// What is left over in every piece of the end rows.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) {
+    const int at = (int)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (at >= total) return;
+    const int b = at / a.pieces, piece = at - b * a.pieces, v0 = piece * kPiece;
+    const Rows rows = rows_of(a, b);
+    if (rows.n <= 0) return;
+    int kept;
+    if (a.logits) {
+        kept = a.kept[b];
+    } else {
+        kept = kept_of_probs<E>(a, b, rows);
+        if (piece == 0 && (threadIdx.x & 63) == 0) a.kept[b] = kept;
+    }
+    const EndRow<E> e(a, b, rows, kept);
+    const float fill = a.logits ? -INFINITY : 0.0f;
+    double r = 0.0, p = 0.0;
+    if (bad(e.np) || bad(e.nq)) {
+        r = p = __builtin_nan("");
+    } else {
+        Piece<E> x, y;
+        x.load(e.zp, v0, a.V, fill);
+        if (e.zq) y.load(e.zq, v0, a.V, fill);
+#pragma unroll
+        for (int i = 0; i < x.N; ++i)
+#pragma unroll
+            for (int k = 0; k < kPerVector<E>; ++k) {
+                const double2 l = e.left(a, x.at(v0, i) + k, x.x[i][k], e.zq ? y.x[i][k] : 0.0f);
+                r += l.x;
+                p += l.y;
+            }
+        r = wave_sum(r);
+        p = wave_sum(p);
+    }
+    if ((threadIdx.x & 63) == 0) a.left[at] = make_double2(r, p);
 }
 
-template <typename E>
-__global__ __launch_bounds__(kThreads) void left_over_kernel(Args a) {
-    __shared__ double red[4];
-    __shared__ double2 norms[2];
-    __shared__ int ok[4];
-    const int chunk = (int)(blockIdx.x % (unsigned)a.chunks), b = (int)(blockIdx.x / (unsigned)a.chunks);
-    const Rows rows = rows_of(a, b);
-    if (rows.n <= 0) {
-        if (chunk == 0 && threadIdx.x == 0) a.kept[b] = rows.n;
-        return;
-    }
-    const int kept = kept_drafts<E>(a, b, rows, ok);
-    const EndRow<E> e = end_row<E>(a, b, rows, kept);
-    double4 n = make_double4(0.0, 1.0, 0.0, 1.0);
-    if (a.logits) {
-        const int wave = threadIdx.x >> 6;
-        const int64_t t = rows.start + kept;
-        if (wave == 0) norms[0] = row_norm(a, t);
-        if (wave == 1) norms[1] = e.zq ? row_norm(a, a.T + t - b) : make_double2(0.0, 0.0);
-        __syncthreads();
-        n = make_double4(norms[0].x, norms[0].y, norms[1].x, norms[1].y);
-    }
-    if (chunk == 0 && threadIdx.x == 0) {
-        a.kept[b] = kept;
-        a.row[b] = n;
-    }
-    const int v0 = chunk * kChunk, v1 = min(a.V, v0 + kChunk);
-    double r = 0.0, p = 0.0;
-    for (int v = v0 + threadIdx.x; v < v1; v += kThreads) {
-        const double2 l = left_over(a, e.zp, e.zq, e.onehot, n, v);
-        r += l.x;
-        p += l.y;
-    }
-    r = block_sum(r, red);
-    p = block_sum(p, red);
-    if (threadIdx.x == 0) a.left[(int64_t)b * a.chunks + chunk] = make_double2(r, p);
+// ---- the draw ----------------------------------------------------------------------
+
+// Whether sequence b begins before an earlier offset (by the whole block): its
+// tokens would be written over another's.
+__device__ __forceinline__ bool overlaps(const Args& a, int b) {
+    const int start = a.offsets[b];
+    bool any = false;
+    for (int i = threadIdx.x; i < b; i += kThreads) any = any || a.offsets[i] > start;
+    return __syncthreads_or(any) != 0;
 }
 
 __device__ __forceinline__ void write_tokens(const Args& a, int b, Rows rows, int kept, int token) {
@@ -222,172 +350,197 @@ __device__ __forceinline__ void write_tokens(const Args& a, int b, Rows rows, in
     if (threadIdx.x == 0) a.accepted[b] = kept;
 }
 
+// Sum of the threads' values before this one's, and of all of them, in a fixed order.
+struct Scan {
+    double before, all;
+};
+__device__ __forceinline__ Scan block_scan(double v, double* red) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const double t = __shfl_up(s, o, 64);
+        if (lane >= o) s += t;
+    }
+    __syncthreads();
+    if (lane == 63) red[wave] = s;
+    __syncthreads();
+    double before = 0.0, all = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w == wave) before = all;
+        all += red[w];
+    }
+    // (what lies before the lane: the lane below's inclusive sum)
+    const double below = __shfl_up(s, 1, 64);
+    return {before + (lane > 0 ? below : 0.0), all};
+}
+
+// The first thread (and its item) that says `hit`, else the last that says
+// `positive`, else -1: items are numbered thread * PER + item, in order.
+__device__ __forceinline__ int first_or_last(int hit, int positive, int* red) {
+    if (threadIdx.x == 0) {
+        red[0] = INT32_MAX;
+        red[1] = -1;
+    }
+    __syncthreads();
+    if (hit >= 0) atomicMin(&red[0], hit);           // (the least, or greatest, integer: the same in any order)
+    if (positive >= 0) atomicMax(&red[1], positive);
+    __syncthreads();
+    return red[0] != INT32_MAX ? red[0] : red[1];
+}
+
 template <typename E>
 __global__ __launch_bounds__(kThreads) void draw_kernel(Args a) {
-    __shared__ double sum[kThreads];
-    __shared__ int found;
+    __shared__ double red[kWaves];
+    __shared__ double start;
+    __shared__ int pick[2];
     const int b = blockIdx.x;
-    const int kept = a.kept[b];
-    const Rows rows = rows_of(a, b);
+    Rows rows = rows_of(a, b);
+    if (overlaps(a, b)) rows.n = -1;
     if (rows.n <= 0) {
         if (threadIdx.x == 0) a.accepted[b] = rows.n;
         return;
     }
-    // totals, and the chunk in which the running sum passes the target
-    const double2* left = a.left + (int64_t)b * a.chunks;
-    double rt = 0.0, pt = 0.0;
-    for (int c = 0; c < a.chunks; ++c) {
-        rt += left[c].x;
-        pt += left[c].y;
+    const int kept = a.kept[b];
+    // the piece: each thread some of them in a row
+    const double2* left = a.left + (int64_t)b * a.pieces;
+    const int per = (a.pieces + kThreads - 1) / kThreads;
+    const int c0 = min(a.pieces, (int)threadIdx.x * per), c1 = min(a.pieces, c0 + per);
+    double rs = 0.0, ps = 0.0;
+    for (int c = c0; c < c1; ++c) {
+        rs += left[c].x;
+        ps += left[c].y;
     }
-    const bool use_p = !(rt > 0.0);
-    const double total = use_p ? pt : rt;
-    if (!(pt > 0.0 && pt < kInf && rt >= 0.0)) {
+    const Scan r = block_scan(rs, red), p = block_scan(ps, red);
+    if (!(p.all > 0.0 && p.all < kInf && r.all >= 0.0)) {
         write_tokens(a, b, rows, kept, -1);
         return;
     }
-    const double goal = (double)a.us[b] * total;
-    int chunk = -1, last = 0;
-    double before = 0.0, run = 0.0, last_before = 0.0;
-    for (int c = 0; c < a.chunks; ++c) {
-        const double s = use_p ? left[c].y : left[c].x;
-        if (s > 0.0) {
-            last = c;
-            last_before = run;
-        }
-        if (chunk < 0 && run + s > goal) {
-            chunk = c;
-            before = run;
-        }
-        run += s;
+    const bool use_p = !(r.all > 0.0);
+    const Scan s = use_p ? p : r;
+    const double goal = (double)a.us[b] * s.all;
+    int hit = -1, positive = -1;
+    double run = s.before;
+    for (int c = c0; c < c1; ++c) {
+        const double x = use_p ? left[c].y : left[c].x;
+        if (x > 0.0) positive = c;
+        if (hit < 0 && x > 0.0 && run + x > goal) hit = c;
+        run += x;
     }
-    if (chunk < 0) {
-        chunk = last;
-        before = last_before;
-    }
-    // within the chunk: each thread a run of entries
-    const EndRow<E> e = end_row<E>(a, b, rows, kept);
-    const double4 n = a.row[b];
-    constexpr int PER = kChunk / kThreads;
-    const int v0 = chunk * kChunk + threadIdx.x * PER, v1 = min(a.V, v0 + PER);
-    double s = 0.0;
-    for (int v = v0; v < v1; ++v) {
-        const double2 l = left_over(a, e.zp, e.zq, e.onehot, n, v);
-        s += use_p ? l.y : l.x;
-    }
-    sum[threadIdx.x] = s;
-    if (threadIdx.x == 0) found = -1;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double at = before;
-        int lastt = 0;
-        double last_at = before;
-        for (int i = 0; i < kThreads; ++i) {
-            if (sum[i] > 0.0) {
-                lastt = i;
-                last_at = at;
-            }
-            if (at + sum[i] > goal) {
-                lastt = i;
-                last_at = at;
-                break;
-            }
-            at += sum[i];
-        }
-        found = lastt;
-        sum[0] = last_at;
+    const int piece = first_or_last(hit, positive, pick);
+    run = s.before;
+    for (int c = c0; c < c1; ++c) {
+        if (c == piece) start = run;
+        run += use_p ? left[c].y : left[c].x;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        const int f0 = chunk * kChunk + found * PER, f1 = min(a.V, f0 + PER);
-        double at = sum[0];
-        int token = -1;
-        for (int v = f0; v < f1; ++v) {
-            const double2 l = left_over(a, e.zp, e.zq, e.onehot, n, v);
-            const double x = use_p ? l.y : l.x;
-            at += x;
-            if (x > 0.0) token = v;
-            if (at > goal) break;
+    // the entry: each thread eight of the piece in a row
+    constexpr int PER = kPiece / kThreads;
+    const EndRow<E> e(a, b, rows, kept);
+    const int v0 = piece * kPiece + threadIdx.x * PER;
+    double w[PER], sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int v = v0 + k;
+        w[k] = 0.0;
+        if (v < a.V) {
+            const double2 l = e.left(a, v, value(e.zp, v), e.zq ? value(e.zq, v) : 0.0f);
+            w[k] = use_p ? l.y : l.x;
         }
-        found = token;
+        sum += w[k];
     }
-    __syncthreads();
-    write_tokens(a, b, rows, kept, found);
+    run = start + block_scan(sum, red).before;
+    hit = positive = -1;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        run += w[k];
+        if (w[k] > 0.0) positive = v0 + k;
+        if (hit < 0 && w[k] > 0.0 && run > goal) hit = v0 + k;
+    }
+    write_tokens(a, b, rows, kept, first_or_last(hit, positive, pick));
 }
 
-// ---- temperature 0: (largest logit, its lowest id) of every chunk of the target's rows.
+// ---- temperature 0: (largest logit, its lowest id) of every piece of the target's rows.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void chunk_max_kernel(Args a) {
-    __shared__ float redm[4];
-    __shared__ int redi[4];
-    const int chunk = (int)(blockIdx.x % (unsigned)a.chunks), r = (int)(blockIdx.x / (unsigned)a.chunks);
-    const E* z = (const E*)a.target + (int64_t)r * a.ld_t;
-    const int v0 = chunk * kChunk, v1 = min(a.V, v0 + kChunk);
+__global__ __launch_bounds__(kThreads) void piece_max_kernel(Args a, int total) {
+    const int at = (int)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (at >= total) return;
+    const int r = at / a.pieces, v0 = (at - r * a.pieces) * kPiece;
+    Piece<E> x;
+    x.load(target_row<E>(a, r), v0, a.V, -INFINITY);
     float m = -INFINITY;
-    int at = a.V;
-    auto take = [&](float x, int v) {
-        if (x > m || (x == m && v < at) || (x != x && m == m)) { m = x; at = v; }
+    int id = a.V;
+    auto take = [&](float v, int i) {
+        if (v > m || (v == m && i < id) || (v != v && m == m)) { m = v; id = i; }
     };
-    for (int v = v0 + threadIdx.x; v < v1; v += kThreads) take(value(z, v), v);
+#pragma unroll
+    for (int i = 0; i < x.N; ++i)
+#pragma unroll
+        for (int e = 0; e < kPerVector<E>; ++e) take(x.x[i][e], x.at(v0, i) + e);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
-        const float x = __shfl_xor(m, o, 64);
-        const int v = __shfl_xor(at, o, 64);
-        take(x, v);
+        const float v = __shfl_xor(m, o, 64);
+        const int i = __shfl_xor(id, o, 64);
+        take(v, i);
     }
-    if ((threadIdx.x & 63) == 0) { redm[threadIdx.x >> 6] = m; redi[threadIdx.x >> 6] = at; }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 4; ++w) take(redm[w], redi[w]);
-        a.stats[(int64_t)r * a.chunks + chunk] = make_double2((double)m, (double)at);
-    }
+    if ((threadIdx.x & 63) == 0) a.stats[at] = make_double2((double)m, (double)id);
 }
 
-// A row's choice, -1 where it has none (NaN, +infinity or nothing but -infinity).
+// A row's choice, -1 where it has none (NaN, +infinity or nothing but -infinity), by
+// one wave.
 __device__ __forceinline__ int row_choice(const Args& a, int64_t r) {
-    const double2* st = a.stats + r * a.chunks;
-    double m = -kInf;
-    int at = -1;
-    for (int c = 0; c < a.chunks; ++c) {
-        if (st[c].x != st[c].x || st[c].x == kInf) return -1;
-        if (st[c].x > m) { m = st[c].x; at = (int)st[c].y; }
+    const double2* st = a.stats + r * a.pieces;
+    double m = -kInf, id = 0.0;
+    auto take = [&](double v, double i) {
+        if (v > m || (v == m && i < id) || (v != v && m == m)) { m = v; id = i; }
+    };
+    for (int c = threadIdx.x & 63; c < a.pieces; c += 64) take(st[c].x, st[c].y);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        const double v = __shfl_xor(m, o, 64), i = __shfl_xor(id, o, 64);
+        take(v, i);
     }
-    return at;
+    return m > -kInf && m < kInf ? (int)id : -1;
 }
 
 __global__ __launch_bounds__(kThreads) void greedy_kernel(Args a) {
-    __shared__ int first;
-    const int b = blockIdx.x;
-    const Rows rows = rows_of(a, b);
+    __shared__ int choice[kWaves];
+    const int b = blockIdx.x, wave = threadIdx.x >> 6;
+    Rows rows = rows_of(a, b);
+    if (overlaps(a, b)) rows.n = -1;
     if (rows.n <= 0) {
         if (threadIdx.x == 0) a.accepted[b] = rows.n;
         return;
     }
-    if (threadIdx.x == 0) first = rows.n - 1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < rows.n - 1; i += kThreads) {
-        const int c = row_choice(a, rows.start + i);
-        if (c < 0 || c != a.ids[rows.start + i]) {
-            atomicMin(&first, i);      // (the least of integers: the same in any order)
-            break;
+    for (int i0 = 0;; i0 += kWaves) {
+        if (i0 + wave < rows.n) {
+            const int c = row_choice(a, rows.start + i0 + wave);
+            if ((threadIdx.x & 63) == 0) choice[wave] = c;
         }
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) {
+            const int i = i0 + w;
+            if (i == rows.n - 1 || choice[w] < 0 || choice[w] != a.ids[rows.start + i]) {
+                write_tokens(a, b, rows, i, choice[w]);
+                return;
+            }
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    const int kept = first;
-    write_tokens(a, b, rows, kept, row_choice(a, rows.start + kept));
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 struct Layout {
-    int chunks;
-    size_t stats, left, row, kept, total;
+    int pieces;
+    size_t left, row, kept, total;       // (the rows' sums first)
 };
 Layout layout(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
     Layout l{};
-    l.chunks = (int)((V + kChunk - 1) / kChunk);
-    l.left = up((size_t)(T + draft_rows) * l.chunks * sizeof(double2));
-    l.row = l.left + up((size_t)B * l.chunks * sizeof(double2));
+    l.pieces = (int)((V + kPiece - 1) / kPiece);
+    l.left = up((size_t)(T + draft_rows) * l.pieces * sizeof(double2));
+    l.row = l.left + up((size_t)B * l.pieces * sizeof(double2));
     l.kept = l.row + up((size_t)B * sizeof(double4));
     l.total = l.kept + up((size_t)B * sizeof(int));
     return l;
@@ -395,14 +548,20 @@ Layout layout(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
 
 template <typename E>
 void launch(const Args& a, hipStream_t stream) {
+    auto blocks = [](int64_t n) { return (unsigned)((n + kWaves - 1) / kWaves); };
     if (a.temperature == 0.0) {
-        if (a.T > 0) chunk_max_kernel<E><<<(unsigned)a.T * a.chunks, kThreads, 0, stream>>>(a);
+        const int total = a.T * a.pieces;
+        if (total > 0) piece_max_kernel<E><<<blocks(total), kThreads, 0, stream>>>(a, total);
         greedy_kernel<<<a.B, kThreads, 0, stream>>>(a);
         return;
     }
-    const unsigned rows = (unsigned)(a.T + (a.draft ? a.draft_rows : 0));
-    if (a.logits && rows > 0) chunk_sums_kernel<E><<<rows * a.chunks, kThreads, 0, stream>>>(a);
-    left_over_kernel<E><<<(unsigned)a.B * a.chunks, kThreads, 0, stream>>>(a);
+    if (a.logits) {
+        const int total = (a.T + (a.draft ? a.draft_rows : 0)) * a.pieces;
+        if (total > 0) piece_sums_kernel<E><<<blocks(total), kThreads, 0, stream>>>(a, total);
+        end_rows_kernel<E><<<a.B, kEndWaves * 64, 0, stream>>>(a);
+    }
+    const int total = a.B * a.pieces;
+    left_over_kernel<E><<<blocks(total), kThreads, 0, stream>>>(a, total);
     draw_kernel<E><<<a.B, kThreads, 0, stream>>>(a);
 }
 
@@ -415,7 +574,7 @@ void launch_verify(const VerifyArgs& v, void* ws, hipStream_t stream) {
     uint8_t* w = reinterpret_cast<uint8_t*>(ws);
     Args a;
     static_cast<VerifyArgs&>(a) = v;
-    a.chunks = l.chunks;
+    a.pieces = l.pieces;
     a.c = v.temperature == 0.0 ? 0.0 : 1.4426950408889634 / v.temperature;
     a.stats = reinterpret_cast<double2*>(w);
     a.left = reinterpret_cast<double2*>(w + l.left);

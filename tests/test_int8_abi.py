@@ -82,9 +82,9 @@ def test_verification(puro):  # noqa: F811
         return L.puro_verify_drafts(B, T, rows, V, kind, t, p, ldp, q, ldq, ids, off, u, us, tau, tok, acc, ws, nb, None)
     assert f(B=-1) == f(T=-1) == f(rows=-1) == f(V=0) == f(rows=10) == f(ldp=99) == f(ldq=99) == ERR_SHAPE
     big = (1 << 22) + 1
-    assert f(ldp=big) == f(ldq=big) == f(V=(1 << 21) + 1, ldp=1 << 22, ldq=1 << 22) == f(B=(1 << 20) + 1) == ERR_SHAPE
+    assert f(ldp=big) == f(ldq=big) == f(V=(1 << 21) + 1, ldp=1 << 22, ldq=1 << 22) == f(B=(1 << 16) + 1) == ERR_SHAPE
     assert f(T=(1 << 20) + 1) == f(T=1 << 20, V=1 << 16, ldp=1 << 16, ldq=1 << 16) == ERR_SHAPE
-    assert f(B=1 << 20, V=1 << 16, ldp=1 << 16, ldq=1 << 16) == ERR_SHAPE
+    assert f(B=1 << 16, V=1 << 20, ldp=1 << 20, ldq=1 << 20) == ERR_SHAPE
     assert f(kind=2) == f(t=2) == ERR_UNSUPPORTED
     for tau in (-1.0, float("nan"), float("inf"), 1e-7, 2e6):
         assert f(tau=tau) == ERR_UNSUPPORTED

@@ -35,12 +35,24 @@ constexpr double kInf = __builtin_huge_val();
 
 struct Args : VerifyArgs {
     int pieces;           // of a row
-    double c;             // log2(e) / temperature
+    Divisor by_pieces;
+    double c, span;       // log2(e) / temperature; 1000 / c
     double2* stats;       // [T + draft_rows][pieces]: largest logit; sum of 2^((z - largest) c) (greedy: its id)
     double2* left;        // [B][pieces]: sums of max(p - q, 0) and of p
     double4* row;         // [B]: the end row's largest logits and reciprocal sums, target and draft
     int* kept;            // [B]: drafts kept
 };
+
+// The wave's piece of `total`: its index, row and place in it.
+struct Item {
+    int at, row, piece;
+    bool live;
+};
+__device__ __forceinline__ Item item(const Args& a, int total) {
+    const int at = (int)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int row = (int)a.by_pieces.quotient((uint32_t)at);
+    return {at, row, at - row * a.pieces, at < total};
+}
 
 // ---- values of a row ---------------------------------------------------------
 
@@ -92,30 +104,106 @@ struct Piece {
 
 // ---- arithmetic ----------------------------------------------------------------
 
-// 2^t in binary64 within 2^-45 relative, 0 far below: 2^n by the exponent, n the
-// nearest integer, times a polynomial of the rest f in [-1/2, 1/2] (interpolation
-// of degree 9 at the Chebyshev nodes, relative error 1.9e-14). t finite or
-// -infinity, at most 1000.
+// 2^f in binary64 for f in [-1/2, 1/2]: interpolation of degree 8 at the Chebyshev
+// nodes, relative error 1.1e-12. Of N values at a time, whose chains of dependent
+// instructions fill each other's waits.
+template <int N>
+__device__ __forceinline__ void exp2_fractions(const double f[N], double p[N]) {
+    constexpr double kC[9] = {0x1.63d1363a681b4p-20, 0x1.00dc4a5344ef5p-16, 0x1.4308ac85a69f8p-13, 0x1.5d8745a728209p-10, 0x1.3b2ab7181b77dp-7,
+                              0x1.c6b08dd6fd236p-5,  0x1.ebfbdff823cedp-3,  0x1.62e42fef84cf0p-1,  1.0};
+#pragma unroll
+    for (int k = 0; k < N; ++k) p[k] = kC[0];
+#pragma unroll
+    for (int c = 1; c < 9; ++c)
+#pragma unroll
+        for (int k = 0; k < N; ++k) p[k] = __builtin_fma(p[k], f[k], kC[c]);
+}
+// 2^t, 0 below 2^-1074; t at most 0 or -infinity.
 __device__ __forceinline__ double exp2_f64(double t) {
     t = fmax(t, -2000.0);
-    const double n = __builtin_rint(t), f = t - n;
-    double p = 0x1.b6571d9fbc782p-24;
-    p = __builtin_fma(p, f, 0x1.63ef9699f65f0p-20);
-    p = __builtin_fma(p, f, 0x1.ffcb7678dfe12p-17);
-    p = __builtin_fma(p, f, 0x1.43088e257f900p-13);
-    p = __builtin_fma(p, f, 0x1.5d87fe908f6f7p-10);
-    p = __builtin_fma(p, f, 0x1.3b2ab72b175e9p-7);
-    p = __builtin_fma(p, f, 0x1.c6b08d704411ap-5);
-    p = __builtin_fma(p, f, 0x1.ebfbdff8149f2p-3);
-    p = __builtin_fma(p, f, 0x1.62e42fefa39f7p-1);
-    p = __builtin_fma(p, f, 0x1.000000000003dp+0);
-    return __builtin_ldexp(p, (int)n);
+    const double n = __builtin_rint(t);
+    const double f[1] = {t - n};
+    double p[1];
+    exp2_fractions<1>(f, p);
+    return __builtin_ldexp(p[0], (int)n);
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
+// The largest of two or three, NaN passed over (one instruction; written as fmaxf the
+// compiler quiets each operand first).
+__device__ __forceinline__ float max2(float a, float b) {
+    float m;
+    asm("v_max_f32 %0, %1, %2" : "=v"(m) : "v"(a), "v"(b));
+    return m;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
+
+// What is no more than this counts as no probability at all.
+constexpr double kLeast = 0x1p-990;
+
+// 2^((x - m) c) of logits x no larger than m, of N at a time. Where m c is of ordinary
+// size (near: binary32's spacing at m is less than 1 in the exponent) logits are
+// clamped, as they stand, to where that is about 2^-1000 (below kLeast), and the
+// power of two is added to the exponent of 2^f: fewer instructions.
+struct Exponential {
+    double c, mc;
+    float lo;
+    bool near;
+    __device__ __forceinline__ Exponential(const Args& a, double m) : c(a.c), mc(m * a.c), lo((float)(m - a.span)), near(fabs(m) * a.c < 0x1p22) {}
+    template <bool NEAR, int N>
+    __device__ __forceinline__ void of(const float x[N], double e[N]) const {
+        if constexpr (!NEAR) {
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+            for (int k = 0; k < N; ++k) e[k] = exp2_f64(__builtin_fma((double)x[k], c, -mc));
+            return;
+        }
+        constexpr double kInt = 0x1.8p52;            // its last place is 1
+        double f[N], s[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] = __builtin_fma((double)max2(x[k], lo), c, -mc);
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k] = f[k] + kInt;
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] -= s[k] - kInt;
+        exp2_fractions<N>(f, e);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            e[k] = __hiloint2double(__double2hiint(e[k]) + (__double2loint(s[k]) << 20), __double2loint(e[k]));
+    }
+};
+
+// Sums and maxima over a wave, in every lane: rotations within 16 lanes, then swaps of
+// rows (no LDS).
+template <int ROR>
+__device__ __forceinline__ int rotated(int v) { return __builtin_amdgcn_update_dpp(0, v, 0x120 + ROR, 0xF, 0xF, false); }
+template <int ROR>
+__device__ __forceinline__ double rotated(double v) {
+    return __hiloint2double(rotated<ROR>(__double2hiint(v)), rotated<ROR>(__double2loint(v)));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    v += rotated<8>(v);
+    v += rotated<4>(v);
+    v += rotated<2>(v);
+    v += rotated<1>(v);
+    auto lo = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
+    auto hi = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
+    v = __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
+    lo = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
+    hi = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
+    return __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = max2(v, __int_as_float(rotated<8>(__float_as_int(v))));
+    v = max2(v, __int_as_float(rotated<4>(__float_as_int(v))));
+    v = max2(v, __int_as_float(rotated<2>(__float_as_int(v))));
+    v = max2(v, __int_as_float(rotated<1>(__float_as_int(v))));
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+    v = max2(__int_as_float(a[0]), __int_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return max2(__int_as_float(b[0]), __int_as_float(b[1]));
 }
 // The larger of two values, NaN if either is.
 template <typename F>
@@ -126,9 +214,15 @@ __device__ __forceinline__ F max_nan(F a, F b) { return a > b || a != a ? a : b;
 struct Norm {
     double m, inv;
 };
-// The probability of a logit x, or x itself.
-__device__ __forceinline__ double prob(const Args& a, float x, const Norm& n) {
-    return a.logits ? exp2_f64(__builtin_fma((double)x, a.c, -(n.m * a.c))) * n.inv : (double)x;
+// (an entry's probability: of a logit, or the value itself)
+__device__ __forceinline__ double prob_at(const Args& a, float x, const Norm& n) {
+    if (!a.logits) return (double)x;
+    const Exponential e(a, n.m);
+    const float v[1] = {x};
+    double p[1];
+    if (e.near) e.of<true, 1>(v, p);
+    else e.of<false, 1>(v, p);
+    return p[0] * n.inv;
 }
 __device__ __forceinline__ bool bad(const Norm& n) { return !(n.inv < kInf); }
 
@@ -156,31 +250,44 @@ __device__ __forceinline__ const E* draft_row(const Args& a, int64_t t) { return
 // an entry.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void piece_sums_kernel(Args a, int total) {
-    const int at = (int)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (at >= total) return;
-    const int r = at / a.pieces, v0 = (at - r * a.pieces) * kPiece;
+    const Item it = item(a, total);
+    if (!it.live) return;
+    const int r = it.row, v0 = it.piece * kPiece;
     const E* z = r < a.T ? target_row<E>(a, r) : draft_row<E>(a, r - a.T);
     Piece<E> x;
     x.load(z, v0, a.V, -INFINITY);
+    // the largest, and whether there is a NaN (which it passes over) or +infinity
     float m = -INFINITY;
+    uint64_t nan = 0;
 #pragma unroll
     for (int i = 0; i < x.N; ++i)
 #pragma unroll
-        for (int e = 0; e < kPerVector<E>; ++e) m = max_nan(m, x.x[i][e]);
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) m = max_nan(m, __shfl_xor(m, o, 64));
+        for (int e = 0; e < kPerVector<E>; e += 2) {
+            m = max3(m, x.x[i][e], x.x[i][e + 1]);
+            nan |= __builtin_amdgcn_ballot_w64(__builtin_isunordered(x.x[i][e], x.x[i][e + 1]));
+        }
+    m = wave_max(m);
     double s = 0.0;
-    if (m > -INFINITY && m < INFINITY) {
-        const double mc = (double)m * a.c;
-#pragma unroll
-        for (int i = 0; i < x.N; ++i)
-#pragma unroll
-            for (int e = 0; e < kPerVector<E>; ++e) s += exp2_f64(__builtin_fma((double)x.x[i][e], a.c, -mc));
-        s = wave_sum(s);
-    } else if (m != -INFINITY) {
+    if (nan != 0 || m == INFINITY) {
+        m = __builtin_nanf("");
         s = __builtin_nan("");
+    } else if (m > -INFINITY) {
+        const Exponential exponential(a, (double)m);
+        auto sum = [&](auto near_c) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < x.N; ++i)
+#pragma unroll
+                for (int e = 0; e < kPerVector<E>; e += 4) {
+                    double t[4];
+                    exponential.template of<decltype(near_c)::value, 4>(x.x[i] + e, t);
+                    s += (t[0] + t[1]) + (t[2] + t[3]);
+                }
+        };
+        if (exponential.near) sum(std::true_type{});
+        else sum(std::false_type{});
+        s = wave_sum(s);
     }
-    if ((threadIdx.x & 63) == 0) a.stats[at] = make_double2((double)m, s);
+    if ((threadIdx.x & 63) == 0) a.stats[it.at] = make_double2((double)m, s);
 }
 
 // A row's normaliser from its pieces, by one wave.
@@ -195,7 +302,7 @@ __device__ __forceinline__ Norm row_norm(const Args& a, int64_t r) {
     double s = 0.0;
     for (int c = lane; c < a.pieces; c += 64) {
         const double2 v = st[c];
-        s += v.y * exp2_f64(__builtin_fma(v.x, a.c, -(m * a.c)));
+        s += v.y * exp2_f64((v.x - m) * a.c);
     }
     return {m, 1.0 / wave_sum(s)};
 }
@@ -223,9 +330,9 @@ __global__ __launch_bounds__(kEndWaves * 64) void end_rows_kernel(Args a) {
             bool keep = false;
             const int d = drafted ? a.ids[t] : -1;
             if (d >= 0 && d < a.V && !bad(norms[wave])) {
-                const double p = prob(a, value(target_row<E>(a, t), d), norms[wave]);
-                const double q = a.draft ? prob(a, value(draft_row<E>(a, t - b), d), norms[wave + kEndRows]) : 1.0;
-                keep = (double)a.u[t] * q < p;
+                const double p = prob_at(a, value(target_row<E>(a, t), d), norms[wave]);
+                const double q = a.draft ? prob_at(a, value(draft_row<E>(a, t - b), d), norms[wave + kEndRows]) : 1.0;
+                keep = (double)a.u[t] * q < p && p > kLeast;
             }
             ok[wave] = keep;
         }
@@ -258,7 +365,7 @@ __device__ __forceinline__ int kept_of_probs(const Args& a, int b, Rows rows) {
             if (d >= 0 && d < a.V) {
                 const double p = (double)value(target_row<E>(a, t), d);
                 const double q = a.draft ? (double)value(draft_row<E>(a, t - b), d) : 1.0;
-                keep = (double)a.u[t] * q < p;
+                keep = (double)a.u[t] * q < p && p > kLeast;
             }
         }
         const uint64_t not_kept = __builtin_amdgcn_ballot_w64(!keep);
@@ -286,21 +393,51 @@ struct EndRow {
             nq = {n.z, n.w};
         }
     }
-    // (max(p - q, 0), p) of entry v with the values x and y, NaN where p or q is
-    __device__ __forceinline__ double2 left(const Args& a, int v, float x, float y) const {
-        const double p = prob(a, x, np);
-        const double q = zq ? prob(a, y, nq) : v == onehot ? 1.0 : 0.0;
-        const double d = p - q;
-        return make_double2(d <= 0.0 ? 0.0 : d, p);
-    }
 };
+// (max(p - q, 0), p), NaN where p or q is
+__device__ __forceinline__ double2 left(double p, double q) {
+    const double d = p - q;
+    return make_double2(d <= kLeast ? 0.0 : d, p);
+}
+// f(g), where g(v, x, y, l) gives N entries from v on with the values x and y (the
+// draft's) their l = left(p, q), by the kind of the row's entries: logits of
+// ordinary size, others, probabilities.
+template <int N, typename E, typename F>
+__device__ __forceinline__ void with_left(const Args& a, const EndRow<E>& e, F&& f) {
+    auto run = [&](auto kind_c, auto q_c) __attribute__((always_inline)) {
+        constexpr int KIND = decltype(kind_c)::value;          // 0: probabilities, 1, 2: logits
+        constexpr bool Q = decltype(q_c)::value;
+        const Exponential ep(a, e.np.m), eq(a, e.nq.m);
+        f([&](int v, const float* x, const float* y, double2* l) __attribute__((always_inline)) {
+            double p[N], q[N];
+            if constexpr (KIND != 0) {
+                ep.template of<KIND == 1, N>(x, p);
+                if constexpr (Q) eq.template of<KIND == 1, N>(y, q);
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const double pk = KIND != 0 ? p[k] * e.np.inv : (double)x[k];
+                double qk = v + k == e.onehot ? 1.0 : 0.0;
+                if constexpr (Q) qk = KIND != 0 ? q[k] * e.nq.inv : (double)y[k];
+                l[k] = left(pk, qk);
+            }
+        });
+    };
+    auto with_q = [&](auto kind_c) __attribute__((always_inline)) {
+        if (e.zq) run(kind_c, std::true_type{});
+        else run(kind_c, std::false_type{});
+    };
+    if (!a.logits) with_q(std::integral_constant<int, 0>{});
+    else if (Exponential(a, e.np.m).near && Exponential(a, e.nq.m).near) with_q(std::integral_constant<int, 1>{});
+    else with_q(std::integral_constant<int, 2>{});
+}
 
 // What is left over in every piece of the end rows.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) {
-    const int at = (int)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (at >= total) return;
-    const int b = at / a.pieces, piece = at - b * a.pieces, v0 = piece * kPiece;
+    const Item it = item(a, total);
+    if (!it.live) return;
+    const int b = it.row, v0 = it.piece * kPiece;
     const Rows rows = rows_of(a, b);
     if (rows.n <= 0) return;
     int kept;
@@ -308,7 +445,7 @@ __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) 
         kept = a.kept[b];
     } else {
         kept = kept_of_probs<E>(a, b, rows);
-        if (piece == 0 && (threadIdx.x & 63) == 0) a.kept[b] = kept;
+        if (it.piece == 0 && (threadIdx.x & 63) == 0) a.kept[b] = kept;
     }
     const EndRow<E> e(a, b, rows, kept);
     const float fill = a.logits ? -INFINITY : 0.0f;
@@ -319,29 +456,35 @@ __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) 
         Piece<E> x, y;
         x.load(e.zp, v0, a.V, fill);
         if (e.zq) y.load(e.zq, v0, a.V, fill);
+        else y = x;
+        with_left<4>(a, e, [&](auto&& left_at) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < x.N; ++i)
+            for (int i = 0; i < x.N; ++i)
 #pragma unroll
-            for (int k = 0; k < kPerVector<E>; ++k) {
-                const double2 l = e.left(a, x.at(v0, i) + k, x.x[i][k], e.zq ? y.x[i][k] : 0.0f);
-                r += l.x;
-                p += l.y;
-            }
+                for (int k = 0; k < kPerVector<E>; k += 4) {
+                    double2 l[4];
+                    left_at(x.at(v0, i) + k, x.x[i] + k, y.x[i] + k, l);
+                    r += (l[0].x + l[1].x) + (l[2].x + l[3].x);
+                    p += (l[0].y + l[1].y) + (l[2].y + l[3].y);
+                }
+        });
         r = wave_sum(r);
         p = wave_sum(p);
     }
-    if ((threadIdx.x & 63) == 0) a.left[at] = make_double2(r, p);
+    if ((threadIdx.x & 63) == 0) a.left[it.at] = make_double2(r, p);
 }
 
 // ---- the draw ----------------------------------------------------------------------
+// One block per sequence, a chain of short steps: what they need of memory is asked
+// for at the start, and every wave finds the piece by itself (no barrier).
 
-// Whether sequence b begins before an earlier offset (by the whole block): its
-// tokens would be written over another's.
+// Whether sequence b begins before an earlier offset (its tokens would be written
+// over another's); by every wave.
 __device__ __forceinline__ bool overlaps(const Args& a, int b) {
     const int start = a.offsets[b];
     bool any = false;
-    for (int i = threadIdx.x; i < b; i += kThreads) any = any || a.offsets[i] > start;
-    return __syncthreads_or(any) != 0;
+    for (int i = threadIdx.x & 63; i < b; i += 64) any = any || a.offsets[i] > start;
+    return __builtin_amdgcn_ballot_w64(any) != 0;
 }
 
 __device__ __forceinline__ void write_tokens(const Args& a, int b, Rows rows, int kept, int token) {
@@ -350,125 +493,144 @@ __device__ __forceinline__ void write_tokens(const Args& a, int b, Rows rows, in
     if (threadIdx.x == 0) a.accepted[b] = kept;
 }
 
-// Sum of the threads' values before this one's, and of all of them, in a fixed order.
-struct Scan {
-    double before, all;
-};
-__device__ __forceinline__ Scan block_scan(double v, double* red) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double s = v;
+// The sum of the lanes' values up to and with this one's, in a fixed order.
+__device__ __forceinline__ double wave_scan(double v) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const double t = __shfl_up(s, o, 64);
-        if (lane >= o) s += t;
+        const double t = __shfl_up(v, o, 64);
+        if (lane >= o) v += t;
     }
-    __syncthreads();
-    if (lane == 63) red[wave] = s;
-    __syncthreads();
-    double before = 0.0, all = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) before = all;
-        all += red[w];
-    }
-    // (what lies before the lane: the lane below's inclusive sum)
-    const double below = __shfl_up(s, 1, 64);
-    return {before + (lane > 0 ? below : 0.0), all};
+    return v;
 }
-
-// The first thread (and its item) that says `hit`, else the last that says
-// `positive`, else -1: items are numbered thread * PER + item, in order.
-__device__ __forceinline__ int first_or_last(int hit, int positive, int* red) {
-    if (threadIdx.x == 0) {
-        red[0] = INT32_MAX;
-        red[1] = -1;
-    }
-    __syncthreads();
-    if (hit >= 0) atomicMin(&red[0], hit);           // (the least, or greatest, integer: the same in any order)
-    if (positive >= 0) atomicMax(&red[1], positive);
-    __syncthreads();
-    return red[0] != INT32_MAX ? red[0] : red[1];
+__device__ __forceinline__ double lane_below(double v) {
+    const double t = __shfl_up(v, 1, 64);
+    return (threadIdx.x & 63) > 0 ? t : 0.0;
 }
 
 template <typename E>
 __global__ __launch_bounds__(kThreads) void draw_kernel(Args a) {
-    __shared__ double red[kWaves];
-    __shared__ double start;
-    __shared__ int pick[2];
-    const int b = blockIdx.x;
+    __shared__ double sums[kWaves];
+    __shared__ int hits[kWaves], positives[kWaves];
+    const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // the pieces: each lane some of them in a row
+    const double2* left = a.left + (int64_t)b * a.pieces;
+    const int per = (a.pieces + 63) / 64;
+    const int c0 = min(a.pieces, lane * per), c1 = min(a.pieces, c0 + per);
+    const float us = a.T > 0 ? a.us[b] : 0.0f;        // (none are given for no rows)
+    const int kept_at = a.kept[b];
+    double2 l0 = make_double2(0.0, 0.0);
+    if (c0 < c1) l0 = left[c0];
     Rows rows = rows_of(a, b);
     if (overlaps(a, b)) rows.n = -1;
     if (rows.n <= 0) {
         if (threadIdx.x == 0) a.accepted[b] = rows.n;
         return;
     }
-    const int kept = a.kept[b];
-    // the piece: each thread some of them in a row
-    const double2* left = a.left + (int64_t)b * a.pieces;
-    const int per = (a.pieces + kThreads - 1) / kThreads;
-    const int c0 = min(a.pieces, (int)threadIdx.x * per), c1 = min(a.pieces, c0 + per);
-    double rs = 0.0, ps = 0.0;
-    for (int c = c0; c < c1; ++c) {
+    const int kept = kept_at;
+    const EndRow<E> e(a, b, rows, kept);
+    double rs = l0.x, ps = l0.y;
+    for (int c = c0 + 1; c < c1; ++c) {
         rs += left[c].x;
         ps += left[c].y;
     }
-    const Scan r = block_scan(rs, red), p = block_scan(ps, red);
-    if (!(p.all > 0.0 && p.all < kInf && r.all >= 0.0)) {
+    const double r = wave_scan(rs), p = wave_scan(ps);
+    const double r_all = __shfl(r, 63, 64), p_all = __shfl(p, 63, 64);
+    if (!(p_all > 0.0 && p_all < kInf && r_all >= 0.0)) {
         write_tokens(a, b, rows, kept, -1);
         return;
     }
-    const bool use_p = !(r.all > 0.0);
-    const Scan s = use_p ? p : r;
-    const double goal = (double)a.us[b] * s.all;
+    const bool use_p = !(r_all > 0.0);
+    const double goal = (double)us * (use_p ? p_all : r_all);
+    // (where rounding leaves no piece: the last one with a share)
     int hit = -1, positive = -1;
-    double run = s.before;
+    double run = lane_below(use_p ? p : r), hit_at = 0.0, positive_at = 0.0;
     for (int c = c0; c < c1; ++c) {
-        const double x = use_p ? left[c].y : left[c].x;
-        if (x > 0.0) positive = c;
-        if (hit < 0 && x > 0.0 && run + x > goal) hit = c;
+        const double2 l = c == c0 ? l0 : left[c];
+        const double x = use_p ? l.y : l.x;
+        if (x > 0.0) {
+            positive = c;
+            positive_at = run;
+            if (hit < 0 && run + x > goal) {
+                hit = c;
+                hit_at = run;
+            }
+        }
         run += x;
     }
-    const int piece = first_or_last(hit, positive, pick);
-    run = s.before;
-    for (int c = c0; c < c1; ++c) {
-        if (c == piece) start = run;
-        run += use_p ? left[c].y : left[c].x;
-    }
-    __syncthreads();
+    const uint64_t hits_in = __builtin_amdgcn_ballot_w64(hit >= 0), any_in = __builtin_amdgcn_ballot_w64(positive >= 0);
+    const int from = hits_in ? __builtin_ctzll(hits_in) : 63 - __builtin_clzll(any_in);
+    const int piece = __shfl(hits_in ? hit : positive, from, 64);
+    const double start = __shfl(hits_in ? hit_at : positive_at, from, 64);
     // the entry: each thread eight of the piece in a row
-    constexpr int PER = kPiece / kThreads;
-    const EndRow<E> e(a, b, rows, kept);
+    constexpr int PER = kPiece / kThreads, NV = PER / kPerVector<E>;
     const int v0 = piece * kPiece + threadIdx.x * PER;
-    double w[PER], sum = 0.0;
+    float x[PER], y[PER];
+    auto values = [&](const E* z, float* to) __attribute__((always_inline)) {
+        if (v0 + PER <= a.V) {
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int v = v0 + k;
-        w[k] = 0.0;
-        if (v < a.V) {
-            const double2 l = e.left(a, v, value(e.zp, v), e.zq ? value(e.zq, v) : 0.0f);
-            w[k] = use_p ? l.y : l.x;
+            for (int i = 0; i < NV; ++i) {
+                uint4 w;
+                __builtin_memcpy(&w, z + v0 + i * kPerVector<E>, 16);
+                unpack(w, to + i * kPerVector<E>, z);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) to[k] = v0 + k < a.V ? value(z, v0 + k) : a.logits ? -INFINITY : 0.0f;
         }
-        sum += w[k];
-    }
-    run = start + block_scan(sum, red).before;
+    };
+    values(e.zp, x);
+    values(e.zq ? e.zq : e.zp, y);
+    double w[PER], sum = 0.0;
+    with_left<PER>(a, e, [&](auto&& left_at) __attribute__((always_inline)) {
+        double2 l[PER];
+        left_at(v0, x, y, l);
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            w[k] = use_p ? (l[k].y > kLeast ? l[k].y : 0.0) : l[k].x;
+            sum += w[k];
+        }
+    });
+    const double up_to = wave_scan(sum);
+    if (lane == 63) sums[wave] = up_to;
+    __syncthreads();
+    run = start;
+#pragma unroll
+    for (int i = 0; i < kWaves - 1; ++i) run += i < wave ? sums[i] : 0.0;
+    run += lane_below(up_to);
     hit = positive = -1;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         run += w[k];
-        if (w[k] > 0.0) positive = v0 + k;
-        if (hit < 0 && w[k] > 0.0 && run > goal) hit = v0 + k;
+        if (w[k] > 0.0) {
+            positive = v0 + k;
+            if (hit < 0 && run > goal) hit = v0 + k;
+        }
     }
-    write_tokens(a, b, rows, kept, first_or_last(hit, positive, pick));
+    const uint64_t wave_hits = __builtin_amdgcn_ballot_w64(hit >= 0), wave_any = __builtin_amdgcn_ballot_w64(positive >= 0);
+    const int h = __shfl(hit, wave_hits ? __builtin_ctzll(wave_hits) : 0, 64);
+    const int q = __shfl(positive, wave_any ? 63 - __builtin_clzll(wave_any) : 0, 64);
+    if (lane == 0) {
+        hits[wave] = h;
+        positives[wave] = q;
+    }
+    __syncthreads();
+    int token = -1;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) token = max(token, positives[i]);
+#pragma unroll
+    for (int i = kWaves - 1; i >= 0; --i) token = hits[i] >= 0 ? hits[i] : token;
+    write_tokens(a, b, rows, kept, token);
 }
 
 // ---- temperature 0: (largest logit, its lowest id) of every piece of the target's rows.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void piece_max_kernel(Args a, int total) {
-    const int at = (int)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (at >= total) return;
-    const int r = at / a.pieces, v0 = (at - r * a.pieces) * kPiece;
+    const Item it = item(a, total);
+    if (!it.live) return;
+    const int v0 = it.piece * kPiece;
     Piece<E> x;
-    x.load(target_row<E>(a, r), v0, a.V, -INFINITY);
+    x.load(target_row<E>(a, it.row), v0, a.V, -INFINITY);
     float m = -INFINITY;
     int id = a.V;
     auto take = [&](float v, int i) {
@@ -484,7 +646,7 @@ __global__ __launch_bounds__(kThreads) void piece_max_kernel(Args a, int total) 
         const int i = __shfl_xor(id, o, 64);
         take(v, i);
     }
-    if ((threadIdx.x & 63) == 0) a.stats[at] = make_double2((double)m, (double)id);
+    if ((threadIdx.x & 63) == 0) a.stats[it.at] = make_double2((double)m, (double)id);
 }
 
 // A row's choice, -1 where it has none (NaN, +infinity or nothing but -infinity), by
@@ -575,7 +737,9 @@ void launch_verify(const VerifyArgs& v, void* ws, hipStream_t stream) {
     Args a;
     static_cast<VerifyArgs&>(a) = v;
     a.pieces = l.pieces;
+    a.by_pieces = Divisor::of((uint32_t)l.pieces);
     a.c = v.temperature == 0.0 ? 0.0 : 1.4426950408889634 / v.temperature;
+    a.span = v.temperature == 0.0 ? 0.0 : 1000.0 / a.c;
     a.stats = reinterpret_cast<double2*>(w);
     a.left = reinterpret_cast<double2*>(w + l.left);
     a.row = reinterpret_cast<double4*>(w + l.row);

@@ -615,6 +615,26 @@ puro_status puro_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* A, int
                            int64_t ldd, int accumulate, const uint16_t* bias, const uint16_t* residual, int64_t ldr,
                            void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* The int8 linear layer: Y = X W^T with X [M, K] and W [N, K] in BF16 (dense rows)
+ * and its backward, as a sequence of the calls above: X and dY quantised per token
+ * for the products that reduce over channels and per channel for the one that
+ * reduces over tokens, W per output and per input channel.
+ *   saved: xq_t [K, M16] (int8; M16 = M rounded up to 16, zeros behind the tokens),
+ *   x_scale [K], wq_t [K, N], w_scale [K]: the transposed copies for the backward.
+ * Forward: Y [M, N] (BF16); saved NULL: no backward follows, the copies are not made.
+ * Backward: dX [M, K] (BF16) and dW [N, K] (FP32; += when accumulate_dW != 0); either
+ * may be NULL to skip it. M = 0 is valid (dW: zeros, or as it was).
+ * Requirements: N and K multiples of 16 (else PURO_ERR_ALIGN), M, N and K at most
+ * 131056; all pointers and ws 16-byte aligned; ws: the matching
+ * *_workspace_size(M, N, K) bytes. */
+size_t puro_int8_linear_fwd_workspace_size(int64_t M, int64_t N, int64_t K);
+size_t puro_int8_linear_bwd_workspace_size(int64_t M, int64_t N, int64_t K);
+puro_status puro_int8_linear_fwd(const uint16_t* X, const uint16_t* W, int64_t M, int64_t N, int64_t K, uint16_t* Y,
+                                 const puro_linear_saved* saved, void* ws, size_t ws_bytes, hipStream_t stream);
+puro_status puro_int8_linear_bwd(const uint16_t* dY, const puro_linear_saved* saved, int64_t M, int64_t N, int64_t K,
+                                 uint16_t* dX, float* dW, int accumulate_dW, void* ws, size_t ws_bytes,
+                                 hipStream_t stream);
+
 /* --------------------------------------- verification of drafted tokens ---
  * A distilled student (puro_lm_head_distill_*) proposes tokens; the model itself
  * scores them all in one pass, and each is kept with the probability that leaves
@@ -630,7 +650,8 @@ puro_status puro_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* A, int
  *     or after all, the token drawn from max(p - q, 0) (from p in the last row,
  *     and where that is 0 everywhere): the least v with
  *     sum_{w <= v} rest[w] > uniform_sample[b] sum_w rest[w]
- *     (the last v with rest[v] > 0 where rounding leaves none).
+ *     (the last v with rest[v] > 0 where rounding leaves none). What is no more than
+ *     2^-990 counts as 0.
  * tokens[offsets[b] ..]: the kept ids, the drawn token, then -1; accepted[b]: how
  * many were kept. temperature 0 (LOGITS): the row's largest logit, the lowest id
  * among equals, is the token, and a draft is kept where it is that; draft,

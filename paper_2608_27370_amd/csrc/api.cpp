@@ -1030,8 +1030,9 @@ puro_status puro_quantize_int8(const uint16_t* x, int64_t rows, int64_t cols, in
         if (!aligned16(ws)) return PURO_ERR_ALIGN;
         if (ws_bytes < quant_int8_ws_bytes(rows, cols)) return PURO_ERR_WORKSPACE;
     }
-    if (q) launch_quantize_int8(QuantInt8Args{x, rows, cols, ld, q, scale, nullptr, 0.0f, nullptr, 0}, stream);
-    if (qT) launch_quantize_int8_t(x, rows, cols, ld, qT, ld_qT, scaleT, ws, stream);
+    const QuantInt8Args a{x, rows, cols, ld, q, scale, nullptr, 0.0f, nullptr, 0};
+    if (qT) launch_quantize_int8_both(a, qT, ld_qT, scaleT, ws, stream);
+    else launch_quantize_int8(a, stream);
     return launched();
 }
 
@@ -1098,6 +1099,135 @@ puro_status puro_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* A, int
     }
     launch_int8_gemm(Int8Problem{M, N, K, A, B, lda, ldb, a_scale, b_scale, D, ldd, f32, accumulate != 0, bias, residual, ldr},
                      ws, stream);
+    return launched();
+}
+
+}  // extern "C"
+
+// ------------------------------------------------- the int8 linear layer
+namespace {
+
+int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
+
+puro_status check_int8_linear(int64_t M, int64_t N, int64_t K) {
+    if (M < 0 || N < 0 || K < 0 || M > kMaxInt8K || N > kMaxInt8K || K > kMaxInt8K) return PURO_ERR_SHAPE;
+    return (N % 16) == 0 && (K % 16) == 0 ? PURO_OK : PURO_ERR_ALIGN;
+}
+
+// The workspace of one tensor [rows, cols] quantised for a pass: its codes, scales,
+// and (both) the transposed copy and what makes it.
+struct Int8Copies {
+    size_t q, scale, qT, scaleT, part;
+    Int8Copies(Carver& c, int64_t rows, int64_t cols, bool row, bool transposed) : q(0), scale(0), qT(0), scaleT(0), part(0) {
+        if (row) {
+            q = c.take((size_t)rows * cols);
+            scale = c.take((size_t)rows * sizeof(float));
+        }
+        if (transposed) {
+            qT = c.take((size_t)up16(rows) * cols);
+            scaleT = c.take((size_t)cols * sizeof(float));
+        }
+        part = c.take(rows > 0 && cols > 0 ? quant_int8_ws_bytes(rows, cols) : 0);
+    }
+};
+
+struct Int8FwdLayout {
+    Carver c;
+    Int8Copies x, w;
+    size_t gemm;
+    Int8FwdLayout(int64_t M, int64_t N, int64_t K)
+        : x(c, M, K, true, false), w(c, N, K, true, false), gemm(c.take(int8_gemm_ws_bytes(M, N, K))) {}
+};
+
+struct Int8BwdLayout {
+    Carver c;
+    Int8Copies dy;
+    size_t gemm;
+    Int8BwdLayout(int64_t M, int64_t N, int64_t K) : dy(c, M, N, true, true) {
+        const size_t a = int8_gemm_ws_bytes(M, K, N), b = int8_gemm_ws_bytes(N, K, up16(M));
+        gemm = c.take(a > b ? a : b);
+    }
+};
+
+// One product D [M, N] of dense operands (a reduction of 0: zeros).
+void int8_product(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* sa, const void* B, int64_t ldb,
+                  const float* sb, void* D, bool f32, int accumulate, void* ws, hipStream_t stream) {
+    if (M == 0 || N == 0) return;
+    launch_int8_gemm(Int8Problem{M, N, K, (const int8_t*)A, (const int8_t*)B, lda, ldb, sa, sb, D, N, f32, accumulate, nullptr, nullptr, 0},
+                     ws, stream);
+}
+
+puro_status check_int8_saved(const puro_linear_saved* s) {
+    if (!s->xq_t || !s->x_scale || !s->wq_t || !s->w_scale) return PURO_ERR_NULL;
+    return aligned16(s->xq_t) && aligned16(s->x_scale) && aligned16(s->wq_t) && aligned16(s->w_scale) ? PURO_OK : PURO_ERR_ALIGN;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t puro_int8_linear_fwd_workspace_size(int64_t M, int64_t N, int64_t K) {
+    return check_int8_linear(M, N, K) == PURO_OK ? Int8FwdLayout(M, N, K).c.used : 0;
+}
+
+size_t puro_int8_linear_bwd_workspace_size(int64_t M, int64_t N, int64_t K) {
+    return check_int8_linear(M, N, K) == PURO_OK ? Int8BwdLayout(M, N, K).c.used : 0;
+}
+
+puro_status puro_int8_linear_fwd(const uint16_t* X, const uint16_t* W, int64_t M, int64_t N, int64_t K, uint16_t* Y,
+                                 const puro_linear_saved* saved, void* ws, size_t ws_bytes, hipStream_t stream) {
+    puro_status st = check_int8_linear(M, N, K);
+    if (st != PURO_OK) return st;
+    const Int8FwdLayout l(M, N, K);
+    if (l.c.used > 0 && !ws) return PURO_ERR_NULL;
+    if ((M > 0 && K > 0 && !X) || (N > 0 && K > 0 && !W) || (M > 0 && N > 0 && !Y)) return PURO_ERR_NULL;
+    if (saved && K > 0 && M > 0 && N > 0 && (st = check_int8_saved(saved)) != PURO_OK) return st;
+    if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(ws)) return PURO_ERR_ALIGN;
+    if (ws_bytes < l.c.used) return PURO_ERR_WORKSPACE;
+    uint8_t* w = reinterpret_cast<uint8_t*>(ws);
+    auto quantise = [&](const uint16_t* x, int64_t rows, const Int8Copies& at, uint8_t* qT, float* scaleT) {
+        if (rows == 0 || K == 0) return;
+        const QuantInt8Args a{x, rows, K, K, (int8_t*)(w + at.q), (float*)(w + at.scale), nullptr, 0.0f, nullptr, 0};
+        if (saved) launch_quantize_int8_both(a, (int8_t*)qT, up16(rows), scaleT, w + at.part, stream);
+        else launch_quantize_int8(a, stream);
+    };
+    if (M == 0) return PURO_OK;
+    quantise(X, M, l.x, saved ? saved->xq_t : nullptr, saved ? saved->x_scale : nullptr);
+    quantise(W, N, l.w, saved ? saved->wq_t : nullptr, saved ? saved->w_scale : nullptr);
+    int8_product(M, N, K, w + l.x.q, K, (float*)(w + l.x.scale), w + l.w.q, K, (float*)(w + l.w.scale), Y, false, 0, w + l.gemm, stream);
+    return launched();
+}
+
+puro_status puro_int8_linear_bwd(const uint16_t* dY, const puro_linear_saved* saved, int64_t M, int64_t N, int64_t K,
+                                 uint16_t* dX, float* dW, int accumulate_dW, void* ws, size_t ws_bytes,
+                                 hipStream_t stream) {
+    puro_status st = check_int8_linear(M, N, K);
+    if (st != PURO_OK) return st;
+    if (!aligned16(dY) || !aligned16(dX) || !aligned16(dW) || !aligned16(ws)) return PURO_ERR_ALIGN;
+    if (K == 0 || N == 0) {
+        // (dX is a sum over no channels)
+        if (!dX || M == 0 || K == 0) return PURO_OK;
+        launch_zero(dX, M * K * 2, stream);
+        return launched();
+    }
+    if (M == 0) {
+        if (!dW || accumulate_dW) return PURO_OK;
+        launch_zero(dW, N * K * 4, stream);
+        return launched();
+    }
+    const Int8BwdLayout l(M, N, K);
+    if (!dY || !saved || !ws) return PURO_ERR_NULL;
+    if ((st = check_int8_saved(saved)) != PURO_OK) return st;
+    if (ws_bytes < l.c.used) return PURO_ERR_WORKSPACE;
+    if (!dX && !dW) return PURO_OK;
+    uint8_t* w = reinterpret_cast<uint8_t*>(ws);
+    const QuantInt8Args a{dY, M, N, N, dX ? (int8_t*)(w + l.dy.q) : nullptr, (float*)(w + l.dy.scale), nullptr, 0.0f, nullptr, 0};
+    if (dW) launch_quantize_int8_both(a, (int8_t*)(w + l.dy.qT), up16(M), (float*)(w + l.dy.scaleT), w + l.dy.part, stream);
+    else launch_quantize_int8(a, stream);
+    if (dX) int8_product(M, K, N, w + l.dy.q, N, a.scale, saved->wq_t, N, saved->w_scale, dX, false, 0, w + l.gemm, stream);
+    if (dW)
+        int8_product(N, K, up16(M), w + l.dy.qT, up16(M), (float*)(w + l.dy.scaleT), saved->xq_t, up16(M), saved->x_scale, dW, true,
+                     accumulate_dW != 0, w + l.gemm, stream);
     return launched();
 }
 

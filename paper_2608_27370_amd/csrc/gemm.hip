@@ -43,10 +43,17 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
     if (b_tensor) alpha *= sb[0];
     float4 s;
     if constexpr (INT) {
-        int4 v = *reinterpret_cast<const int4*>(partial + m * N + n);
-        for (int k = 1; k < splits; ++k) {
-            const int4 t = *reinterpret_cast<const int4*>(partial + ((int64_t)k * M + m) * N + n);
-            v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
+        // (integers: eight ranges' loads at a time, past the last one that one again, not
+        // added; one after the other 77x1531 of 10 ranges took 4.5 us)
+        int4 v = make_int4(0, 0, 0, 0);
+        for (int k0 = 0; k0 < splits; k0 += 8) {
+            int4 t[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                t[u] = *reinterpret_cast<const int4*>(partial + ((int64_t)min(k0 + u, splits - 1) * M + m) * N + n);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (k0 + u < splits) { v.x += t[u].x; v.y += t[u].y; v.z += t[u].z; v.w += t[u].w; }
         }
         const float r = sa[m];
         float c[4];

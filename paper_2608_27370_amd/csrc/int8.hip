@@ -94,12 +94,10 @@ __device__ __forceinline__ void swiglu_values(const uint32_t g[4], const uint32_
 }
 
 template <int SRC, int TPR, int NC>
-__global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args a) {
-    __shared__ uint32_t red[4];
-    __shared__ float sums[4];
+__device__ __forceinline__ void quant_rows(const QuantInt8Args& a, int64_t block, uint32_t* red, float* sums) {
     constexpr bool WAVE = TPR == 64;
     const int t = WAVE ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+    const int64_t row = WAVE ? block * 4 + (threadIdx.x >> 6) : block;
     if (WAVE && row >= a.rows) return;          // (a whole wave; its block meets at no barrier)
     const int cpr = (int)(a.cols / 8);
     const uint16_t* xr = a.x + row * a.ld;
@@ -178,6 +176,13 @@ __global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args
     }
 }
 
+template <int SRC, int TPR, int NC>
+__global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args a) {
+    __shared__ uint32_t red[4];
+    __shared__ float sums[4];
+    quant_rows<SRC, TPR, NC>(a, blockIdx.x, red, sums);
+}
+
 // Rows longer than the registers hold: one block per row, the values formed twice
 // (the second time from the caches).
 template <int SRC>
@@ -235,12 +240,19 @@ __global__ __launch_bounds__(kThreads) void quant_long_rows_int8_kernel(QuantInt
 // A block has 512 columns (a lane 8 of them), its four waves take the range's rows
 // in turn, eight rows' loads in flight each.
 constexpr int kColBlock = 512;
-__global__ __launch_bounds__(kThreads) void col_max_kernel(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, int P,
-                                                           uint16_t* part) {
-    __shared__ uint4 red[kThreads];
+struct ColMax {
+    const uint16_t* x;
+    int64_t rows, cols, ld;
+    int P;
+    uint16_t* part;
+};
+__device__ __forceinline__ void col_max(const ColMax& a, int bx, int by, uint4* red) {
+    const uint16_t* const x = a.x;
+    const int64_t rows = a.rows, cols = a.cols, ld = a.ld;
+    const int P = a.P;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * kColBlock + lane * 8;
-    const int64_t r0 = rows * blockIdx.y / P, r1 = rows * (blockIdx.y + 1) / P;
+    const int64_t col = (int64_t)bx * kColBlock + lane * 8;
+    const int64_t r0 = rows * by / P, r1 = rows * (by + 1) / P;
     uint4 m = make_uint4(0, 0, 0, 0);
     if (col < cols) {
         constexpr int U = 8;
@@ -267,8 +279,23 @@ __global__ __launch_bounds__(kThreads) void col_max_kernel(const uint16_t* x, in
             const uint4 v = red[w * 64 + lane];
             m.x = pk_max_u16(m.x, v.x); m.y = pk_max_u16(m.y, v.y); m.z = pk_max_u16(m.z, v.z); m.w = pk_max_u16(m.w, v.w);
         }
-        *reinterpret_cast<uint4*>(part + (int64_t)blockIdx.y * cols + col) = m;
+        *reinterpret_cast<uint4*>(a.part + (int64_t)by * cols + col) = m;
     }
+}
+
+__global__ __launch_bounds__(kThreads) void col_max_kernel(ColMax a, int blocks_x) {
+    __shared__ uint4 red[kThreads];
+    col_max(a, (int)blockIdx.x % blocks_x, (int)blockIdx.x / blocks_x, red);
+}
+
+// Both in one launch, the rows' blocks behind the columns': neither waits for the
+// other, and a launch of its own costs a short tensor as much as the work.
+template <int TPR, int NC>
+__global__ __launch_bounds__(kThreads) void rows_and_col_max_kernel(QuantInt8Args a, ColMax c, int blocks_x, int col_blocks) {
+    __shared__ uint4 red[kThreads];
+    const int b = (int)blockIdx.x;
+    if (b < col_blocks) col_max(c, b % blocks_x, b / blocks_x, red);
+    else quant_rows<kRowBf16, TPR, NC>(a, b - col_blocks, reinterpret_cast<uint32_t*>(red), nullptr);
 }
 
 // The transposed copy by 128x128 tiles, each thread an 8x8 block. The tile's
@@ -529,33 +556,35 @@ __global__ __launch_bounds__(kStreamWaves * 64, 4) void int8_stream_kernel(Int8P
     }
 }
 
-// A wave per row where there are rows enough to fill the chip with four a block,
-// else a block; in as few chunks a thread as hold the row.
+// f(Int<threads per row>, Int<chunks a thread>) for rows of `cols` values: a wave per
+// row where there are rows enough to fill the chip with four a block, else a block;
+// in as few chunks a thread as hold the row. False: the row is too long.
 template <int N> using Int = std::integral_constant<int, N>;
-template <int SRC>
-void launch_rows(const QuantInt8Args& a, hipStream_t stream) {
-    const int64_t cpr = a.cols / 8;
-    auto run = [&](auto tpr, auto nc) {
-        constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
-        quant_rows_int8_kernel<SRC, TPR, NC><<<(unsigned)(TPR == 64 ? (a.rows + 3) / 4 : a.rows), kThreads, 0, stream>>>(a);
-    };
+template <typename F>
+bool fit_rows(int64_t rows, int64_t cols, F&& f) {
+    const int64_t cpr = cols / 8;
     auto fit = [&](auto tpr, auto... nc) {
-        constexpr int TPR = decltype(tpr)::value;
         bool done = false;
         auto one = [&](auto n) {
-            if (!done && cpr <= TPR * decltype(n)::value) { run(tpr, n); done = true; }
+            if (!done && cpr <= decltype(tpr)::value * decltype(n)::value) {
+                f(tpr, n);
+                done = true;
+            }
         };
         (one(nc), ...);
         return done;
     };
-    if (a.rows >= 1024 && fit(Int<64>{}, Int<1>{}, Int<2>{},
-                              Int<4>{}))
-        return;
-    if (fit(Int<256>{}, Int<1>{}, Int<2>{},
-            Int<3>{}, Int<5>{}, Int<8>{},
-            Int<12>{}))
-        return;
-    quant_long_rows_int8_kernel<SRC><<<(unsigned)a.rows, kThreads, 0, stream>>>(a);
+    return (rows >= 1024 && fit(Int<64>{}, Int<1>{}, Int<2>{}, Int<4>{})) ||
+           fit(Int<256>{}, Int<1>{}, Int<2>{}, Int<3>{}, Int<5>{}, Int<8>{}, Int<12>{});
+}
+
+template <int SRC>
+void launch_rows(const QuantInt8Args& a, hipStream_t stream) {
+    const bool fits = fit_rows(a.rows, a.cols, [&](auto tpr, auto nc) {
+        constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
+        quant_rows_int8_kernel<SRC, TPR, NC><<<(unsigned)(TPR == 64 ? (a.rows + 3) / 4 : a.rows), kThreads, 0, stream>>>(a);
+    });
+    if (!fits) quant_long_rows_int8_kernel<SRC><<<(unsigned)a.rows, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -568,16 +597,23 @@ void launch_quantize_int8(const QuantInt8Args& a, hipStream_t stream) {
 
 size_t quant_int8_ws_bytes(int64_t rows, int64_t cols) { return (size_t)col_ranges(rows) * cols * 2; }
 
-void launch_quantize_int8_t(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, int8_t* qT, int64_t ld_qT,
-                            float* scaleT, void* ws, hipStream_t stream) {
-    const int P = col_ranges(rows);
-    uint16_t* part = reinterpret_cast<uint16_t*>(ws);
-    col_max_kernel<<<dim3((unsigned)((cols + kColBlock - 1) / kColBlock), P), kThreads, 0, stream>>>(x, rows, cols, ld, P, part);
-    QuantArgs a{};
-    a.x = x; a.rows = (rows + 15) / 16 * 16; a.cols = cols; a.ld = ld;
-    a.qT = reinterpret_cast<uint8_t*>(qT); a.scaleT = scaleT;
-    const dim3 grid((unsigned)((cols + kTile - 1) / kTile), (unsigned)((rows + kTile - 1) / kTile));
-    quant_cols_int8_kernel<<<grid, kThreads, 0, stream>>>(a, rows, ld_qT, part, P);
+void launch_quantize_int8_both(const QuantInt8Args& a, int8_t* qT, int64_t ld_qT, float* scaleT, void* ws, hipStream_t stream) {
+    const ColMax c{a.x, a.rows, a.cols, a.ld, col_ranges(a.rows), reinterpret_cast<uint16_t*>(ws)};
+    const int blocks_x = (int)((a.cols + kColBlock - 1) / kColBlock), col_blocks = blocks_x * c.P;
+    const bool together = a.q && fit_rows(a.rows, a.cols, [&](auto tpr, auto nc) {
+        constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
+        const unsigned grid = (unsigned)(col_blocks + (TPR == 64 ? (a.rows + 3) / 4 : a.rows));
+        rows_and_col_max_kernel<TPR, NC><<<grid, kThreads, 0, stream>>>(a, c, blocks_x, col_blocks);
+    });
+    if (!together) {
+        if (a.q) launch_quantize_int8(a, stream);
+        col_max_kernel<<<(unsigned)col_blocks, kThreads, 0, stream>>>(c, blocks_x);
+    }
+    QuantArgs t{};
+    t.x = a.x; t.rows = (a.rows + 15) / 16 * 16; t.cols = a.cols; t.ld = a.ld;
+    t.qT = reinterpret_cast<uint8_t*>(qT); t.scaleT = scaleT;
+    const dim3 grid((unsigned)((a.cols + kTile - 1) / kTile), (unsigned)((a.rows + kTile - 1) / kTile));
+    quant_cols_int8_kernel<<<grid, kThreads, 0, stream>>>(t, a.rows, ld_qT, c.part, c.P);
 }
 
 // Whether a product takes the kernels of few rows: those read A's fragments from

@@ -315,11 +315,11 @@ struct QuantInt8Args {
     int swiglu;
 };
 void launch_quantize_int8(const QuantInt8Args& a, hipStream_t stream);
-// The transposed copy qT [cols, rows] (pitch ld_qT, zeros up to the next 16
-// columns) with a scale per column; ws holds quant_int8_ws_bytes.
+// The rows of a BF16 tensor (a.q, or NULL: not wanted) and the transposed copy qT
+// [cols, rows] (pitch ld_qT, zeros up to the next 16 columns) with a scale per
+// column; ws holds quant_int8_ws_bytes.
 size_t quant_int8_ws_bytes(int64_t rows, int64_t cols);
-void launch_quantize_int8_t(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, int8_t* qT, int64_t ld_qT,
-                            float* scaleT, void* ws, hipStream_t stream);
+void launch_quantize_int8_both(const QuantInt8Args& a, int8_t* qT, int64_t ld_qT, float* scaleT, void* ws, hipStream_t stream);
 
 struct Int8Problem {
     int64_t M, N, K;

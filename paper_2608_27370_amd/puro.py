@@ -111,6 +111,10 @@ _SIGS = {
     "puro_swiglu_quantize_int8": (_i, [_p, _i64, _i64, _i64, _p, _p, _p]),
     "puro_int8_gemm_workspace_size": (_sz, [_i64, _i64, _i64]),
     "puro_int8_gemm": (_i, [_i64, _i64, _i64, _p, _i64, _p, _p, _i64, _p, _p, _i, _i64, _i, _p, _p, _i64, _p, _sz, _p]),
+    "puro_int8_linear_fwd_workspace_size": (_sz, [_i64, _i64, _i64]),
+    "puro_int8_linear_bwd_workspace_size": (_sz, [_i64, _i64, _i64]),
+    "puro_int8_linear_fwd": (_i, [_p, _p, _i64, _i64, _i64, _p, ctypes.POINTER(Saved), _p, _sz, _p]),
+    "puro_int8_linear_bwd": (_i, [_p, ctypes.POINTER(Saved), _i64, _i64, _i64, _p, _p, _i, _p, _sz, _p]),
     "puro_verify_drafts_workspace_size": (_sz, [_i64, _i64, _i64, _i64]),
     "puro_verify_drafts": (_i, [_i64, _i64, _i64, _i64, _i, _i, _p, _i64, _p, _i64, _p, _p, _p, _p, ctypes.c_double, _p, _p,
                                 _p, _sz, _p]),
@@ -876,9 +880,12 @@ def _matrix(t, what, dtypes, device):
         raise ValueError("%s: 2-D expected, got %s" % (what, tuple(t.shape)))
     rows, cols = t.shape
     ld, one = t.stride()
-    if rows <= 1 or cols == 0:
-        ld = -(-cols // 16) * 16               # (the pitch of one row, or of none, is any)
-    if one != 1 and cols > 1 and rows > 0:
+    if rows <= 1 or cols <= 1:
+        if one != 1 and cols > 1 and rows > 0:
+            raise ValueError("%s: the values of a row are contiguous" % what)
+        if rows <= 1 or cols == 0:
+            ld = -(-cols // 16) * 16           # (the pitch of one row, or of none, is any)
+    elif one != 1:
         raise ValueError("%s: the values of a row are contiguous" % what)
     return rows, cols, ld, t.data_ptr()
 
@@ -886,18 +893,25 @@ def _matrix(t, what, dtypes, device):
 def _vector(t, what, dtypes, n, device):
     if t.dtype not in dtypes or t.get_device() != device:
         _check_tensor(t, what, dtypes, device)
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s: %d contiguous values expected, got %s" % (what, n, tuple(t.shape)))
     return t.data_ptr()
 
 
 def _int8_rows(rows, cols, out, like, dev):
     """q [rows, cols] and scale [rows], given or new, and their addresses."""
-    out = out or {}
-    q, scale = out.get("q"), out.get("scale")
-    q = like.new_empty((rows, cols), dtype=torch.int8) if q is None else q
-    scale = like.new_empty(rows, dtype=torch.float32) if scale is None else scale
-    return q, scale, _dense(q, "q", _INT8, (rows, cols), dev), _vector(scale, "scale", _FP32, rows, dev)
+    q = scale = None
+    if out:
+        q, scale = out.get("q"), out.get("scale")
+    if q is None:
+        q = like.new_empty((rows, cols), dtype=torch.int8)
+    else:
+        _dense(q, "q", _INT8, (rows, cols), dev)
+    if scale is None:
+        scale = like.new_empty(rows, dtype=torch.float32)
+    else:
+        _vector(scale, "scale", _FP32, rows, dev)
+    return q, scale, q.data_ptr(), scale.data_ptr()
 
 
 def quantize_int8(x, want_q=True, want_qT=False, out=None, ws=None):
@@ -925,17 +939,18 @@ def quantize_int8(x, want_q=True, want_qT=False, out=None, ws=None):
     return dict(q=q, scale=scale, qT=qT, scaleT=scaleT)
 
 
-def rmsnorm_quantize_int8(x, gamma, eps, out=None):
+def rmsnorm_quantize_int8(x, gamma, eps, want_rstd=False, out=None):
     """int8 codes of y = x rstd gamma (RMSNorm of each row of x) with a scale per row, y not written (nor rounded to
-    BF16); returns dict(q, scale, rstd)."""
+    BF16); returns dict(q, scale, rstd), rstd [rows] FP32 if it is wanted."""
     dev = _current()
     rows, cols, ld, px = _matrix(x, "x", _BF16_BITS, dev)
     q, scale, pq, ps = _int8_rows(rows, cols, out, x, dev)
-    rstd = (out or {}).get("rstd")
-    rstd = x.new_empty(rows, dtype=torch.float32) if rstd is None else rstd
+    rstd = out.get("rstd") if out else None
+    if rstd is None and want_rstd:
+        rstd = x.new_empty(rows, dtype=torch.float32)
     _check("puro_rmsnorm_quantize_int8", lib().puro_rmsnorm_quantize_int8(
-        px, _vector(gamma, "gamma", _BF16_BITS, cols, dev), rows, cols, ld, eps, pq, ps, _vector(rstd, "rstd", _FP32, rows, dev),
-        _stream()))
+        px, _vector(gamma, "gamma", _BF16_BITS, cols, dev), rows, cols, ld, eps, pq, ps,
+        _vector(rstd, "rstd", _FP32, rows, dev) if rstd is not None else None, _stream()))
     return dict(q=q, scale=scale, rstd=rstd)
 
 
@@ -984,23 +999,47 @@ def int8_gemm(A, a_scale, B, b_scale, out_dtype=OUT_BF16, D=None, accumulate=Fal
     return D
 
 
-def int8_linear_fwd(X, W):
-    """Y = X W^T [M, N] (BF16) with both quantised to int8, a scale per token and per output channel; returns (Y, saved):
-    the transposed copies with scales per channel that ``int8_linear_bwd`` takes."""
-    x = quantize_int8(X, want_qT=True)
-    w = quantize_int8(W, want_qT=True)
-    Y = int8_gemm(x["q"], x["scale"], w["q"], w["scale"])
-    return Y, dict(xq_t=x["qT"], x_scale=x["scaleT"], wq_t=w["qT"], w_scale=w["scaleT"])
+def int8_linear_fwd(X, W, Y=None, want_saved=True, ws=None):
+    """Y = X W^T [M, N] (BF16) of BF16 X [M, K] and W [N, K], both quantised to int8, a scale per token and per output
+    channel; returns (Y, saved): the transposed copies with scales per channel that ``int8_linear_bwd`` takes (None
+    without want_saved)."""
+    dev = _current()
+    (M, K), N = X.shape, W.shape[0]
+    px, pw = _dense(X, "X", _BF16_BITS, (M, K), dev), _dense(W, "W", _BF16_BITS, (N, K), dev)
+    if Y is None:
+        Y = X.new_empty((M, N), dtype=torch.bfloat16)
+    saved = s = None
+    if want_saved:
+        saved = dict(xq_t=X.new_empty((K, -(-M // 16) * 16), dtype=torch.int8), x_scale=X.new_empty(K, dtype=torch.float32),
+                     wq_t=X.new_empty((K, N), dtype=torch.int8), w_scale=X.new_empty(K, dtype=torch.float32))
+        s = ctypes.byref(_saved_struct(saved))
+    w, nb = _ws(_size("puro_int8_linear_fwd_workspace_size", M, N, K), ws, X.device)
+    _check("puro_int8_linear_fwd", lib().puro_int8_linear_fwd(
+        px, pw, M, N, K, _dense(Y, "Y", (torch.bfloat16,), (M, N), dev), s, _ptr(w), nb, _stream()))
+    return Y, saved
 
 
-def int8_linear_bwd(dY, saved, want_dx=True, want_dw=True, dX=None, dW=None, accumulate_dw=False):
-    """dX = dY W [M, K] (BF16) and dW = dY^T X [N, K] (FP32) with dY [M, N] quantised to int8 per token for the one and
-    per channel for the other; returns (dX, dW)."""
-    q = quantize_int8(dY, want_q=want_dx, want_qT=want_dw)
+def int8_linear_bwd(dY, saved, want_dx=True, want_dw=True, dX=None, dW=None, accumulate_dw=False, ws=None):
+    """dX = dY W [M, K] (BF16) and dW = dY^T X [N, K] (FP32) with dY [M, N] (BF16) quantised to int8 per token for the one
+    and per channel for the other; returns (dX, dW)."""
+    dev = _current()
+    (M, N), xq, wq = dY.shape, saved["xq_t"], saved["wq_t"]
+    K = xq.shape[0]
+    pdy = _dense(dY, "dY", _BF16_BITS, (M, N), dev)
+    s = Saved(_dense(xq, "xq_t", _INT8, (K, -(-M // 16) * 16), dev), _vector(saved["x_scale"], "x_scale", _FP32, K, dev),
+              _dense(wq, "wq_t", _INT8, (K, N), dev), _vector(saved["w_scale"], "w_scale", _FP32, K, dev))
+    pdx = pdw = None
     if want_dx:
-        dX = int8_gemm(q["q"], q["scale"], saved["wq_t"], saved["w_scale"], D=dX)
+        if dX is None:
+            dX = dY.new_empty((M, K), dtype=torch.bfloat16)
+        pdx = _dense(dX, "dX", (torch.bfloat16,), (M, K), dev)
     if want_dw:
-        dW = int8_gemm(q["qT"], q["scaleT"], saved["xq_t"], saved["x_scale"], OUT_FP32, D=dW, accumulate=accumulate_dw)
+        if dW is None:
+            dW = (dY.new_zeros if accumulate_dw else dY.new_empty)((N, K), dtype=torch.float32)
+        pdw = _dense(dW, "dW", _FP32, (N, K), dev)
+    w, nb = _ws(_size("puro_int8_linear_bwd_workspace_size", M, N, K), ws, dY.device)
+    _check("puro_int8_linear_bwd", lib().puro_int8_linear_bwd(
+        pdy, ctypes.byref(s), M, N, K, pdx, pdw, int(bool(accumulate_dw)), _ptr(w), nb, _stream()))
     return (dX if want_dx else None), (dW if want_dw else None)
 
 
@@ -1055,17 +1094,22 @@ def verify_drafts(target, draft, draft_ids, offsets, uniform=None, uniform_sampl
         if V_d != V:
             raise ValueError("target %s and draft %s differ in their columns" % (tuple(target.shape), tuple(draft.shape)))
         pd = pd or pt                          # (no rows have no address; none is read)
+    pids = _vector(draft_ids, "draft_ids", _INT32, T, dev)
     if tokens is None:
         tokens = draft_ids.new_empty(T)
+    else:
+        _vector(tokens, "tokens", _INT32, T, dev)
     if accepted is None:
         accepted = draft_ids.new_empty(B)
+    else:
+        _vector(accepted, "accepted", _INT32, B, dev)
     w, nb = _ws(_size("puro_verify_drafts_workspace_size", B, T, rows, V), ws, target.device)
     _check("puro_verify_drafts", lib().puro_verify_drafts(
         B, T, rows, V, kind, OUT_BF16 if target.dtype == torch.bfloat16 else OUT_FP32, pt, ldt, pd, ldd,
-        _vector(draft_ids, "draft_ids", _INT32, T, dev), _vector(offsets, "offsets", _INT32, B + 1, dev),
+        pids, _vector(offsets, "offsets", _INT32, B + 1, dev),
         _vector(uniform, "uniform", _FP32, T, dev) if uniform is not None else None,
         _vector(uniform_sample, "uniform_sample", _FP32, B, dev) if uniform_sample is not None else None, temperature,
-        _vector(tokens, "tokens", _INT32, T, dev), _vector(accepted, "accepted", _INT32, B, dev), _ptr(w), nb, _stream()))
+        tokens.data_ptr(), accepted.data_ptr(), _ptr(w), nb, _stream()))
     return tokens, accepted
 
 

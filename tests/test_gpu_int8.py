@@ -100,7 +100,7 @@ def check_band(q, scale, values, e, what):
 def test_rmsnorm(P, R, C):
     x, g = activations(R, R, C), bf16.from_f64_rne(1 + 0.3 * np.random.default_rng(C).normal(size=C))
     x[R // 2] = 0
-    r = P.rmsnorm_quantize_int8(to_dev_bf16(x), to_dev_bf16(g), 1e-6)
+    r = P.rmsnorm_quantize_int8(to_dev_bf16(x), to_dev_bf16(g), 1e-6, want_rstd=True)
     y, rstd, e = int8.rmsnorm(f64(x), f64(g), np.float64(np.float32(1e-6)))
     check_band(r["q"], r["scale"], y, e, "rmsnorm %dx%d" % (R, C))
     assert (np.abs(host(r["rstd"]) - rstd) <= e * rstd).all()
@@ -329,6 +329,31 @@ def test_linear_accumulates_into_main_grad(P):
     Y = P.int8_linear(X.detach(), W)
     assert Y.requires_grad
     P.int8_linear(X, W.detach()).sum().backward()                 # an expanded gradient; dX alone
+
+
+@pytest.mark.parametrize("M,N,K", [(0, 32, 48), (1, 16, 16), (21, 48, 64)])
+def test_linear_calls_are_the_calls_they_are_made_of(P, M, N, K):
+    """(and without what one does not want, and no tokens at all)"""
+    import torch
+    X, W, dY = (to_dev_bf16(activations(s, r, c)) for s, r, c in ((1, M, K), (2, N, K), (3, M, N)))
+    Y, saved = P.int8_linear_fwd(X, W)
+    w = P.quantize_int8(W, want_qT=True)
+    if M:
+        x = P.quantize_int8(X, want_qT=True)
+        assert torch.equal(Y.view(torch.int16), P.int8_gemm(x["q"], x["scale"], w["q"], w["scale"]).view(torch.int16))
+        for got, want in ((saved["xq_t"], x["qT"]), (saved["x_scale"], x["scaleT"]), (saved["wq_t"], w["qT"]), (saved["w_scale"], w["scaleT"])):
+            assert torch.equal(got, want)
+    only, none = P.int8_linear_fwd(X, W, want_saved=False)
+    assert none is None and torch.equal(only.view(torch.int16), Y.view(torch.int16))
+    dX, dW = P.int8_linear_bwd(dY, saved)
+    assert dX.shape == (M, K) and dW.shape == (N, K)
+    if M == 0:
+        assert not dW.any().item()
+    kept = torch.full((N, K), 3.0, device="cuda")
+    none, same = P.int8_linear_bwd(dY, saved, want_dx=False, dW=kept, accumulate_dw=True)
+    assert none is None and same is kept and torch.equal(kept, 3.0 + dW)
+    alone, none = P.int8_linear_bwd(dY, saved, want_dw=False)
+    assert none is None and torch.equal(alone.view(torch.int16), dX.view(torch.int16))
 
 
 # ------------------------------------------------- together, streams, graphs

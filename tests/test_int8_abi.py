@@ -74,6 +74,35 @@ def test_product(puro):  # noqa: F811
         assert g(nb=need - 1) == ERR_WORKSPACE and g(ws=None) == ERR_NULL and g(ws=FAKE + 8) == ERR_ALIGN
 
 
+def test_linear_layer(puro):  # noqa: F811
+    import ctypes
+    L = puro.lib()
+    good = puro.Saved(FAKE, FAKE, FAKE, FAKE)
+
+    def fwd(X=FAKE, W=FAKE, M=13, N=32, K=48, Y=FAKE, saved=good, ws=FAKE, nb=BIG):
+        return L.puro_int8_linear_fwd(X, W, M, N, K, Y, ctypes.byref(saved) if saved else None, ws, nb, None)
+
+    def bwd(dY=FAKE, saved=good, M=13, N=32, K=48, dX=FAKE, dW=FAKE, acc=0, ws=FAKE, nb=BIG):
+        return L.puro_int8_linear_bwd(dY, ctypes.byref(saved) if saved else None, M, N, K, dX, dW, acc, ws, nb, None)
+    for f, size in ((fwd, L.puro_int8_linear_fwd_workspace_size), (bwd, L.puro_int8_linear_bwd_workspace_size)):
+        assert f(M=-1) == f(N=-16) == f(K=-16) == f(M=131057) == f(N=131072) == f(K=131072) == ERR_SHAPE
+        assert f(N=40) == f(K=40) == f(ws=FAKE + 8) == ERR_ALIGN
+        assert f(ws=None) == ERR_NULL and f(nb=size(13, 32, 48) - 1) == ERR_WORKSPACE
+        for i in range(4):
+            v = [FAKE] * 4
+            v[i] = None
+            assert f(saved=puro.Saved(*v)) == ERR_NULL, i
+            v[i] = FAKE + 8
+            assert f(saved=puro.Saved(*v)) == ERR_ALIGN, i
+        assert size(-1, 16, 16) == size(4, 8, 16) == size(4, 16, 131072) == 0 < size(1, 16, 16)
+    for n in ("X", "W", "Y"):
+        assert fwd(**{n: None}) == ERR_NULL and fwd(**{n: FAKE + 8}) == ERR_ALIGN
+    assert fwd(M=0, X=None, Y=None) == OK
+    assert bwd(dY=None) == bwd(saved=None) == ERR_NULL
+    assert bwd(dY=FAKE + 8) == bwd(dX=FAKE + 8) == bwd(dW=FAKE + 8) == ERR_ALIGN
+    assert bwd(dX=None, dW=None) == bwd(M=0, dY=None, dX=None, acc=1) == bwd(K=0, dX=None, dW=None) == OK
+
+
 def test_verification(puro):  # noqa: F811
     L = puro.lib()
 

@@ -1306,7 +1306,10 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     // size, which the range check must not see).
     const int vrows = min(WTM, p.M - mrow0), vcols = min(WTN, out_n - ncol0);
     if (vrows <= 0 || vcols <= 0) return;
-    const bool edge = !fast && out_n % 4 == 0 && (OUT == 2 || OUT == kOutF32 || !p.accumulate) &&
+    // (int8: any N; the columns past the last whole vector follow one by one)
+    constexpr bool kTail = FA == kInt8 && OUT != 2;
+    const int whole = kTail ? vcols & ~3 : vcols;
+    const bool edge = !fast && (kTail || out_n % 4 == 0) && (OUT == 2 || OUT == kOutF32 || !p.accumulate) &&
                       (int64_t)WTM * ldo * ES <= INT32_MAX &&
                       (OUT != kOutBF16Epi || (int64_t)WTM * p.ldr * 2 <= INT32_MAX);
     const bool sized = fast || edge;
@@ -1328,8 +1331,8 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     for (int vv = 0; vv < FP; ++vv) {
         const int q = vv * 64 + lane;
         const int rv = q / ECPR, cv = q % ECPR;
-        goff[vv] = cv * 4 < vcols ? rv * row_bytes + cv * 4 * ES : kOOB;
-        roff[vv] = cv * 4 < vcols ? rv * rrow_bytes + cv * 8 : kOOB;
+        goff[vv] = cv * 4 < whole ? rv * row_bytes + cv * 4 * ES : kOOB;
+        roff[vv] = cv * 4 < whole ? rv * rrow_bytes + cv * 8 : kOOB;
 #pragma unroll
         for (int ph = 0; ph < NPH; ++ph) {
             const int r = ph * FR + rv;
@@ -1485,6 +1488,23 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
             };
             if (fast) run(std::false_type{});
             else run(std::true_type{});
+            if constexpr (kTail) {
+                // (a lane a row of the pass; its columns' addresses as staged)
+                for (int r = lane; r < min(RPP, vrows - pass * RPP); r += 64)
+                    for (int c = whole; c < vcols; ++c) {
+                        const float v = *reinterpret_cast<const float*>(ep + r * ROWB + (((c >> 2) ^ (r & SWZ)) << 4) + (c & 3) * 4);
+                        const int64_t m = mrow0 + pass * RPP + r;
+                        const int n = ncol0 + c;
+                        if constexpr (OUT == kOutF32) {
+                            float* const dst = reinterpret_cast<float*>(p.D) + m * p.ldd + n;
+                            *dst = p.accumulate ? *dst + v : v;
+                        } else {
+                            uint16_t* const dst = reinterpret_cast<uint16_t*>(p.D) + m * p.ldd + n;
+                            const float o = OUT == kOutBF16Epi ? add_epilogue1(v, p.bias, p.residual, p.ldr, m, n, p.res_scale) : v;
+                            __builtin_nontemporal_store(to_bf16(o), dst);
+                        }
+                    }
+            }
             return;
         }
 #pragma unroll

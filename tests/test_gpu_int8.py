@@ -225,6 +225,22 @@ def test_product_kinds(P, M, N, K, kind):
         product(P, M, N, K, least=-128)
 
 
+@pytest.mark.parametrize("M,N,K", [(130, 257, 512), (300, 999, 208), (513, 1027, 64), (70, 131, 16)])
+def test_columns_past_the_last_vector_of_four(P, M, N, K):
+    product(P, M, N, K, bias=True, res="other")
+    product(P, M, N, K, res="inplace")
+    product(P, M, N, K, "fp32", accumulate=True)
+    product(P, M, N, K, "fp32", pad=1)
+
+
+# rows and columns of the streaming kernels: whole and ragged groups of 16 rows, the longest reductions that stay in LDS
+@pytest.mark.parametrize("M", [1, 5, 16, 17, 32, 33, 49, 64])
+@pytest.mark.parametrize("N,K", [(32768, 144), (33000, 2048), (32771, 1536), (40000, 16), (9001, 2032), (20000, 2064)])
+def test_few_rows_of_wide_products(P, M, N, K):
+    product(P, M, N, K, "fp32")
+    product(P, M, N, K, bias=True, res="inplace", seed=30)
+
+
 @pytest.mark.parametrize("M,N", [(1, 16), (20, 24), (150, 300)])
 def test_longest_sums_are_exact(P, M, N):
     """Codes of -128 over the longest reduction: sums just below 2^31."""

@@ -556,102 +556,6 @@ __global__ __launch_bounds__(kStreamWaves * 64, 4) void int8_stream_kernel(Int8P
     }
 }
 
-// 17 to 64 rows past many columns, the rows' codes in LDS (so 16 MT K of them have to
-// fit): one block of eight waves a CU holds them in the order in which the matrix
-// instruction takes them (fragment by fragment, a lane's 16 bytes side by side: no
-// bank conflicts) and each wave goes through groups of 16 columns by itself, no
-// barrier after the first. B streams from memory into registers, kUnit steps of
-// 128 values of k ahead of the ones that are multiplied.
-constexpr int kStagedBytes = 128 * 1024, kStagedWaves = 8, kUnit = 6;
-template <int MT>
-__global__ __launch_bounds__(kStagedWaves * 64) void int8_staged_kernel(Int8Problem p) {
-    __shared__ v4i32 rows[kStagedBytes / 16];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int r = lane & 15, q = lane >> 4;
-    const int K = (int)p.K, steps = (K + 127) / 128;
-    const int groups = (int)((p.N + 15) / 16), stride = (int)gridDim.x * kStagedWaves;
-    int g = (int)blockIdx.x * kStagedWaves + wave;
-    struct Set {
-        v4i32 b[kUnit][2];
-    };
-    // unit u of group g: its values, zeros past the reduction's end and in rows that
-    // are not there
-    auto load = [&](Set& t, int g_, int u) __attribute__((always_inline)) {
-        const int64_t n0 = (int64_t)g_ * 16;
-        const int count = g_ < groups ? (int)min((int64_t)16, p.N - n0) : 0;
-        const __amdgpu_buffer_rsrc_t rb = buffer_rsrc(count > 0 ? p.B + n0 * p.ldb : p.B, count > 0 ? (uint32_t)((count - 1) * p.ldb + K) : 0u);
-#pragma unroll
-        for (int s = 0; s < kUnit; ++s)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = (u * kUnit + s) * 128 + q * 32 + h * 16;
-                t.b[s][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, r < count && k < K ? (uint32_t)(r * p.ldb + k) : kOOB, 0, 0);
-            }
-    };
-    auto scales = [&](int g_) __attribute__((always_inline)) {
-        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const int64_t n = (int64_t)g_ * 16 + q * 4;
-        if (n + 3 < p.N) s = *reinterpret_cast<const float4*>(p.sb + n);
-        else if (n < p.N) {
-            s.x = p.sb[n];
-            if (n + 1 < p.N) s.y = p.sb[n + 1];
-            if (n + 2 < p.N) s.z = p.sb[n + 2];
-        }
-        return s;
-    };
-    Set t0, t1;
-    load(t0, g, 0);
-    // A's fragments: row i * 16 + r at step s, half h, as lane (q, r) reads it
-    const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(p.A, (uint32_t)((p.M - 1) * p.lda + K));
-    for (int f = wave; f < steps * 2 * MT; f += kStagedWaves) {
-        const int i = f % MT, sh = f / MT, k = (sh >> 1) * 128 + q * 32 + (sh & 1) * 16, m = i * 16 + r;
-        rows[f * 64 + lane] = __builtin_amdgcn_raw_buffer_load_b128(ra, m < p.M && k < K ? (uint32_t)(m * p.lda + k) : kOOB, 0, 0);
-    }
-    float sa[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) sa[i] = i * 16 + r < p.M ? p.sa[i * 16 + r] : 0.0f;
-    __syncthreads();
-    const int units = (steps + kUnit - 1) / kUnit;
-    v4i32 acc[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) acc[i] = v4i32{0, 0, 0, 0};
-    int u = 0;
-    float4 sb = scales(g);
-    // one unit: the next one's loads, then this one's products; a group's last stores
-    auto unit = [&](Set& cur, Set& next) __attribute__((always_inline)) {
-        const bool last = u + 1 == units;
-        const int gn = last ? g + stride : g, un = last ? 0 : u + 1;
-        load(next, gn, un);
-        const float4 sn = last ? scales(gn) : sb;
-#pragma unroll
-        for (int s = 0; s < kUnit; ++s) {
-            // (past the last step B is zero: any fragment does)
-            const int at = min(u * kUnit + s, steps - 1);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-                    acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cur.b[s][h], rows[((at * 2 + h) * MT + i) * 64 + lane], acc[i], 0, 0, 0);
-        }
-        if (last) {
-            const float c[4] = {sb.x, sb.y, sb.z, sb.w};
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                store_int8_outputs(p, i * 16 + r, (int64_t)g * 16 + q * 4, acc[i], sa[i], c);
-                acc[i] = v4i32{0, 0, 0, 0};
-            }
-        }
-        g = gn;
-        u = un;
-        sb = sn;
-    };
-    while (g < groups) {
-        unit(t0, t1);
-        if (g >= groups) break;
-        unit(t1, t0);
-    }
-}
-
 // f(Int<threads per row>, Int<chunks a thread>) for rows of `cols` values: a wave per
 // row where there are rows enough to fill the chip with four a block, else a block;
 // in as few chunks a thread as hold the row. False: the row is too long.
@@ -736,17 +640,7 @@ size_t int8_gemm_ws_bytes(int64_t M, int64_t N, int64_t K) {
     return few_rows(M, N, K) ? 0 : gemm_workspace_bytes(M, (N + 3) / 4 * 4, K, kOutBF16);
 }
 
-#include <cstdlib>
 void launch_int8_gemm(const Int8Problem& p, void* ws, hipStream_t stream) {
-    static const int V = getenv("V") ? atoi(getenv("V")) : 0;
-    const int64_t Kp = (p.K + 127) / 128 * 128;
-    if (V && p.K > 0 && p.M <= 64 && p.N >= V && ((p.M + 15) / 16 == 3 ? 4 : (p.M + 15) / 16) * 16 * Kp <= kStagedBytes) {
-        const unsigned grid = (unsigned)std::min<int64_t>(256, (p.N + 127) / 128);
-        if (p.M <= 16) int8_staged_kernel<1><<<grid, 512, 0, stream>>>(p);
-        else if (p.M <= 32) int8_staged_kernel<2><<<grid, 512, 0, stream>>>(p);
-        else int8_staged_kernel<4><<<grid, 512, 0, stream>>>(p);
-        return;
-    }
     if (few_rows(p.M, p.N, p.K)) {
         if (p.M <= 16 && p.K <= kStreamK && p.N % 4 == 0 && p.N >= kStreamColumns)
             int8_stream_kernel<<<kStreamBlocks, kStreamWaves * 64, 0, stream>>>(p);

@@ -367,6 +367,11 @@ size_t gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int out, int batch)
     return w;
 }
 
+size_t gemm_int8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    const int64_t cols = (N + 3) / 4 * 4;
+    return plan_workspace_bytes(M, cols, make_plan(M, cols, K, false));
+}
+
 size_t gemm_long_k_workspace_bytes(int64_t M, int64_t N, int64_t K, int out) {
     Plan pl;
     return long_k_plan(M, N, K, &pl) ? plan_workspace_bytes(M, N, pl) : gemm_workspace_bytes(M, N, K, out);

@@ -637,7 +637,7 @@ static void launch_few(const Int8Problem& p, hipStream_t stream) {
 }
 
 size_t int8_gemm_ws_bytes(int64_t M, int64_t N, int64_t K) {
-    return few_rows(M, N, K) ? 0 : gemm_workspace_bytes(M, (N + 3) / 4 * 4, K, kOutBF16);
+    return few_rows(M, N, K) ? 0 : gemm_int8_workspace_bytes(M, N, K);
 }
 
 void launch_int8_gemm(const Int8Problem& p, void* ws, hipStream_t stream) {

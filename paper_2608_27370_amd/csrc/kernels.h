@@ -233,6 +233,9 @@ struct GemmProblem {
 // K in bytes of an operand row (2 K for BF16 operands).
 size_t gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int out, int batch = 1);
 size_t gemm_long_k_workspace_bytes(int64_t M, int64_t N, int64_t K, int out);
+// The same of int8 operands (whose plan is made, and whose partial sums lie, at N
+// rounded up to 4).
+size_t gemm_int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 // The plan launch_gemm takes: tile, ring depth, k ranges.
 void gemm_plan(int64_t M, int64_t N, int64_t K, bool grouped, int* tile_m, int* tile_n, int* stages,
                int* splits);

@@ -6,7 +6,7 @@
 // draw from max(p - q, 0) / sum max(p - q, 0): the kept or drawn token is then
 // distributed as p.
 //
-// A vocabulary row is worked on in pieces of 2048 entries, a wave each; every sum
+// A vocabulary row is worked on in pieces of 1024 or 2048 entries, a wave each; every sum
 // over a row is made of its pieces' sums, in a fixed order.
 //  * LOGITS: of every row the pieces' largest logits and sums of exponentials, then
 //    of every sequence, by a block of 16 waves (a row each), the row where its
@@ -30,7 +30,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kPiece = 2048;       // entries per wave
 constexpr double kInf = __builtin_huge_val();
 
 struct Args : VerifyArgs {
@@ -71,15 +70,15 @@ __device__ __forceinline__ void unpack(const uint4& w, float x[4], const float*)
     x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
 }
 
-// The lane's entries of a piece, vector i at v0 + (i 64 + lane) * kPerVector, `fill`
-// past the row's end.
-template <typename E>
+// The lane's entries of a piece of LEN, vector i at v0 + (i 64 + lane) * kPerVector,
+// `fill` past the row's end.
+template <typename E, int LEN>
 struct Piece {
-    static constexpr int N = kPiece / 64 / kPerVector<E>;
+    static constexpr int N = LEN / 64 / kPerVector<E>;
     float x[N][kPerVector<E>];
     __device__ __forceinline__ static int at(int v0, int i) { return v0 + (i * 64 + (threadIdx.x & 63)) * kPerVector<E>; }
     __device__ __forceinline__ void load(const E* row, int v0, int V, float fill) {
-        if (v0 + kPiece <= V) {
+        if (v0 + LEN <= V) {
             uint4 w[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) __builtin_memcpy(&w[i], row + at(v0, i), 16);
@@ -248,13 +247,13 @@ __device__ __forceinline__ const E* draft_row(const Args& a, int64_t t) { return
 // ---- LOGITS: (largest, sum of 2^((z - largest) c)) of every piece of every row.
 // Bound by memory and, as closely, by its arithmetic: some 17 binary64 instructions
 // an entry.
-template <typename E>
+template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void piece_sums_kernel(Args a, int total) {
     const Item it = item(a, total);
     if (!it.live) return;
-    const int r = it.row, v0 = it.piece * kPiece;
+    const int r = it.row, v0 = it.piece * LEN;
     const E* z = r < a.T ? target_row<E>(a, r) : draft_row<E>(a, r - a.T);
-    Piece<E> x;
+    Piece<E, LEN> x;
     x.load(z, v0, a.V, -INFINITY);
     // the largest, and whether there is a NaN (which it passes over) or +infinity
     float m = -INFINITY;
@@ -433,11 +432,11 @@ __device__ __forceinline__ void with_left(const Args& a, const EndRow<E>& e, F&&
 }
 
 // What is left over in every piece of the end rows.
-template <typename E>
+template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) {
     const Item it = item(a, total);
     if (!it.live) return;
-    const int b = it.row, v0 = it.piece * kPiece;
+    const int b = it.row, v0 = it.piece * LEN;
     const Rows rows = rows_of(a, b);
     if (rows.n <= 0) return;
     int kept;
@@ -453,7 +452,7 @@ __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) 
     if (bad(e.np) || bad(e.nq)) {
         r = p = __builtin_nan("");
     } else {
-        Piece<E> x, y;
+        Piece<E, LEN> x, y;
         x.load(e.zp, v0, a.V, fill);
         if (e.zq) y.load(e.zq, v0, a.V, fill);
         else y = x;
@@ -508,7 +507,7 @@ __device__ __forceinline__ double lane_below(double v) {
     return (threadIdx.x & 63) > 0 ? t : 0.0;
 }
 
-template <typename E>
+template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void draw_kernel(Args a) {
     __shared__ double sums[kWaves];
     __shared__ int hits[kWaves], positives[kWaves];
@@ -562,18 +561,16 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(Args a) {
     const int from = hits_in ? __builtin_ctzll(hits_in) : 63 - __builtin_clzll(any_in);
     const int piece = __shfl(hits_in ? hit : positive, from, 64);
     const double start = __shfl(hits_in ? hit_at : positive_at, from, 64);
-    // the entry: each thread eight of the piece in a row
-    constexpr int PER = kPiece / kThreads, NV = PER / kPerVector<E>;
-    const int v0 = piece * kPiece + threadIdx.x * PER;
+    // the entry: each thread some of the piece in a row
+    constexpr int PER = LEN / kThreads;
+    const int v0 = piece * LEN + threadIdx.x * PER;
     float x[PER], y[PER];
     auto values = [&](const E* z, float* to) __attribute__((always_inline)) {
         if (v0 + PER <= a.V) {
+            E raw[PER];
+            __builtin_memcpy(raw, z + v0, sizeof(raw));
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                uint4 w;
-                __builtin_memcpy(&w, z + v0 + i * kPerVector<E>, 16);
-                unpack(w, to + i * kPerVector<E>, z);
-            }
+            for (int k = 0; k < PER; ++k) to[k] = value(raw, k);
         } else {
 #pragma unroll
             for (int k = 0; k < PER; ++k) to[k] = v0 + k < a.V ? value(z, v0 + k) : a.logits ? -INFINITY : 0.0f;
@@ -624,12 +621,12 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(Args a) {
 }
 
 // ---- temperature 0: (largest logit, its lowest id) of every piece of the target's rows.
-template <typename E>
+template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void piece_max_kernel(Args a, int total) {
     const Item it = item(a, total);
     if (!it.live) return;
-    const int v0 = it.piece * kPiece;
-    Piece<E> x;
+    const int v0 = it.piece * LEN;
+    Piece<E, LEN> x;
     x.load(target_row<E>(a, it.row), v0, a.V, -INFINITY);
     float m = -INFINITY;
     int id = a.V;
@@ -694,13 +691,20 @@ __global__ __launch_bounds__(kThreads) void greedy_kernel(Args a) {
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
+// Entries of a piece: as many as make the fewest instructions an entry, 2048, or half
+// of them where all rows together are too few waves for the chip (eight a SIMD).
+// 84 rows of 50257: 512 20.8 us, 1024 20.8, 2048 23.3, 4096 30.2; 768 rows of 151936:
+// 119, 115, 113, 118.
+int piece_length(int64_t T, int64_t V) { return T * V < (int64_t)8192 * 2048 ? 1024 : 2048; }
+
 struct Layout {
-    int pieces;
+    int len, pieces;
     size_t left, row, kept, total;       // (the rows' sums first)
 };
 Layout layout(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
     Layout l{};
-    l.pieces = (int)((V + kPiece - 1) / kPiece);
+    l.len = piece_length(T, V);
+    l.pieces = (int)((V + l.len - 1) / l.len);
     l.left = up((size_t)(T + draft_rows) * l.pieces * sizeof(double2));
     l.row = l.left + up((size_t)B * l.pieces * sizeof(double2));
     l.kept = l.row + up((size_t)B * sizeof(double4));
@@ -708,23 +712,23 @@ Layout layout(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
     return l;
 }
 
-template <typename E>
+template <typename E, int LEN>
 void launch(const Args& a, hipStream_t stream) {
     auto blocks = [](int64_t n) { return (unsigned)((n + kWaves - 1) / kWaves); };
     if (a.temperature == 0.0) {
         const int total = a.T * a.pieces;
-        if (total > 0) piece_max_kernel<E><<<blocks(total), kThreads, 0, stream>>>(a, total);
+        if (total > 0) piece_max_kernel<E, LEN><<<blocks(total), kThreads, 0, stream>>>(a, total);
         greedy_kernel<<<a.B, kThreads, 0, stream>>>(a);
         return;
     }
     if (a.logits) {
         const int total = (a.T + (a.draft ? a.draft_rows : 0)) * a.pieces;
-        if (total > 0) piece_sums_kernel<E><<<blocks(total), kThreads, 0, stream>>>(a, total);
+        if (total > 0) piece_sums_kernel<E, LEN><<<blocks(total), kThreads, 0, stream>>>(a, total);
         end_rows_kernel<E><<<a.B, kEndWaves * 64, 0, stream>>>(a);
     }
     const int total = a.B * a.pieces;
-    left_over_kernel<E><<<blocks(total), kThreads, 0, stream>>>(a, total);
-    draw_kernel<E><<<a.B, kThreads, 0, stream>>>(a);
+    left_over_kernel<E, LEN><<<blocks(total), kThreads, 0, stream>>>(a, total);
+    draw_kernel<E, LEN><<<a.B, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -744,8 +748,13 @@ void launch_verify(const VerifyArgs& v, void* ws, hipStream_t stream) {
     a.left = reinterpret_cast<double2*>(w + l.left);
     a.row = reinterpret_cast<double4*>(w + l.row);
     a.kept = reinterpret_cast<int*>(w + l.kept);
-    if (v.bf16) launch<uint16_t>(a, stream);
-    else launch<float>(a, stream);
+    auto run = [&](auto len) {
+        constexpr int LEN = decltype(len)::value;
+        if (v.bf16) launch<uint16_t, LEN>(a, stream);
+        else launch<float, LEN>(a, stream);
+    };
+    if (l.len == 1024) run(std::integral_constant<int, 1024>{});
+    else run(std::integral_constant<int, 2048>{});
 }
 
 }  // namespace puro

@@ -126,6 +126,12 @@ def test_temperature_zero(P, V, dtype):
     assert host(tokens).tolist() == want[0].tolist() and host(accepted).tolist() == want[1].tolist()
 
 
+@pytest.mark.parametrize("kind,dtype,tau", [(LG, "bf16", 0.8), (LG, "fp32", 1.0), (PR, "fp32", 1.0), (LG, "bf16", 0.0)])
+def test_many_rows_of_a_large_vocabulary(P, kind, dtype, tau):
+    """(where the rows' pieces are the longer ones)"""
+    Batch(21, [1, 6, 3, 5] * 8, 150001, kind, dtype, tau).check(P)
+
+
 def test_ties_go_to_the_lowest_id(P):
     b = Batch(1, [3, 2], 20000, LG, "bf16", 0.0)
     b.target[:] = 0

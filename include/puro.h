@@ -570,7 +570,8 @@ puro_status puro_lm_head_distill_bwd(const uint16_t* X, const uint16_t* W, const
  * encoded from the BF16 values. The copy's columns from `rows` up to the next
  * multiple of 16 are filled with zeros, so that any number of tokens can be a
  * product's reduction dimension; what lies beyond is left alone. Either of q and
- * qT may be NULL (not wanted), each comes with its scales.
+ * qT may be NULL (not wanted), each comes with its scales. An empty tensor writes
+ * nothing.
  * Requirements: cols % 16 == 0, ld % 8 == 0, ld < 2^23, x, q and qT 16-byte
  * aligned, ld_qT % 16 == 0 and >= rows; rows at most 65535 * 128. ws (16-byte
  * aligned): *_workspace_size(rows, cols) bytes, needed for qT only. */
@@ -586,7 +587,9 @@ puro_status puro_quantize_int8(const uint16_t* x, int64_t rows, int64_t cols, in
  *   swiglu:   h = silu(gate) up of gu [rows, 2 cols].
  * The values are encoded as binary32 has them, without a rounding to BF16
  * between. Requirements as puro_quantize_int8; gamma BF16 [cols], 16-byte
- * aligned; eps finite and >= 0; gu's pitch ld >= 2 cols. */
+ * aligned; eps finite and >= 0 (with eps = 0 a row of zeros has scale NaN); gu's
+ * pitch ld >= 2 cols. Rows whose sum of squares overflows binary32 are outside
+ * the statement. */
 puro_status puro_rmsnorm_quantize_int8(const uint16_t* x, const uint16_t* gamma, int64_t rows, int64_t cols,
                                        int64_t ld, float eps, int8_t* q, float* scale, float* rstd,
                                        hipStream_t stream);
@@ -606,7 +609,7 @@ puro_status puro_swiglu_quantize_int8(const uint16_t* gu, int64_t rows, int64_t 
  * and X (K then is the number of tokens rounded up to 16).
  * Requirements: K % 16 == 0; lda, ldb % 16 == 0, at least K and at most 2^22;
  * ldd, ldr % 4 == 0 and at least N, ldr at most 2^22; data pointers, a_scale and
- * b_scale 16-byte aligned; M and N at most 2^22, M N at most 2^38; ws (16-byte
+ * b_scale 16-byte aligned; M and N at most 2^22, M N at most 2^36; ws (16-byte
  * aligned): puro_int8_gemm_workspace_size(M, N, K) bytes. M = 0 or N = 0 is a
  * valid empty call; K = 0 is an empty sum. */
 size_t puro_int8_gemm_workspace_size(int64_t M, int64_t N, int64_t K);

@@ -22,11 +22,14 @@ Training", and Appendix C, "FP8 implementation pipeline"):
 * ``lm_head`` -- the language-model head with its cross-entropy loss,
                 forward and backward;
 * ``muonh``  -- the MuonH optimiser step of one matrix: momentum,
-                Newton-Schulz orthogonalisation and the hyperball update.
+                Newton-Schulz orthogonalisation and the hyperball update;
+* ``int8``   -- 8-bit integer codes with a scale per row or column, and the
+                product of such codes;
+* ``verify`` -- drafted tokens kept or replaced by a target's probabilities.
 
 It is test infrastructure: only ``tests/``, ``__graft_entry__.smoke()`` and
 the ``cpu_baseline`` leg of ``bench.py`` may import it. It shares no code with
 the HIP library and never imports it.
 """
 
-from . import bf16, fp8, quant, gemm, linear, rmsnorm, swiglu, lm_head, muonh  # noqa: F401
+from . import bf16, fp8, quant, gemm, linear, rmsnorm, swiglu, lm_head, muonh, int8, verify  # noqa: F401

@@ -1072,7 +1072,8 @@ puro_status puro_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* A, int
                            int64_t ldd, int accumulate, const uint16_t* bias, const uint16_t* residual, int64_t ldr,
                            void* ws, size_t ws_bytes, hipStream_t stream) {
     if (M < 0 || N < 0 || K < 0 || M > kMaxPitch || N > kMaxPitch || K > kMaxInt8K) return PURO_ERR_SHAPE;
-    if (M * N > (int64_t)1 << 38) return PURO_ERR_SHAPE;
+    // (a launch holds fewer than 2^32 threads: 2^22 tiles of 128 x 128 with 512)
+    if (M * N > (int64_t)1 << 36) return PURO_ERR_SHAPE;
     if (d_type != PURO_OUT_BF16 && d_type != PURO_OUT_FP32) return PURO_ERR_UNSUPPORTED;
     const bool f32 = d_type == PURO_OUT_FP32;
     if ((accumulate && !f32) || ((bias || residual) && f32)) return PURO_ERR_UNSUPPORTED;

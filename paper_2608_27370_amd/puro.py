@@ -934,6 +934,10 @@ def quantize_int8(x, want_q=True, want_qT=False, out=None, ws=None):
         _, _, ldT, pT = _matrix(qT, "qT", _INT8, dev)
         psT = _vector(scaleT, "scaleT", _FP32, cols, dev)
         ws, nb = _ws(_size("puro_quantize_int8_workspace_size", rows, cols), ws, x.device)
+    if rows == 0 or cols == 0:                 # (sums of nothing are scaled by these)
+        for s in (scale, scaleT):
+            if s is not None:
+                s.fill_(1.0)
     _check("puro_quantize_int8", lib().puro_quantize_int8(px, rows, cols, ld, pq, ps, pT, ldT, psT, _ptr(ws) if nb else None, nb,
                                                           _stream()))
     return dict(q=q, scale=scale, qT=qT, scaleT=scaleT)
@@ -1043,15 +1047,19 @@ def int8_linear_bwd(dY, saved, want_dx=True, want_dw=True, dX=None, dW=None, acc
     return (dX if want_dx else None), (dW if want_dw else None)
 
 
+def _dense_rows(t):
+    """A tensor as the int8 linear layer takes it: contiguous, 16-byte aligned."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 class _Int8LinearFn(torch.autograd.Function):
     """Y = X W^T through int8_linear_fwd; the backward takes the rounding's derivative as 1. With a ``main_grad`` FP32
     buffer on W, dW is accumulated into it and W gets no .grad; otherwise W's .grad is dW in W's dtype."""
 
     @staticmethod
     def forward(ctx, X, W):
-        if X.dtype != torch.bfloat16 or W.dtype != torch.bfloat16:
-            raise TypeError("the int8 linear layer takes BF16 X and W")
-        Y, saved = int8_linear_fwd(X.contiguous(), W.contiguous())
+        Y, saved = int8_linear_fwd(_dense_rows(X), _dense_rows(W))
         ctx.save_for_backward(*saved.values())
         ctx.main_grad = getattr(W, "main_grad", None)
         return Y
@@ -1062,14 +1070,20 @@ class _Int8LinearFn(torch.autograd.Function):
         saved = dict(zip(("xq_t", "x_scale", "wq_t", "w_scale"), ctx.saved_tensors))
         want_dx, want_dw = ctx.needs_input_grad
         mg = ctx.main_grad if want_dw else None
-        dX, dW = int8_linear_bwd(dY.to(torch.bfloat16).contiguous(), saved, want_dx, want_dw, dW=mg, accumulate_dw=mg is not None)
+        dX, dW = int8_linear_bwd(_dense_rows(dY.to(torch.bfloat16)), saved, want_dx, want_dw, dW=mg, accumulate_dw=mg is not None)
         return dX, dW.to(torch.bfloat16) if want_dw and mg is None else None
 
 
 def int8_linear(X, W):
     """The int8 linear layer as an autograd operation: X [..., K], W [N, K] (BF16); returns Y [..., N] (BF16). N and K are
     multiples of 16, the number of tokens is any."""
-    Y = _Int8LinearFn.apply(X.reshape(-1, X.shape[-1]), W)
+    if X.dtype != torch.bfloat16 or W.dtype != torch.bfloat16:
+        raise TypeError("the int8 linear layer takes BF16 X and W")
+    rows = X.reshape(-1, X.shape[-1])
+    if torch.is_grad_enabled() and (X.requires_grad or W.requires_grad):
+        Y = _Int8LinearFn.apply(rows, W)
+    else:
+        Y, _ = int8_linear_fwd(_dense_rows(rows.detach()), _dense_rows(W.detach()), want_saved=False)
     return Y.reshape(*X.shape[:-1], Y.shape[-1])
 
 
@@ -1087,6 +1101,8 @@ def verify_drafts(target, draft, draft_ids, offsets, uniform=None, uniform_sampl
     int32: a sequence's kept ids, its drawn token and -1 from there on; rows behind the last sequence are left alone."""
     dev = _current()
     T, V, ldt, pt = _matrix(target, "target", (torch.bfloat16, torch.float32), dev)
+    if offsets.dim() != 1 or offsets.shape[0] == 0:
+        raise ValueError("offsets: one more than there are sequences")
     B = offsets.shape[0] - 1
     rows, ldd, pd = T, 0, None
     if draft is not None:

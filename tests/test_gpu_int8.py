@@ -263,6 +263,11 @@ def test_empty_sums_and_nan_scales(P):
     D = P.int8_gemm(z[:8], s[:8], z[:24], s[:24], bias=bias)
     assert torch.equal(D, bias.expand(8, 24))
     assert P.int8_gemm(z[:0], s[:0], z[:24], s[:24]).shape == (0, 24)
+    wide = torch.zeros(300, 0, dtype=torch.int8, device="cuda")
+    D = P.int8_gemm(wide, torch.ones(300, device="cuda"), wide, torch.ones(300, device="cuda"), P.OUT_FP32)
+    assert D.shape == (300, 300) and not D.any().item()
+    empty = P.quantize_int8(torch.empty(0, 32, dtype=torch.bfloat16, device="cuda"), want_qT=True)
+    assert empty["qT"].shape == (32, 0) and (empty["scaleT"] == 1).all().item()
     x = activations(3, 8, 64)
     x[2, 1], x[5, 60] = 0x7F80, 0x7FC0
     q = P.quantize_int8(to_dev_bf16(x))
@@ -345,6 +350,21 @@ def test_linear_accumulates_into_main_grad(P):
     Y = P.int8_linear(X.detach(), W)
     assert Y.requires_grad
     P.int8_linear(X, W.detach()).sum().backward()                 # an expanded gradient; dX alone
+    with torch.no_grad():
+        assert torch.equal(P.int8_linear(X, W).view(torch.int16), Y.detach().view(torch.int16))
+    # rows that do not begin at 16 bytes, of the input and of the gradient
+    room = torch.zeros(M * K + 4, dtype=torch.bfloat16, device="cuda")
+    odd = room[4:].view(M, K)
+    odd.copy_(X.detach())
+    odd = odd.requires_grad_()
+    Z = P.int8_linear(odd, W)
+    grad = torch.zeros(M * N + 1, dtype=torch.bfloat16, device="cuda")[1:].view(M, N)
+    Z.backward(grad.copy_(dY))
+    X.grad = None
+    P.int8_linear(X, W).backward(dY)
+    assert torch.equal(odd.grad.view(torch.int16), X.grad.view(torch.int16))
+    with pytest.raises(TypeError):
+        P.int8_linear(X.float(), W)
 
 
 @pytest.mark.parametrize("M,N,K", [(0, 32, 48), (1, 16, 16), (21, 48, 64)])

@@ -54,7 +54,7 @@ def test_product(puro):  # noqa: F811
         return L.puro_int8_gemm(M, N, K, A, lda, sa, B, ldb, sb, D, t, ldd, acc, bias, res, ldr, ws, nb, None)
     assert f(M=-1) == f(N=-1) == f(K=-16) == f(lda=48) == f(ldb=48) == f(ldd=16) == ERR_SHAPE
     assert f(M=(1 << 22) + 1) == f(N=(1 << 22) + 1, ldd=1 << 23) == f(K=131072, lda=131072, ldb=131072) == ERR_SHAPE
-    assert f(M=1 << 22, N=(1 << 16) + 4, ldd=1 << 17) == f(lda=(1 << 22) + 16) == ERR_SHAPE
+    assert f(M=1 << 22, N=(1 << 14) + 4, ldd=1 << 15) == f(lda=(1 << 22) + 16) == ERR_SHAPE
     assert f(K=56) == f(lda=72) == f(ldb=72) == f(ldd=22) == ERR_ALIGN
     for n in ("A", "B", "sa", "sb", "D", "bias", "res"):
         assert f(**{n: FAKE + 8}, **(dict(ldr=20) if n == "res" else {})) == ERR_ALIGN, n

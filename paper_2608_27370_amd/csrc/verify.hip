@@ -144,19 +144,21 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 constexpr double kLeast = 0x1p-990;
 
 // 2^((x - m) c) of logits x no larger than m, of N at a time. Where m c is of ordinary
-// size (near: binary32's spacing at m is less than 1 in the exponent) logits are
-// clamped, as they stand, to where that is about 2^-1000 (below kLeast), and the
-// power of two is added to the exponent of 2^f: fewer instructions.
+// size (near: the exponent x c - m c errs by no more than 2^-40, and binary32's
+// spacing at m is far less than 1 in it) logits are clamped, as they stand, to where
+// that is about 2^-1000 (below kLeast), and the power of two is added to the exponent
+// of 2^f: fewer instructions.
 struct Exponential {
-    double c, mc;
+    double m, c, mc;
     float lo;
     bool near;
-    __device__ __forceinline__ Exponential(const Args& a, double m) : c(a.c), mc(m * a.c), lo((float)(m - a.span)), near(fabs(m) * a.c < 0x1p22) {}
+    __device__ __forceinline__ Exponential(const Args& a, double m_)
+        : m(m_), c(a.c), mc(m_ * a.c), lo((float)(m_ - a.span)), near(fabs(m_) * a.c < 0x1p13) {}
     template <bool NEAR, int N>
     __device__ __forceinline__ void of(const float x[N], double e[N]) const {
         if constexpr (!NEAR) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) e[k] = exp2_f64(__builtin_fma((double)x[k], c, -mc));
+            for (int k = 0; k < N; ++k) e[k] = exp2_f64(((double)x[k] - m) * c);
             return;
         }
         constexpr double kInt = 0x1.8p52;            // its last place is 1

@@ -132,6 +132,26 @@ def test_many_rows_of_a_large_vocabulary(P, kind, dtype, tau):
     Batch(21, [1, 6, 3, 5] * 8, 150001, kind, dtype, tau).check(P)
 
 
+@pytest.mark.parametrize("tau", [2.0 ** -20, 1e-3, 0.05, 300.0, 2.0 ** 20])
+def test_extreme_temperatures(P, tau):
+    for drafted in (True, False):
+        Batch(31, [5, 1, 3, 4], 9001, LG, "fp32", tau, drafted).check(P)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shift", [3000.0, -9000.0, 1e5, -3e7, 1e30, -3.3e38])
+def test_logits_far_from_zero(P, dtype, shift):
+    """Rows moved by a large amount (as the type holds them then), some of their entries as large the other way."""
+    b = Batch(32, [4, 2, 6], 5000, LG, dtype, 0.9)
+    for name in ("target", "draft"):
+        v = b.values(getattr(b, name))
+        v = np.where(np.isfinite(v), v * (1 + abs(shift) * 2.0 ** -9) + shift, v)
+        v[:, 7] = -abs(shift)
+        setattr(b, name, b.store(np.clip(v, -3.38e38, 3.38e38) if shift < 0 or shift > 1e30 else v))
+    b.u[:] = np.linspace(0, 0.9, b.u.size)
+    b.check(P)
+
+
 def test_ties_go_to_the_lowest_id(P):
     b = Batch(1, [3, 2], 20000, LG, "bf16", 0.0)
     b.target[:] = 0

@@ -395,10 +395,13 @@ struct EndRow {
         }
     }
 };
-// (max(p - q, 0), p), NaN where p or q is
+// (max(p - q, 0), p), NaN where p or q is; 0 where no more than kLeast, so that a
+// piece with a share has an entry with one. p and q are rounded products: fused into the
+// difference, one of them unrounded, equal ones would leave 10^-17 of noise.
 __device__ __forceinline__ double2 left(double p, double q) {
+#pragma clang fp contract(off)
     const double d = p - q;
-    return make_double2(d <= kLeast ? 0.0 : d, p);
+    return make_double2(d <= kLeast ? 0.0 : d, p <= kLeast ? 0.0 : p);
 }
 // f(g), where g(v, x, y, l) gives N entries from v on with the values x and y (the
 // draft's) their l = left(p, q), by the kind of the row's entries: logits of
@@ -586,7 +589,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(Args a) {
         left_at(v0, x, y, l);
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            w[k] = use_p ? (l[k].y > kLeast ? l[k].y : 0.0) : l[k].x;
+            w[k] = use_p ? l[k].y : l[k].x;
             sum += w[k];
         }
     });

@@ -187,6 +187,20 @@ def test_draft_like_the_target(P):
     assert b.check(P)[1].tolist() == [0, 0, 0]
 
 
+@pytest.mark.parametrize("low", [-np.inf, -1e30, -5000.0])
+def test_draft_like_the_target_behind_masked_entries(P, low):
+    """Nothing is left over and the first thousands of entries have no probability: the least random number takes the first that has."""
+    b = Batch(33, [2, 3], 7000, LG, "fp32", 1.0)
+    b.target[:, :5000] = low
+    b.target[:, 5000] = 0.0
+    b.draft = b.target[[0, 2, 3]].copy()
+    b.ids[:] = b.V
+    for us in (0.0, 1e-30, 0.5):
+        b.us[:] = us
+        tokens, accepted = b.check(P)
+        assert accepted.tolist() == [0, 0] and tokens[[0, 2]].min() >= 5000
+
+
 @pytest.mark.parametrize("tau", [1.0, 0.0])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_special_logits(P, tau, dtype):

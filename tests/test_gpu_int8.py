@@ -55,6 +55,15 @@ def test_codes_and_scales(P, R, C):
     assert_bytes_equal(host(other["qT"]), int8.encode_cols(f64(x))[0])
 
 
+@pytest.mark.parametrize("R,C", [(9000, 64), (2500, 528), (16399, 2064), (701, 48016)])
+def test_both_copies_of_long_and_large_tensors(P, R, C):
+    g = np.random.default_rng(R)
+    x = g.integers(0, 1 << 16, (R, C), dtype=np.uint16)
+    x[(x & 0x7F80) > 0x5000] &= 0xCFFF                # (finite, of many magnitudes)
+    x[:, : C // 2][: R // 3] = 0
+    check_both(P, x, R, C)
+
+
 def special(R=48, C=64):
     x = activations(9, R, C)
     x[0] = 0

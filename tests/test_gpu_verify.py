@@ -257,6 +257,23 @@ def test_invalid_offsets(P, tau):
         b.check(P)
 
 
+@pytest.mark.parametrize("tau", [1.0, 0.0])
+@pytest.mark.parametrize("B", [512, 513, 1100, 3001])
+def test_many_sequences_some_of_them_invalid(P, B, tau):
+    g = np.random.default_rng(B)
+    b = Batch(34, g.integers(0, 4, B).tolist(), 41, LG, "fp32", tau, drafted=tau != 0)
+    if tau == 0:
+        b.draft = None
+    b.check(P)
+    for k in g.integers(1, B, 6):                    # jumps ahead: the sequences behind begin before them
+        b.offsets[k] += int(g.integers(1, 12))
+        b.check(P)
+    b.offsets[B // 2] = -1
+    b.check(P)
+    b.offsets[3] = 2 ** 31 - 1
+    assert (b.check(P)[1][4:] == -1).all()
+
+
 def test_no_sequences_and_no_drafts_at_all(P):
     import torch
     z = torch.zeros(0, 40, device="cuda")

@@ -44,10 +44,11 @@ __device__ __forceinline__ uint2 encode_int8(const float v[8], const Int8Scale& 
 }
 
 // ---------------------------------------------------------------- rows ---
-// TPR threads (a wave or the block) per row, whose NC chunks of 8 values a thread
+// TPR threads (16, a wave or the block) per row, whose NC chunks of 8 values a thread
 // are loaded once, all together, and stay in registers between the row's largest
 // magnitude and its codes. Bound by memory: a row is read once and its codes
-// written.
+// written (8192x8960: 38 us, 5.8 TB/s; SwiGLU 75 us, 4.9; RMSNorm 41 us; a short tensor
+// is a launch and its latency, 1x1536 2.4 us).
 enum : int { kRowBf16 = 0, kRowNorm = 1, kRowSwiglu = 2 };
 
 __device__ __forceinline__ void words(const uint4& v, uint32_t w[4]) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
@@ -60,9 +61,17 @@ __device__ __forceinline__ uint32_t max_bits(const float v[8], uint32_t m) {
     for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
     return m;
 }
-__device__ __forceinline__ float wave_sum(float v) {
+// over the N lanes of a row
+template <int N>
+__device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    for (int o = N / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+template <int N>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+#pragma unroll
+    for (int o = N / 2; o >= 1; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
     return v;
 }
 __device__ __forceinline__ float sum_squares(const uint32_t w[4], float ss) {
@@ -95,10 +104,10 @@ __device__ __forceinline__ void swiglu_values(const uint32_t g[4], const uint32_
 
 template <int SRC, int TPR, int NC>
 __device__ __forceinline__ void quant_rows(const QuantInt8Args& a, int64_t block, uint32_t* red, float* sums) {
-    constexpr bool WAVE = TPR == 64;
-    const int t = WAVE ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t row = WAVE ? block * 4 + (threadIdx.x >> 6) : block;
-    if (WAVE && row >= a.rows) return;          // (a whole wave; its block meets at no barrier)
+    constexpr bool WAVE = TPR <= 64;
+    const int t = threadIdx.x % TPR;
+    const int64_t row = block * (kThreads / TPR) + threadIdx.x / TPR;
+    if (WAVE && row >= a.rows) return;          // (all of a row's lanes; the block meets at no barrier)
     const int cpr = (int)(a.cols / 8);
     const uint16_t* xr = a.x + row * a.ld;
     constexpr int SECOND = SRC == kRowBf16 ? 0 : NC;
@@ -123,7 +132,7 @@ __device__ __forceinline__ void quant_rows(const QuantInt8Args& a, int64_t block
             words(x[i], w);
             ss = sum_squares(w, ss);
         }
-        ss = wave_sum(ss);
+        ss = lanes_sum<WAVE ? TPR : 64>(ss);
         if constexpr (!WAVE) {
             if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
             __syncthreads();
@@ -164,7 +173,7 @@ __device__ __forceinline__ void quant_rows(const QuantInt8Args& a, int64_t block
             m = max_bits(v, m);
         }
     }
-    m = WAVE ? wave_max(m) : block_max(m, red);
+    m = WAVE ? lanes_max<TPR>(m) : block_max(m, red);
     const Int8Scale s = int8_scale(m);
     if (t == 0) a.scale[row] = s.s;
 #pragma unroll
@@ -214,7 +223,7 @@ __global__ __launch_bounds__(kThreads) void quant_long_rows_int8_kernel(QuantInt
             words(*reinterpret_cast<const uint4*>(xr + c * 8), w);
             ss = sum_squares(w, ss);
         }
-        ss = wave_sum(ss);
+        ss = lanes_sum<64>(ss);
         if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
         __syncthreads();
         rstd = 1.0f / sqrtf(((sums[0] + sums[1]) + (sums[2] + sums[3])) / (float)a.cols + a.eps);
@@ -238,7 +247,9 @@ __global__ __launch_bounds__(kThreads) void quant_long_rows_int8_kernel(QuantInt
 // ---------------------------------------------------------------- columns ---
 // Largest magnitude patterns of the columns over P ranges of rows: part [P][cols].
 // A block has 512 columns (a lane 8 of them), its four waves take the range's rows
-// in turn, eight rows' loads in flight each.
+// in turn, eight rows' loads in flight each. Bound by memory: a column's scale needs all
+// of its rows, so that a transposed copy reads its tensor twice (8192x8960: 74 us for
+// 367 MB, 5.0 TB/s).
 constexpr int kColBlock = 512;
 constexpr int64_t kFarElements = (int64_t)1 << 25;
 struct ColMax {
@@ -305,7 +316,8 @@ __global__ __launch_bounds__(kThreads) void rows_and_col_max_kernel(QuantInt8Arg
 // The transposed copy by 128x128 tiles, each thread an 8x8 block. The tile's
 // values are on their way while the partial maxima of its columns are read, 16
 // threads a chunk of 8 columns, and 64 threads make the scales of two columns
-// each. `a`: x, its rows rounded up to 16 (which are written; the rows behind
+// each. Bound by memory and its stores: 8187x1536 8.7 us, 8192x2048 10.1 (50 MB, 5.0 TB/s).
+// `a`: x, its rows rounded up to 16 (which are written; the rows behind
 // `rows` read as zeros), ld, qT, scaleT.
 __global__ __launch_bounds__(kThreads) void quant_cols_int8_kernel(QuantArgs a, int64_t rows, int64_t ld_qT,
                                                                    const uint16_t* part, int P) {
@@ -385,7 +397,8 @@ int col_ranges(int64_t rows, int64_t cols) {
 }
 
 // ---------------------------------------------------------------- product of few rows ---
-// Up to 64 rows of A: the time is that of reading B once. A block has 16 NT columns
+// Up to 64 rows of A: the time is that of reading B once (1x17920x1536 8.3 us, 3.3 TB/s;
+// a small B is a launch and the latency of its loads, 1x2048x1536 3.8). A block has 16 NT columns
 // and WK waves that take steps of 128 values of k in turn, straight from memory
 // into registers (a lane 32 bytes of its row, four lanes a whole cache line), U
 // steps' loads in flight; nothing but the rows of A that exist is read of A, from
@@ -501,7 +514,7 @@ __global__ __launch_bounds__(WK * 64) void int8_rows_kernel(Int8Problem p) {
 // values stay in registers (a wave has two steps of k at most) and a block goes
 // through many groups of 16 columns, the next one's loads (and scales) in flight
 // while one is summed. Two LDS buffers and one barrier a group; the waves take
-// turns in storing.
+// turns in storing. Bound by memory: 5x151936x1536 43.4 us, 5.4 TB/s of B.
 constexpr int kStreamWaves = 8, kStreamK = kStreamWaves * 2 * 128;
 __global__ __launch_bounds__(kStreamWaves * 64, 4) void int8_stream_kernel(Int8Problem p) {
     __shared__ v4i32 sums[2][kStreamWaves * 64];
@@ -566,9 +579,11 @@ __global__ __launch_bounds__(kStreamWaves * 64, 4) void int8_stream_kernel(Int8P
 }
 
 // f(Int<threads per row>, Int<chunks a thread>) for rows of `cols` values: a wave per
-// row where there are rows enough to fill the chip with four a block, else a block;
-// in as few chunks a thread as hold the row. False: the row is too long.
+// row where there are rows enough to fill the chip with four a block (short rows 16
+// lanes: 100000x64 21.7 -> 7.7 us), else a block; in as few chunks a thread as hold the
+// row. False: the row is too long.
 template <int N> using Int = std::integral_constant<int, N>;
+int64_t row_blocks(int64_t rows, int tpr) { return (rows + kThreads / tpr - 1) / (kThreads / tpr); }
 template <typename F>
 bool fit_rows(int64_t rows, int64_t cols, F&& f) {
     const int64_t cpr = cols / 8;
@@ -583,7 +598,7 @@ bool fit_rows(int64_t rows, int64_t cols, F&& f) {
         (one(nc), ...);
         return done;
     };
-    return (rows >= 1024 && fit(Int<64>{}, Int<1>{}, Int<2>{}, Int<4>{})) ||
+    return (rows >= 4096 && fit(Int<16>{}, Int<1>{})) || (rows >= 1024 && fit(Int<64>{}, Int<1>{}, Int<2>{}, Int<4>{})) ||
            fit(Int<256>{}, Int<1>{}, Int<2>{}, Int<3>{}, Int<5>{}, Int<8>{}, Int<12>{});
 }
 
@@ -591,7 +606,7 @@ template <int SRC>
 void launch_rows(const QuantInt8Args& a, hipStream_t stream) {
     const bool fits = fit_rows(a.rows, a.cols, [&](auto tpr, auto nc) {
         constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
-        quant_rows_int8_kernel<SRC, TPR, NC><<<(unsigned)(TPR == 64 ? (a.rows + 3) / 4 : a.rows), kThreads, 0, stream>>>(a);
+        quant_rows_int8_kernel<SRC, TPR, NC><<<(unsigned)row_blocks(a.rows, TPR), kThreads, 0, stream>>>(a);
     });
     if (!fits) quant_long_rows_int8_kernel<SRC><<<(unsigned)a.rows, kThreads, 0, stream>>>(a);
 }
@@ -611,7 +626,7 @@ void launch_quantize_int8_both(const QuantInt8Args& a, int8_t* qT, int64_t ld_qT
     const int blocks_x = (int)((a.cols + kColBlock - 1) / kColBlock), col_blocks = blocks_x * c.P;
     const bool together = a.q && fit_rows(a.rows, a.cols, [&](auto tpr, auto nc) {
         constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
-        const unsigned grid = (unsigned)(col_blocks + (TPR == 64 ? (a.rows + 3) / 4 : a.rows));
+        const unsigned grid = (unsigned)(col_blocks + row_blocks(a.rows, TPR));
         // (of a small tensor the columns' blocks first, as the longer ones)
         const unsigned group = a.rows * a.cols < kFarElements ? (unsigned)blocks_x : grid / (unsigned)c.P;
         rows_and_col_max_kernel<TPR, NC><<<grid, kThreads, 0, stream>>>(a, c, blocks_x, Divisor::of(group));

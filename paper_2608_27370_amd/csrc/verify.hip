@@ -249,8 +249,10 @@ template <typename E>
 __device__ __forceinline__ const E* draft_row(const Args& a, int64_t t) { return (const E*)a.draft + t * a.ld_d; }
 
 // ---- LOGITS: (largest, sum of 2^((z - largest) c)) of every piece of every row.
-// Bound by memory and, as closely, by its arithmetic: some 17 binary64 instructions
-// an entry.
+// Bound by its arithmetic and, nearly as closely, by memory: 19.5 instructions an entry,
+// 12 of them binary64, keep the vector units busy for 85% of the time (768 BF16 rows of
+// 151936: 75 us, 3.1 TB/s; a copy's rate would be 49). The next piece's loads in flight
+// while one is summed: 79 to 84.
 template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void piece_sums_kernel(Args a, int total) {
     const Item it = item(a, total);
@@ -311,7 +313,8 @@ __device__ __forceinline__ Norm row_norm(const Args& a, int64_t r) {
 }
 
 // Where a sequence's drafts end, by a block of 16 waves: eight rows at a time, a
-// wave for each one's normaliser and for its draft's.
+// wave for each one's normaliser and for its draft's. Latency: 6.1 us for 96 sequences of
+// up to eight rows of 151936, 4.3 for 33 of up to four of 50257.
 constexpr int kEndWaves = 16, kEndRows = kEndWaves / 2;
 template <typename E>
 __global__ __launch_bounds__(kEndWaves * 64) void end_rows_kernel(Args a) {
@@ -438,7 +441,8 @@ __device__ __forceinline__ void with_left(const Args& a, const EndRow<E>& e, F&&
     else with_q(std::integral_constant<int, 2>{});
 }
 
-// What is left over in every piece of the end rows.
+// What is left over in every piece of the end rows. Of LOGITS two exponentials an
+// entry: 25 us for 96 rows of 151936 and their drafts', found in the caches.
 template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) {
     const Item it = item(a, total);
@@ -482,7 +486,7 @@ __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) 
 
 // ---- the draw ----------------------------------------------------------------------
 // One block per sequence, a chain of short steps: what they need of memory is asked
-// for at the start, and every wave finds the piece by itself (no barrier).
+// for at the start, and every wave finds the piece by itself (no barrier). 4 to 6 us.
 
 // Whether sequence b begins before an earlier offset (its tokens would be written
 // over another's); by every wave, of many sequences in a launch before (65536 of them

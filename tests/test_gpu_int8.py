@@ -30,7 +30,7 @@ def activations(seed, R, C):
 
 
 SHAPES = [(1, 16), (1, 1536), (3, 48), (16, 512), (17, 528), (33, 2048), (128, 2064), (300, 1536), (5, 17920), (2, 65552),
-          (257, 4112), (1000, 64), (64, 8960), (4100, 32)]
+          (257, 4112), (1000, 64), (64, 8960), (4100, 32), (4097, 128), (5003, 112)]
 
 
 def check_both(P, x, R, C, dev=None, **kw):

@@ -659,8 +659,8 @@ puro_status puro_int8_linear_bwd(const uint16_t* dY, const puro_linear_saved* sa
  * many were kept. temperature 0 (LOGITS): the row's largest logit, the lowest id
  * among equals, is the token, and a draft is kept where it is that; draft,
  * uniform and uniform_sample are not read then.
- * Exponentials and sums in binary64, in a fixed order: over 10^5 entries the
- * drawn token moves with differences of 10^-8.
+ * Exponentials (to 10^-10) and sums in binary64, in a fixed order: over 10^5
+ * entries the drawn token moves with differences of 10^-8.
  * Special values: logits of -infinity have probability 0; an id outside [0, V) is
  * not kept, nor is one whose p or q is NaN; a row of logits with a NaN or a
  * +infinity, or with no probability at all, keeps nothing; a token that would be

@@ -14,8 +14,8 @@
 //  * the pieces of that row: what is left over of each, and of p;
 //  * a block per sequence: the piece, then the entry where the running sum passes
 //    the random number's share.
-// Exponentials, probabilities and sums are binary64: with 10^5 entries a running
-// sum that errs by 10^-8 moves the drawn token once in 10^3 draws.
+// Exponentials (to 10^-10), probabilities and sums are binary64: with 10^5 entries a
+// running sum that errs by 10^-8 moves the drawn token once in 10^3 draws.
 
 #include <algorithm>
 #include <climits>
@@ -105,28 +105,27 @@ struct Piece {
 
 // ---- arithmetic ----------------------------------------------------------------
 
-// 2^f in binary64 for f in [-1/2, 1/2]: interpolation of degree 8 at the Chebyshev
-// nodes, relative error 1.1e-12. Of N values at a time, whose chains of dependent
-// instructions fill each other's waits.
+// 2^-f in binary64 for f in [0, 1]: the polynomial of degree 7, 1 at 0, of the least
+// largest relative error, 4.4e-11 (the random numbers are of steps of 6e-8). Of N
+// values at a time, whose chains of dependent instructions fill each other's waits.
 template <int N>
 __device__ __forceinline__ void exp2_fractions(const double f[N], double p[N]) {
-    constexpr double kC[9] = {0x1.63d1363a681b4p-20, 0x1.00dc4a5344ef5p-16, 0x1.4308ac85a69f8p-13, 0x1.5d8745a728209p-10, 0x1.3b2ab7181b77dp-7,
-                              0x1.c6b08dd6fd236p-5,  0x1.ebfbdff823cedp-3,  0x1.62e42fef84cf0p-1,  1.0};
+    constexpr double kC[8] = {-0x1.69fa9638ac087p-17, 0x1.349aa24075c04p-13, -0x1.5c09ebe989994p-10, 0x1.3b149cd8db03cp-7,
+                              -0x1.c6af2acf64e86p-5, 0x1.ebfbd54ce8792p-3, -0x1.62e42fd37055cp-1, 1.0};
 #pragma unroll
     for (int k = 0; k < N; ++k) p[k] = kC[0];
 #pragma unroll
-    for (int c = 1; c < 9; ++c)
+    for (int c = 1; c < 8; ++c)
 #pragma unroll
         for (int k = 0; k < N; ++k) p[k] = __builtin_fma(p[k], f[k], kC[c]);
 }
-// 2^t, 0 below 2^-1074; t at most 0 or -infinity.
-__device__ __forceinline__ double exp2_f64(double t) {
-    t = fmax(t, -2000.0);
-    const double n = __builtin_rint(t);
-    const double f[1] = {t - n};
+// 2^-u, 0 above 1074; u at least 0, or infinity.
+__device__ __forceinline__ double exp2_minus(double u) {
+    u = fmin(u, 2000.0);
+    const double f[1] = {__builtin_amdgcn_fract(u)};
     double p[1];
     exp2_fractions<1>(f, p);
-    return __builtin_ldexp(p[0], (int)n);
+    return __builtin_ldexp(p[0], (int)-u);
 }
 
 // The largest of two or three, NaN passed over (one instruction; written as fmaxf the
@@ -149,32 +148,33 @@ constexpr double kLeast = 0x1p-990;
 // size (near: the exponent x c - m c errs by no more than 2^-40, and binary32's
 // spacing at m is far less than 1 in it) logits are clamped, as they stand, to where
 // that is about 2^-1000 (below kLeast), and the power of two is added to the exponent
-// of 2^f: fewer instructions.
+// of 2^-f: fewer instructions. The exponent's whole and fractional parts are taken
+// apart as those of a number that is not negative, which m c, moved up by 2^-51 of
+// itself, makes sure of.
 struct Exponential {
     double m, c, mc;
     float lo;
     bool near;
     __device__ __forceinline__ Exponential(const Args& a, double m_)
-        : m(m_), c(a.c), mc(m_ * a.c), lo((float)(m_ - a.span)), near(fabs(m_) * a.c < 0x1p13) {}
+        : m(m_), c(a.c), mc(__builtin_fma(fabs(m_ * a.c), 0x1p-51, m_ * a.c)), lo((float)(m_ - a.span)), near(fabs(m_) * a.c < 0x1p13) {}
     template <bool NEAR, int N>
     __device__ __forceinline__ void of(const float x[N], double e[N]) const {
         if constexpr (!NEAR) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) e[k] = exp2_f64(((double)x[k] - m) * c);
+            for (int k = 0; k < N; ++k) e[k] = exp2_minus((m - (double)x[k]) * c);
             return;
         }
-        constexpr double kInt = 0x1.8p52;            // its last place is 1
-        double f[N], s[N];
+        double u[N], f[N];
 #pragma unroll
-        for (int k = 0; k < N; ++k) f[k] = __builtin_fma((double)max2(x[k], lo), c, -mc);
+        for (int k = 0; k < N; ++k) u[k] = __builtin_fma(-(double)max2(x[k], lo), c, mc);
 #pragma unroll
-        for (int k = 0; k < N; ++k) s[k] = f[k] + kInt;
-#pragma unroll
-        for (int k = 0; k < N; ++k) f[k] -= s[k] - kInt;
+        for (int k = 0; k < N; ++k) f[k] = __builtin_amdgcn_fract(u[k]);
         exp2_fractions<N>(f, e);
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            e[k] = __hiloint2double(__double2hiint(e[k]) + (__double2loint(s[k]) << 20), __double2loint(e[k]));
+        for (int k = 0; k < N; ++k) {
+            const uint32_t n = (uint32_t)(int)-u[k];
+            e[k] = __hiloint2double((int)((uint32_t)__double2hiint(e[k]) + (n << 20)), __double2loint(e[k]));
+        }
     }
 };
 
@@ -249,10 +249,11 @@ template <typename E>
 __device__ __forceinline__ const E* draft_row(const Args& a, int64_t t) { return (const E*)a.draft + t * a.ld_d; }
 
 // ---- LOGITS: (largest, sum of 2^((z - largest) c)) of every piece of every row.
-// Bound by its arithmetic and, nearly as closely, by memory: 19.5 instructions an entry,
-// 12 of them binary64, keep the vector units busy for 85% of the time (768 BF16 rows of
-// 151936: 75 us, 3.1 TB/s; a copy's rate would be 49). The next piece's loads in flight
-// while one is summed: 79 to 84.
+// Bound by its arithmetic and, nearly as closely, by memory: 17.5 instructions an entry,
+// 11 of them binary64, keep the vector units busy for 85% of the time (768 BF16 rows of
+// 151936: 69 us, 3.4 TB/s; a copy's rate would be 49). With a polynomial of degree 8 and
+// the exponent rounded by an addition, 19.5: 76; the next piece's loads in flight while
+// one is summed: 79 to 84.
 template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void piece_sums_kernel(Args a, int total) {
     const Item it = item(a, total);
@@ -307,7 +308,7 @@ __device__ __forceinline__ Norm row_norm(const Args& a, int64_t r) {
     double s = 0.0;
     for (int c = lane; c < a.pieces; c += 64) {
         const double2 v = st[c];
-        s += v.y * exp2_f64((v.x - m) * a.c);
+        s += v.y * exp2_minus((m - v.x) * a.c);
     }
     return {m, 1.0 / wave_sum(s)};
 }

@@ -1,7 +1,7 @@
 """GPU parity of the verification of drafted tokens (puro_verify_drafts) against
-the oracle (oracle/verify.py): tokens and counts equal. Both sum in binary64; an
-entry of the running sum would have to lie within about 10^-13 of the random
-number's share for the two to choose differently."""
+the oracle (oracle/verify.py): tokens and counts equal. Both sum in binary64, with
+exponentials to 4.4e-11 here; an entry of the running sum would have to lie within
+about 10^-10 of the random number's share for the two to choose differently."""
 
 import numpy as np
 import pytest

@@ -654,7 +654,7 @@ puro_status puro_int8_linear_bwd(const uint16_t* dY, const puro_linear_saved* sa
  *     and where that is 0 everywhere): the least v with
  *     sum_{w <= v} rest[w] > uniform_sample[b] sum_w rest[w]
  *     (the last v with rest[v] > 0 where rounding leaves none). What is no more than
- *     2^-990 counts as 0.
+ *     2^-970 may count as 0.
  * tokens[offsets[b] ..]: the kept ids, the drawn token, then -1; accepted[b]: how
  * many were kept. temperature 0 (LOGITS): the row's largest logit, the lowest id
  * among equals, is the token, and a draft is kept where it is that; draft,

@@ -188,12 +188,14 @@ def test_draft_like_the_target(P):
 
 
 @pytest.mark.parametrize("low", [-np.inf, -1e30, -5000.0])
-def test_draft_like_the_target_behind_masked_entries(P, low):
-    """Nothing is left over and the first thousands of entries have no probability: the least random number takes the first that has."""
+@pytest.mark.parametrize("drafted", [True, False])
+def test_nothing_left_over_behind_masked_entries(P, low, drafted):
+    """Nothing is left over and the first thousands of entries have no probability: the least random number takes the first that has (without
+    the draft's predictions everything is left over of an id that is none)."""
     b = Batch(33, [2, 3], 7000, LG, "fp32", 1.0)
     b.target[:, :5000] = low
     b.target[:, 5000] = 0.0
-    b.draft = b.target[[0, 2, 3]].copy()
+    b.draft = b.target[[0, 2, 3]].copy() if drafted else None
     b.ids[:] = b.V
     for us in (0.0, 1e-30, 0.5):
         b.us[:] = us

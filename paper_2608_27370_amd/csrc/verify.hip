@@ -250,6 +250,23 @@ __device__ __forceinline__ const E* target_row(const Args& a, int64_t t) { retur
 template <typename E>
 __device__ __forceinline__ const E* draft_row(const Args& a, int64_t t) { return (const E*)a.draft + t * a.ld_d; }
 
+// A piece's largest entry, in every lane of its wave, and whether there is a NaN (which it
+// passes over).
+template <typename E, int LEN>
+__device__ __forceinline__ bool largest(const Piece<E, LEN>& x, float& m) {
+    m = -INFINITY;
+    uint64_t nan = 0;
+#pragma unroll
+    for (int i = 0; i < x.N; ++i)
+#pragma unroll
+        for (int e = 0; e < kPerVector<E>; e += 2) {
+            m = max3(m, x.x[i][e], x.x[i][e + 1]);
+            nan |= __builtin_amdgcn_ballot_w64(__builtin_isunordered(x.x[i][e], x.x[i][e + 1]));
+        }
+    m = wave_max(m);
+    return nan != 0;
+}
+
 // ---- LOGITS: (largest, sum of 2^((z - largest) c)) of every piece of every row.
 // Bound by its arithmetic and, nearly as closely, by memory: 17.5 instructions an entry,
 // 11 of them binary64, keep the vector units busy for 85% of the time (768 BF16 rows of
@@ -264,19 +281,10 @@ __global__ __launch_bounds__(kThreads) void piece_sums_kernel(Args a, int total)
     const E* z = r < a.T ? target_row<E>(a, r) : draft_row<E>(a, r - a.T);
     Piece<E, LEN> x;
     x.load(z, v0, a.V, -INFINITY);
-    // the largest, and whether there is a NaN (which it passes over) or +infinity
-    float m = -INFINITY;
-    uint64_t nan = 0;
-#pragma unroll
-    for (int i = 0; i < x.N; ++i)
-#pragma unroll
-        for (int e = 0; e < kPerVector<E>; e += 2) {
-            m = max3(m, x.x[i][e], x.x[i][e + 1]);
-            nan |= __builtin_amdgcn_ballot_w64(__builtin_isunordered(x.x[i][e], x.x[i][e + 1]));
-        }
-    m = wave_max(m);
+    float m;
+    const bool nan = largest(x, m);
     double s = 0.0;
-    if (nan != 0 || m == INFINITY) {
+    if (nan || m == INFINITY) {
         m = __builtin_nanf("");
         s = __builtin_nan("");
     } else if (m > -INFINITY) {
@@ -757,7 +765,10 @@ __global__ __launch_bounds__(kEndWaves * 64) void end_and_draw_kernel(Args a) {
     draw<LEN, kEndWaves>(a, b, rows, end.kept, e, us, mine, mine.c0 < mine.c1 ? left(mine.c0) : make_double2(0.0, 0.0), left, scratch);
 }
 
-// ---- temperature 0: (largest logit, its lowest id) of every piece of the target's rows.
+// ---- temperature 0: (largest logit, its lowest id) of every piece of the target's rows:
+// the largest first, then which of the lane's entries is it. Bound by memory and as
+// closely by latency: 480 BF16 rows of 151936 30 us (both in one pass, with ties and NaN
+// compared at every entry: 49).
 template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void piece_max_kernel(Args a, int total) {
     const Item it = item(a, total);
@@ -765,22 +776,16 @@ __global__ __launch_bounds__(kThreads) void piece_max_kernel(Args a, int total) 
     const int v0 = it.piece * LEN;
     Piece<E, LEN> x;
     x.load(target_row<E>(a, it.row), v0, a.V, -INFINITY);
-    float m = -INFINITY;
+    float m;
+    const bool nan = largest(x, m);
     int id = a.V;
-    auto take = [&](float v, int i) {
-        if (v > m || (v == m && i < id) || (v != v && m == m)) { m = v; id = i; }
-    };
 #pragma unroll
-    for (int i = 0; i < x.N; ++i)
+    for (int i = x.N - 1; i >= 0; --i)
 #pragma unroll
-        for (int e = 0; e < kPerVector<E>; ++e) take(x.x[i][e], x.at(v0, i) + e);
+        for (int e = kPerVector<E> - 1; e >= 0; --e) id = x.x[i][e] == m ? x.at(v0, i) + e : id;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const float v = __shfl_xor(m, o, 64);
-        const int i = __shfl_xor(id, o, 64);
-        take(v, i);
-    }
-    if ((threadIdx.x & 63) == 0) a.stats[it.at] = make_double2((double)m, (double)id);
+    for (int o = 32; o >= 1; o >>= 1) id = min(id, __shfl_xor(id, o, 64));
+    if ((threadIdx.x & 63) == 0) a.stats[it.at] = make_double2(nan ? __builtin_nan("") : (double)m, (double)id);
 }
 
 // A row's choice, -1 where it has none (NaN, +infinity or nothing but -infinity), by

@@ -162,6 +162,23 @@ def test_ties_go_to_the_lowest_id(P):
     assert b.check(P)[1].tolist() == [0, 0]
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_the_smallest_values_and_signed_zeros(P, dtype):
+    b = Batch(35, [1] * 6, 3001, LG, dtype, 0.0)
+    b.draft = None
+    word = np.uint16 if dtype == "bf16" else np.uint32
+    x = np.full(b.target.shape, 0xFF80 if dtype == "bf16" else 0xFF800000, word)
+    sign = 0x8000 if dtype == "bf16" else 0x80000000
+    x[0, [7, 2999]] = 1, 2                           # the two smallest positive numbers
+    x[1, [7, 2999]] = sign | 2, sign | 1
+    x[2, [1030, 2]] = 0, sign                        # zeros are equal: the first of them
+    x[3, [1030, 2]] = sign, 0
+    x[4, 3000] = sign
+    x[5] = sign | 3
+    b.target = x.view(b.target.dtype)
+    assert host(b.run(P)[0]).tolist() == b.want()[0].tolist() == [2999, 2999, 2, 2, 3000, 0]
+
+
 def test_many_drafts_of_one_sequence(P):
     b = Batch(3, [200, 1, 70], 300, LG, "fp32", 1.0)
     b.check(P)

@@ -332,34 +332,35 @@ struct End {
 };
 struct EndScratch {
     Norm norms[kEndWaves];
-    int ok[kEndWaves];
+    double prob[kEndWaves];         // of the row's draft
+    float u[kEndWaves];
 };
 template <typename E>
 __device__ __forceinline__ End find_end(const Args& a, int b, Rows rows, EndScratch& s) {
     const int wave = threadIdx.x >> 6, per = a.draft ? kEndWaves / 2 : kEndWaves;
+    const bool of_target = wave < per;
     for (int i0 = 0;; i0 += per) {
-        const int i = i0 + (wave < per ? wave : wave - per);
+        const int i = i0 + (of_target ? wave : wave - per);
         const int64_t t = rows.start + i;
         const bool drafted = i < rows.n - 1;
-        if (wave < per ? i < rows.n : drafted) {
-            const Norm n = row_norm(a, wave < per ? t : a.T + t - b);
-            if ((threadIdx.x & 63) == 0) s.norms[wave] = n;
-        }
-        __syncthreads();
-        if (wave < per && (threadIdx.x & 63) == 0) {
-            bool keep = false;
-            const int d = drafted ? a.ids[t] : -1;
-            if (d >= 0 && d < a.V && !bad(s.norms[wave])) {
-                const double p = prob_at(a, value(target_row<E>(a, t), d), s.norms[wave]);
-                const double q = a.draft ? prob_at(a, value(draft_row<E>(a, t - b), d), s.norms[wave + per]) : 1.0;
-                keep = (double)a.u[t] * q < p && p > kLeast;
+        // (asked for ahead of the row's sums)
+        const int d = drafted ? a.ids[t] : -1;
+        const bool has = d >= 0 && d < a.V;
+        const float x = has ? value(of_target ? target_row<E>(a, t) : draft_row<E>(a, t - b), d) : 0.0f;
+        const float u = drafted && of_target ? a.u[t] : 0.0f;
+        if (of_target ? i < rows.n : drafted) {
+            const Norm n = row_norm(a, of_target ? t : a.T + t - b);
+            const double prob = has && !bad(n) ? prob_at(a, x, n) : __builtin_nan("");
+            if ((threadIdx.x & 63) == 0) {
+                s.norms[wave] = n;
+                s.prob[wave] = prob;
+                s.u[wave] = u;
             }
-            s.ok[wave] = keep;
         }
         __syncthreads();
+        // (the last row is not kept, at the latest, whose id is not one)
         int w = 0;
-        while (w < per && s.ok[w]) ++w;
-        // (the last row is not kept, at the latest)
+        while (w < per && (double)s.u[w] * (a.draft ? s.prob[w + per] : 1.0) < s.prob[w] && s.prob[w] > kLeast) ++w;
         if (w < per) return {i0 + w, s.norms[w], i0 + w == rows.n - 1 || !a.draft ? Norm{0.0, 0.0} : s.norms[w + per]};
         __syncthreads();
     }

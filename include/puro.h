@@ -669,6 +669,8 @@ puro_status puro_int8_linear_bwd(const uint16_t* dY, const puro_linear_saved* sa
  * of a batch with room to spare: rows behind the last sequence are not written);
  * one whose offsets decrease or leave [0, T], that begins before an earlier
  * offset, or whose draft rows leave [0, draft_rows), has accepted -1 and no token.
+ * tokens may be draft_ids itself (then the ids are replaced); tokens and accepted
+ * overlap the ids and offsets in no other way (PURO_ERR_SHAPE).
  * dtype: PURO_OUT_BF16 or PURO_OUT_FP32 for both target [T, V] (pitch ld_target)
  * and draft [draft_rows, V] (pitch ld_draft); any V from 1 to 2^21 and pitches
  * from V to 2^22 (rows need no more than their element's alignment); T at

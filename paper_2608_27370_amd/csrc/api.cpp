@@ -1240,7 +1240,7 @@ namespace {
 puro_status check_verify_sizes(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
     if (B < 0 || T < 0 || draft_rows < 0 || V < 1) return PURO_ERR_SHAPE;
     const int64_t rows = (int64_t)1 << 20;
-    // (a launch holds fewer than 2^24 blocks of 256 threads, a block at least 8192 entries of a long row)
+    // (a launch holds fewer than 2^24 blocks of 256 threads, a block at least 4096 entries of a long row)
     if (B > (int64_t)1 << 16 || T > rows || draft_rows > T || V > (int64_t)1 << 21) return PURO_ERR_SHAPE;
     if (T * V > (int64_t)1 << 35 || B * V > (int64_t)1 << 35) return PURO_ERR_SHAPE;
     return PURO_OK;
@@ -1278,6 +1278,14 @@ puro_status puro_verify_drafts(int64_t B, int64_t T, int64_t draft_rows, int64_t
                           (const void*)tokens, (const void*)accepted})
         if (((uintptr_t)p & 3) != 0) return PURO_ERR_ALIGN;
     if (ws_bytes < verify_ws_bytes(B, T, draft_rows, V)) return PURO_ERR_WORKSPACE;
+    // what is written overlaps nothing that is read but, as a whole, the ids
+    auto overlap = [](const void* p, int64_t n, const void* q, int64_t m) {
+        const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+        return p && q && a < b + (uintptr_t)(4 * m) && b < a + (uintptr_t)(4 * n);
+    };
+    if ((tokens != draft_ids && overlap(tokens, T, draft_ids, T)) || overlap(tokens, T, offsets, B + 1) || overlap(tokens, T, accepted, B) ||
+        overlap(accepted, B, draft_ids, T) || overlap(accepted, B, offsets, B + 1))
+        return PURO_ERR_SHAPE;
     launch_verify(VerifyArgs{target, drafted ? draft : nullptr, ld_target, ld_draft, draft_ids, offsets, uniform, uniform_sample,
                              (int)B, (int)T, (int)draft_rows, (int)V, logits, dtype == PURO_OUT_BF16, logits ? temperature : 1.0, tokens,
                              accepted},

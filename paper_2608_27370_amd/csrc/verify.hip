@@ -824,6 +824,7 @@ __global__ __launch_bounds__(kThreads) void greedy_kernel(Args a) {
         for (int w = 0; w < kWaves; ++w) {
             const int i = i0 + w;
             if (i == rows.n - 1 || choice[w] < 0 || choice[w] != a.ids[rows.start + i]) {
+                __syncthreads();         // (tokens may be the ids themselves)
                 write_tokens<kThreads>(a, b, rows, i, choice[w]);
                 return;
             }

@@ -293,6 +293,19 @@ def test_many_sequences_some_of_them_invalid(P, B, tau):
     assert (b.check(P)[1][4:] == -1).all()
 
 
+@pytest.mark.parametrize("kind,tau,drafted", [(LG, 0.0, False), (LG, 1.0, True), (LG, 1.0, False), (PR, 1.0, True)])
+def test_tokens_over_the_ids(P, kind, tau, drafted):
+    b = Batch(36, [70, 1, 9, 300, 5], 50, kind, "fp32", tau, drafted)
+    if tau == 0:
+        b.ids[:300] = np.where(np.arange(300) < 200, b.values(b.target)[:300].argmax(1), b.ids[:300])
+    want, ids = b.want(), to_dev(b.ids)
+    for _ in range(5):
+        ids.copy_(to_dev(b.ids))
+        tokens, accepted = P.verify_drafts(b.up(b.target), b.up(b.draft), ids, to_dev(b.offsets), to_dev(b.u), to_dev(b.us),
+                                           temperature=tau, kind=kind, tokens=ids)
+        assert tokens is ids and host(ids).tolist() == want[0].tolist() and host(accepted).tolist() == want[1].tolist()
+
+
 def test_no_sequences_and_no_drafts_at_all(P):
     import torch
     z = torch.zeros(0, 40, device="cuda")

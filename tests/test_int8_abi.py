@@ -125,6 +125,11 @@ def test_verification(puro):  # noqa: F811
     need = L.puro_verify_drafts_workspace_size(3, 9, 6, 100)
     assert need > 0 and f(nb=need - 1) == ERR_WORKSPACE
     assert f(B=0, p=None, ids=None, off=None, u=None, us=None, tok=None, acc=None, ws=None, nb=0) == OK
+    # outputs over inputs (9 ids and tokens, 4 offsets, 3 counts)
+    at = dict(ids=FAKE, off=FAKE + 256, tok=FAKE + 512, acc=FAKE + 768)
+    for n, over in (("tok", FAKE + 4), ("tok", FAKE + 256 + 12), ("tok", FAKE + 256 - 32), ("tok", FAKE + 768 + 8), ("acc", FAKE + 32),
+                    ("acc", FAKE + 256 + 12), ("acc", FAKE + 256 - 8)):
+        assert f(**dict(at, **{n: over})) == ERR_SHAPE, (n, over - FAKE)
     for bad in ((0, 1, 1, 5), (1, 1, 2, 5), (1, 1, 1, 0), (-1, 1, 1, 5), (1, 1 << 20, 1, 1 << 20)):
         assert L.puro_verify_drafts_workspace_size(*bad) == 0
 

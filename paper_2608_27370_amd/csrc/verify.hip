@@ -129,8 +129,8 @@ __device__ __forceinline__ double exp2_minus(double u) {
     return __builtin_ldexp(p[0], (int)-u);
 }
 
-// The largest of two or three, NaN passed over (one instruction; written as fmaxf the
-// compiler quiets each operand first).
+// The larger of two, NaN passed over, and the largest of three, NaN if one is (one
+// instruction; written as fmaxf the compiler quiets each operand first).
 __device__ __forceinline__ float max2(float a, float b) {
     float m;
     asm("v_max_f32 %0, %1, %2" : "=v"(m) : "v"(a), "v"(b));
@@ -138,7 +138,7 @@ __device__ __forceinline__ float max2(float a, float b) {
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float m;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
     return m;
 }
 
@@ -201,14 +201,14 @@ __device__ __forceinline__ double wave_sum(double v) {
     return __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
 }
 __device__ __forceinline__ float wave_max(float v) {
-    v = max2(v, __int_as_float(rotated<8>(__float_as_int(v))));
-    v = max2(v, __int_as_float(rotated<4>(__float_as_int(v))));
-    v = max2(v, __int_as_float(rotated<2>(__float_as_int(v))));
-    v = max2(v, __int_as_float(rotated<1>(__float_as_int(v))));
+    v = max3(v, v, __int_as_float(rotated<8>(__float_as_int(v))));
+    v = max3(v, v, __int_as_float(rotated<4>(__float_as_int(v))));
+    v = max3(v, v, __int_as_float(rotated<2>(__float_as_int(v))));
+    v = max3(v, v, __int_as_float(rotated<1>(__float_as_int(v))));
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
-    v = max2(__int_as_float(a[0]), __int_as_float(a[1]));
+    v = max3(v, __int_as_float(a[0]), __int_as_float(a[1]));
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
-    return max2(__int_as_float(b[0]), __int_as_float(b[1]));
+    return max3(v, __int_as_float(b[0]), __int_as_float(b[1]));
 }
 // The larger of two values, NaN if either is.
 template <typename F>
@@ -250,27 +250,21 @@ __device__ __forceinline__ const E* target_row(const Args& a, int64_t t) { retur
 template <typename E>
 __device__ __forceinline__ const E* draft_row(const Args& a, int64_t t) { return (const E*)a.draft + t * a.ld_d; }
 
-// A piece's largest entry, in every lane of its wave, and whether there is a NaN (which it
-// passes over).
+// A piece's largest entry, NaN if one is, in every lane of its wave.
 template <typename E, int LEN>
-__device__ __forceinline__ bool largest(const Piece<E, LEN>& x, float& m) {
-    m = -INFINITY;
-    uint64_t nan = 0;
+__device__ __forceinline__ float largest(const Piece<E, LEN>& x) {
+    float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < x.N; ++i)
 #pragma unroll
-        for (int e = 0; e < kPerVector<E>; e += 2) {
-            m = max3(m, x.x[i][e], x.x[i][e + 1]);
-            nan |= __builtin_amdgcn_ballot_w64(__builtin_isunordered(x.x[i][e], x.x[i][e + 1]));
-        }
-    m = wave_max(m);
-    return nan != 0;
+        for (int e = 0; e < kPerVector<E>; e += 2) m = max3(m, x.x[i][e], x.x[i][e + 1]);
+    return wave_max(m);
 }
 
 // ---- LOGITS: (largest, sum of 2^((z - largest) c)) of every piece of every row.
-// Bound by its arithmetic and, nearly as closely, by memory: 17.5 instructions an entry,
+// Bound by its arithmetic and, nearly as closely, by memory: 16.5 instructions an entry,
 // 11 of them binary64, keep the vector units busy for 85% of the time (768 BF16 rows of
-// 151936: 69 us, 3.4 TB/s; a copy's rate would be 49). With a polynomial of degree 8 and
+// 151936: 65 us, 3.6 TB/s; a copy's rate would be 49). With a polynomial of degree 8 and
 // the exponent rounded by an addition, 19.5: 76; the next piece's loads in flight while
 // one is summed: 79 to 84.
 template <typename E, int LEN>
@@ -281,10 +275,9 @@ __global__ __launch_bounds__(kThreads) void piece_sums_kernel(Args a, int total)
     const E* z = r < a.T ? target_row<E>(a, r) : draft_row<E>(a, r - a.T);
     Piece<E, LEN> x;
     x.load(z, v0, a.V, -INFINITY);
-    float m;
-    const bool nan = largest(x, m);
+    float m = largest(x);
     double s = 0.0;
-    if (nan || m == INFINITY) {
+    if (!(m < INFINITY)) {
         m = __builtin_nanf("");
         s = __builtin_nan("");
     } else if (m > -INFINITY) {
@@ -431,10 +424,17 @@ __device__ __forceinline__ double2 left(double p, double q) {
     const double d = p - q;
     return make_double2(d <= kLeast ? 0.0 : d, p <= kLeast ? 0.0 : p);
 }
+// The same of values that are not NaN, for a sum that piece_share follows: fewer
+// instructions.
+__device__ __forceinline__ double2 left_about(double p, double q) {
+#pragma clang fp contract(off)
+    return make_double2(__builtin_fmax(p - q, 0.0), p);
+}
+__device__ __forceinline__ double piece_share(double sum) { return sum <= 0x1p20 * kLeast ? 0.0 : sum; }
 // f(g), where g(v, x, y, l) gives N entries from v on with the values x and y (the
 // draft's) their l = left(p, q), by the kind of the row's entries: logits of
 // ordinary size, others, probabilities.
-template <int N, typename E, typename F>
+template <int N, bool SUM, typename E, typename F>
 __device__ __forceinline__ void with_left(const Args& a, const EndRow<E>& e, F&& f) {
     auto run = [&](auto kind_c, auto q_c) __attribute__((always_inline)) {
         constexpr int KIND = decltype(kind_c)::value;          // 0: probabilities, 1, 2: logits
@@ -451,7 +451,7 @@ __device__ __forceinline__ void with_left(const Args& a, const EndRow<E>& e, F&&
                 const double pk = KIND != 0 ? p[k] * e.np.inv : (double)x[k];
                 double qk = v + k == e.onehot ? 1.0 : 0.0;
                 if constexpr (Q) qk = KIND != 0 ? q[k] * e.nq.inv : (double)y[k];
-                l[k] = left(pk, qk);
+                l[k] = SUM && KIND != 0 ? left_about(pk, qk) : left(pk, qk);
             }
         });
     };
@@ -468,12 +468,13 @@ __device__ __forceinline__ void with_left(const Args& a, const EndRow<E>& e, F&&
 __device__ __forceinline__ double share(const Args& a, int64_t t, int c, const Norm& n) {
     const double2 st = a.stats[t * a.pieces + c];
     const double p = st.y * exp2_minus((n.m - st.x) * a.c) * n.inv;
-    return p <= 0x1p20 * kLeast ? 0.0 : p;
+    return piece_share(p);
 }
 
 // What is left over in every piece of the end rows. Of LOGITS two exponentials an
-// entry: 21 us for 96 rows of 151936 and their drafts', found in the caches (of rows
-// without a draft's, the sums of their pieces: 25 -> 21).
+// entry: 19 us for 96 rows of 151936 and their drafts', found in the caches (of rows
+// without a draft's, the sums of their pieces: 25 -> 21; the least shares dropped by the
+// piece, not by the entry: 20 -> 19).
 template <typename E, int LEN>
 __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) {
     const Item it = item(a, total);
@@ -500,7 +501,7 @@ __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) 
         x.load(e.zp, v0, a.V, fill);
         if (e.zq) y.load(e.zq, v0, a.V, fill);
         else y = x;
-        with_left<4>(a, e, [&](auto&& left_at) __attribute__((always_inline)) {
+        with_left<4, true>(a, e, [&](auto&& left_at) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < x.N; ++i)
 #pragma unroll
@@ -511,8 +512,8 @@ __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) 
                     p += (l[0].y + l[1].y) + (l[2].y + l[3].y);
                 }
         });
-        r = wave_sum(r);
-        p = wave_sum(p);
+        r = piece_share(wave_sum(r));
+        p = piece_share(wave_sum(p));
     }
     if ((threadIdx.x & 63) == 0) a.left[it.at] = make_double2(r, p);
 }
@@ -597,7 +598,7 @@ __device__ __forceinline__ void with_entries(const Args& a, const EndRow<E>& e, 
     };
     values(e.zp, x);
     values(e.zq ? e.zq : e.zp, y);
-    with_left<PER>(a, e, [&](auto&& left_at) __attribute__((always_inline)) {
+    with_left<PER, false>(a, e, [&](auto&& left_at) __attribute__((always_inline)) {
         double2 l[PER];
         left_at(v0, x, y, l);
         f(l);
@@ -777,8 +778,7 @@ __global__ __launch_bounds__(kThreads) void piece_max_kernel(Args a, int total) 
     const int v0 = it.piece * LEN;
     Piece<E, LEN> x;
     x.load(target_row<E>(a, it.row), v0, a.V, -INFINITY);
-    float m;
-    const bool nan = largest(x, m);
+    const float m = largest(x);
     int id = a.V;
 #pragma unroll
     for (int i = x.N - 1; i >= 0; --i)
@@ -786,7 +786,7 @@ __global__ __launch_bounds__(kThreads) void piece_max_kernel(Args a, int total) 
         for (int e = kPerVector<E> - 1; e >= 0; --e) id = x.x[i][e] == m ? x.at(v0, i) + e : id;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) id = min(id, __shfl_xor(id, o, 64));
-    if ((threadIdx.x & 63) == 0) a.stats[it.at] = make_double2(nan ? __builtin_nan("") : (double)m, (double)id);
+    if ((threadIdx.x & 63) == 0) a.stats[it.at] = make_double2((double)m, (double)id);
 }
 
 // A row's choice, -1 where it has none (NaN, +infinity or nothing but -infinity), by

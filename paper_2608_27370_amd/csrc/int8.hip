@@ -313,33 +313,24 @@ __global__ __launch_bounds__(kThreads) void rows_and_col_max_kernel(QuantInt8Arg
     else quant_rows<kRowBf16, TPR, NC>(a, b - min(c.P, g + 1) * blocks_x, reinterpret_cast<uint32_t*>(red), nullptr);
 }
 
-// The transposed copy by 128x128 tiles, each thread an 8x8 block. The tile's
-// values are on their way while the partial maxima of its columns are read, 16
-// threads a chunk of 8 columns, and 64 threads make the scales of two columns
-// each. Bound by memory and its stores: 8187x1536 8.7 us, 8192x2048 10.1 (50 MB, 5.0 TB/s).
-// `a`: x, its rows rounded up to 16 (which are written; the rows behind
-// `rows` read as zeros), ld, qT, scaleT.
-__global__ __launch_bounds__(kThreads) void quant_cols_int8_kernel(QuantArgs a, int64_t rows, int64_t ld_qT,
-                                                                   const uint16_t* part, int P) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kTile * kTile];
-    __shared__ __attribute__((aligned(16))) float factor[kTile], before[kTile];
-    const Tile t = tile_coords(a.cols);
-    const int64_t tr0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * kTile;     // (the last rows first: the pass before has just read them)
+// The transposed copy by 128x128 tiles, each thread an 8x8 block. `a`: x, its rows
+// rounded up to 16 (which are written; the rows behind `rows` read as zeros), ld, qT,
+// scaleT.
+struct ColScratch {
+    __attribute__((aligned(16))) uint8_t lds[kTile * kTile];
+    __attribute__((aligned(16))) float factor[kTile], before[kTile];
+};
+__device__ __forceinline__ void load_cols(const QuantArgs& a, int64_t rows, int64_t tr0, const Tile& t, v4i w[8]) {
     const int64_t vr = max((int64_t)0, min((int64_t)kTile, rows - tr0));
     const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(vr == 0 ? a.x : a.x + tr0 * a.ld, vr == 0 ? 0u : (uint32_t)(((vr - 1) * a.ld + a.cols) * 2));
-    v4i w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         w[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, t.col_ok ? (uint32_t)(((t.rg * 8 + i) * a.ld + t.col) * 2) : kOOB, 0, 0);
-    uint4 m = make_uint4(0, 0, 0, 0);
-    if (t.col_ok) {
-#pragma unroll 4
-        for (int p = t.rg; p < P; p += 16) {
-            const uint4 v = *reinterpret_cast<const uint4*>(part + (int64_t)p * a.cols + t.col);
-            m.x = pk_max_u16(m.x, v.x); m.y = pk_max_u16(m.y, v.y); m.z = pk_max_u16(m.z, v.z); m.w = pk_max_u16(m.w, v.w);
-        }
-    }
-    uint32_t* const maxima = reinterpret_cast<uint32_t*>(lds);      // [16 groups][64 words of two columns]
+}
+// The scales of the tile's columns from 16 threads' maxima of each chunk of 8; 64
+// threads make those of two columns each.
+__device__ __forceinline__ void col_factors(const QuantArgs& a, const Tile& t, uint4 m, int64_t col0, bool write, ColScratch& s) {
+    uint32_t* const maxima = reinterpret_cast<uint32_t*>(s.lds);      // [16 groups][64 words of two columns]
     *reinterpret_cast<uint4*>(maxima + t.rg * 64 + t.cc * 4) = m;
     __syncthreads();
     if (threadIdx.x < 64) {
@@ -349,17 +340,18 @@ __global__ __launch_bounds__(kThreads) void quant_cols_int8_kernel(QuantArgs a, 
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int j = 2 * threadIdx.x + e;
-            const Int8Scale s = int8_scale((e ? v >> 16 : v & 0xFFFFu) << 16);
-            factor[j] = s.r;
-            before[j] = s.pre;
-            const int64_t col = (int64_t)blockIdx.x * kTile + j;
-            if (blockIdx.y == 0 && col < a.cols) a.scaleT[col] = s.s;
+            const Int8Scale sc = int8_scale((e ? v >> 16 : v & 0xFFFFu) << 16);
+            s.factor[j] = sc.r;
+            s.before[j] = sc.pre;
+            if (write && col0 + j < a.cols) a.scaleT[col0 + j] = sc.s;
         }
     }
     __syncthreads();
+}
+__device__ __forceinline__ void store_cols(const QuantArgs& a, const Tile& t, const v4i w[8], int64_t tr0, int64_t col0, int64_t ld_qT, ColScratch& s) {
     float r[8], pre[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { r[j] = factor[t.cc * 8 + j]; pre[j] = before[t.cc * 8 + j]; }
+    for (int j = 0; j < 8; ++j) { r[j] = s.factor[t.cc * 8 + j]; pre[j] = s.before[t.cc * 8 + j]; }
     uint2 c[8], ct[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -376,18 +368,87 @@ __global__ __launch_bounds__(kThreads) void quant_cols_int8_kernel(QuantArgs a, 
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int r8 = t.cc * 8 + j;
-        *reinterpret_cast<uint2*>(lds + r8 * kTile + (((t.rg >> 1) ^ (r8 >> 3 & 7)) << 4) + ((t.rg & 1) << 3)) = ct[j];
+        *reinterpret_cast<uint2*>(s.lds + r8 * kTile + (((t.rg >> 1) ^ (r8 >> 3 & 7)) << 4) + ((t.rg & 1) << 3)) = ct[j];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kTile * kTile / 16 / kThreads; ++i) {
         const int q = i * kThreads + threadIdx.x;
         const int r8 = q >> 3, h = q & 7;
-        const uint4 v = *reinterpret_cast<const uint4*>(lds + r8 * kTile + ((h ^ (r8 >> 3 & 7)) << 4));
-        const int64_t col = (int64_t)blockIdx.x * kTile + r8, row = tr0 + h * 16;
+        const uint4 v = *reinterpret_cast<const uint4*>(s.lds + r8 * kTile + ((h ^ (r8 >> 3 & 7)) << 4));
+        const int64_t col = col0 + r8, row = tr0 + h * 16;
         if (col < a.cols && row < a.rows) *reinterpret_cast<uint4*>(a.qT + col * ld_qT + row) = v;
     }
 }
+__device__ __forceinline__ void max_mag(uint4& m, const uint4& v) {
+    m.x = pk_max_u16(m.x, v.x); m.y = pk_max_u16(m.y, v.y); m.z = pk_max_u16(m.z, v.z); m.w = pk_max_u16(m.w, v.w);
+}
+
+// The second pass of a long tensor: a tile's values are on their way while the partial
+// maxima of its columns are read. Bound by memory and its stores: 8187x1536 8.7 us,
+// 8192x2048 10.1 (50 MB, 5.0 TB/s).
+__global__ __launch_bounds__(kThreads) void quant_cols_int8_kernel(QuantArgs a, int64_t rows, int64_t ld_qT,
+                                                                   const uint16_t* part, int P) {
+    __shared__ ColScratch s;
+    const Tile t = tile_coords(a.cols);
+    const int64_t tr0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * kTile;     // (the last rows first: the pass before has just read them)
+    const int64_t col0 = (int64_t)blockIdx.x * kTile;
+    v4i w[8];
+    load_cols(a, rows, tr0, t, w);
+    uint4 m = make_uint4(0, 0, 0, 0);
+    if (t.col_ok) {
+#pragma unroll 4
+        for (int p = t.rg; p < P; p += 16) max_mag(m, *reinterpret_cast<const uint4*>(part + (int64_t)p * a.cols + t.col));
+    }
+    col_factors(a, t, m, col0, blockIdx.y == 0, s);
+    store_cols(a, t, w, tr0, col0, ld_qT, s);
+}
+
+// A tensor of few rows: every block reads all of its columns' rows, the others' tiles
+// for the maxima alone, and one launch makes both copies, the rows' blocks behind the
+// columns'. Latency: 128x2048 4.1 us, by two launches 6.0; 333x2048 5.9 and 7.4.
+__device__ __forceinline__ void quant_short_cols(const QuantArgs& a, int64_t rows, int64_t ld_qT, int64_t bx, int by, int tiles, ColScratch& s) {
+    const Tile t = tile_coords(a.cols, bx, by);
+    constexpr int U = 3;
+    v4i own[8], w[U][8];
+    load_cols(a, rows, (int64_t)by * kTile, t, own);
+    uint4 m = make_uint4(0, 0, 0, 0);
+    auto take = [&](const v4i v[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            max_mag(m, make_uint4(mag2((uint32_t)v[i].x), mag2((uint32_t)v[i].y), mag2((uint32_t)v[i].z), mag2((uint32_t)v[i].w)));
+    };
+    for (int k = 1; k < tiles; k += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            // (by, and on from there; past the last one: none)
+            const int other = k + u >= tiles ? tiles : by + k + u - (by + k + u >= tiles ? tiles : 0);
+            load_cols(a, rows, (int64_t)other * kTile, t, w[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) take(w[u]);
+    }
+    take(own);
+    col_factors(a, t, m, bx * kTile, by == 0, s);
+    store_cols(a, t, own, (int64_t)by * kTile, bx * kTile, ld_qT, s);
+}
+__global__ __launch_bounds__(kThreads) void quant_short_cols_int8_kernel(QuantArgs a, int64_t rows, int64_t ld_qT, int tiles) {
+    __shared__ ColScratch s;
+    quant_short_cols(a, rows, ld_qT, blockIdx.x / tiles, (int)blockIdx.x % tiles, tiles, s);
+}
+template <int TPR, int NC>
+__global__ __launch_bounds__(kThreads) void quant_short_both_int8_kernel(QuantInt8Args a, QuantArgs t, int64_t ld_qT, int tiles, int col_blocks) {
+    __shared__ ColScratch s;
+    const int b = (int)blockIdx.x;
+    if (b < col_blocks) quant_short_cols(t, a.rows, ld_qT, b / tiles, b % tiles, tiles, s);
+    else quant_rows<kRowBf16, TPR, NC>(a, b - col_blocks, reinterpret_cast<uint32_t*>(s.lds), nullptr);
+}
+
+// Whether a tensor's columns are of few rows: the tiles are read as often as there are
+// tiles of rows, a few at a time (700x2048, 576 reads: 7.5 us, by two launches 8.5; 333x
+// 17920, 1260: 12.4 and 14.2; 512x17920, 2240: 18.6 and 18.0; 1000x2048, eight tiles of
+// rows: 9.9 and 9.3).
+bool short_cols(int64_t tiles_x, int64_t tiles_y) { return tiles_y <= 6 && tiles_x * tiles_y * tiles_y <= 1280; }
 
 // Ranges of rows: their blocks fill the chip, and every tile of the second pass reads all
 // of their maxima (both copies of 8192x2048: 64 ranges 25.9 us, 128 27.9), of which one
@@ -622,6 +683,22 @@ void launch_quantize_int8(const QuantInt8Args& a, hipStream_t stream) {
 size_t quant_int8_ws_bytes(int64_t rows, int64_t cols) { return (size_t)col_ranges(rows, cols) * cols * 2; }
 
 void launch_quantize_int8_both(const QuantInt8Args& a, int8_t* qT, int64_t ld_qT, float* scaleT, void* ws, hipStream_t stream) {
+    QuantArgs t{};
+    t.x = a.x; t.rows = (a.rows + 15) / 16 * 16; t.cols = a.cols; t.ld = a.ld;
+    t.qT = reinterpret_cast<uint8_t*>(qT); t.scaleT = scaleT;
+    const int64_t tiles_x = (a.cols + kTile - 1) / kTile, tiles_y = (a.rows + kTile - 1) / kTile;
+    if (short_cols(tiles_x, tiles_y)) {
+        const int tiles = (int)tiles_y, col_blocks = (int)(tiles_x * tiles_y);
+        const bool together = a.q && fit_rows(a.rows, a.cols, [&](auto tpr, auto nc) {
+            constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
+            const unsigned grid = (unsigned)(col_blocks + row_blocks(a.rows, TPR));
+            quant_short_both_int8_kernel<TPR, NC><<<grid, kThreads, 0, stream>>>(a, t, ld_qT, tiles, col_blocks);
+        });
+        if (together) return;
+        if (a.q) launch_quantize_int8(a, stream);
+        quant_short_cols_int8_kernel<<<(unsigned)col_blocks, kThreads, 0, stream>>>(t, a.rows, ld_qT, tiles);
+        return;
+    }
     const ColMax c{a.x, a.rows, a.cols, a.ld, col_ranges(a.rows, a.cols), reinterpret_cast<uint16_t*>(ws)};
     const int blocks_x = (int)((a.cols + kColBlock - 1) / kColBlock), col_blocks = blocks_x * c.P;
     const bool together = a.q && fit_rows(a.rows, a.cols, [&](auto tpr, auto nc) {
@@ -635,10 +712,7 @@ void launch_quantize_int8_both(const QuantInt8Args& a, int8_t* qT, int64_t ld_qT
         if (a.q) launch_quantize_int8(a, stream);
         col_max_kernel<<<(unsigned)col_blocks, kThreads, 0, stream>>>(c, blocks_x);
     }
-    QuantArgs t{};
-    t.x = a.x; t.rows = (a.rows + 15) / 16 * 16; t.cols = a.cols; t.ld = a.ld;
-    t.qT = reinterpret_cast<uint8_t*>(qT); t.scaleT = scaleT;
-    const dim3 grid((unsigned)((a.cols + kTile - 1) / kTile), (unsigned)((a.rows + kTile - 1) / kTile));
+    const dim3 grid((unsigned)tiles_x, (unsigned)tiles_y);
     quant_cols_int8_kernel<<<grid, kThreads, 0, stream>>>(t, a.rows, ld_qT, c.part, c.P);
 }
 

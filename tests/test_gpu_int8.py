@@ -30,7 +30,8 @@ def activations(seed, R, C):
 
 
 SHAPES = [(1, 16), (1, 1536), (3, 48), (16, 512), (17, 528), (33, 2048), (128, 2064), (300, 1536), (5, 17920), (2, 65552),
-          (257, 4112), (1000, 64), (64, 8960), (4100, 32), (4097, 128), (5003, 112)]
+          (257, 4112), (1000, 64), (64, 8960), (4100, 32), (4097, 128), (5003, 112), (385, 4096), (500, 144), (768, 2048),
+          (769, 128), (640, 3200), (129, 20480), (129, 20496)]
 
 
 def check_both(P, x, R, C, dev=None, **kw):

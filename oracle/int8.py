@@ -77,7 +77,8 @@ def rmsnorm(x, gamma, eps):
 def swiglu(gu):
     """(h, relative allowance) of float64 gu [R, 2 C]."""
     g, u = np.split(gu, 2, axis=1)
-    return g / (1.0 + np.exp(-g)) * u, 2.0 ** -20
+    with np.errstate(over="ignore"):                 # (a far negative gate: 0)
+        return g / (1.0 + np.exp(-g)) * u, 2.0 ** -20
 
 
 def gemm(A, sa, B, sb, bias=None, residual=None, add=None):

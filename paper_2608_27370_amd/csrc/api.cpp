@@ -1186,15 +1186,17 @@ puro_status puro_int8_linear_fwd(const uint16_t* X, const uint16_t* W, int64_t M
     if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(ws)) return PURO_ERR_ALIGN;
     if (ws_bytes < l.c.used) return PURO_ERR_WORKSPACE;
     uint8_t* w = reinterpret_cast<uint8_t*>(ws);
-    auto quantise = [&](const uint16_t* x, int64_t rows, const Int8Copies& at, uint8_t* qT, float* scaleT) {
-        if (rows == 0 || K == 0) return;
-        const QuantInt8Args a{x, rows, K, K, (int8_t*)(w + at.q), (float*)(w + at.scale), nullptr, 0.0f, nullptr, 0};
-        if (saved) launch_quantize_int8_both(a, (int8_t*)qT, up16(rows), scaleT, w + at.part, stream);
-        else launch_quantize_int8(a, stream);
+    auto rows_of = [&](const uint16_t* x, int64_t rows, const Int8Copies& at) {
+        return QuantInt8Args{x, rows, K, K, (int8_t*)(w + at.q), (float*)(w + at.scale), nullptr, 0.0f, nullptr, 0};
     };
-    if (M == 0) return PURO_OK;
-    quantise(X, M, l.x, saved ? saved->xq_t : nullptr, saved ? saved->x_scale : nullptr);
-    quantise(W, N, l.w, saved ? saved->wq_t : nullptr, saved ? saved->w_scale : nullptr);
+    if (M == 0 || N == 0) return PURO_OK;          // (the backward reads nothing of what is saved then)
+    const QuantInt8Args x = rows_of(X, M, l.x), v = rows_of(W, N, l.w);
+    if (K > 0 && !saved) {
+        launch_quantize_int8_two(x, v, stream);
+    } else if (K > 0) {
+        launch_quantize_int8_both(x, (int8_t*)saved->xq_t, up16(M), saved->x_scale, w + l.x.part, stream);
+        launch_quantize_int8_both(v, (int8_t*)saved->wq_t, up16(N), saved->w_scale, w + l.w.part, stream);
+    }
     int8_product(M, N, K, w + l.x.q, K, (float*)(w + l.x.scale), w + l.w.q, K, (float*)(w + l.w.scale), Y, false, 0, w + l.gemm, stream);
     return launched();
 }

@@ -192,6 +192,14 @@ __global__ __launch_bounds__(kThreads) void quant_rows_int8_kernel(QuantInt8Args
     quant_rows<SRC, TPR, NC>(a, blockIdx.x, red, sums);
 }
 
+// The rows of two tensors of one width, `b`'s blocks behind `a`'s.
+template <int TPR, int NC>
+__global__ __launch_bounds__(kThreads) void quant_two_rows_int8_kernel(QuantInt8Args a, QuantInt8Args b, int blocks) {
+    __shared__ uint32_t red[4];
+    const int i = (int)blockIdx.x;
+    quant_rows<kRowBf16, TPR, NC>(i < blocks ? a : b, i < blocks ? i : i - blocks, red, nullptr);
+}
+
 // Rows longer than the registers hold: one block per row, the values formed twice
 // (the second time from the caches).
 template <int SRC>
@@ -678,6 +686,17 @@ void launch_quantize_int8(const QuantInt8Args& a, hipStream_t stream) {
     if (a.swiglu) launch_rows<kRowSwiglu>(a, stream);
     else if (a.gamma) launch_rows<kRowNorm>(a, stream);
     else launch_rows<kRowBf16>(a, stream);
+}
+
+void launch_quantize_int8_two(const QuantInt8Args& a, const QuantInt8Args& b, hipStream_t stream) {
+    const bool together = fit_rows(a.rows + b.rows, a.cols, [&](auto tpr, auto nc) {
+        constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
+        const int64_t blocks = row_blocks(a.rows, TPR);
+        quant_two_rows_int8_kernel<TPR, NC><<<(unsigned)(blocks + row_blocks(b.rows, TPR)), kThreads, 0, stream>>>(a, b, (int)blocks);
+    });
+    if (together) return;
+    launch_quantize_int8(a, stream);
+    launch_quantize_int8(b, stream);
 }
 
 size_t quant_int8_ws_bytes(int64_t rows, int64_t cols) { return (size_t)col_ranges(rows, cols) * cols * 2; }

@@ -322,6 +322,7 @@ void launch_quantize_int8(const QuantInt8Args& a, hipStream_t stream);
 // [cols, rows] (pitch ld_qT, zeros up to the next 16 columns) with a scale per
 // column; ws holds quant_int8_ws_bytes.
 size_t quant_int8_ws_bytes(int64_t rows, int64_t cols);
+void launch_quantize_int8_two(const QuantInt8Args& a, const QuantInt8Args& b, hipStream_t stream);   // rows of one width
 void launch_quantize_int8_both(const QuantInt8Args& a, int8_t* qT, int64_t ld_qT, float* scaleT, void* ws, hipStream_t stream);
 
 struct Int8Problem {

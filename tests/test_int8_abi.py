@@ -97,7 +97,7 @@ def test_linear_layer(puro):  # noqa: F811
         assert size(-1, 16, 16) == size(4, 8, 16) == size(4, 16, 131072) == 0 < size(1, 16, 16)
     for n in ("X", "W", "Y"):
         assert fwd(**{n: None}) == ERR_NULL and fwd(**{n: FAKE + 8}) == ERR_ALIGN
-    assert fwd(M=0, X=None, Y=None) == OK
+    assert fwd(M=0, X=None, Y=None) == fwd(N=0, W=None, Y=None) == OK
     assert bwd(dY=None) == bwd(saved=None) == ERR_NULL
     assert bwd(dY=FAKE + 8) == bwd(dX=FAKE + 8) == bwd(dW=FAKE + 8) == ERR_ALIGN
     assert bwd(dX=None, dW=None) == bwd(M=0, dY=None, dX=None, acc=1) == bwd(K=0, dX=None, dW=None) == OK

@@ -1150,7 +1150,7 @@ struct Int8BwdLayout {
     }
 };
 
-// One product D [M, N] of dense operands (a reduction of 0: zeros).
+// One product D [M, N] of dense operands.
 void int8_product(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* sa, const void* B, int64_t ldb,
                   const float* sb, void* D, bool f32, int accumulate, void* ws, hipStream_t stream) {
     if (M == 0 || N == 0) return;
@@ -1190,10 +1190,14 @@ puro_status puro_int8_linear_fwd(const uint16_t* X, const uint16_t* W, int64_t M
         return QuantInt8Args{x, rows, K, K, (int8_t*)(w + at.q), (float*)(w + at.scale), nullptr, 0.0f, nullptr, 0};
     };
     if (M == 0 || N == 0) return PURO_OK;          // (the backward reads nothing of what is saved then)
+    if (K == 0) {                                  // (sums of nothing: there are no scales to multiply them by)
+        launch_zero(Y, M * N * 2, stream);
+        return launched();
+    }
     const QuantInt8Args x = rows_of(X, M, l.x), v = rows_of(W, N, l.w);
-    if (K > 0 && !saved) {
+    if (!saved) {
         launch_quantize_int8_two(x, v, stream);
-    } else if (K > 0) {
+    } else {
         launch_quantize_int8_both(x, (int8_t*)saved->xq_t, up16(M), saved->x_scale, w + l.x.part, stream);
         launch_quantize_int8_both(v, (int8_t*)saved->wq_t, up16(N), saved->w_scale, w + l.w.part, stream);
     }

@@ -1079,7 +1079,7 @@ def int8_linear(X, W):
     multiples of 16, the number of tokens is any."""
     if X.dtype != torch.bfloat16 or W.dtype != torch.bfloat16:
         raise TypeError("the int8 linear layer takes BF16 X and W")
-    rows = X.reshape(-1, X.shape[-1])
+    rows = X.reshape(X.shape[:-1].numel(), X.shape[-1])
     if torch.is_grad_enabled() and (X.requires_grad or W.requires_grad):
         Y = _Int8LinearFn.apply(rows, W)
     else:

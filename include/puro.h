@@ -645,8 +645,10 @@ puro_status puro_int8_linear_bwd(const uint16_t* dY, const puro_linear_saved* sa
  * after another: sequence b has the target rows offsets[b] .. offsets[b + 1] - 1,
  * the i-th of them the target's prediction of the place where the draft put
  * draft_ids[offsets[b] + i]; the last row has no draft (its id is not read). The
- * draft's own prediction for target row t is row t - b of `draft`; draft NULL:
- * the drafts were chosen without probabilities (q = 1 at the id).
+ * draft's own predictions lie one after another in `draft`, a row for each draft:
+ * for target row t of sequence b row t - (b - e), e the sequences before b that have
+ * no rows (equal offsets); draft NULL: the drafts were chosen without probabilities
+ * (q = 1 at the id).
  *     p, q: softmax of row / temperature (PURO_VERIFY_LOGITS), or the row as it
  *           stands, not negative (PURO_VERIFY_PROBS)
  *     draft i is kept while uniform[t] q[id] < p[id]; at the first that is not,
@@ -665,8 +667,8 @@ puro_status puro_int8_linear_bwd(const uint16_t* dY, const puro_linear_saved* sa
  * not kept, nor is one whose p or q is NaN; a row of logits with a NaN or a
  * +infinity, or with no probability at all, keeps nothing; a token that would be
  * drawn from such a row, or from one with a NaN or an infinity in its rest, is -1.
- * A sequence without rows has accepted 0 and no token (as behind the last one
- * of a batch with room to spare: rows behind the last sequence are not written);
+ * A sequence without rows (an idle slot, anywhere in the batch) has accepted 0, no
+ * token and no row of the draft's; rows behind the last sequence are not written;
  * one whose offsets decrease or leave [0, T], that begins before an earlier
  * offset, or whose draft rows leave [0, draft_rows), has accepted -1 and no token.
  * tokens may be draft_ids itself (then the ids are replaced); tokens and accepted

@@ -62,17 +62,21 @@ def sequence(target, draft, ids, u, us, kind, tau):
 
 
 def verify(target, draft, ids, offsets, u, us, kind, tau, tokens):
-    """(tokens, accepted); `tokens` holds what the rows behind the last sequence have."""
+    """(tokens, accepted); `tokens` holds what the rows behind the last sequence have. The draft's rows lie one after
+    another like the target's, but for the last one of every sequence that has rows."""
     tokens, B, T = np.array(tokens), len(offsets) - 1, len(ids)
     accepted = np.zeros(B, np.int32)
+    left_out = 0                     # last rows of the sequences before, which the draft has none for
     for b in range(B):
         lo, hi = int(offsets[b]), int(offsets[b + 1])
-        if lo < 0 or hi < lo or hi > T or max(offsets[:b + 1]) > lo or (draft is not None and hi - lo > 1 and (lo - b < 0 or hi - 1 - b > len(draft))):
+        first = lo - left_out
+        left_out += lo != hi
+        if lo < 0 or hi < lo or hi > T or max(offsets[:b + 1]) > lo or (draft is not None and hi - lo > 1 and (first < 0 or first + hi - lo - 1 > len(draft))):
             accepted[b] = -1
             continue
         if lo == hi:
             continue
-        d = None if draft is None else draft[lo - b:hi - 1 - b]
+        d = None if draft is None else draft[first:first + hi - lo - 1]
         kept, token = sequence(target[lo:hi], d, ids[lo:hi], u[lo:hi], us[b], kind, tau)
         accepted[b] = kept
         tokens[lo:hi] = -1

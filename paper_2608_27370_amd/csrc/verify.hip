@@ -41,8 +41,8 @@ struct Args : VerifyArgs {
     double2* stats;       // [T + draft_rows][pieces]: largest logit; sum of 2^((z - largest) c) (greedy: its id)
     double2* left;        // [B][pieces]: sums of max(p - q, 0) and of p
     double4* row;         // [B]: the end row's largest logits and reciprocal sums, target and draft
-    int* kept;            // [B]: drafts kept
-    int* before;          // [B], of many sequences: the largest offset before each
+    int2* end;            // [B]: drafts kept (-1: no rows, -2: invalid ones) and Rows::shift
+    int2* before;         // [B], of many sequences: the largest offset before each, and how many before it have no rows
 };
 
 // The wave's piece of `total`: its index, row and place in it.
@@ -233,17 +233,48 @@ __device__ __forceinline__ bool bad(const Norm& n) { return !(n.inv < kInf); }
 
 // ---- sequences -------------------------------------------------------------------
 
-// Rows of sequence b: its first, and how many (0: none; -1: invalid).
+// Rows of sequence b: its first, how many (0: none; -1: invalid), and what the draft's
+// row of a target row is less than that: the sequences before whose last rows the draft
+// has none for, those without rows not among them. Waves look through the offsets
+// before (a sequence that begins before one of them would write its tokens over
+// another's); of many sequences that is done in a launch before (65536 of them of two
+// rows of 20 entries 4.5 ms and 1.2 in all).
 struct Rows {
-    int start, n;
+    int start, n, shift;
 };
+constexpr int kManySequences = 512;
 __device__ __forceinline__ Rows rows_of(const Args& a, int b) {
     const int64_t start = a.offsets[b], end = a.offsets[b + 1];
-    if (start < 0 || end < start || end > a.T) return {0, -1};
+    bool overlaps = false;
+    int empty = 0;
+    if (a.before) {
+        const int2 v = a.before[b];
+        overlaps = v.x > start;
+        empty = v.y;
+    } else {
+        int mine = 0;
+        for (int i = threadIdx.x & 63; i < b; i += 64) {
+            const int at = a.offsets[i];
+            overlaps = overlaps || at > start;
+            mine += at == a.offsets[i + 1];
+        }
+        overlaps = __builtin_amdgcn_ballot_w64(overlaps) != 0;
+        static_assert(kManySequences / 64 < 1 << 4, "a lane's count");
+#pragma unroll
+        for (int k = 0; k < 4; ++k) empty += __builtin_popcountll(__builtin_amdgcn_ballot_w64((mine >> k & 1) != 0)) << k;
+    }
+    const int shift = b - empty;
+    if (overlaps || start < 0 || end < start || end > a.T) return {0, -1, 0};
     const int n = (int)(end - start);
-    // its draft rows: start - b .. end - 2 - b
-    if (a.draft && n > 1 && (start - b < 0 || end - 1 - b > a.draft_rows)) return {0, -1};
-    return {(int)start, n};
+    // its draft rows: start - shift .. end - 2 - shift
+    if (a.draft && n > 1 && (start - shift < 0 || end - 1 - shift > a.draft_rows)) return {0, -1, 0};
+    return {(int)start, n, shift};
+}
+// The same as an earlier launch left it in end[b].
+__device__ __forceinline__ int2 ended(Rows rows, int kept) { return make_int2(rows.n > 0 ? kept : rows.n - 1, rows.shift); }
+__device__ __forceinline__ Rows rows_of(const Args& a, int b, int2 end) {
+    const int start = a.offsets[b];
+    return {start, end.x < 0 ? end.x + 1 : a.offsets[b + 1] - start, end.y};
 }
 template <typename E>
 __device__ __forceinline__ const E* target_row(const Args& a, int64_t t) { return (const E*)a.target + t * a.ld_t; }
@@ -329,7 +360,7 @@ struct EndScratch {
     float u[kEndWaves];
 };
 template <typename E>
-__device__ __forceinline__ End find_end(const Args& a, int b, Rows rows, EndScratch& s) {
+__device__ __forceinline__ End find_end(const Args& a, Rows rows, EndScratch& s) {
     const int wave = threadIdx.x >> 6, per = a.draft ? kEndWaves / 2 : kEndWaves;
     const bool of_target = wave < per;
     for (int i0 = 0;; i0 += per) {
@@ -339,10 +370,10 @@ __device__ __forceinline__ End find_end(const Args& a, int b, Rows rows, EndScra
         // (asked for ahead of the row's sums)
         const int d = drafted ? a.ids[t] : -1;
         const bool has = d >= 0 && d < a.V;
-        const float x = has ? value(of_target ? target_row<E>(a, t) : draft_row<E>(a, t - b), d) : 0.0f;
+        const float x = has ? value(of_target ? target_row<E>(a, t) : draft_row<E>(a, t - rows.shift), d) : 0.0f;
         const float u = drafted && of_target ? a.u[t] : 0.0f;
         if (of_target ? i < rows.n : drafted) {
-            const Norm n = row_norm(a, of_target ? t : a.T + t - b);
+            const Norm n = row_norm(a, of_target ? t : a.T + t - rows.shift);
             const double prob = has && !bad(n) ? prob_at(a, x, n) : __builtin_nan("");
             if ((threadIdx.x & 63) == 0) {
                 s.norms[wave] = n;
@@ -365,10 +396,13 @@ __global__ __launch_bounds__(kEndWaves * 64) void end_rows_kernel(Args a) {
     __shared__ EndScratch scratch;
     const int b = blockIdx.x;
     const Rows rows = rows_of(a, b);
-    if (rows.n <= 0) return;
-    const End e = find_end<E>(a, b, rows, scratch);
+    if (rows.n <= 0) {
+        if (threadIdx.x == 0) a.end[b] = ended(rows, 0);
+        return;
+    }
+    const End e = find_end<E>(a, rows, scratch);
     if (threadIdx.x == 0) {
-        a.kept[b] = e.kept;
+        a.end[b] = ended(rows, e.kept);
         a.row[b] = make_double4(e.p.m, e.p.inv, e.q.m, e.q.inv);
     }
 }
@@ -376,7 +410,7 @@ __global__ __launch_bounds__(kEndWaves * 64) void end_rows_kernel(Args a) {
 // The same of probabilities, whose entries say it alone: by one wave, 64 drafts at a
 // time (every wave of every block that needs it, rather than a launch of its own).
 template <typename E>
-__device__ __forceinline__ int kept_of_probs(const Args& a, int b, Rows rows) {
+__device__ __forceinline__ int kept_of_probs(const Args& a, Rows rows) {
     for (int i0 = 0;; i0 += 64) {
         const int i = i0 + (threadIdx.x & 63);
         const int64_t t = rows.start + i;
@@ -385,7 +419,7 @@ __device__ __forceinline__ int kept_of_probs(const Args& a, int b, Rows rows) {
             const int d = a.ids[t];
             if (d >= 0 && d < a.V) {
                 const double p = (double)value(target_row<E>(a, t), d);
-                const double q = a.draft ? (double)value(draft_row<E>(a, t - b), d) : 1.0;
+                const double q = a.draft ? (double)value(draft_row<E>(a, t - rows.shift), d) : 1.0;
                 keep = (double)a.u[t] * q < p && p > kLeast;
             }
         }
@@ -401,19 +435,19 @@ struct EndRow {
     const E *zp, *zq;
     int onehot;
     Norm np, nq;
-    __device__ __forceinline__ EndRow(const Args& a, int b, Rows rows, int kept, Norm p, Norm q) : zq(nullptr), onehot(-1), np(p), nq(q) {
+    __device__ __forceinline__ EndRow(const Args& a, Rows rows, int kept, Norm p, Norm q) : zq(nullptr), onehot(-1), np(p), nq(q) {
         const int64_t t = rows.start + kept;
         zp = target_row<E>(a, t);
         if (kept < rows.n - 1) {
-            if (a.draft) zq = draft_row<E>(a, t - b);
+            if (a.draft) zq = draft_row<E>(a, t - rows.shift);
             else onehot = a.ids[t];
         }
     }
     // (as end_rows_kernel left them)
     __device__ __forceinline__ static EndRow of(const Args& a, int b, Rows rows, int kept) {
-        if (!a.logits) return EndRow(a, b, rows, kept, {0.0, 1.0}, {0.0, 1.0});
+        if (!a.logits) return EndRow(a, rows, kept, {0.0, 1.0}, {0.0, 1.0});
         const double4 n = a.row[b];
-        return EndRow(a, b, rows, kept, {n.x, n.y}, {n.z, n.w});
+        return EndRow(a, rows, kept, {n.x, n.y}, {n.z, n.w});
     }
 };
 // (max(p - q, 0), p), NaN where p or q is; 0 where no more than kLeast, so that a
@@ -480,15 +514,18 @@ __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) 
     const Item it = item(a, total);
     if (!it.live) return;
     const int b = it.row, v0 = it.piece * LEN;
-    const Rows rows = rows_of(a, b);
-    if (rows.n <= 0) return;
-    int kept;
+    Rows rows;
+    int kept = 0;
     if (a.logits) {
-        kept = a.kept[b];
+        const int2 end = a.end[b];
+        rows = rows_of(a, b, end);
+        kept = end.x;
     } else {
-        kept = kept_of_probs<E>(a, b, rows);
-        if (it.piece == 0 && (threadIdx.x & 63) == 0) a.kept[b] = kept;
+        rows = rows_of(a, b);
+        if (rows.n > 0) kept = kept_of_probs<E>(a, rows);
+        if (it.piece == 0 && (threadIdx.x & 63) == 0) a.end[b] = ended(rows, kept);
     }
+    if (rows.n <= 0) return;
     const EndRow<E> e = EndRow<E>::of(a, b, rows, kept);
     const float fill = a.logits ? -INFINITY : 0.0f;
     double r = 0.0, p = 0.0;
@@ -522,40 +559,40 @@ __global__ __launch_bounds__(kThreads) void left_over_kernel(Args a, int total) 
 // One block per sequence, a chain of short steps: what they need of memory is asked
 // for at the start, and every wave finds the piece by itself (no barrier). 4 to 6 us.
 
-// Whether sequence b begins before an earlier offset (its tokens would be written
-// over another's); by every wave, of many sequences in a launch before (65536 of them
-// of two rows of 20 entries 4.5 ms and 1.2 in all).
-__device__ __forceinline__ bool overlaps(const Args& a, int b) {
-    const int start = a.offsets[b];
-    if (a.before) return a.before[b] > start;
-    bool any = false;
-    for (int i = threadIdx.x & 63; i < b; i += 64) any = any || a.offsets[i] > start;
-    return __builtin_amdgcn_ballot_w64(any) != 0;
-}
-
-constexpr int kScanThreads = 1024, kManySequences = 512;
-// before[b] = the largest of offsets[0 .. b - 1]: one block, each thread some sequences
-// in a row.
-__global__ __launch_bounds__(kScanThreads) void offset_maxima_kernel(Args a) {
-    __shared__ int waves[kScanThreads / 64];
+constexpr int kScanThreads = 1024;
+// before[b] = the largest of offsets[0 .. b - 1], and how many i < b have offsets[i] ==
+// offsets[i + 1]: one block, each thread some sequences in a row.
+__global__ __launch_bounds__(kScanThreads) void offsets_before_kernel(Args a) {
+    __shared__ int2 waves[kScanThreads / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (a.B + kScanThreads - 1) / kScanThreads;
     const int b0 = min(a.B, (int)threadIdx.x * per), b1 = min(a.B, b0 + per);
-    int m = INT_MIN;
+    int m = INT_MIN, n = 0;
 #pragma unroll 8
-    for (int b = b0; b < b1; ++b) m = max(m, a.offsets[b]);
+    for (int b = b0; b < b1; ++b) {
+        m = max(m, a.offsets[b]);
+        n += a.offsets[b] == a.offsets[b + 1];
+    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int t = __shfl_up(m, o, 64);
-        if (lane >= o) m = max(m, t);
+        const int t = __shfl_up(m, o, 64), k = __shfl_up(n, o, 64);
+        if (lane >= o) {
+            m = max(m, t);
+            n += k;
+        }
     }
-    if (lane == 63) waves[wave] = m;
+    if (lane == 63) waves[wave] = make_int2(m, n);
     __syncthreads();
-    const int below = __shfl_up(m, 1, 64);
+    const int below = __shfl_up(m, 1, 64), fewer = __shfl_up(n, 1, 64);
     m = lane > 0 ? below : INT_MIN;
-    for (int w = 0; w < wave; ++w) m = max(m, waves[w]);
+    n = lane > 0 ? fewer : 0;
+    for (int w = 0; w < wave; ++w) {
+        m = max(m, waves[w].x);
+        n += waves[w].y;
+    }
     for (int b = b0; b < b1; ++b) {
-        a.before[b] = m;
+        a.before[b] = make_int2(m, n);
         m = max(m, a.offsets[b]);
+        n += a.offsets[b] == a.offsets[b + 1];
     }
 }
 
@@ -708,17 +745,16 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(Args a) {
     const double2* left = a.left + (int64_t)b * a.pieces;
     const Lane mine(a);
     const float us = a.T > 0 ? a.us[b] : 0.0f;        // (none are given for no rows)
-    const int kept_at = a.kept[b];
+    const int2 end = a.end[b];
     double2 l0 = make_double2(0.0, 0.0);
     if (mine.c0 < mine.c1) l0 = left[mine.c0];
-    Rows rows = rows_of(a, b);
-    if (overlaps(a, b)) rows.n = -1;
+    const Rows rows = rows_of(a, b, end);
     if (rows.n <= 0) {
         if (threadIdx.x == 0) a.accepted[b] = rows.n;
         return;
     }
-    const EndRow<E> e = EndRow<E>::of(a, b, rows, kept_at);
-    draw<LEN, kWaves>(a, b, rows, kept_at, e, us, mine, l0, [&](int c) __attribute__((always_inline)) { return left[c]; }, scratch);
+    const EndRow<E> e = EndRow<E>::of(a, b, rows, end.x);
+    draw<LEN, kWaves>(a, b, rows, end.x, e, us, mine, l0, [&](int c) __attribute__((always_inline)) { return left[c]; }, scratch);
 }
 
 // LOGITS without the draft's: the end row and the draw in one launch. Nothing but the
@@ -731,18 +767,17 @@ __global__ __launch_bounds__(kEndWaves * 64) void end_and_draw_kernel(Args a) {
     __shared__ DrawScratch<kEndWaves> scratch;
     const int b = blockIdx.x;
     const float us = a.us[b];
-    Rows rows = rows_of(a, b);
-    if (overlaps(a, b)) rows.n = -1;
+    const Rows rows = rows_of(a, b);
     if (rows.n <= 0) {
         if (threadIdx.x == 0) a.accepted[b] = rows.n;
         return;
     }
-    const End end = find_end<E>(a, b, rows, end_scratch);
+    const End end = find_end<E>(a, rows, end_scratch);
     if (bad(end.p)) {
         write_tokens<kEndWaves * 64>(a, b, rows, end.kept, -1);
         return;
     }
-    const EndRow<E> e(a, b, rows, end.kept, end.p, {0.0, 1.0});
+    const EndRow<E> e(a, rows, end.kept, end.p, {0.0, 1.0});
     const int without = e.onehot >= 0 && e.onehot < a.V ? e.onehot / LEN : -1;
     double rest = 0.0;
     if (without >= 0) {
@@ -809,8 +844,7 @@ __device__ __forceinline__ int row_choice(const Args& a, int64_t r) {
 __global__ __launch_bounds__(kThreads) void greedy_kernel(Args a) {
     __shared__ int choice[kWaves];
     const int b = blockIdx.x, wave = threadIdx.x >> 6;
-    Rows rows = rows_of(a, b);
-    if (overlaps(a, b)) rows.n = -1;
+    const Rows rows = rows_of(a, b);
     if (rows.n <= 0) {
         if (threadIdx.x == 0) a.accepted[b] = rows.n;
         return;
@@ -843,7 +877,7 @@ int piece_length(int64_t T, int64_t V) { return T * V < (int64_t)8192 * 2048 ? 1
 
 struct Layout {
     int len, pieces;
-    size_t left, row, kept, before, total;       // (the rows' sums first)
+    size_t left, row, end, before, total;       // (the rows' sums first)
 };
 Layout layout(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
     Layout l{};
@@ -851,16 +885,16 @@ Layout layout(int64_t B, int64_t T, int64_t draft_rows, int64_t V) {
     l.pieces = (int)((V + l.len - 1) / l.len);
     l.left = up((size_t)(T + draft_rows) * l.pieces * sizeof(double2));
     l.row = l.left + up((size_t)B * l.pieces * sizeof(double2));
-    l.kept = l.row + up((size_t)B * sizeof(double4));
-    l.before = l.kept + up((size_t)B * sizeof(int));
-    l.total = l.before + (B > kManySequences ? up((size_t)B * sizeof(int)) : 0);
+    l.end = l.row + up((size_t)B * sizeof(double4));
+    l.before = l.end + up((size_t)B * sizeof(int2));
+    l.total = l.before + (B > kManySequences ? up((size_t)B * sizeof(int2)) : 0);
     return l;
 }
 
 template <typename E, int LEN>
 void launch(const Args& a, hipStream_t stream) {
     auto blocks = [](int64_t n) { return (unsigned)((n + kWaves - 1) / kWaves); };
-    if (a.before) offset_maxima_kernel<<<1, kScanThreads, 0, stream>>>(a);
+    if (a.before) offsets_before_kernel<<<1, kScanThreads, 0, stream>>>(a);
     if (a.temperature == 0.0) {
         const int total = a.T * a.pieces;
         if (total > 0) piece_max_kernel<E, LEN><<<blocks(total), kThreads, 0, stream>>>(a, total);
@@ -897,8 +931,8 @@ void launch_verify(const VerifyArgs& v, void* ws, hipStream_t stream) {
     a.stats = reinterpret_cast<double2*>(w);
     a.left = reinterpret_cast<double2*>(w + l.left);
     a.row = reinterpret_cast<double4*>(w + l.row);
-    a.kept = reinterpret_cast<int*>(w + l.kept);
-    a.before = v.B > kManySequences ? reinterpret_cast<int*>(w + l.before) : nullptr;
+    a.end = reinterpret_cast<int2*>(w + l.end);
+    a.before = v.B > kManySequences ? reinterpret_cast<int2*>(w + l.before) : nullptr;
     auto run = [&](auto len) {
         constexpr int LEN = decltype(len)::value;
         if (v.bf16) launch<uint16_t, LEN>(a, stream);

@@ -1094,9 +1094,9 @@ VERIFY_LOGITS, VERIFY_PROBS = 0, 1
 def verify_drafts(target, draft, draft_ids, offsets, uniform=None, uniform_sample=None, temperature=1.0, kind=VERIFY_LOGITS,
                   tokens=None, accepted=None, ws=None):
     """Which drafted tokens to keep, and the token after them. target [T, V] (BF16 or FP32): the rows of all sequences one
-    after another, sequence b's from offsets[b] to offsets[b + 1] (int32 [B + 1]), one more than it has drafts; draft
-    [drafts, V] of target's type: the draft model's predictions (row t - b for target row t), None where it has none;
-    draft_ids [T] int32, the last of a sequence not read. Logits, at a temperature (0: the largest), or probabilities
+    after another, sequence b's from offsets[b] to offsets[b + 1] (int32 [B + 1]), one more than it has drafts (or none: an
+    idle slot); draft [drafts, V] of target's type: the draft model's predictions, a row for each draft, sequence by
+    sequence, None where it has none; draft_ids [T] int32, the last of a sequence not read. Logits, at a temperature (0: the largest), or probabilities
     (VERIFY_PROBS). uniform [T] and uniform_sample [B]: FP32 random numbers in [0, 1). Returns (tokens [T], accepted [B])
     int32: a sequence's kept ids, its drawn token and -1 from there on; rows behind the last sequence are left alone."""
     dev = _current()

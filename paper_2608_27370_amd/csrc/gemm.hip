@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
         } else {
             for (int e = 0; e < 4; ++e) c[e] = n + e < cols ? sb[n + e] : 0.0f;
         }
-        s = make_float4((float)v.x * r * c[0], (float)v.y * r * c[1], (float)v.z * r * c[2], (float)v.w * r * c[3]);
+        s = make_float4(scaled_sum(v.x, r, c[0]), scaled_sum(v.y, r, c[1]), scaled_sum(v.z, r, c[2]), scaled_sum(v.w, r, c[3]));
         if (OUT != kOutF32 && n + 3 >= cols) {
             const float w[4] = {s.x, s.y, s.z, s.w};
             uint16_t* const dst = reinterpret_cast<uint16_t*>(D) + m * ldd + n;

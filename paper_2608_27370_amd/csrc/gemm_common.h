@@ -133,6 +133,14 @@ constexpr int spare_units(int bm, int bn, int sl, int nst, int xa, bool grouped)
                                                                         : xa;
 }
 
+// An int8 product's sum times its row's and its column's scale, each step rounded,
+// also where a term is added next (the compiler would fuse the last product into
+// that sum where both meet in registers, and an output would depend on its tile).
+__device__ __forceinline__ float scaled_sum(int sum, float sa, float sb) {
+#pragma clang fp contract(off)
+    return (float)sum * sa * sb;
+}
+
 // The bias / residual epilogue: the BF16 bias of columns n..n+3 and the BF16
 // residual of row m at those columns added to four binary32 results (the
 // sum stays binary32 until the output's one rounding).

@@ -913,8 +913,8 @@ __global__ __launch_bounds__(WM * WN * 64 * (PROD ? 2 : 1)) void gemm_fp8_kernel
     auto scale4 = [&](int i, int j, int g, float& v0, float& v1, float& v2, float& v3) __attribute__((always_inline)) {
         if constexpr (kInt) {
             const v4f c = *reinterpret_cast<const v4f*>(lds_cols + j * 32 + 8 * g + 4 * (lane >> 5));
-            v0 = (float)__float_as_int(v0) * row_s[i] * c.x; v1 = (float)__float_as_int(v1) * row_s[i] * c.y;
-            v2 = (float)__float_as_int(v2) * row_s[i] * c.z; v3 = (float)__float_as_int(v3) * row_s[i] * c.w;
+            v0 = scaled_sum(__float_as_int(v0), row_s[i], c.x); v1 = scaled_sum(__float_as_int(v1), row_s[i], c.y);
+            v2 = scaled_sum(__float_as_int(v2), row_s[i], c.z); v3 = scaled_sum(__float_as_int(v3), row_s[i], c.w);
         }
     };
     (void)scale4; (void)lds_cols;

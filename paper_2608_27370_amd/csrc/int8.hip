@@ -9,6 +9,7 @@ namespace puro {
 
 using gemm_detail::add_epilogue1;
 using gemm_detail::add_epilogue4;
+using gemm_detail::scaled_sum;
 
 namespace {
 
@@ -480,7 +481,7 @@ typedef int v4i32 __attribute__((ext_vector_type(4)));
 
 // Outputs [m, n .. n + 3]: the scaled sums, bias, residual, one rounding.
 __device__ __forceinline__ void store_int8_outputs(const Int8Problem& p, int64_t m, int64_t n, v4i32 acc, float sa, const float sb[4]) {
-    float4 v = make_float4((float)acc.x * sa * sb[0], (float)acc.y * sa * sb[1], (float)acc.z * sa * sb[2], (float)acc.w * sa * sb[3]);
+    float4 v = make_float4(scaled_sum(acc.x, sa, sb[0]), scaled_sum(acc.y, sa, sb[1]), scaled_sum(acc.z, sa, sb[2]), scaled_sum(acc.w, sa, sb[3]));
     if (m >= p.M || n >= p.N) return;
     if (p.N % 4 == 0) {
         if (!p.f32) {

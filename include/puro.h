@@ -587,9 +587,10 @@ puro_status puro_quantize_int8(const uint16_t* x, int64_t rows, int64_t cols, in
  *   swiglu:   h = silu(gate) up of gu [rows, 2 cols].
  * The values are encoded as binary32 has them, without a rounding to BF16
  * between. Requirements as puro_quantize_int8; gamma BF16 [cols], 16-byte
- * aligned; eps finite and >= 0 (with eps = 0 a row of zeros has scale NaN); gu's
- * pitch ld >= 2 cols. Rows whose sum of squares overflows binary32 are outside
- * the statement. */
+ * aligned; eps finite and >= 0 (with eps = 0 a row of zeros has scale NaN; any
+ * other row has its norm, down to BF16's smallest values, its rstd infinity where
+ * binary32 has no larger number); gu's pitch ld >= 2 cols. Rows whose sum of squares
+ * overflows binary32 are outside the statement. */
 puro_status puro_rmsnorm_quantize_int8(const uint16_t* x, const uint16_t* gamma, int64_t rows, int64_t cols,
                                        int64_t ld, float eps, int8_t* q, float* scale, float* rstd,
                                        hipStream_t stream);

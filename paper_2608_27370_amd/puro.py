@@ -1058,20 +1058,21 @@ class _Int8LinearFn(torch.autograd.Function):
     buffer on W, dW is accumulated into it and W gets no .grad; otherwise W's .grad is dW in W's dtype."""
 
     @staticmethod
-    def forward(ctx, X, W):
-        Y, saved = int8_linear_fwd(_dense_rows(X), _dense_rows(W))
-        ctx.save_for_backward(*saved.values())
-        ctx.main_grad = getattr(W, "main_grad", None)
+    def forward(ctx, X, W, keep):
+        Y, saved = int8_linear_fwd(_dense_rows(X), _dense_rows(W), want_saved=keep)
+        if keep:
+            ctx.save_for_backward(*saved.values())
+            ctx.main_grad = getattr(W, "main_grad", None)
         return Y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dY):
         saved = dict(zip(("xq_t", "x_scale", "wq_t", "w_scale"), ctx.saved_tensors))
-        want_dx, want_dw = ctx.needs_input_grad
+        want_dx, want_dw, _ = ctx.needs_input_grad
         mg = ctx.main_grad if want_dw else None
         dX, dW = int8_linear_bwd(_dense_rows(dY.to(torch.bfloat16)), saved, want_dx, want_dw, dW=mg, accumulate_dw=mg is not None)
-        return dX, dW.to(torch.bfloat16) if want_dw and mg is None else None
+        return dX, dW.to(torch.bfloat16) if want_dw and mg is None else None, None
 
 
 def int8_linear(X, W):
@@ -1080,8 +1081,10 @@ def int8_linear(X, W):
     if X.dtype != torch.bfloat16 or W.dtype != torch.bfloat16:
         raise TypeError("the int8 linear layer takes BF16 X and W")
     rows = X.reshape(X.shape[:-1].numel(), X.shape[-1])
-    if torch.is_grad_enabled() and (X.requires_grad or W.requires_grad):
-        Y = _Int8LinearFn.apply(rows, W)
+    keep = torch.is_grad_enabled() and (X.requires_grad or W.requires_grad)
+    # (a tangent of forward mode is refused there, rather than lost)
+    if keep or any(torch.autograd.forward_ad.unpack_dual(t).tangent is not None for t in (X, W)):
+        Y = _Int8LinearFn.apply(rows, W, keep)
     else:
         Y, _ = int8_linear_fwd(_dense_rows(rows.detach()), _dense_rows(W.detach()), want_saved=False)
     return Y.reshape(*X.shape[:-1], Y.shape[-1])

@@ -626,6 +626,8 @@ puro_status puro_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* A, int
  *   saved: xq_t [K, M16] (int8; M16 = M rounded up to 16, zeros behind the tokens),
  *   x_scale [K], wq_t [K, N], w_scale [K]: the transposed copies for the backward.
  * Forward: Y [M, N] (BF16); saved NULL: no backward follows, the copies are not made.
+ * A backward reads W's copy for dX and X's for dW: of saved either, with its scales,
+ * may be NULL where that gradient is not wanted.
  * Backward: dX [M, K] (BF16) and dW [N, K] (FP32; += when accumulate_dW != 0); either
  * may be NULL to skip it. M = 0 is valid (dW: zeros, or as it was), and K = 0 (Y: zeros).
  * Requirements: N and K multiples of 16 (else PURO_ERR_ALIGN), M, N and K at most

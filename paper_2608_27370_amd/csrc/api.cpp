@@ -1158,8 +1158,9 @@ void int8_product(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, c
                      ws, stream);
 }
 
+// The copies of X (for dW) and of W (for dX), each with its scales or not there.
 puro_status check_int8_saved(const puro_linear_saved* s) {
-    if (!s->xq_t || !s->x_scale || !s->wq_t || !s->w_scale) return PURO_ERR_NULL;
+    if (!s->xq_t != !s->x_scale || !s->wq_t != !s->w_scale) return PURO_ERR_NULL;
     return aligned16(s->xq_t) && aligned16(s->x_scale) && aligned16(s->wq_t) && aligned16(s->w_scale) ? PURO_OK : PURO_ERR_ALIGN;
 }
 
@@ -1195,11 +1196,15 @@ puro_status puro_int8_linear_fwd(const uint16_t* X, const uint16_t* W, int64_t M
         return launched();
     }
     const QuantInt8Args x = rows_of(X, M, l.x), v = rows_of(W, N, l.w);
-    if (!saved) {
+    auto quantize = [&](const QuantInt8Args& a, void* qT, float* scaleT, size_t part) {
+        if (qT) launch_quantize_int8_both(a, (int8_t*)qT, up16(a.rows), scaleT, w + part, stream);
+        else launch_quantize_int8(a, stream);
+    };
+    if (!saved || (!saved->xq_t && !saved->wq_t)) {
         launch_quantize_int8_two(x, v, stream);
     } else {
-        launch_quantize_int8_both(x, (int8_t*)saved->xq_t, up16(M), saved->x_scale, w + l.x.part, stream);
-        launch_quantize_int8_both(v, (int8_t*)saved->wq_t, up16(N), saved->w_scale, w + l.w.part, stream);
+        quantize(x, saved->xq_t, saved->x_scale, l.x.part);
+        quantize(v, saved->wq_t, saved->w_scale, l.w.part);
     }
     int8_product(M, N, K, w + l.x.q, K, (float*)(w + l.x.scale), w + l.w.q, K, (float*)(w + l.w.scale), Y, false, 0, w + l.gemm, stream);
     return launched();
@@ -1225,6 +1230,7 @@ puro_status puro_int8_linear_bwd(const uint16_t* dY, const puro_linear_saved* sa
     const Int8BwdLayout l(M, N, K);
     if (!dY || !saved || !ws) return PURO_ERR_NULL;
     if ((st = check_int8_saved(saved)) != PURO_OK) return st;
+    if ((dX && !saved->wq_t) || (dW && !saved->xq_t)) return PURO_ERR_NULL;
     if (ws_bytes < l.c.used) return PURO_ERR_WORKSPACE;
     if (!dX && !dW) return PURO_OK;
     uint8_t* w = reinterpret_cast<uint8_t*>(ws);

@@ -1003,10 +1003,10 @@ def int8_gemm(A, a_scale, B, b_scale, out_dtype=OUT_BF16, D=None, accumulate=Fal
     return D
 
 
-def int8_linear_fwd(X, W, Y=None, want_saved=True, ws=None):
+def int8_linear_fwd(X, W, Y=None, want_saved=True, ws=None, want_dx=True, want_dw=True):
     """Y = X W^T [M, N] (BF16) of BF16 X [M, K] and W [N, K], both quantised to int8, a scale per token and per output
     channel; returns (Y, saved): the transposed copies with scales per channel that ``int8_linear_bwd`` takes (None
-    without want_saved)."""
+    without want_saved), W's for dX and X's for dW, None where that gradient will not be wanted."""
     dev = _current()
     (M, K), N = X.shape, W.shape[0]
     px, pw = _dense(X, "X", _BF16_BITS, (M, K), dev), _dense(W, "W", _BF16_BITS, (N, K), dev)
@@ -1014,9 +1014,11 @@ def int8_linear_fwd(X, W, Y=None, want_saved=True, ws=None):
         Y = X.new_empty((M, N), dtype=torch.bfloat16)
     saved = s = None
     if want_saved:
-        saved = dict(xq_t=X.new_empty((K, -(-M // 16) * 16), dtype=torch.int8), x_scale=X.new_empty(K, dtype=torch.float32),
-                     wq_t=X.new_empty((K, N), dtype=torch.int8), w_scale=X.new_empty(K, dtype=torch.float32))
-        s = ctypes.byref(_saved_struct(saved))
+        saved = dict(xq_t=X.new_empty((K, -(-M // 16) * 16), dtype=torch.int8) if want_dw else None,
+                     x_scale=X.new_empty(K, dtype=torch.float32) if want_dw else None,
+                     wq_t=X.new_empty((K, N), dtype=torch.int8) if want_dx else None,
+                     w_scale=X.new_empty(K, dtype=torch.float32) if want_dx else None)
+        s = ctypes.byref(Saved(*map(_ptr, saved.values())))
     w, nb = _ws(_size("puro_int8_linear_fwd_workspace_size", M, N, K), ws, X.device)
     _check("puro_int8_linear_fwd", lib().puro_int8_linear_fwd(
         px, pw, M, N, K, _dense(Y, "Y", (torch.bfloat16,), (M, N), dev), s, _ptr(w), nb, _stream()))
@@ -1028,10 +1030,15 @@ def int8_linear_bwd(dY, saved, want_dx=True, want_dw=True, dX=None, dW=None, acc
     and per channel for the other; returns (dX, dW)."""
     dev = _current()
     (M, N), xq, wq = dY.shape, saved["xq_t"], saved["wq_t"]
-    K = xq.shape[0]
+    if (want_dw and xq is None) or (want_dx and wq is None):
+        raise ValueError("the forward did not save what %s is made of" % ("dW" if want_dw and xq is None else "dX"))
+    K = (wq if xq is None else xq).shape[0] if xq is not None or wq is not None else 0
     pdy = _dense(dY, "dY", _BF16_BITS, (M, N), dev)
-    s = Saved(_dense(xq, "xq_t", _INT8, (K, -(-M // 16) * 16), dev), _vector(saved["x_scale"], "x_scale", _FP32, K, dev),
-              _dense(wq, "wq_t", _INT8, (K, N), dev), _vector(saved["w_scale"], "w_scale", _FP32, K, dev))
+    s = Saved(None, None, None, None)
+    if xq is not None:
+        s.xq_t, s.x_scale = _dense(xq, "xq_t", _INT8, (K, -(-M // 16) * 16), dev), _vector(saved["x_scale"], "x_scale", _FP32, K, dev)
+    if wq is not None:
+        s.wq_t, s.w_scale = _dense(wq, "wq_t", _INT8, (K, N), dev), _vector(saved["w_scale"], "w_scale", _FP32, K, dev)
     pdx = pdw = None
     if want_dx:
         if dX is None:
@@ -1059,7 +1066,8 @@ class _Int8LinearFn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, X, W, keep):
-        Y, saved = int8_linear_fwd(_dense_rows(X), _dense_rows(W), want_saved=keep)
+        want_dx, want_dw, _ = ctx.needs_input_grad
+        Y, saved = int8_linear_fwd(_dense_rows(X), _dense_rows(W), want_saved=keep, want_dx=want_dx, want_dw=want_dw)
         if keep:
             ctx.save_for_backward(*saved.values())
             ctx.main_grad = getattr(W, "main_grad", None)

@@ -1,5 +1,5 @@
 """The int8 linear layer as an autograd operation: its gradients against central
-differences of its own outputs, forward mode."""
+differences of its own outputs, what it keeps for a backward, forward mode."""
 
 import numpy as np
 import pytest
@@ -74,3 +74,60 @@ def test_forward_mode_is_refused(P):
             with torch.no_grad(), pytest.raises((NotImplementedError, RuntimeError)):
                 P.int8_linear(x, w)
     assert not P.int8_linear(X, W).requires_grad
+
+
+def test_what_is_kept_is_what_the_backward_reads(P, monkeypatch):
+    import torch
+    g = np.random.default_rng(2)
+    M, N, K = 37, 48, 64
+    X, W, dY = bf16(g.normal(size=(M, K))), bf16(g.normal(size=(N, K))), bf16(g.normal(size=(M, N)))
+    made, forward = [], P.int8_linear_fwd
+
+    def recorded(*a, **kw):
+        y, saved = forward(*a, **kw)
+        made.append(saved)
+        return y, saved
+    monkeypatch.setattr(P, "int8_linear_fwd", recorded)
+
+    def call(want_x, want_w):
+        x, w = X.clone().requires_grad_(want_x), W.clone().requires_grad_(want_w)
+        Y = P.int8_linear(x, w)
+        if Y.requires_grad:
+            Y.backward(dY)
+        return Y.detach(), x.grad, w.grad, made[-1]
+    Y, dX, dW, both = call(True, True)
+    assert all(v is not None for v in both.values())
+    for want_x, want_w in ((True, False), (False, True), (False, False)):
+        y, dx, dw, kept = call(want_x, want_w)
+        assert torch.equal(y, Y)
+        assert dx is None or torch.equal(dx, dX)
+        assert dw is None or torch.equal(dw, dW)
+        assert (dx is not None, dw is not None) == (want_x, want_w)
+        kept = kept or {}
+        assert (kept.get("wq_t") is not None, kept.get("w_scale") is not None) == (want_x, want_x)
+        assert (kept.get("xq_t") is not None, kept.get("x_scale") is not None) == (want_w, want_w)
+    with torch.no_grad():
+        assert torch.equal(P.int8_linear(X.requires_grad_(), W.requires_grad_()), Y) and not made[-1]
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 16, 32), (333, 512, 272), (0, 16, 16)])
+def test_one_of_the_copies_alone(P, M, N, K):
+    """Each gradient from the copy that it reads, bit for bit; without that copy it is refused."""
+    import torch
+    g = np.random.default_rng(M)
+    X, W, dY = bf16(g.normal(size=(M, K))), bf16(g.normal(size=(N, K))), bf16(g.normal(size=(M, N)))
+    Y, saved = P.int8_linear_fwd(X, W)
+    dX, dW = P.int8_linear_bwd(dY, saved)
+    y, for_dx = P.int8_linear_fwd(X, W, want_dw=False)
+    z, for_dw = P.int8_linear_fwd(X, W, want_dx=False)
+    none, nothing = P.int8_linear_fwd(X, W, want_dx=False, want_dw=False)
+    assert torch.equal(y, Y) and torch.equal(z, Y) and torch.equal(none, Y) and not any(v is not None for v in nothing.values())
+    if M:
+        for part, names in ((for_dx, ("wq_t", "w_scale")), (for_dw, ("xq_t", "x_scale"))):
+            assert {k for k, v in part.items() if v is not None} == set(names)
+            assert all(torch.equal(part[k], saved[k]) for k in names)
+    assert torch.equal(P.int8_linear_bwd(dY, for_dx, want_dw=False)[0], dX)
+    assert torch.equal(P.int8_linear_bwd(dY, for_dw, want_dx=False)[1], dW)
+    for part in (for_dx, for_dw, nothing):
+        with pytest.raises(ValueError):
+            P.int8_linear_bwd(dY, part)

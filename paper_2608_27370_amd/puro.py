@@ -966,6 +966,8 @@ def swiglu_quantize_int8(gu, cols, out=None):
     if width < 2 * cols:
         raise ValueError("gu: %d columns for two halves of %d" % (width, cols))
     q, scale, pq, ps = _int8_rows(rows, cols, out, gu, dev)
+    if cols == 0:                              # (as quantize_int8)
+        scale.fill_(1.0)
     _check("puro_swiglu_quantize_int8", lib().puro_swiglu_quantize_int8(px, rows, cols, ld, pq, ps, _stream()))
     return dict(q=q, scale=scale)
 

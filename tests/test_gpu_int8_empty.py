@@ -43,3 +43,18 @@ def test_the_autograd_operation_without_input_channels(P):
     assert X.grad.shape == X.shape and W.grad.shape == W.shape
     with torch.no_grad():
         assert not P.int8_linear(X, W).any().item()
+
+
+def test_scales_of_rows_without_columns(P):
+    """1 (as of rows of zeros), new ones and given ones, whatever the memory held."""
+    import torch
+    nan = torch.full((1 << 16,), float("nan"), device="cuda")
+    del nan                                                      # (its memory is what the next call's outputs take)
+    gu = torch.empty(5, 0, dtype=torch.bfloat16, device="cuda")
+    r = P.swiglu_quantize_int8(gu, 0)
+    assert r["q"].shape == (5, 0) and (r["scale"] == 1).all().item()
+    given = torch.full((5,), float("nan"), device="cuda")
+    assert P.swiglu_quantize_int8(gu, 0, out=dict(scale=given))["scale"] is given and (given == 1).all().item()
+    given.fill_(float("nan"))
+    P.quantize_int8(gu, out=dict(scale=given))
+    assert (given == 1).all().item()

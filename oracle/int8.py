@@ -15,10 +15,12 @@ BF16 (u = 2^-24): a value known to a relative e moves v = 127 x / amax by 2 e |v
 (its own error and amax's), r and the product by 2 u |v| more; the codes of both
 ends of that band are accepted, and s within e + 2 u.
 
-  * RMSNorm: the sum of squares has at most cols / 64 fused terms a lane and 8
-    more additions, all positive: cols / 64 + 8 roundings, halved by the root; the
-    mean's division, eps's sum, root, reciprocal and two products at most 6 more:
-    e = (cols / 128 + 10) u.
+  * RMSNorm: a lane sums whole chunks of 8 squares, fused, and the row's lanes are
+    added up, all positive. Rows of up to 2048 values lie on 16 lanes (one chunk, 4
+    additions more), a wave (8 ceil(cols / 512) terms and 6) or four waves (one chunk
+    and 8), longer ones on four waves (8 ceil(cols / 2048) and 8): n roundings at most,
+    halved by the root; the mean's division, eps's sum, root, reciprocal and two
+    products at most 6 more: e = (n / 2 + 6) u.
   * SwiGLU: oracle/swiglu.py's 2^-20.
 """
 
@@ -71,7 +73,9 @@ def band_rows(x, e):
 def rmsnorm(x, gamma, eps):
     """(y, rstd, relative allowance of y) of float64 x [R, C]."""
     rstd = 1.0 / np.sqrt((x * x).mean(axis=1) + eps)
-    return x * rstd[:, None] * gamma, rstd, (x.shape[1] / 128.0 + 10.0) * U
+    cols = x.shape[1]
+    n = max(8 * -(-cols // 512) + 6, 16) if cols <= 2048 else 8 * -(-cols // 2048) + 8
+    return x * rstd[:, None] * gamma, rstd, (n / 2.0 + 6.0) * U
 
 
 def swiglu(gu):

@@ -496,9 +496,9 @@ int col_ranges(int64_t rows, int64_t cols) {
 
 // ---------------------------------------------------------------- product of few rows ---
 // Up to 64 rows of A: the time is that of reading B once (1x17920x1536 8.3 us, 3.3 TB/s;
-// a small B is a launch and the latency of its loads, 1x2048x1536 3.8). A block has 16 NT columns
-// and WK waves that take steps of 128 values of k in turn, straight from memory
-// into registers (a lane 32 bytes of its row, four lanes a whole cache line), U
+// a small B is a launch and the latency of its loads, 1x2048x1536 3.8). A block has 16 columns
+// and eight waves that take steps of 128 values of k in turn, straight from memory
+// into registers (a lane 32 bytes of its row, four lanes a whole cache line), two
 // steps' loads in flight; nothing but the rows of A that exist is read of A, from
 // the caches. (16 columns, 8 waves, 2 steps: 1x2048x1536 3.9 us, 5x151936x1536 52.0;
 // 32 columns 4.6 and 56.1, 4 waves 3.9 and 52.6, 4 steps 4.3 and 73.9, 16 waves with
@@ -538,28 +538,27 @@ __device__ __forceinline__ void store_int8_outputs(const Int8Problem& p, int64_t
     }
 }
 
-template <int MT, int NT, int WK, int U>
-__global__ __launch_bounds__(WK * 64) void int8_rows_kernel(Int8Problem p) {
-    __shared__ v4i32 sums[WK > 1 ? WK * MT * NT * 64 : 1];
+constexpr int kRowsWaves = 8, kRowsSteps = 2;
+template <int MT>
+__global__ __launch_bounds__(kRowsWaves * 64) void int8_rows_kernel(Int8Problem p) {
+    constexpr int WK = kRowsWaves, U = kRowsSteps;
+    __shared__ v4i32 sums[WK * MT * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r = lane & 15, q = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * (16 * NT), m0 = (int64_t)blockIdx.y * (16 * MT);
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
     const int K = (int)p.K;
-    const int rows_n = (int)min((int64_t)16 * NT, p.N - n0), rows_m = (int)min((int64_t)16 * MT, p.M - m0);
+    const int rows_n = (int)min((int64_t)16, p.N - n0);
     const __amdgpu_buffer_rsrc_t rb = buffer_rsrc(p.B + n0 * p.ldb, (uint32_t)((rows_n - 1) * p.ldb + K));
-    const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(p.A + m0 * p.lda, (uint32_t)((rows_m - 1) * p.lda + K));
-    uint32_t ob[NT], oa[MT];
+    const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(p.A, (uint32_t)((p.M - 1) * p.lda + K));
+    const uint32_t ob = r < rows_n ? (uint32_t)(r * p.ldb) : kOOB;
+    uint32_t oa[MT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) ob[j] = j * 16 + r < rows_n ? (uint32_t)((j * 16 + r) * p.ldb) : kOOB;
+    for (int i = 0; i < MT; ++i) oa[i] = i * 16 + r < p.M ? (uint32_t)((i * 16 + r) * p.lda) : kOOB;
+    v4i32 acc[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) oa[i] = i * 16 + r < rows_m ? (uint32_t)((i * 16 + r) * p.lda) : kOOB;
-    v4i32 acc[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = v4i32{0, 0, 0, 0};
+    for (int i = 0; i < MT; ++i) acc[i] = v4i32{0, 0, 0, 0};
     for (int k0 = wave * 128; k0 < K; k0 += WK * 128 * U) {
-        v4i32 b[U][NT][2], a[U][MT][2];
+        v4i32 b[U][2], a[U][MT][2];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -567,8 +566,7 @@ __global__ __launch_bounds__(WK * 64) void int8_rows_kernel(Int8Problem p) {
                 const int k = k0 + u * (WK * 128) + q * 32 + h * 16;
                 // (past the reduction's end, and of rows that are not there: zeros)
                 const bool in = k < K;
-#pragma unroll
-                for (int j = 0; j < NT; ++j) b[u][j][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, in ? ob[j] + k : kOOB, 0, 0);
+                b[u][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, in ? ob + k : kOOB, 0, 0);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) a[u][i][h] = __builtin_amdgcn_raw_buffer_load_b128(ra, in ? oa[i] + k : kOOB, 0, 0);
             }
@@ -577,33 +575,20 @@ __global__ __launch_bounds__(WK * 64) void int8_rows_kernel(Int8Problem p) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[u][j][h], a[u][i][h], acc[i][j], 0, 0, 0);
+                for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[u][h], a[u][i][h], acc[i], 0, 0, 0);
     }
-    if constexpr (WK > 1) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) sums[((i * NT + j) * WK + wave) * 64 + lane] = acc[i][j];
-        __syncthreads();
-    }
-    for (int t = wave; t < MT * NT; t += WK) {
-        const int i = t / NT, j = t % NT;
-        const int64_t m = m0 + i * 16 + r, n = n0 + j * 16 + q * 4;
+    for (int i = 0; i < MT; ++i) sums[(i * WK + wave) * 64 + lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < MT; i += WK) {
+        const int64_t m = i * 16 + r, n = n0 + q * 4;
         float sb[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) sb[e] = n + e < p.N ? p.sb[n + e] : 0.0f;
         const float sa = m < p.M ? p.sa[m] : 0.0f;
-        v4i32 v;
-        if constexpr (WK > 1) {
-            v = sums[t * WK * 64 + lane];
+        v4i32 v = sums[i * WK * 64 + lane];
 #pragma unroll
-            for (int w = 1; w < WK; ++w) v += sums[(t * WK + w) * 64 + lane];
-        } else {
-            v = acc[i][j];
-        }
+        for (int w = 1; w < WK; ++w) v += sums[(i * WK + w) * 64 + lane];
         store_int8_outputs(p, m, n, v, sa, sb);
     }
 }
@@ -782,7 +767,7 @@ constexpr int64_t kStreamColumns = 32768;
 
 template <int MT>
 static void launch_few(const Int8Problem& p, hipStream_t stream) {
-    int8_rows_kernel<MT, 1, 8, 2><<<(unsigned)((p.N + 15) / 16), 512, 0, stream>>>(p);
+    int8_rows_kernel<MT><<<(unsigned)((p.N + 15) / 16), kRowsWaves * 64, 0, stream>>>(p);
 }
 
 size_t int8_gemm_ws_bytes(int64_t M, int64_t N, int64_t K) {

@@ -1117,7 +1117,7 @@ def verify_drafts(target, draft, draft_ids, offsets, uniform=None, uniform_sampl
     if offsets.dim() != 1 or offsets.shape[0] == 0:
         raise ValueError("offsets: one more than there are sequences")
     B = offsets.shape[0] - 1
-    rows, ldd, pd = T, 0, None
+    rows, ldd, pd = 0, 0, None
     if draft is not None:
         rows, V_d, ldd, pd = _matrix(draft, "draft", (target.dtype,), dev)
         if V_d != V:

@@ -51,7 +51,7 @@
 //    binary32 where the accumulators are read and multiplied there by their
 //    row's and column's scales. Bound by the matrix units where K is long (8192 x
 //    8192 x 65536: 2.72 POP/s), by a lone tile's prologue and epilogue where it is
-//    short (8192x17920x1536: 225 us, 2.0 POP/s, 294 MB of output among it).
+//    short (8192x17920x1536: 221 to 246 us, 1.8 to 2.0 POP/s, 294 MB of output among it).
 
 // This file is compiled once per operand-format pair and scale kind
 // (PURO_FA, PURO_FB, PURO_GROUPED), each object holding that variant's tile

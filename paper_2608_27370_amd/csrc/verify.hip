@@ -238,7 +238,7 @@ __device__ __forceinline__ bool bad(const Norm& n) { return !(n.inv < kInf); }
 // has none for, those without rows not among them. Waves look through the offsets
 // before (a sequence that begins before one of them would write its tokens over
 // another's); of many sequences that is done in a launch before (65536 of them of two
-// rows of 20 entries 4.5 ms and 1.2 in all).
+// rows of 20 entries 4.5 ms and 1.1 in all).
 struct Rows {
     int start, n, shift;
 };
@@ -295,7 +295,7 @@ __device__ __forceinline__ float largest(const Piece<E, LEN>& x) {
 // ---- LOGITS: (largest, sum of 2^((z - largest) c)) of every piece of every row.
 // Bound by its arithmetic and, nearly as closely, by memory: 16.5 instructions an entry,
 // 11 of them binary64, keep the vector units busy for 85% of the time (768 BF16 rows of
-// 151936: 65 us, 3.6 TB/s; a copy's rate would be 49). With a polynomial of degree 8 and
+// 151936: 67 to 69 us, 3.4 TB/s; a copy's rate would be 49). With a polynomial of degree 8 and
 // the exponent rounded by an addition, 19.5: 76; the next piece's loads in flight while
 // one is summed: 79 to 84.
 template <typename E, int LEN>
@@ -390,7 +390,7 @@ __device__ __forceinline__ End find_end(const Args& a, Rows rows, EndScratch& s)
     }
 }
 
-// Latency: 6.1 us for 96 sequences of up to eight rows of 151936 and their drafts'.
+// Latency: 6.1 to 6.4 us for 96 sequences of up to eight rows of 151936 and their drafts'.
 template <typename E>
 __global__ __launch_bounds__(kEndWaves * 64) void end_rows_kernel(Args a) {
     __shared__ EndScratch scratch;
@@ -760,7 +760,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(Args a) {
 // LOGITS without the draft's: the end row and the draw in one launch. Nothing but the
 // id's own entry is taken from p there, so that the pieces' shares are those of their
 // sums, and the id's piece alone is summed again without it. 33 sequences of up to four
-// rows of 50257: 4.4 + 6.3 + 4.4 us -> 9.6, of which the chain of short steps is the most.
+// rows of 50257: 4.4 + 6.3 + 4.4 us -> 9.1, of which the chain of short steps is the most.
 template <typename E, int LEN>
 __global__ __launch_bounds__(kEndWaves * 64) void end_and_draw_kernel(Args a) {
     __shared__ EndScratch end_scratch;
